@@ -224,6 +224,77 @@ int bmlp_expand_sign(const uint8_t* x, int64_t n, int32_t D, const uint64_t* E, 
 int bmlp_debug_expand_sign(const uint8_t* x, int64_t n, int32_t D, const uint64_t* E, int32_t K,
                            uint64_t* out, void* cuda_stream, int64_t expired_tile);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit front end for real-valued rows (hidden states of a language model,
+ * features of an encoder): like the expansion layer, a fixed layer in front of
+ * the BMLP (Sec. 3.2, footnote to the binarisation step), for real inputs and
+ * integer weights.  bmlp_norm_quantize takes rows to 8-bit codes,
+ * bmlp_quantize_rows a weight matrix, and bmlp_int8_sign their product to
+ * bmlp_train / bmlp_predict input; bmlp_int8_matmul gives the product itself.
+ * The learning rule passes no gradient below its first layer, so none of the
+ * four has a backward form.
+ *
+ * Common to the four: no handle (errors: bmlp_last_error(NULL)); every pointer
+ * is a device pointer, caller-owned; asynchronous on cuda_stream, nothing is
+ * allocated; may be captured.  Row strides (ld...) are in elements and at
+ * least the row's length where there is more than one row; rows may start at
+ * any element.  n == 0 is a no-op.  Outputs may not overlap inputs except where
+ * said.  BMLP_EINVAL for bad arguments, BMLP_ECUDA if a launch fails.
+ * ------------------------------------------------------------------------- */
+
+/* element types of real-valued buffers (BMLP_I32: bmlp_int8_matmul's output only) */
+#define BMLP_F32 0
+#define BMLP_F16 1
+#define BMLP_BF16 2
+#define BMLP_I32 3
+
+#define BMLP_INT8_MAX_K 131071  /* K 2^14 < 2^31: no sum leaves int32 */
+
+/* Symmetric 8-bit quantisation of rows: with A = max_i |x_i| of a row (fp32),
+ *   q_i = rint(x_i * (127 / A)),  scale = A / 127   (each operation rounded to
+ *   fp32, ties of rint to even), so x_i is about q_i * scale, |q_i| <= 127.
+ * A < 127 * 2^-126: q = 0 and scale = 0.  A row with an infinity or a NaN: q = 0
+ * and scale = NaN (products scaled by it are NaN).
+ *   x: n x K of x_type, row stride ldx.  q: n x K, row stride ldq.  scale: n.
+ * For the channels of a weight matrix n is their number. */
+int bmlp_quantize_rows(const void* x, int32_t x_type, int64_t ldx, int64_t n, int32_t K, int8_t* q,
+                       int64_t ldq, float* scale, void* cuda_stream);
+
+/* Root-mean-square norm of rows with the residual's addition, to 8 bits:
+ *   h = x + res (fp32; h = x where res is NULL),  sum_out = h (rounded to x_type),
+ *   u_i = h_i * gain_i,  A = max_i |u_i|,  rstd = 1 / sqrt(mean_i h_i^2 + eps),
+ *   q_i = rint(u_i * (127 / A)),  scale = (A / 127) * rstd
+ * so h_i rstd gain_i is about q_i * scale.  rstd is common to the row, so the
+ * codes do not depend on it.  Sums are held in fp32.  A < 127 * 2^-126: q = 0 and
+ * scale = 0; a row whose A or sum of squares is not finite: q = 0, scale = NaN.
+ *   x, res, sum_out: n x K of x_type, row strides ldx, ldr, lds; res and sum_out
+ *     may be NULL.  sum_out may be x or res itself (same pointer and stride).
+ *   gain: K values of x_type, or NULL (1).  eps >= 0 and finite.
+ *   q: n x K, row stride ldq.  scale: n. */
+int bmlp_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr, const void* gain,
+                       int32_t x_type, int64_t n, int32_t K, float eps, void* sum_out, int64_t lds,
+                       int8_t* q, int64_t ldq, float* scale, void* cuda_stream);
+
+/* Product of 8-bit integers with scales for each row and channel:
+ *   S_ij = sum_k a_ik w_jk, exact;  out_ij = (S_ij * a_scale_i) * w_scale_j + bias_j
+ * in fp32 (one rounding per operation), rounded to out_type; with BMLP_I32 S
+ * itself (scales and bias NULL).
+ *   a: n x K, row stride lda.  w: N x K, row stride ldw.  All 256 values allowed.
+ *   a_scale: n, w_scale: N, bias: N; each may be NULL (1, 1, 0).
+ *   out: n x N of out_type, row stride ldo.
+ * K in 1..BMLP_INT8_MAX_K, N >= 1. */
+int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
+                     const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
+                     int32_t out_type, int64_t ldo, void* cuda_stream);
+
+/* Signs of the same product, packed: bit j of row i is 1 (+1) iff
+ * S_ij >= threshold_j (threshold: N int32, or NULL for 0: sign(0) = +1); exact.
+ * Scales are positive, so they do not matter here.  out: n rows of ceil(N/64)
+ * words, 8-byte aligned, pad bits 0: bmlp_train / bmlp_predict input for
+ * K_0 = N. */
+int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
+                   int64_t n, int32_t K, int32_t N, uint64_t* out, void* cuda_stream);
+
 /* One layer of forward-only evaluation (Sec. 3.1; Alg. 1 l.8-9):
  * a_out = sign(a_in W_l), sign(0) = +1, for n packed rows.  a_in: n rows of
  * ceil(K_{l-1}/64) words (pad bits 0); a_out: n rows of ceil(K_l/64) words,

@@ -31,6 +31,8 @@ BMLP_ENODEV = -6
 BMLP_EPOCH_END = 1
 BMLP_FWD_AUTO, BMLP_FWD_POPC, BMLP_FWD_TCGEN05, BMLP_FWD_B1MMA, BMLP_FWD_S8MMA = 0, 1, 2, 3, 4
 BMLP_GROUPS_CONTIGUOUS, BMLP_GROUPS_FIXED, BMLP_GROUPS_RESHUFFLED = 0, 1, 2
+BMLP_F32, BMLP_F16, BMLP_BF16, BMLP_I32 = 0, 1, 2, 3
+BMLP_INT8_MAX_K = 131071
 PROFILE_KINDS = ("train_forward", "cls_select", "update", "eval_forward", "eval_out", "copy",
                  "r_events")
 
@@ -88,6 +90,12 @@ SIGNATURES = [
     ("bmlp_debug_fail_alloc", C.c_int, [C.c_int64]),
     ("bmlp_debug_fail_launch", C.c_int, [C.c_int64]),
     ("bmlp_debug_alloc_stats", C.c_int, [_i64p, _i64p]),
+    ("bmlp_quantize_rows", C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, C.c_int64, _vp, _vp]),
+    ("bmlp_norm_quantize", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
+                                     C.c_float, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp]),
+    ("bmlp_int8_matmul", C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int32, C.c_int32,
+                                   _vp, C.c_int32, C.c_int64, _vp]),
+    ("bmlp_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp]),
     ("bmlp_layer_forward_engine", C.c_int, [_vp, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp]),
 ]
 
@@ -134,6 +142,43 @@ def _ptr(buf):
         assert buf.is_contiguous(), "tensor must be contiguous"
         return buf.data_ptr()
     raise TypeError("expected a torch tensor or a numpy array, got %r" % type(buf))
+
+
+_REAL_TYPES = {"torch.float32": BMLP_F32, "torch.float16": BMLP_F16, "torch.bfloat16": BMLP_BF16}
+_OUT_TYPES = dict(_REAL_TYPES, **{"torch.int32": BMLP_I32})
+_types = {}   # of the torch dtypes seen
+
+
+def _type(t, of):
+    """BMLP_* type of a torch tensor's elements; `of`: the types allowed."""
+    name = _types.get(t.dtype)
+    if name is None:
+        name = _types[t.dtype] = str(t.dtype)
+    if name not in of:
+        raise TypeError("expected a tensor of %s, got %s" % (", ".join(of), name))
+    return of[name]
+
+
+def _rows(t, n, K, what, dtype=None):
+    """(pointer, row stride in elements) of an n x K tensor whose rows are contiguous."""
+    if t.shape != (n, K):
+        raise ValueError("%s: expected shape %s, got %s" % (what, (n, K), tuple(t.shape)))
+    ld, step = t.stride()
+    if step != 1 and K > 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % what)
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, what, dtype):
+    """Pointer of a contiguous vector of n elements (None: NULL)."""
+    if t is None:
+        return None
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1) or t.dtype != dtype:
+        raise ValueError("%s: expected %d contiguous values of %s, got %s of %s"
+                         % (what, n, dtype, tuple(t.shape), t.dtype))
+    return t.data_ptr()
 
 
 def _stream(stream):
@@ -227,6 +272,61 @@ def bmlp_expand_sign(x, E, K, out, stream=None):
     """Expansion layer: n x D uint8 patterns (device) -> packed sign(x E^T)."""
     n, D = x.shape
     _check(lib().bmlp_expand_sign(_ptr(x), n, D, _ptr(E), K, _ptr(out), _stream(stream)), None)
+
+
+def bmlp_quantize_rows(x, q, scale, stream=None):
+    """8-bit codes q (n x K int8) and scales (n fp32) of the rows of x (n x K
+    fp32 / fp16 / bf16, on the device; row strides are kept)."""
+    import torch
+    n, K = x.shape
+    px, ldx = _rows(x, n, K, "x")
+    pq, ldq = _rows(q, n, K, "q", torch.int8)
+    _check(lib().bmlp_quantize_rows(px, _type(x, _REAL_TYPES), ldx, n, K, pq, ldq,
+                                    _vector(scale, n, "scale", torch.float32), _stream(stream)), None)
+
+
+def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stream=None):
+    """RMS norm of the rows of x + res times gain as 8-bit codes q (n x K int8)
+    and scales (n fp32); sum_out (may be x or res): x + res in their type.
+    gain, res, sum_out: x's type, each may be None."""
+    import torch
+    n, K = x.shape
+    px, ldx = _rows(x, n, K, "x")
+    pr, ldr = (None, 0) if res is None else _rows(res, n, K, "res", x.dtype)
+    ps, lds = (None, 0) if sum_out is None else _rows(sum_out, n, K, "sum_out", x.dtype)
+    pq, ldq = _rows(q, n, K, "q", torch.int8)
+    _check(lib().bmlp_norm_quantize(px, ldx, pr, ldr, _vector(gain, K, "gain", x.dtype), _type(x, _REAL_TYPES),
+                                    n, K, eps, ps, lds, pq, ldq, _vector(scale, n, "scale", torch.float32),
+                                    _stream(stream)), None)
+
+
+def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=None):
+    """out (n x N fp32 / fp16 / bf16, or int32 without scales and bias) = a (n x K
+    int8) times w (N x K int8) transposed, scaled per row and channel."""
+    import torch
+    n, K = a.shape
+    N = w.shape[0]
+    pa, lda = _rows(a, n, K, "a", torch.int8)
+    pw, ldw = _rows(w, N, K, "w", torch.int8)
+    po, ldo = _rows(out, n, N, "out")
+    f32 = torch.float32
+    _check(lib().bmlp_int8_matmul(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw,
+                                  _vector(w_scale, N, "w_scale", f32), _vector(bias, N, "bias", f32), n, K, N,
+                                  po, _type(out, _OUT_TYPES), ldo, _stream(stream)), None)
+
+
+def bmlp_int8_sign(a, w, out, threshold=None, stream=None):
+    """Packed +-1 words (n x ceil(N/64) int64) of a (n x K int8) times w (N x K
+    int8) transposed against threshold (N int32; None: 0)."""
+    import torch
+    n, K = a.shape
+    N = w.shape[0]
+    pa, lda = _rows(a, n, K, "a", torch.int8)
+    pw, ldw = _rows(w, N, K, "w", torch.int8)
+    if out.shape != (n, (N + 63) // 64) or out.element_size() != 8:
+        raise ValueError("out: expected %d x %d 64-bit words" % (n, (N + 63) // 64))
+    _check(lib().bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
+                                _ptr(out), _stream(stream)), None)
 
 
 def bmlp_debug_expand_sign(x, E, K, out, expired_tile, stream=None):

@@ -192,6 +192,51 @@ void block_tables(double q, int n, unsigned long long* any, unsigned long long* 
 
 double reinforce_q(double p_r, int K) { return p_r * std::sqrt(2.0 / (M_PI * (double)K)); }
 
+// Whether an optional buffer of 2^shift-byte elements is a device buffer, aligned.
+bool usable(const void* p, int shift) {
+  return !p || ((reinterpret_cast<uintptr_t>(p) & ((1u << shift) - 1)) == 0 && is_device_ptr(p));
+}
+
+// The checks and the launch that bmlp_quantize_rows and bmlp_norm_quantize share.
+int quantize_call(const char* name, const QuantArgs& A, bool norm, void* cuda_stream) {
+  if (A.n < 0 || A.K < 1) return fail(nullptr, BMLP_EINVAL, "%s: n < 0 or K < 1", name);
+  if (A.type != BMLP_F32 && A.type != BMLP_F16 && A.type != BMLP_BF16)
+    return fail(nullptr, BMLP_EINVAL, "%s: x_type must be BMLP_F32, BMLP_F16 or BMLP_BF16", name);
+  if (A.n == 0) return BMLP_OK;
+  if (A.n > 1 && (A.ldx < A.K || A.ldq < A.K || (A.res && A.ldr < A.K) || (A.sum && A.lds < A.K)))
+    return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below K", name);
+  if (A.sum && ((A.sum == A.x && A.lds != A.ldx) || (A.sum == A.res && A.lds != A.ldr)) && A.n > 1)
+    return fail(nullptr, BMLP_EINVAL, "%s: sum_out in place needs its input's row stride", name);
+  const int shift = A.type == BMLP_F32 ? 2 : 1;
+  if (!A.x || !A.q || !A.scale || !usable(A.x, shift) || !usable(A.res, shift) || !usable(A.gain, shift) ||
+      !usable(A.sum, shift) || !usable(A.q, 0) || !usable(A.scale, 2))
+    return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
+  const cudaError_t e = launch_quantize(A, norm, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
+  return BMLP_OK;
+}
+
+// The same for bmlp_int8_matmul and bmlp_int8_sign (A.words set).
+int int8_call(const char* name, const Int8Args& A, void* cuda_stream) {
+  if (A.n < 0 || A.K < 1 || A.K > BMLP_INT8_MAX_K || A.N < 1)
+    return fail(nullptr, BMLP_EINVAL, "%s: n < 0, N < 1, or K outside 1..%d", name, BMLP_INT8_MAX_K);
+  if (A.type < BMLP_F32 || A.type > BMLP_I32)
+    return fail(nullptr, BMLP_EINVAL, "%s: unknown out_type", name);
+  if (A.type == BMLP_I32 && (A.a_scale || A.w_scale || A.bias))
+    return fail(nullptr, BMLP_EINVAL, "%s: BMLP_I32 output takes no scales and no bias", name);
+  if (A.n == 0) return BMLP_OK;
+  if ((A.n > 1 && (A.lda < A.K || (A.out && A.ldo < A.N))) || (A.N > 1 && A.ldw < A.K))
+    return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below its row's length", name);
+  const int shift = A.type == BMLP_F32 || A.type == BMLP_I32 ? 2 : 1;
+  if (!A.a || !A.w || (!A.out && !A.words) || !usable(A.a, 0) || !usable(A.w, 0) || !usable(A.a_scale, 2) ||
+      !usable(A.w_scale, 2) || !usable(A.bias, 2) || !usable(A.thr, 2) || !usable(A.out, shift) ||
+      !usable(A.words, 3))
+    return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
+  const cudaError_t e = launch_int8(A, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
+  return BMLP_OK;
+}
+
 int upload_thresholds(bmlp_t* h, cudaStream_t st) {
   std::vector<RTables> rt((size_t)h->L);
   for (int l = 1; l <= h->L; ++l) {
@@ -931,6 +976,41 @@ int bmlp_debug_expand_sign(const uint8_t* x, int64_t n, int32_t D, const uint64_
   const cudaError_t e = launch_expand_sign(x, n, D, E, K, out, static_cast<cudaStream_t>(cuda_stream), expired_tile);
   if (e != cudaSuccess) return cuda_fail(nullptr, e, "k_expand_sign");
   return BMLP_OK;
+}
+
+int bmlp_quantize_rows(const void* x, int32_t x_type, int64_t ldx, int64_t n, int32_t K, int8_t* q,
+                       int64_t ldq, float* scale, void* cuda_stream) {
+  TraceRange trace("bmlp_quantize_rows");
+  QuantArgs A = {};
+  A.x = x; A.q = q; A.scale = scale;
+  A.ldx = ldx; A.ldq = ldq; A.n = n;
+  A.K = K; A.type = x_type;
+  return quantize_call("bmlp_quantize_rows", A, false, cuda_stream);
+}
+
+int bmlp_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr, const void* gain,
+                       int32_t x_type, int64_t n, int32_t K, float eps, void* sum_out, int64_t lds,
+                       int8_t* q, int64_t ldq, float* scale, void* cuda_stream) {
+  TraceRange trace("bmlp_norm_quantize");
+  if (!(eps >= 0.0f) || std::isinf(eps))
+    return fail(nullptr, BMLP_EINVAL, "bmlp_norm_quantize: eps must be finite and >= 0");
+  const QuantArgs A = {x, res, gain, sum_out, q, scale, ldx, ldr, lds, ldq, n, K, x_type, eps};
+  return quantize_call("bmlp_norm_quantize", A, true, cuda_stream);
+}
+
+int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
+                     const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
+                     int32_t out_type, int64_t ldo, void* cuda_stream) {
+  TraceRange trace("bmlp_int8_matmul");
+  const Int8Args A = {a, w, a_scale, w_scale, bias, nullptr, out, nullptr, lda, ldw, ldo, n, K, N, out_type};
+  return int8_call("bmlp_int8_matmul", A, cuda_stream);
+}
+
+int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
+                   int64_t n, int32_t K, int32_t N, uint64_t* out, void* cuda_stream) {
+  TraceRange trace("bmlp_int8_sign");
+  const Int8Args A = {a, w, nullptr, nullptr, nullptr, threshold, nullptr, out, lda, ldw, 0, n, K, N, BMLP_I32};
+  return int8_call("bmlp_int8_sign", A, cuda_stream);
 }
 
 int bmlp_get_state(const bmlp_t* hc, int32_t layer, int16_t* H_out, uint64_t* W_out, int8_t* P_out,

@@ -277,6 +277,34 @@ void launch_expand_weights(uint64_t seed, int K, int D, uint64_t* E, cudaStream_
 // this number as expired.
 cudaError_t launch_expand_sign(const uint8_t* x, int64_t n, int D, const uint64_t* E, int K,
                                uint64_t* out, cudaStream_t st, int64_t fail_tile = -1);
+// 8-bit front end: rows to codes and scales (kern_quantize.cu).
+struct QuantArgs {
+  const void* x;
+  const void* res;      // or null
+  const void* gain;     // or null
+  void* sum;            // or null
+  int8_t* q;
+  float* scale;
+  int64_t ldx, ldr, lds, ldq, n;
+  int32_t K, type;      // BMLP_F32 / F16 / BF16
+  float eps;
+};
+cudaError_t launch_quantize(const QuantArgs& A, bool norm, cudaStream_t st);
+// Product of 8-bit integers (kern_int8.cu): scaled (out, out_type) or its packed
+// signs (words).
+struct Int8Args {
+  const int8_t* a;
+  const int8_t* w;
+  const float* a_scale;   // or null
+  const float* w_scale;   // or null
+  const float* bias;      // or null
+  const int32_t* thr;     // or null (signs)
+  void* out;
+  uint64_t* words;        // null: scaled output
+  int64_t lda, ldw, ldo, n;
+  int32_t K, N, type;
+};
+cudaError_t launch_int8(const Int8Args& A, cudaStream_t st);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W
