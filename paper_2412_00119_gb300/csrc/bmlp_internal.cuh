@@ -305,6 +305,9 @@ struct Int8Args {
   int32_t K, N, type;
 };
 cudaError_t launch_int8(const Int8Args& A, cudaStream_t st);
+// The tensor-core tiles of one CTA (kern_int8_tile.cu).  expire != 0: every CTA takes a
+// wait as expired.
+cudaError_t launch_int8_tile(const Int8Args& A, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W
