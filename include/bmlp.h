@@ -285,7 +285,7 @@ int bmlp_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr,
  * K in 1..BMLP_INT8_MAX_K, N >= 1. */
 int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
                      const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
-                     int32_t out_type, int64_t ldo, void* cuda_stream);
+                     int32_t out_type, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /* Signs of the same product, packed: bit j of row i is 1 (+1) iff
  * S_ij >= threshold_j (threshold: N int32, or NULL for 0: sign(0) = +1); exact.
@@ -293,7 +293,16 @@ int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const i
  * words, 8-byte aligned, pad bits 0: bmlp_train / bmlp_predict input for
  * K_0 = N. */
 int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
-                   int64_t n, int32_t K, int32_t N, uint64_t* out, void* cuda_stream);
+                   int64_t n, int32_t K, int32_t N, uint64_t* out, void* workspace, int64_t workspace_bytes,
+                   void* cuda_stream);
+
+/* Workspace with which bmlp_int8_matmul and bmlp_int8_sign run fastest for this
+ * size, in bytes: 0 for few rows, else room for both operands in fp16 (rows in
+ * slabs, so it does not grow past 65,536 of them).  The two calls take a device
+ * buffer of at least this size, 16-byte aligned, written and read on cuda_stream
+ * (not shared by calls that overlap), or NULL / a smaller one: the same results
+ * without it, slower.  Host only; 0 for sizes that the calls refuse. */
+int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N);
 
 /* One layer of forward-only evaluation (Sec. 3.1; Alg. 1 l.8-9):
  * a_out = sign(a_in W_l), sign(0) = +1, for n packed rows.  a_in: n rows of

@@ -94,8 +94,10 @@ SIGNATURES = [
     ("bmlp_norm_quantize", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
                                      C.c_float, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp]),
     ("bmlp_int8_matmul", C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int32, C.c_int32,
-                                   _vp, C.c_int32, C.c_int64, _vp]),
-    ("bmlp_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp]),
+                                   _vp, C.c_int32, C.c_int64, _vp, C.c_int64, _vp]),
+    ("bmlp_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp,
+                                 C.c_int64, _vp]),
+    ("bmlp_int8_workspace", C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
     ("bmlp_layer_forward_engine", C.c_int, [_vp, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp]),
 ]
 
@@ -300,9 +302,31 @@ def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stre
                                     _stream(stream)), None)
 
 
-def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=None):
+def bmlp_int8_workspace(n, K, N):
+    """Bytes of workspace with which the product of this size runs fastest."""
+    return int(lib().bmlp_int8_workspace(n, K, N))
+
+
+def _workspace(workspace, n, K, N, a, stream):
+    """(pointer, bytes, owner) of the given workspace, or of one from torch's
+    allocator where the size wants it."""
+    if workspace is None:
+        size = lib().bmlp_int8_workspace(n, K, N)
+        if size == 0 or not a.is_cuda:
+            return None, 0, None
+        import torch
+        workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
+        raw = _stream(stream)
+        if raw != torch.cuda.current_stream(a.device).cuda_stream:
+            workspace.record_stream(torch.cuda.ExternalStream(raw, a.device))
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=None, workspace=None):
     """out (n x N fp32 / fp16 / bf16, or int32 without scales and bias) = a (n x K
-    int8) times w (N x K int8) transposed, scaled per row and channel."""
+    int8) times w (N x K int8) transposed, scaled per row and channel.
+    workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: from
+    torch's allocator)."""
     import torch
     n, K = a.shape
     N = w.shape[0]
@@ -310,14 +334,16 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     pw, ldw = _rows(w, N, K, "w", torch.int8)
     po, ldo = _rows(out, n, N, "out")
     f32 = torch.float32
+    ws, wsb, owner = _workspace(workspace, n, K, N, a, stream)
     _check(lib().bmlp_int8_matmul(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw,
                                   _vector(w_scale, N, "w_scale", f32), _vector(bias, N, "bias", f32), n, K, N,
-                                  po, _type(out, _OUT_TYPES), ldo, _stream(stream)), None)
+                                  po, _type(out, _OUT_TYPES), ldo, ws, wsb, _stream(stream)), None)
 
 
-def bmlp_int8_sign(a, w, out, threshold=None, stream=None):
+def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     """Packed +-1 words (n x ceil(N/64) int64) of a (n x K int8) times w (N x K
-    int8) transposed against threshold (N int32; None: 0)."""
+    int8) transposed against threshold (N int32; None: 0).  workspace: as for
+    bmlp_int8_matmul."""
     import torch
     n, K = a.shape
     N = w.shape[0]
@@ -325,8 +351,9 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None):
     pw, ldw = _rows(w, N, K, "w", torch.int8)
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8:
         raise ValueError("out: expected %d x %d 64-bit words" % (n, (N + 63) // 64))
+    ws, wsb, owner = _workspace(workspace, n, K, N, a, stream)
     _check(lib().bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
-                                _ptr(out), _stream(stream)), None)
+                                _ptr(out), ws, wsb, _stream(stream)), None)
 
 
 def bmlp_debug_expand_sign(x, E, K, out, expired_tile, stream=None):

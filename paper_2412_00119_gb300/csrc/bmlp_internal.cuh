@@ -304,10 +304,17 @@ struct Int8Args {
   int64_t lda, ldw, ldo, n;
   int32_t K, N, type;
 };
-cudaError_t launch_int8(const Int8Args& A, cudaStream_t st);
+cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st);
+// Bytes of workspace with which the call is fastest; 0: none is used.
+int64_t int8_workspace(int64_t n, int K, int N);
 // The tensor-core tiles of one CTA (kern_int8_tile.cu).  expire != 0: every CTA takes a
 // wait as expired.
 cudaError_t launch_int8_tile(const Int8Args& A, cudaStream_t st, int expire);
+// Both operands as fp16 in a workspace, then CTA pairs (kern_int8_pair.cu); rows in
+// slabs of kPairSlab.
+constexpr int64_t kPairSlab = 65536;
+int64_t int8_pair_workspace(int64_t n, int K, int64_t N);
+cudaError_t launch_int8_pair(const Int8Args& A, void* workspace, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

@@ -25,6 +25,36 @@ __device__ __forceinline__ uint32_t skew_of(const int8_t* row) {
   return (uint32_t)(reinterpret_cast<uintptr_t>(row) & 3);
 }
 
+// Bytes [k, k + 16) of the K codes at row, zeros from K on (k a multiple of 16).  What is
+// read around them: as below.
+template <int kAlign>
+__device__ __forceinline__ void load16(uint32_t (&v)[4], const int8_t* row, int k, int K) {
+  if constexpr (kAlign == 16) {
+    if (k + 16 <= K) {
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(row + k));
+      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+      return;
+    }
+  }
+  const int skew = (int)skew_of(row);
+  const int8_t* p = row + (k - skew);
+  uint32_t w[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    const int size = K - k + skew - 4 * i;   // codes of the row from this word on
+    w[i] = 0u;
+    if (size >= 4) {
+      w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 3; ++b)
+        if (b < size && K > 0) w[i] |= (uint32_t)(uint8_t)__ldg(p + 4 * i + b) << (8 * b);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * (uint32_t)skew);
+}
+
 // Asynchronous copy of bytes [k, k + 16) of the K codes at row to shared memory, zeros
 // from K on (k a multiple of 16; any: an address to name where nothing is read).  Rows
 // that allow no 16-byte copies: the five aligned words around them.  Nothing past the
@@ -73,6 +103,47 @@ __device__ __forceinline__ void codes_f16(uint32_t x, uint32_t& lo, uint32_t& hi
   const __half2 hb = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
   lo = *reinterpret_cast<const uint32_t*>(&ha);
   hi = *reinterpret_cast<const uint32_t*>(&hb);
+}
+
+// One output: the sum itself, or scaled.
+__device__ __forceinline__ void put_out(const Int8Args& A, int64_t i, int j, int s) {
+  const int64_t at = i * A.ldo + j;
+  if (A.type == BMLP_I32) {
+    static_cast<int32_t*>(A.out)[at] = s;
+    return;
+  }
+  float y = scaled(s, A.a_scale ? A.a_scale[i] : 1.0f, A.w_scale ? A.w_scale[j] : 1.0f);
+  if (A.bias) y = __fadd_rn(y, A.bias[j]);
+  if (A.type == BMLP_F32) static_cast<float*>(A.out)[at] = y;
+  else if (A.type == BMLP_F16) static_cast<__half*>(A.out)[at] = out_cast<__half>(y);
+  else static_cast<__nv_bfloat16*>(A.out)[at] = out_cast<__nv_bfloat16>(y);
+}
+
+__device__ __forceinline__ int plain_sum(const Int8Args& A, int64_t i, int j, int k0, int k1) {
+  const int8_t* ar = A.a + i * A.lda;
+  const int8_t* wr = A.w + (int64_t)j * A.ldw;
+  int sum = 0;
+  for (int k = k0; k < k1; ++k) sum += (int)ar[k] * (int)wr[k];
+  return sum;
+}
+
+// Outputs of `rows` rows from i0 and `channels` (a multiple of 32, as j0) channels from
+// j0 by the whole CTA on CUDA cores: only after a wait has expired.
+static __device__ __noinline__ void plain_tile(const Int8Args& A, int64_t i0, int rows, int j0, int channels) {
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+  const int words = channels / 32, nw32 = 2 * ((A.N + 63) / 64);
+  for (int e = warp; e < rows * words; e += warps) {
+    const int64_t i = i0 + e / words;
+    const int j = j0 + 32 * (e % words) + lane;
+    if (i >= A.n) return;
+    const int s = j < A.N ? plain_sum(A, i, j, 0, A.K) : 0;
+    if (A.words) {
+      const uint32_t w = __ballot_sync(0xffffffffu, j < A.N && s >= (A.thr ? A.thr[j] : 0));
+      if (lane == 0 && (j >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + (j >> 5)] = w;
+    } else if (j < A.N) {
+      put_out(A, i, j, s);
+    }
+  }
 }
 
 // The call's rows from `rows` on.

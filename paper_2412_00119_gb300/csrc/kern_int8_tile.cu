@@ -310,12 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
     const int k0 = KS * first, k1 = min(A.K, KS * (first + steps));
     for (int e = threadIdx.x; e < CM * NT; e += kThreads) {
       const int j = e % CM, i = e / CM;
-      int sum = 0;
-      if (j0 + j < A.N && i0 + i < A.n) {
-        const int8_t* wr = A.w + (int64_t)(j0 + j) * A.ldw;
-        const int8_t* ar = A.a + (i0 + i) * A.lda;
-        for (int k = k0; k < k1; ++k) sum += (int)ar[k] * (int)wr[k];
-      }
+      const int sum = j0 + j < A.N && i0 + i < A.n ? plain_sum(A, i0 + i, j0 + j, k0, k1) : 0;
       sums[i * C::kSumPitch + j] = sum;
     }
     __syncthreads();

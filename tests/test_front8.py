@@ -472,7 +472,7 @@ def test_product_refusals():
     pa, pf, po = a.ctypes.data, f.ctypes.data, out.ctypes.data
 
     def mm(lda=8, ldw=8, n=4, K=8, N=4, typ=B.BMLP_F32, ldo=4, sa=None, sw=None, bias=None, o=po):
-        return lib.bmlp_int8_matmul(pa, lda, sa, pa, ldw, sw, bias, n, K, N, o, typ, ldo, None)
+        return lib.bmlp_int8_matmul(pa, lda, sa, pa, ldw, sw, bias, n, K, N, o, typ, ldo, None, 0, None)
 
     def refused(rc, text):
         assert rc == B.BMLP_EINVAL and text in B.bmlp_last_error(), B.bmlp_last_error()
@@ -491,9 +491,9 @@ def test_product_refusals():
     refused(mm(), "device pointers")
     refused(mm(o=None), "device pointers")
     assert mm(n=0) == B.BMLP_OK
-    assert lib.bmlp_int8_sign(pa, 8, pa, 8, None, 0, 8, 4, None, None) == B.BMLP_OK
-    refused(lib.bmlp_int8_sign(pa, 8, pa, 8, None, 4, 8, 4, None, None), "device pointers")
-    refused(lib.bmlp_int8_sign(pa, 7, pa, 8, None, 4, 8, 4, po, None), "row stride")
+    assert lib.bmlp_int8_sign(pa, 8, pa, 8, None, 0, 8, 4, None, None, 0, None) == B.BMLP_OK
+    refused(lib.bmlp_int8_sign(pa, 8, pa, 8, None, 4, 8, 4, None, None, 0, None), "device pointers")
+    refused(lib.bmlp_int8_sign(pa, 7, pa, 8, None, 4, 8, 4, po, None, 0, None), "row stride")
 
 
 def test_binding_refusals():
