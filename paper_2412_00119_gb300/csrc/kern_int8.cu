@@ -4,7 +4,10 @@
 
 namespace bk {
 
-int64_t int8_workspace(int64_t n, int K, int N) { return n >= 256 ? int8_pair_workspace(n, K, N) : 0; }
+int64_t int8_workspace(int64_t n, int K, int N) {
+  // (blocks are numbered in 31 bits)
+  return n >= 256 && ((int64_t)N + 256) * (K / 64 + 1) < (1ll << 31) ? int8_pair_workspace(n, K, N) : 0;
+}
 
 cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
   const int64_t want = int8_workspace(A.n, A.K, A.N);

@@ -14,11 +14,14 @@
 // 168 registers):
 //   - 8 epilogue warps add a finished chunk's sums to 128 int32 registers per thread (a
 //     lane per channel) and, after a tile's last chunk, write its outputs;
-//   - one thread copies blocks into a ring of kStages;
-//   - on the even CTA one warp issues the MMAs; on the odd CTA three lanes of three
-//     warps forward its "full" barriers in turn.
+//   - one thread copies blocks into a ring of kStages; both CTAs' copies complete on the
+//     even one's barriers (tensor copies of a CTA pair may: forwarding the odd CTA's
+//     completions by a thread there cost 700 clocks of a k-step's round trip);
+//   - on the even CTA one warp issues the MMAs.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
+
+#include <cuda.h>
 
 #include "int8_common.cuh"
 #include "tc_common.cuh"
@@ -32,11 +35,11 @@ using namespace i8;
 constexpr int kBlockRows = 128, kBlockK = 64;
 constexpr int kBlockBytes = kBlockRows * kBlockK * 2;
 constexpr int TP = 256;                  // channels, and rows, of a tile
-constexpr int kStages = 6;
+constexpr int kStages = 7;
 constexpr int kStageBytes = 2 * kBlockBytes;
 constexpr int kChunk = 16;               // k-steps per accumulator: 1024 k
-constexpr int kEpiWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kRelays = 3;
-constexpr int kThreads = 32 * 12;
+constexpr int kEpiWarps = 8, kCopyWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 32 * 12;        // (two warps idle: registers are handed out by fours)
 constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
 
 struct __align__(8) PairShared {
@@ -168,17 +171,36 @@ __device__ __forceinline__ void tile_at(int64_t t, int ctiles, int64_t rtiles, i
   rt = first + in % wide;
 }
 
-// One column's (row's) outputs of a warp: a lane per channel.
-template <typename T>
-__device__ __forceinline__ void put_column(const Int8Args& A, int64_t i, int j, int v, float sa, float sw, float bias) {
-  float y = scaled(v, sa, sw);
-  if (A.bias) y = __fadd_rn(y, bias);
-  if (j < A.N) static_cast<T*>(A.out)[i * A.ldo + j] = out_cast<T>(y);
+// Tensor copy of one block (128 rows of 64 from row y of the map) to this CTA's shared
+// memory, completing on a barrier of either CTA of the pair.
+__device__ __forceinline__ void copy_block(void* dst, const CUtensorMap* map, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(smem_u32(dst)), "l"(map), "r"(0), "r"(y), "r"(bar) : "memory");
+}
+// The barrier at this offset in CTA 0 of the cluster.
+__device__ __forceinline__ uint32_t rank0_address(unsigned long long* bar) {
+  uint32_t remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(smem_u32(bar)));
+  return remote;
 }
 
+// What the kernel writes: one instance each, so that the unrolled stores stay short.
+struct Signs {};
+template <typename T> struct IsSigns { static constexpr bool value = false; };
+template <> struct IsSigns<Signs> { static constexpr bool value = true; };
+
+template <typename T>
+__device__ __forceinline__ T out_of(int s, float sa, float sw, bool has_bias, float bias) {
+  const float y = scaled(s, sa, sw);
+  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
+}
+template <> __device__ __forceinline__ int32_t out_of<int32_t>(int s, float, float, bool, float) { return s; }
+
+template <typename TOut>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    k_int8_pair(const Int8Args A, const uint8_t* __restrict__ wblocks, const uint8_t* __restrict__ ablocks, int nkb,
-                int ctiles, int64_t rtiles, int expire) {
+    k_int8_pair(const Int8Args A, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap,
+                int nkb, int ctiles, int64_t rtiles, int expire) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   PairShared* sh = reinterpret_cast<PairShared*>(base + kStages * kStageBytes);
@@ -191,7 +213,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&sh->full[s], rank == 0 ? 2 : 1);   // its copies and, on the even CTA, the odd one's relay
+      mbar_init(&sh->full[s], 1);
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -253,30 +275,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive_rank0(&sh->drained[b]);
       }
       if (!ok || expire) break;
+      if constexpr (IsSigns<TOut>::value) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int64_t ig = i0 + 32 * g;
-        if (A.words) {
+        for (int g = 0; g < 4; ++g) {
+          const int64_t i = i0 + 32 * g + lane;
           uint32_t mine = 0u;
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const uint32_t w = __ballot_sync(kFull, j < A.N && acc[32 * g + e] >= thr);
             if (lane == e) mine = w;
           }
-          if (ig + lane < A.n && (jw >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[(ig + lane) * nw32 + (jw >> 5)] = mine;
-        } else {
-          const float sal = A.a_scale && ig + lane < A.n ? A.a_scale[ig + lane] : 1.0f;
+          if (i < A.n && (jw >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + (jw >> 5)] = mine;
+        }
+      } else {
+        TOut* to = static_cast<TOut*>(A.out) + i0 * A.ldo + j;
+        const int rows = (int)max((int64_t)0, min((int64_t)128, A.n - i0));
+        const bool has_bias = A.bias != nullptr;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float sa = __shfl_sync(kFull, sal, e);
-            const int64_t i = ig + e;
-            if (i < A.n) {
-              const int v = acc[32 * g + e];
-              if (A.type == BMLP_BF16) put_column<__nv_bfloat16>(A, i, j, v, sa, sw, bias);
-              else if (A.type == BMLP_F16) put_column<__half>(A, i, j, v, sa, sw, bias);
-              else if (A.type == BMLP_F32) put_column<float>(A, i, j, v, sa, sw, bias);
-              else if (j < A.N) static_cast<int32_t*>(A.out)[i * A.ldo + j] = v;
-            }
+        for (int g = 0; g < 4; ++g) {
+          const float sal = A.a_scale && 32 * g + lane < rows ? A.a_scale[i0 + 32 * g + lane] : 1.0f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e, to += A.ldo) {
+            const TOut y = out_of<TOut>(acc[32 * g + e], __shfl_sync(kFull, sal, e), sw, has_bias, bias);
+            if (32 * g + e < rows && j < A.N) *to = y;
           }
         }
       }
@@ -293,16 +314,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int ct;
         int64_t rt;
         tile_at(t, ctiles, rtiles, ct, rt);
-        const uint8_t* wsrc = wblocks + (2 * (int64_t)ct + rank) * nkb * kBlockBytes;
-        const uint8_t* asrc = ablocks + (2 * rt + rank) * nkb * kBlockBytes;
+        const int wy = (2 * ct + (int)rank) * nkb * kBlockRows, ay = (int)((2 * rt + rank) * nkb * kBlockRows);
 #pragma unroll 1
-        for (int ks = 0; ks < nkb; ++ks, wsrc += kBlockBytes, asrc += kBlockBytes) {
+        for (int ks = 0; ks < nkb; ++ks) {
           ok = mbar_wait(&sh->empty[s], ph, failed);
           if (!ok) break;
           uint8_t* to = base + s * kStageBytes;
-          mbar_arrive_tx(&sh->full[s], kStageBytes);
-          bulk_g2s(to, wsrc, kBlockBytes, &sh->full[s]);
-          bulk_g2s(to + kBlockBytes, asrc, kBlockBytes, &sh->full[s]);
+          if (rank == 0) mbar_arrive_tx(&sh->full[s], 2 * kStageBytes);
+          const uint32_t bar = rank0_address(&sh->full[s]);
+          copy_block(to, &wmap, wy + ks * kBlockRows, bar);
+          copy_block(to + kBlockBytes, &amap, ay + ks * kBlockRows, bar);
           ++copied;
           if (++s == kStages) {
             s = 0;
@@ -310,10 +331,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (!ok) {
-        // no copy outlives the CTA: the odd CTA's barriers complete with the copies alone; on
-        // the even one a missing relay leaves a phase open, so its wait only bounds the time
-        for (int64_t k = std::max<int64_t>(0, copied - kStages); k < copied; ++k)
+      if (!ok && rank == 0) {
+        // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd one
+        // stopped earlier, the wait's limit is time enough for what is in flight)
+        for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
           mbar_wait(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
@@ -362,16 +383,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       mbar_wait(&sh->left, 0, &sh->left_failed);
     }
     __syncwarp();
-  } else if (rank != 0 && warp >= kMmaWarp && lane == 0) {
-    // relays of the odd CTA: its stage is full -> one arrival on the even CTA's
-    const uint64_t last = pair < tiles ? (uint64_t)((tiles - pair + pairs - 1) / pairs) * (uint64_t)nkb : 0ull;
-    bool ok = true;
-#pragma unroll 1
-    for (uint64_t k = (uint64_t)(warp - kMmaWarp); k < last && ok; k += kRelays) {
-      const uint32_t s = (uint32_t)(k % kStages);
-      ok = mbar_wait(&sh->full[s], (uint32_t)(k / kStages) & 1u, failed);
-      if (ok) mbar_arrive_rank0(&sh->full[s]);
-    }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -412,10 +423,45 @@ int64_t int8_pair_workspace(int64_t n, int K, int64_t N) {
   return row_bytes(K) * (padded(N) + std::min(padded(n), kPairSlab));
 }
 
-cudaError_t launch_int8_pair(const Int8Args& all, void* workspace, cudaStream_t st, int expire) {
-  const cudaError_t e =
-      cudaFuncSetAttribute(k_int8_pair, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+namespace {
+
+// Map of an operand's blocks: rows of 64 fp16 (already in the order that shared memory
+// holds), 128 at a time.
+bool block_map(CUtensorMap* map, void* blocks, int64_t rows) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)kBlockK, (cuuint64_t)rows}, strides[1] = {2 * kBlockK};
+  const cuuint32_t box[2] = {kBlockK, kBlockRows}, steps[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, blocks, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
+}
+
+template <typename TOut>
+cudaError_t launch_out(const Int8Args& A, const CUtensorMap& wmap, const CUtensorMap& amap, int nkb, cudaStream_t st,
+                       int expire) {
+  const cudaError_t e = cudaFuncSetAttribute(k_int8_pair<TOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
+  const int ctiles = (int)(padded(A.N) / TP);
+  const int64_t rtiles = padded(A.n) / TP;
+  const int64_t pairs = std::min<int64_t>(sm_count() / 2, (int64_t)ctiles * rtiles);
+  return launch_kernel(k_int8_pair<TOut>, dim3((unsigned)(2 * pairs)), dim3(kThreads), (size_t)kSmem, st, true, A, wmap,
+                       amap, nkb, ctiles, rtiles, expire);
+}
+
+}  // namespace
+
+cudaError_t launch_int8_pair(const Int8Args& all, void* workspace, cudaStream_t st, int expire) {
   const int nkb = (all.K + kBlockK - 1) / kBlockK;
   uint8_t* wblocks = static_cast<uint8_t*>(workspace);
   uint8_t* ablocks = wblocks + row_bytes(all.K) * padded(all.N);
@@ -431,14 +477,17 @@ cudaError_t launch_int8_pair(const Int8Args& all, void* workspace, cudaStream_t 
     E.units = E.units0 + padded(A.n) / 8;
     E.blocks0 = wblocks; E.blocks1 = ablocks;
     E.K = A.K; E.nkb = nkb;
-    const cudaError_t ee = wide ? expand<16>(E, st) : expand<1>(E, st);
-    if (ee != cudaSuccess) return ee;
-    const int ctiles = (int)(padded(A.N) / TP);
-    const int64_t rtiles = padded(A.n) / TP;
-    const int64_t pairs = std::min<int64_t>(sm_count() / 2, (int64_t)ctiles * rtiles);
-    const cudaError_t ep = launch_kernel(k_int8_pair, dim3((unsigned)(2 * pairs)), dim3(kThreads), (size_t)kSmem, st, true,
-                                         A, (const uint8_t*)wblocks, (const uint8_t*)ablocks, nkb, ctiles, rtiles, expire);
-    if (ep != cudaSuccess) return ep;
+    CUtensorMap wmap, amap;
+    if (!block_map(&wmap, wblocks, padded(A.N) * nkb) || !block_map(&amap, ablocks, padded(A.n) * nkb))
+      return cudaErrorNotSupported;
+    cudaError_t e = wide ? expand<16>(E, st) : expand<1>(E, st);
+    if (e != cudaSuccess) return e;
+    if (A.words) e = launch_out<Signs>(A, wmap, amap, nkb, st, expire);
+    else if (A.type == BMLP_F32) e = launch_out<float>(A, wmap, amap, nkb, st, expire);
+    else if (A.type == BMLP_F16) e = launch_out<__half>(A, wmap, amap, nkb, st, expire);
+    else if (A.type == BMLP_BF16) e = launch_out<__nv_bfloat16>(A, wmap, amap, nkb, st, expire);
+    else e = launch_out<int32_t>(A, wmap, amap, nkb, st, expire);
+    if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
