@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libbmlp.so")
 SOURCES = ["bmlp_api.cu", "bmlp_noalloc.cu", "kern_forward.cu", "kern_forward_tc.cu", "kern_eval_tc.cu",
            "kern_update.cu", "kern_binarize.cu", "kern_expand.cu", "kern_peaks.cu", "kern_forward_b1.cu",
            "kern_update_rows.cu", "kern_update_ws.cu", "kern_quantize.cu", "kern_int8.cu",
-           "kern_int8_tile.cu", "kern_int8_pair.cu"]
+           "kern_int8_few.cu", "kern_int8_tile.cu", "kern_int8_pair.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-ffp-contract=off",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include")]

@@ -307,6 +307,9 @@ struct Int8Args {
 cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st);
 // Bytes of workspace with which the call is fastest; 0: none is used.
 int64_t int8_workspace(int64_t n, int K, int N);
+// At most kFewRows rows, on CUDA cores (kern_int8_few.cu).
+constexpr int kFewRows = 8;
+cudaError_t launch_int8_few(const Int8Args& A, cudaStream_t st);
 // The tensor-core tiles of one CTA (kern_int8_tile.cu).  expire != 0: every CTA takes a
 // wait as expired.
 cudaError_t launch_int8_tile(const Int8Args& A, cudaStream_t st, int expire);

@@ -25,6 +25,24 @@ __device__ __forceinline__ uint32_t skew_of(const int8_t* row) {
   return (uint32_t)(reinterpret_cast<uintptr_t>(row) & 3);
 }
 
+// Bytes [k, k + 16) of a row that has them and (kAlign 1) four more after them (k a
+// multiple of 16).
+template <int kAlign>
+__device__ __forceinline__ void load16_inside(uint32_t (&v)[4], const int8_t* row, int k) {
+  if constexpr (kAlign == 16) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(row + k));
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  } else {
+    const uint32_t skew = skew_of(row);
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(row + (k - (int)skew));
+    uint32_t w[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = __ldg(p + i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * skew);
+  }
+}
+
 // Bytes [k, k + 16) of the K codes at row, zeros from K on (k a multiple of 16).  What is
 // read around them: as below.
 template <int kAlign>
@@ -55,42 +73,46 @@ __device__ __forceinline__ void load16(uint32_t (&v)[4], const int8_t* row, int 
   for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * (uint32_t)skew);
 }
 
-// Asynchronous copy of bytes [k, k + 16) of the K codes at row to shared memory, zeros
-// from K on (k a multiple of 16; any: an address to name where nothing is read).  Rows
-// that allow no 16-byte copies: the five aligned words around them.  Nothing past the
-// row's K codes is read, and before them at most the rest of the first one's aligned
-// word, which lies in the same allocation.
+// Rows that allow no 16-byte copies (kAlign 1) are copied as the aligned 16-byte chunks
+// around them: chunk i holds codes 16 i - s .. + 15, s the bytes between the row's start and
+// the aligned address before it, and the codes [16 i, 16 i + 16) are merged from chunks i and i + 1.
 template <int kAlign>
-__device__ __forceinline__ void copy16(uint32_t to, const int8_t* row, int k, int K, const int8_t* any) {
-  if constexpr (kAlign == 16) {
-    const int size = min(16, max(0, K - k));
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                 ::"r"(to), "l"(size > 0 ? row + k : any), "r"(size) : "memory");
-  } else {
-    const int skew = (int)skew_of(row);
-    const int8_t* p = row + (k - skew);
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      const int size = K > 0 ? min(4, max(0, K - k + skew - 4 * i)) : 0;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
-                   ::"r"(to + 4u * i), "l"(size > 0 ? p + 4 * i : any - skew_of(any)), "r"(size) : "memory");
-    }
-  }
+__device__ __forceinline__ int row_shift(const int8_t* row) {
+  return kAlign == 16 ? 0 : (int)(reinterpret_cast<uintptr_t>(row) & 15);
 }
 
-// Those sixteen codes back from shared memory, in the row's byte order.
-template <int kAlign>
-__device__ __forceinline__ void piece16(uint32_t (&v)[4], uint32_t from, const int8_t* row) {
-  if constexpr (kAlign == 16) {
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(from) : "memory");
-  } else {
-    uint32_t w[5];
+// Asynchronous copy of the chunk that starts at code k (a multiple of 16) of the row's
+// aligned chunks to shared memory, zeros from code K on; dead: K = -16.  Nothing past the
+// row's K codes is read, and before them at most the rest of the first one's aligned 16
+// bytes, which lie in the same allocation.  any: an address to name where nothing is read.
+__device__ __forceinline__ void copy_chunk(uint32_t to, const int8_t* row, int shift, int k, int K, const int8_t* any) {
+  const int size = min(16, max(0, K - k + shift));
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+               ::"r"(to), "l"(size > 0 ? row + (k - shift) : any), "r"(size) : "memory");
+}
+__device__ __forceinline__ const int8_t* aligned16(const int8_t* p) {
+  return reinterpret_cast<const int8_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+}
+
+__device__ __forceinline__ void lds_chunk(uint32_t (&v)[4], uint32_t from) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(from) : "memory");
+}
+
+// Sixteen codes from two neighbouring chunks of a row with that shift.
+__device__ __forceinline__ void merge16(uint32_t (&v)[4], const uint32_t (&lo)[4], const uint32_t (&hi)[4], int shift) {
+  const bool two = shift & 8, one = shift & 4;
+  uint32_t t[6], u[5];
 #pragma unroll
-    for (int i = 0; i < 5; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(from + 4u * i) : "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * skew_of(row));
+  for (int i = 0; i < 6; ++i) {
+    const uint32_t a = i < 4 ? lo[i < 4 ? i : 0] : hi[i < 4 ? 0 : i - 4];
+    const uint32_t b = i + 2 < 4 ? lo[i + 2 < 4 ? i + 2 : 0] : hi[i + 2 < 4 ? 0 : i - 2];
+    t[i] = two ? b : a;
   }
+#pragma unroll
+  for (int i = 0; i < 5; ++i) u[i] = one ? t[i + 1] : t[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(u[i], u[i + 1], 8u * (uint32_t)(shift & 3));
 }
 
 // Four codes as fp16: a code's byte with its sign bit flipped is code + 128, under the

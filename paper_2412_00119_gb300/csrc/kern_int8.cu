@@ -10,6 +10,7 @@ int64_t int8_workspace(int64_t n, int K, int N) {
 }
 
 cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
+  if (A.n <= kFewRows) return launch_int8_few(A, st);
   const int64_t want = int8_workspace(A.n, A.K, A.N);
   if (want > 0 && workspace && workspace_bytes >= want) return launch_int8_pair(A, workspace, st, 0);
   return launch_int8_tile(A, st, 0);

@@ -7,16 +7,17 @@
 // chunk's sums are added to int32 registers while the next chunk's MMAs run.
 //
 // A CTA computes 128 channels (MMA M; lanes of tensor memory) x NT rows (MMA N) over
-// its share of K; the kSplit CTAs of a cluster share K, and add their int32 sums
-// through distributed shared memory in a fixed order (integers: any order gives the
-// same).  Channels on M: a narrow batch costs narrow MMAs, and a warp's lanes hold 32
+// its share of K; the CTAs of a cluster share K, and add their int32 sums through
+// distributed shared memory in a fixed order (integers: any order gives the same).
+// Channels on M: a narrow batch costs narrow MMAs, and a warp's lanes hold 32
 // neighbouring channels of a row, as the output wants them.  Warps of a CTA:
 //   - 16 workers in four groups that take the k-steps (64 codes of every row) in turn: a
-//     lane copies its 16 codes of each row kDeep turns ahead (asynchronous copies to
-//     places that it alone reads: no barrier, and more in flight than registers allow),
-//     turns them into fp16 (128B swizzle) and its warp arrives on "full"; between them
-//     the workers drain finished chunks;
-//   - one warp issues the MMAs, committing to "empty" per k-step and "done" per chunk.
+//     warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring of
+//     its own: more in flight than registers allow), turns them into fp16 (128B
+//     swizzle) and arrives on "full"; between them the workers drain finished chunks;
+//   - two warps issue the MMAs of even and odd k-steps, each into accumulators of its own
+//     (one issuer's wait, fence, four MMAs and commit take 450 clocks, narrow ones' pace),
+//     committing to "empty" per k-step and "done" per chunk.
 // Every wait is bounded; if one expires the CTA's partial sums are made again on CUDA
 // cores, so the output is always whole.
 #include <algorithm>
@@ -34,26 +35,31 @@ using namespace i8;
 constexpr int CM = 128;                 // channels of a tile
 constexpr int KS = 64;                  // codes of a k-step (a 128-byte row of fp16)
 constexpr int kWorkers = 16;
-constexpr int kThreads = 32 * (kWorkers + 1);
+constexpr int kIssuers = 2;
+constexpr int kThreads = 32 * (kWorkers + kIssuers);
 constexpr int kMaxSplit = 8;
 constexpr int kGroups = 4;              // worker groups, each a k-step of its own
-constexpr int kChunk = 16;              // k-steps per accumulator: 1024 k
+constexpr int kChunk = 16 * kIssuers;   // k-steps between drains: 1024 k per accumulator
 constexpr int kSmemBytes = 225 * 1024;  // for stages and copies in flight
 constexpr int64_t kMaxRows = 65535ll * 128;   // rows of a launch (the grid's y limit)
 
 template <int NT, int kAlign> struct Cfg {
   static constexpr int kUnits = (CM + NT) / 32;                // 8-row units of a k-step per warp
-  static constexpr int kPieceBytes = kAlign == 16 ? 16 : 20;   // a lane's copy of 16 codes
-  static constexpr int kTurnBytes = 32 * kWorkers * kUnits * kPieceBytes;
+  // a unit in the ring: 4 chunks of 16 codes per row, or 5 (int8_common.cuh)
+  static constexpr int kUnitBytes = 8 * 16 * (kAlign == 16 ? 4 : 5);
+  static constexpr int kTurnBytes = kWorkers * kUnits * kUnitBytes;
   static constexpr int kStageBytes = (CM + NT) * 128;
-  static constexpr int stages(int deep) { return std::min(8, (kSmemBytes - deep * kTurnBytes) / kStageBytes); }
-  // Turns in flight, and stages: at least one per group.  (A warp that waits for its
-  // stage's last use has seen the k-step kGroups + kStages back consumed; with fewer
-  // stages that says nothing of the use before the last, whose phase has the same parity.)
+  static constexpr int stages(int deep) {
+    return std::min(8, (kSmemBytes - deep * kTurnBytes) / kStageBytes) / kIssuers * kIssuers;
+  }
+  // Turns in flight, and stages: at least one per group, and a stage always the same
+  // issuer's.  (A warp that waits for its stage's last use has seen the k-step kGroups +
+  // kStages back consumed; with fewer stages that says nothing of the use before the last,
+  // whose phase has the same parity.)
   static constexpr int kDeep = stages(3) >= kGroups ? 3 : (stages(2) >= kGroups ? 2 : 1);
   static constexpr int kRingBytes = kDeep * kTurnBytes;
   static constexpr int kStages = stages(kDeep);
-  static constexpr int kTmemCols = NT <= 32 ? 64 : (NT <= 64 ? 128 : 256);
+  static constexpr int kTmemCols = NT <= 32 ? 128 : (NT <= 64 ? 256 : 512);
   static constexpr int kSumPitch = CM + 4;                     // int32 per row of the exchange
   static_assert(4 * kSumPitch * NT <= kStages * kStageBytes, "exchange fits the stages");
   static_assert(kStages >= kGroups && kStages <= kChunk, "a chunk is drained before the one after the next starts");
@@ -134,10 +140,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sh->done[b], 1);
+      mbar_init(&sh->done[b], kIssuers);
       mbar_init(&sh->drained[b], kWorkers);
     }
-    mbar_init(&sh->left, 1);
+    mbar_init(&sh->left, kIssuers);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -150,31 +156,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sh->tmem_base;
+  // Unit u: rows 32 u + 8 q .. + 7 of the tile's CM weight and NT activation rows, a lane 16
+  // codes of a row.
+  const int grp = warp >> 2, q = warp & 3;
+  const int r = 8 * q + (lane >> 2), c = lane & 3;
+  if (warp < kWorkers && c == 0) {
+    // the first turn's weights on their way to L2 while the launch before this one ends
+    const int k = KS * (first + grp);
+#pragma unroll
+    for (int u = 0; u < CM / 32; ++u)
+      if (j0 + r + 32 * u < A.N && k < A.K)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(A.w + (int64_t)(j0 + r + 32 * u) * A.ldw + k));
+  }
   pdl_wait();
   pdl_trigger();
 
   if (warp < kWorkers) {
     // ---------------- workers ----------------
-    // Unit u: rows 32 u + 8 q .. + 7 of the tile's CM weight and NT activation rows, a
-    // lane 16 codes of a row.
-    const int grp = warp >> 2, q = warp & 3;
-    const int r = 8 * q + (lane >> 2), c = lane & 3;
     const int8_t* wrow = A.w + (int64_t)(j0 + r) * A.ldw;
     const int8_t* arow = A.a + (i0 + r) * A.lda;
+    const int8_t* any = aligned16(A.w);
+    const int64_t wstep = 32 * A.ldw, astep = 32 * A.lda;
     // 32 bytes of fp16 per lane: chunks 2 c and 2 c + 1 of the row, swizzled
     const uint32_t at = smem_u32(base) + 128u * (uint32_t)r + ((32u * (uint32_t)c) ^ (16u * (uint32_t)(r & 7)));
-    // the lane's pieces: written by its own copies, read by itself alone
-    constexpr uint32_t kPieceStep = 32 * C::kPieceBytes;
-    const uint32_t mine = smem_u32(ring) + (uint32_t)(warp * kDeep * kUnits) * kPieceStep + (uint32_t)(lane * C::kPieceBytes);
-    auto row_of = [&](int u) { return u < CM / 32 ? wrow + 32 * u * A.ldw : arow + 32 * (u - CM / 32) * A.lda; };
+    const uint32_t mine = smem_u32(ring) + (uint32_t)(warp * kDeep * kUnits * C::kUnitBytes) +
+                          (uint32_t)((lane >> 2) * (C::kUnitBytes / 8) + 16 * c);
     auto copy = [&](int ks, int slot) {
-      const int k = KS * (first + ks) + 16 * c;
-      const uint32_t to = mine + (uint32_t)(slot * kUnits) * kPieceStep;
       if (ks < steps) {
+        const int k = KS * (first + ks) + 16 * c;
+        uint32_t to = mine + (uint32_t)(slot * kUnits * C::kUnitBytes);
+        const int8_t* row = wrow;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
+        for (int u = 0; u < kUnits; ++u, to += C::kUnitBytes) {
+          if (u == CM / 32) row = arow;
           const bool live = u < CM / 32 ? j0 + r + 32 * u < A.N : i0 + r + 32 * (u - CM / 32) < A.n;
-          copy16<kAlign>(to + u * kPieceStep, row_of(u), k, live ? A.K : 0, A.w);
+          const int shift = row_shift<kAlign>(row);
+          copy_chunk(to, row, shift, k, live ? A.K : -16, any);
+          if (kAlign != 16 && c == 0) copy_chunk(to + 64, row, shift, k + 64, live ? A.K : -16, any);
+          row += u < CM / 32 ? wstep : astep;
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -193,13 +212,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
       ok = __all_sync(kFull, mbar_wait(&sh->done[b], (uint32_t)(drained >> 1) & 1u, failed));
       if (!ok) return;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      // (the odd k-steps' accumulator has nothing in a chunk of one)
+      const int both = min(kIssuers, steps - drained * kChunk);
+#pragma unroll 1
+      for (int m = 0; m < both; ++m)
 #pragma unroll
-      for (int e = 0; e < kCols; e += 8) {
-        uint32_t v[8];
-        tmem_load8(v, tacc + (uint32_t)(b * NT + e));
+        for (int e = 0; e < kCols; e += 8) {
+          uint32_t v[8];
+          tmem_load8(v, tacc + (uint32_t)((kIssuers * b + m) * NT + e));
 #pragma unroll
-        for (int x = 0; x < 8; ++x) acc[e + x] += __float2int_rn(__uint_as_float(v[x]));
-      }
+          for (int x = 0; x < 8; ++x) acc[e + x] += __float2int_rn(__uint_as_float(v[x]));
+        }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->drained[b]);
@@ -224,17 +247,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
       if (!ok) break;
       asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
       const uint32_t to = at + s * (uint32_t)C::kStageBytes;
-      const uint32_t from = mine + (uint32_t)(slot * kUnits) * kPieceStep;
+      if (kAlign != 16) __syncwarp();   // (chunks that other lanes copied)
+      const uint32_t from = mine + (uint32_t)(slot * kUnits * C::kUnitBytes);
+      constexpr int kBatch = 4;   // units whose loads are in flight together
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        uint32_t v[4], h[4];
-        piece16<kAlign>(v, from + u * kPieceStep, row_of(u));
-        codes_f16(v[0], h[0], h[1]);
-        codes_f16(v[1], h[2], h[3]);
-        sts128(to + 4096u * u, h);
-        codes_f16(v[2], h[0], h[1]);
-        codes_f16(v[3], h[2], h[3]);
-        sts128((to + 4096u * u) ^ 16u, h);
+      for (int u0 = 0; u0 < kUnits; u0 += kBatch) {
+        uint32_t v[kBatch][4], h[4];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (u0 + u < kUnits) lds_chunk(v[u], from + (uint32_t)((u0 + u) * C::kUnitBytes));
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          if (u0 + u < kUnits) {
+            if constexpr (kAlign != 16) {
+              uint32_t lo[4], hi[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) lo[i] = v[u][i];
+              lds_chunk(hi, from + (uint32_t)((u0 + u) * C::kUnitBytes) + 16u);
+              merge16(v[u], lo, hi,
+                      row_shift<kAlign>(u0 + u < CM / 32 ? wrow + (u0 + u) * wstep : arow + (u0 + u - CM / 32) * astep));
+            }
+            const uint32_t dst = to + 4096u * (uint32_t)(u0 + u);
+            codes_f16(v[u][0], h[0], h[1]);
+            codes_f16(v[u][1], h[2], h[3]);
+            sts128(dst, h);
+            codes_f16(v[u][2], h[0], h[1]);
+            codes_f16(v[u][3], h[2], h[3]);
+            sts128(dst ^ 16u, h);
+          }
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->full[s]);
@@ -253,12 +294,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
       for (int e = 0; e < kCols; ++e) to[(kCols * (warp >> 2) + e) * C::kSumPitch] = acc[e];
     }
   } else {
-    // ---------------- MMA issuer ----------------
+    // ---------------- MMA issuers ----------------
+    const int m = warp - kWorkers;
     const bool lead = elect_one();
-    const uint32_t d = uniform(tmem);
+    const uint32_t d = uniform(tmem) + (uint32_t)(m * NT);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
     constexpr uint32_t kIdesc = idesc_f16(CM, NT);
-    uint32_t s = 0, ph = 0;
+    uint32_t s = (uint32_t)m, ph = 0;
     bool ok = true;
 #pragma unroll 1
     for (int ch = 0; ch < chunks && ok; ++ch) {
@@ -268,8 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
       const int end = min(steps, (ch + 1) * kChunk);
+      uint32_t accumulate = 0u;
 #pragma unroll 1
-      for (int ks = ch * kChunk; ks < end && ok; ++ks) {
+      for (int ks = ch * kChunk + m; ks < end && ok; ks += kIssuers) {
         ok = __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
         if (!ok) break;
         // the workers' stores, acquired above, before the MMAs' reads
@@ -280,11 +323,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
         if (lead) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            mma_f16(d + (uint32_t)(b * NT), ad + 2 * e, bd + 2 * e, kIdesc, (ks > ch * kChunk || e > 0) ? 1u : 0u);
+            mma_f16(d + (uint32_t)(kIssuers * b * NT), ad + 2 * e, bd + 2 * e, kIdesc, e > 0 ? 1u : accumulate);
           mma_commit(&sh->empty[s]);
         }
-        if (++s == (uint32_t)kStages) {
-          s = 0;
+        accumulate = 1u;
+        s += kIssuers;
+        if (s >= (uint32_t)kStages) {
+          s -= kStages;
           ph ^= 1u;
         }
       }
@@ -331,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
   const int size = A.type == BMLP_F32 || A.type == BMLP_I32 ? 4 : 2;
   const bool vec = ((reinterpret_cast<uintptr_t>(A.out) | (uintptr_t)(A.ldo * size)) & (uintptr_t)(4 * size - 1)) == 0;
   const int nw32 = 2 * ((A.N + 63) / 64);
-  for (int t = (int)rank + split * warp; t < NT; t += split * (kWorkers + 1)) {
+  for (int t = (int)rank + split * warp; t < NT; t += split * (kWorkers + kIssuers)) {
     const int64_t i = i0 + t;
     if (i >= A.n) break;
     const uint32_t src = smem_u32(sums) + 4u * (uint32_t)(t * C::kSumPitch + 4 * lane);

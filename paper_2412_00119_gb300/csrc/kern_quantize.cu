@@ -10,7 +10,14 @@
 // The maximum is taken on the bits of |u| as unsigned integers, whose order is the
 // values' order with infinities and NaNs on top: one comparison finds those too.
 //
-// A CTA per row: the values are read twice (the second time from L1 or L2).
+// k_quantize_regs: a row's threads (a warp, or a CTA of up to 1,024) hold it in
+// registers, so memory is read and written once.  Vectors of 16 bytes where the rows
+// of every buffer allow them, else of 4 bytes or single values.  Bound: memory.
+//
+// k_quantize_long: rows too long for that, read twice.
+#include <algorithm>
+#include <type_traits>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -48,75 +55,323 @@ __device__ __forceinline__ RowScale row_scale(uint32_t abits, float sumsq, int K
   return r;
 }
 
-// A value's code; inv == 0 (nothing to code, or a row that is not finite): 0.
-__device__ __forceinline__ int code(float u, float inv) {
-  const float c = inv == 0.0f ? 0.0f : __fmul_rn(u, inv);
-  return min(127, max(-127, __float2int_rn(c)));
+// |a| against the maximum so far; NaN if either is.
+__device__ __forceinline__ float max_nan(float m, float a) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(a)));
+  return r;
 }
 
-constexpr int kThreads = 256;
+// A code in the low byte: rint by an addition that leaves a unit in the last place
+// (|u inv| <= 127 (1 + 2^-22)).
+__device__ __forceinline__ uint32_t code(float u, float inv) {
+  return __float_as_uint(__fadd_rn(__fmul_rn(u, inv), 12582912.0f));   // 1.5 2^23
+}
 
-template <typename T, bool kNorm>
-__global__ void __launch_bounds__(kThreads) k_quantize(const QuantArgs A) {
-  __shared__ float ssum[kThreads / 32];
-  __shared__ uint32_t smax[kThreads / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const T* gain = static_cast<const T*>(A.gain);
-  for (int64_t row = blockIdx.x; row < A.n; row += gridDim.x) {
-    const T* x = static_cast<const T*>(A.x) + row * A.ldx;
-    const T* res = kNorm && A.res ? static_cast<const T*>(A.res) + row * A.ldr : nullptr;
-    T* sum = kNorm && A.sum ? static_cast<T*>(A.sum) + row * A.lds : nullptr;
-    auto h_of = [&](int i) { return res ? __fadd_rn(to_f32(x[i]), to_f32(res[i])) : to_f32(x[i]); };
-    auto u_of = [&](float h, int i) { return kNorm && gain ? __fmul_rn(h, to_f32(gain[i])) : h; };
-    float sq = 0.0f;
-    uint32_t most = 0u;
-    for (int i = threadIdx.x; i < A.K; i += kThreads) {
-      const float h = h_of(i);
-      sq += h * h;
-      most = max(most, __float_as_uint(u_of(h, i)) & 0x7FFFFFFFu);
-    }
+// Sum and maximum over a row's threads: the warp, or the CTA's warps (one barrier).
+template <bool kWarpRow>
+__device__ __forceinline__ void row_reduce(float& sq, uint32_t& most, bool norm, int turn) {
+  if (norm) {
+#pragma unroll
     for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(kFullMask, sq, o);
-    most = __reduce_max_sync(kFullMask, most);
+  }
+  most = __reduce_max_sync(kFullMask, most);
+  if constexpr (!kWarpRow) {
+    // rows alternate between two places: a warp may write the next row's while another
+    // still reads this one's
+    __shared__ float ssums[2][32];
+    __shared__ uint32_t smaxs[2][32];
+    float* ssum = ssums[turn & 1];
+    uint32_t* smax = smaxs[turn & 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     if (lane == 0) {
       ssum[warp] = sq;
       smax[warp] = most;
     }
     __syncthreads();
-    sq = 0.0f;
-    most = 0u;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      sq += ssum[w];
-      most = max(most, smax[w]);
+    sq = lane < warps ? ssum[lane] : 0.0f;
+    most = lane < warps ? smax[lane] : 0u;
+    if (norm) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(kFullMask, sq, o);
     }
-    const RowScale r = row_scale(most, sq, A.K, A.eps, kNorm);
-    // the row's values again: a thread writes its own elements of sum_out only after
-    // it has read them (sum_out may be x or res)
-    for (int i = threadIdx.x; i < A.K; i += kThreads) {
-      const float h = h_of(i);
-      if (sum) sum[i] = from_f32<T>(h);
-      A.q[row * A.ldq + i] = (int8_t)code(u_of(h, i), r.inv);
-    }
-    if (threadIdx.x == 0) A.scale[row] = r.scale;
-    __syncthreads();
+    most = __reduce_max_sync(kFullMask, most);
   }
 }
 
+// V values as they lie in memory.
+template <typename T, int V> struct Pack {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  uint32_t w[(kBytes + 3) / 4];
+  // `left` values of the row from p on, zeros after them
+  __device__ __forceinline__ void load(const T* p, int left) {
+#pragma unroll
+    for (int i = 0; i < (kBytes + 3) / 4; ++i) w[i] = 0u;
+    if (left >= V) {
+      if constexpr (kBytes == 16) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else if constexpr (kBytes == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else {
+        w[0] = *reinterpret_cast<const uint16_t*>(p);
+      }
+    } else if constexpr (V > 1) {
+#pragma unroll
+      for (int i = 0; i < V - 1; ++i)
+        if (i < left) {
+          if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+          else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
+        }
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int left) const {
+    if (left >= V) {
+      if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+      else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+      else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    } else if constexpr (V > 1) {
+#pragma unroll
+      for (int i = 0; i < V - 1; ++i)
+        if (i < left) {
+          if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i) = w[i];
+          else *reinterpret_cast<uint16_t*>(p + i) = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+        }
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[i]);
+    else if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (16 * (i % 2)))));
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&f)[V]) {
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[i] = __float_as_uint(f[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        const T a = from_f32<T>(f[i]), b = from_f32<T>(i + 1 < V ? f[i + 1] : 0.0f);
+        w[i / 2] = (uint32_t)*reinterpret_cast<const uint16_t*>(&a) | (uint32_t)*reinterpret_cast<const uint16_t*>(&b) << 16;
+      }
+    }
+  }
+};
+
+template <int V>
+__device__ __forceinline__ void store_codes(int8_t* p, const float (&u)[V], float inv, uint32_t live, int left) {
+  uint32_t w[(V + 3) / 4];
+#pragma unroll
+  for (int i = 0; i < (V + 3) / 4; ++i) {
+    uint32_t c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = 4 * i + e < V ? code(u[4 * i + e < V ? 4 * i + e : 0], inv) : 0u;
+    const uint32_t lo = V > 1 ? __byte_perm(c[0], c[1], 0x0040) : c[0];
+    w[i] = (V > 2 ? __byte_perm(lo, __byte_perm(c[2], c[3], 0x0040), 0x5410) : lo) & live;
+  }
+  if (left >= V) {
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else if constexpr (V == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    else *p = (int8_t)w[0];
+  } else if constexpr (V > 1) {
+#pragma unroll
+    for (int i = 0; i < V - 1; ++i)
+      if (i < left) p[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+constexpr int kRowsPerCta = 8;   // rows of a CTA with a warp each
+// What is done to a row (residual: its registers are there only where it is).
+constexpr int kPlain = 0, kNormed = 1, kResidual = 2;
+
+// A row's T threads hold it: vector v of thread t is v T + t, NV vectors of V values
+// each.  The grid walks the rows; a row's values are loaded while the row before is
+// reduced and written, and the gain stays in registers (kAhead; without it neither,
+// where the registers do not hold both).
+template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead>
+__global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize_regs(const QuantArgs A) {
+  pdl_wait();
+  pdl_trigger();
+  const int threads = kWarpRow ? 32 : (int)blockDim.x;
+  const int tid = kWarpRow ? (int)(threadIdx.x & 31) : (int)threadIdx.x;
+  const int64_t step = kWarpRow ? (int64_t)gridDim.x * kRowsPerCta : (int64_t)gridDim.x;
+  int64_t row = kWarpRow ? (int64_t)blockIdx.x * kRowsPerCta + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
+  const T* x = static_cast<const T*>(A.x);
+  constexpr bool kNorm = kMode != kPlain, kRes = kMode == kResidual;
+  const T* res = static_cast<const T*>(A.res);
+  T* sum = kNorm ? static_cast<T*>(A.sum) : nullptr;
+  const T* gain = kNorm ? static_cast<const T*>(A.gain) : nullptr;
+  auto at = [&](int v) { return (v * threads + tid) * V; };
+  Pack<T, V> px[NV], pr[kRes ? NV : 1], pg[kAhead ? NV : 1];
+  if (kAhead && gain) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) pg[kAhead ? v : 0].load(gain + at(v), A.K - at(v));
+  }
+  auto load = [&](int64_t i) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) px[v].load(x + i * A.ldx + at(v), A.K - at(v));
+    if constexpr (kRes) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) pr[v].load(res + i * A.ldr + at(v), A.K - at(v));
+    }
+  };
+  if (kAhead && row < A.n) load(row);
+  for (int turn = 0; row < A.n; row += step, turn ^= 1) {
+    if (!kAhead) load(row);
+    float u[NV][V];
+    float sq = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        u[v][i] = px[v].get(i);
+        if constexpr (kRes) u[v][i] = __fadd_rn(u[v][i], pr[v].get(i));
+      }
+    // (this row is read: sum_out may be x or res)
+    if (kAhead && row + step < A.n) load(row + step);
+    if (sum) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        Pack<T, V> ps;
+        ps.set(u[v]);
+        ps.store(sum + row * A.lds + at(v), A.K - at(v));
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (!kAhead && gain) pg[0].load(gain + at(v), A.K - at(v));
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (kNorm) sq += u[v][i] * u[v][i];
+        if (gain) u[v][i] = __fmul_rn(u[v][i], pg[kAhead ? v : 0].get(i));
+        most = max_nan(most, u[v][i]);
+      }
+    }
+    uint32_t mbits = __float_as_uint(most);
+    row_reduce<kWarpRow>(sq, mbits, kNorm, turn);
+    const RowScale r = row_scale(mbits, sq, A.K, A.eps, kNorm);
+    const uint32_t live = r.inv == 0.0f ? 0u : 0xFFFFFFFFu;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) store_codes<V>(A.q + row * A.ldq + at(v), u[v], r.inv, live, A.K - at(v));
+    if (tid == 0) A.scale[row] = r.scale;
+  }
+}
+
+constexpr int kThreads = 1024;
+
+template <typename T, int kMode>
+__global__ void __launch_bounds__(kThreads) k_quantize_long(const QuantArgs A) {
+  constexpr bool kNorm = kMode != kPlain;
+  pdl_wait();
+  pdl_trigger();
+  const T* gain = static_cast<const T*>(A.gain);
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+  const T* res = kNorm && A.res ? static_cast<const T*>(A.res) + row * A.ldr : nullptr;
+  T* sum = kNorm && A.sum ? static_cast<T*>(A.sum) + row * A.lds : nullptr;
+  auto h_of = [&](uint32_t i) { return res ? __fadd_rn(to_f32(x[i]), to_f32(res[i])) : to_f32(x[i]); };
+  auto u_of = [&](float h, uint32_t i) { return kNorm && gain ? __fmul_rn(h, to_f32(gain[i])) : h; };
+  float sq = 0.0f, most = 0.0f;
+  for (uint32_t i = threadIdx.x; i < (uint32_t)A.K; i += kThreads) {
+    const float h = h_of(i);
+    sq += h * h;
+    most = max_nan(most, u_of(h, i));
+  }
+  uint32_t mbits = __float_as_uint(most);
+  row_reduce<false>(sq, mbits, kNorm, 0);
+  const RowScale r = row_scale(mbits, sq, A.K, A.eps, kNorm);
+  const uint32_t live = r.inv == 0.0f ? 0u : 0xFFFFFFFFu;
+  // the row's values again: a thread writes its own elements of sum_out only after
+  // it has read them (sum_out may be x or res)
+  for (uint32_t i = threadIdx.x; i < (uint32_t)A.K; i += kThreads) {
+    const float h = h_of(i);
+    if (sum) sum[i] = from_f32<T>(h);
+    A.q[row * A.ldq + i] = (int8_t)(code(u_of(h, i), r.inv) & live);
+  }
+  if (threadIdx.x == 0) A.scale[row] = r.scale;
+}
+
+// A warp per row.  With 32 values per lane the next row is loaded ahead where a 16-bit row's
+// norm is made (65,536 x 784 34 us on four CTAs per SM, without 42); fp32 rows and rows that
+// are only coded run faster from more warps (60,000 x 784 fp32 46, ahead 55; 60,000 x 1000
+// bf16 coded 28.6, ahead 32.5).
+template <typename T, int kMode, int V, int NV>
+cudaError_t launch_warp_rows(const QuantArgs& A, cudaStream_t st) {
+  constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain);
+  const int64_t ctas = std::min((A.n + kRowsPerCta - 1) / kRowsPerCta, (int64_t)(kAhead && V * NV > 16 ? 4 : 8) * sm_count());
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta), 0, st,
+                       true, A);
+}
+
+// A CTA per row: 1,024 threads an SM.
+template <typename T, int kMode, int V, int NV>
+cudaError_t launch_cta_rows(const QuantArgs& A, cudaStream_t st) {
+  const int threads = (A.K + 32 * V * NV - 1) / (32 * V * NV) * 32;
+  constexpr bool kAhead = !(kMode != kPlain && V * NV > (sizeof(T) == 2 ? 16 : 8));
+  const int64_t ctas = kAhead ? std::min(A.n, (int64_t)(1024 / threads) * sm_count()) : A.n;
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead>, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st,
+                       true, A);
+}
+
+// Which form (us, rows in bf16 unless said): rows that a warp holds in at most kWarpMost
+// vectors per lane get a warp each (65,536 x 784 34, by CTAs 58; 60,000 x 784 fp32 46, by CTAs
+// 62).  Else a CTA per row, with one vector per thread for few rows (1 x 8192 2.5, two 2.8, four 4.1), and
+// for many as many as the registers hold beside the next row's: four without a norm
+// (8192 x 8192 30, two 34, one 44), two with it (8191 x 4096 with residual 40, four 57 for want of registers).
+template <typename T, int kMode, int V>
+cudaError_t launch_v(const QuantArgs& A, cudaStream_t st) {
+  constexpr int kWarpMost = V == 8 ? 4 : 8;
+  const int vecs = A.K / V + (A.K % V != 0);
+  if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1>(A, st);
+  if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2>(A, st);
+  if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4>(A, st);
+  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost>(A, st);
+  if (vecs > 4096)
+    return launch_kernel(k_quantize_long<T, kMode>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
+  const bool few = A.n <= 2 * sm_count();
+  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4>(A, st);
+  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2>(A, st);
+  return launch_cta_rows<T, kMode, V, 1>(A, st);
+}
+
+template <typename T, int kMode>
+cudaError_t launch_type(const QuantArgs& A, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool many = A.n > 1;
+  const uintptr_t wide = reinterpret_cast<uintptr_t>(A.x) | reinterpret_cast<uintptr_t>(A.res) |
+                         reinterpret_cast<uintptr_t>(A.gain) | reinterpret_cast<uintptr_t>(A.sum) |
+                         (many ? (uintptr_t)((A.ldx | (A.res ? A.ldr : 0) | (A.sum ? A.lds : 0)) * (int64_t)sizeof(T)) : 0);
+  const uintptr_t codes = reinterpret_cast<uintptr_t>(A.q) | (many ? (uintptr_t)A.ldq : 0);
+  if (wide % 16 == 0 && codes % V == 0) return launch_v<T, kMode, V>(A, st);
+  if (sizeof(T) == 2 && wide % 4 == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1>(A, st);
+  return launch_v<T, kMode, 1>(A, st);
+}
+
 template <typename T>
-cudaError_t launch_type(const QuantArgs& A, bool norm, cudaStream_t st) {
-  const unsigned grid = (unsigned)(A.n < 65536 ? A.n : 65536);
-  if (norm) k_quantize<T, true><<<grid, kThreads, 0, st>>>(A);
-  else k_quantize<T, false><<<grid, kThreads, 0, st>>>(A);
-  return cudaGetLastError();
+cudaError_t launch_any(const QuantArgs& A, bool norm, cudaStream_t st) {
+  return !norm ? launch_type<T, kPlain>(A, st) : (A.res ? launch_type<T, kResidual>(A, st) : launch_type<T, kNormed>(A, st));
 }
 
 }  // namespace
 
-cudaError_t launch_quantize(const QuantArgs& A, bool norm, cudaStream_t st) {
-  switch (A.type) {
-    case BMLP_F32: return launch_type<float>(A, norm, st);
-    case BMLP_F16: return launch_type<__half>(A, norm, st);
-    default: return launch_type<__nv_bfloat16>(A, norm, st);
+cudaError_t launch_quantize(const QuantArgs& all, bool norm, cudaStream_t st) {
+  constexpr int64_t kMaxRows = 1ll << 30;   // of a launch
+  const int64_t size = all.type == BMLP_F32 ? 4 : 2;
+  for (int64_t off = 0; off < all.n; off += kMaxRows) {
+    QuantArgs A = all;
+    A.n = all.n - off < kMaxRows ? all.n - off : kMaxRows;
+    A.x = static_cast<const uint8_t*>(all.x) + off * all.ldx * size;
+    if (all.res) A.res = static_cast<const uint8_t*>(all.res) + off * all.ldr * size;
+    if (all.sum) A.sum = static_cast<uint8_t*>(all.sum) + off * all.lds * size;
+    A.q += off * all.ldq;
+    A.scale += off;
+    const cudaError_t e = all.type == BMLP_F32 ? launch_any<float>(A, norm, st)
+                          : all.type == BMLP_F16 ? launch_any<__half>(A, norm, st)
+                                                 : launch_any<__nv_bfloat16>(A, norm, st);
+    if (e != cudaSuccess) return e;
   }
+  return cudaSuccess;
 }
 
 }  // namespace bk
