@@ -11,13 +11,17 @@
 // distributed shared memory in a fixed order (integers: any order gives the same).
 // Channels on M: a narrow batch costs narrow MMAs, and a warp's lanes hold 32
 // neighbouring channels of a row, as the output wants them.  Warps of a CTA:
-//   - 16 workers in four groups that take the k-steps (64 codes of every row) in turn: a
-//     warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring of
-//     its own: more in flight than registers allow), turns them into fp16 (128B
-//     swizzle) and arrives on "full"; between them the workers drain finished chunks;
-//   - two warps issue the MMAs of even and odd k-steps, each into accumulators of its own
-//     (one issuer's wait, fence, four MMAs and commit take 450 clocks, narrow ones' pace),
-//     committing to "empty" per k-step and "done" per chunk.
+//   - 16 workers in four groups that take the k-steps (128 codes of every row, or 64) in
+//     turn: a warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring
+//     of its own: more in flight than registers allow), turns them into fp16, the weights
+//     into tensor memory (a lane per channel) and the activations into shared memory (128B
+//     swizzle), and arrives on "full"; between them the workers drain finished chunks;
+//   - one or two warps issue the MMAs (two: of even and odd k-steps, each into accumulators
+//     of its own), committing to "empty" per k-step and "done" per chunk.
+// Bound: the workers' instructions (about 110 a warp for 64 codes of its rows, and 140 for
+// a turn whatever its length: k-steps of 128 where the ring has room), then the weights'
+// bytes.  With the fp16 weights in shared memory too, 60 KB moved through it per 64 codes at
+// NT = 32 and 96 KB at 128, in 570 and 750 clocks whatever the instructions.
 // Every wait is bounded; if one expires the CTA's partial sums are made again on CUDA
 // cores, so the output is always whole.
 #include <algorithm>
@@ -33,36 +37,46 @@ using namespace tc;
 using namespace i8;
 
 constexpr int CM = 128;                 // channels of a tile
-constexpr int KS = 64;                  // codes of a k-step (a 128-byte row of fp16)
 constexpr int kWorkers = 16;
-constexpr int kIssuers = 2;
-constexpr int kThreads = 32 * (kWorkers + kIssuers);
 constexpr int kMaxSplit = 8;
 constexpr int kGroups = 4;              // worker groups, each a k-step of its own
-constexpr int kChunk = 16 * kIssuers;   // k-steps between drains: 1024 k per accumulator
 constexpr int kSmemBytes = 225 * 1024;  // for stages and copies in flight
 constexpr int64_t kMaxRows = 65535ll * 128;   // rows of a launch (the grid's y limit)
 
 template <int NT, int kAlign> struct Cfg {
-  static constexpr int kUnits = (CM + NT) / 32;                // 8-row units of a k-step per warp
-  // a unit in the ring: 4 chunks of 16 codes per row, or 5 (int8_common.cuh)
-  static constexpr int kUnitBytes = 8 * 16 * (kAlign == 16 ? 4 : 5);
-  static constexpr int kTurnBytes = kWorkers * kUnits * kUnitBytes;
-  static constexpr int kStageBytes = (CM + NT) * 128;
+  static constexpr int kSub = NT <= 96 ? 2 : 1;                // 64 codes (a 128-byte row of fp16) each
+  static constexpr int kStep = 64 * kSub;                      // codes of a k-step
+  static constexpr int kIssuers = NT <= 64 ? 2 : 1;
+  static constexpr int kThreads = 32 * (kWorkers + kIssuers);
+  static constexpr int kChunk = 1024 / kStep * kIssuers;       // k-steps between drains: 1024 k per accumulator
+  // a row of the ring: chunks of 16 codes, one more where they are merged (int8_common.cuh)
+  static constexpr int kRow = kStep + (kAlign == 16 ? 0 : 16);
+  static constexpr int kTurnRows = 32 + NT / 4;                // rows of a warp: channels, activations
+  static constexpr int kTurnBytes = kWorkers * kTurnRows * kRow;
+  static constexpr int kStageBytes = NT * 128 * kSub;          // activations
+  static constexpr int kStageCols = 32 * kSub;                 // weights
+  static constexpr int kAccCols = 2 * kIssuers * NT;
   static constexpr int stages(int deep) {
-    return std::min(8, (kSmemBytes - deep * kTurnBytes) / kStageBytes) / kIssuers * kIssuers;
+    return std::min((512 - kAccCols) / kStageCols, std::min(8, (kSmemBytes - deep * kTurnBytes) / kStageBytes)) / 2 * 2;
   }
   // Turns in flight, and stages: at least one per group, and a stage always the same
   // issuer's.  (A warp that waits for its stage's last use has seen the k-step kGroups +
   // kStages back consumed; with fewer stages that says nothing of the use before the last,
   // whose phase has the same parity.)
-  static constexpr int kDeep = stages(3) >= kGroups ? 3 : (stages(2) >= kGroups ? 2 : 1);
+  static constexpr int kDeep = stages(4) >= kGroups ? 4 : (stages(3) >= kGroups ? 3 : (stages(2) >= kGroups ? 2 : 1));
   static constexpr int kRingBytes = kDeep * kTurnBytes;
   static constexpr int kStages = stages(kDeep);
-  static constexpr int kTmemCols = NT <= 32 ? 128 : (NT <= 64 ? 256 : 512);
+  static constexpr int kTmemCols = kAccCols + kStageCols * kStages <= 256 ? 256 : 512;
   static constexpr int kSumPitch = CM + 4;                     // int32 per row of the exchange
-  static_assert(4 * kSumPitch * NT <= kStages * kStageBytes, "exchange fits the stages");
+  static_assert(kAccCols + kStageCols * kStages <= 512, "tensor memory");
+  static_assert(4 * kSumPitch * NT <= kStages * kStageBytes + kRingBytes, "exchange fits");
   static_assert(kStages >= kGroups && kStages <= kChunk, "a chunk is drained before the one after the next starts");
+  // Place of chunk c of row r of the ring, from its row's start: swapped so that eight lanes
+  // that read a chunk of eight rows are on different banks (rows of 80 and 144 bytes are by
+  // themselves).
+  static __device__ __forceinline__ int chunk_at(int r, int c) {
+    return 16 * (kAlign != 16 ? c : (kSub == 2 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)));
+  }
 };
 
 struct __align__(8) TileShared {
@@ -116,10 +130,75 @@ __device__ __forceinline__ void store4(const Int8Args& A, int64_t i, int j, cons
   }
 }
 
+// What a lane's outputs need from memory: asked for before the sums are there.
+struct Factors {
+  float sw[4], bias[4], sa;
+  int thr[4];
+};
+
+// Outputs of a worker warp: rows rank + S (warp + 16 x) of the tile, a lane four channels, the
+// S partial sums of a row from the S CTAs' shared memory, all of them in flight together.
+template <int NT, int S>
+__device__ __forceinline__ void write_rows(const Int8Args& A, const int* sums, int pitch, int64_t i0, int j0, uint32_t rank,
+                                           const Factors& F) {
+  constexpr int kRows = (NT + kWorkers * S - 1) / (kWorkers * S);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = j0 + 4 * lane;
+  const int size = A.type == BMLP_F32 || A.type == BMLP_I32 ? 4 : 2;
+  const bool vec = ((reinterpret_cast<uintptr_t>(A.out) | (uintptr_t)(A.ldo * size)) & (uintptr_t)(4 * size - 1)) == 0;
+  const int nw32 = 2 * ((A.N + 63) / 64);
+  int4 p[kRows][S];
+#pragma unroll
+  for (int x = 0; x < kRows; ++x) {
+    const int t = (int)rank + S * (warp + kWorkers * x);
+    if (t < NT && i0 + t < A.n) {
+      const int* row = sums + t * pitch + 4 * lane;
+#pragma unroll
+      for (int q = 0; q < S; ++q) {
+        if constexpr (S == 1) p[x][q] = *reinterpret_cast<const int4*>(row);
+        else p[x][q] = ld_cluster(smem_u32(row), (uint32_t)q);
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < kRows; ++x) {
+    const int t = (int)rank + S * (warp + kWorkers * x);
+    const int64_t i = i0 + t;
+    if (t >= NT || i >= A.n) continue;
+    int4 v = p[x][0];
+#pragma unroll
+    for (int q = 1; q < S; ++q) {
+      v.x += p[x][q].x; v.y += p[x][q].y; v.z += p[x][q].z; v.w += p[x][q].w;
+    }
+    if (A.words) {
+      uint32_t bits = 0u;
+      bits |= (j + 0 < A.N && v.x >= F.thr[0]) ? 1u : 0u;
+      bits |= (j + 1 < A.N && v.y >= F.thr[1]) ? 2u : 0u;
+      bits |= (j + 2 < A.N && v.z >= F.thr[2]) ? 4u : 0u;
+      bits |= (j + 3 < A.N && v.w >= F.thr[3]) ? 8u : 0u;
+      bits <<= 4 * (lane & 7);
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(kFull, bits, o);
+      const int word = j0 / 32 + (lane >> 3);
+      if ((lane & 7) == 0 && word < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + word] = bits;
+    } else {
+      const float sa = __shfl_sync(kFull, F.sa, x);
+      switch (A.type) {
+        case BMLP_F32: store4<float>(A, i, j, v, sa, F.sw, F.bias, vec); break;
+        case BMLP_F16: store4<__half>(A, i, j, v, sa, F.sw, F.bias, vec); break;
+        case BMLP_BF16: store4<__nv_bfloat16>(A, i, j, v, sa, F.sw, F.bias, vec); break;
+        default: store4<int32_t>(A, i, j, v, sa, F.sw, F.bias, vec);
+      }
+    }
+  }
+}
+
 template <int NT, int kAlign>
-__global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int split, int expire) {
+__global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(const Int8Args A, int split, int expire) {
   using C = Cfg<NT, kAlign>;
-  constexpr int kStages = C::kStages, kUnits = C::kUnits, kDeep = C::kDeep;
+  constexpr int kStages = C::kStages, kDeep = C::kDeep, kIssuers = C::kIssuers, kChunk = C::kChunk;
+  // a warp's copies: units of kUnit rows, 4 kSub lanes per row
+  constexpr int kSub = C::kSub, kUnit = 8 / kSub;
+  constexpr int kUnitsA = 32 / kUnit, kUnitsB = NT / 4 / kUnit, kUnits = kUnitsA + kUnitsB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* ring = base + kStages * C::kStageBytes;
@@ -130,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
   const int64_t i0 = (int64_t)blockIdx.y * NT;
   volatile int* failed = &sh->failed;
   // this CTA's k-steps
-  const int all = (A.K + KS - 1) / KS;
+  const int all = (A.K + C::kStep - 1) / C::kStep;
   const int first = (int)((int64_t)all * rank / split), steps = (int)((int64_t)all * (rank + 1) / split) - first;
   const int chunks = (steps + kChunk - 1) / kChunk;
 
@@ -156,50 +235,77 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sh->tmem_base;
-  // Unit u: rows 32 u + 8 q .. + 7 of the tile's CM weight and NT activation rows, a lane 16
-  // codes of a row.
+  // A warp's rows of a k-step: channels 32 q .. + 31 of the tile and NT / 4 activation rows.
   const int grp = warp >> 2, q = warp & 3;
-  const int r = 8 * q + (lane >> 2), c = lane & 3;
+  const int r = lane / (4 * kSub), c = lane % (4 * kSub);   // copies: row of a unit, 16 of its codes
+  const int ja = j0 + 32 * q + r;                 // channel, + kUnit per unit
+  const int64_t ib = i0 + NT / 4 * q + r;         // row, + kUnit per unit
   if (warp < kWorkers && c == 0) {
     // the first turn's weights on their way to L2 while the launch before this one ends
-    const int k = KS * (first + grp);
+    const int k = C::kStep * (first + grp);
 #pragma unroll
-    for (int u = 0; u < CM / 32; ++u)
-      if (j0 + r + 32 * u < A.N && k < A.K)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(A.w + (int64_t)(j0 + r + 32 * u) * A.ldw + k));
+    for (int u = 0; u < kUnitsA; ++u)
+      if (ja + kUnit * u < A.N && k < A.K)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(A.w + (int64_t)(ja + kUnit * u) * A.ldw + k));
   }
   pdl_wait();
   pdl_trigger();
 
   if (warp < kWorkers) {
     // ---------------- workers ----------------
-    const int8_t* wrow = A.w + (int64_t)(j0 + r) * A.ldw;
-    const int8_t* arow = A.a + (i0 + r) * A.lda;
+    const int8_t* wrow = A.w + (int64_t)ja * A.ldw;
+    const int8_t* arow = A.a + ib * A.lda;
     const int8_t* any = aligned16(A.w);
-    const int64_t wstep = 32 * A.ldw, astep = 32 * A.lda;
-    // 32 bytes of fp16 per lane: chunks 2 c and 2 c + 1 of the row, swizzled
-    const uint32_t at = smem_u32(base) + 128u * (uint32_t)r + ((32u * (uint32_t)c) ^ (16u * (uint32_t)(r & 7)));
-    const uint32_t mine = smem_u32(ring) + (uint32_t)(warp * kDeep * kUnits * C::kUnitBytes) +
-                          (uint32_t)((lane >> 2) * (C::kUnitBytes / 8) + 16 * c);
+    const int64_t wstep = kUnit * A.ldw, astep = kUnit * A.lda;
+    uint8_t* const mine = ring + warp * kDeep * C::kTurnRows * C::kRow;
+    const bool whole = j0 + CM <= A.N && i0 + NT <= A.n;   // every row of the tile is one
+    const uint32_t ring_to = smem_u32(mine) + (uint32_t)(r * C::kRow);
     auto copy = [&](int ks, int slot) {
       if (ks < steps) {
-        const int k = KS * (first + ks) + 16 * c;
-        uint32_t to = mine + (uint32_t)(slot * kUnits * C::kUnitBytes);
-        const int8_t* row = wrow;
+        const int k = C::kStep * (first + ks) + 16 * c;
+        const uint32_t to = ring_to + (uint32_t)(slot * C::kTurnRows * C::kRow);
+        if (kAlign == 16 && whole && C::kStep * (first + ks + 1) <= A.K) {
+          const int8_t* row = wrow + k;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u, to += C::kUnitBytes) {
-          if (u == CM / 32) row = arow;
-          const bool live = u < CM / 32 ? j0 + r + 32 * u < A.N : i0 + r + 32 * (u - CM / 32) < A.n;
-          const int shift = row_shift<kAlign>(row);
-          copy_chunk(to, row, shift, k, live ? A.K : -16, any);
-          if (kAlign != 16 && c == 0) copy_chunk(to + 64, row, shift, k + 64, live ? A.K : -16, any);
-          row += u < CM / 32 ? wstep : astep;
+          for (int u = 0; u < kUnits; ++u) {
+            if (u == kUnitsA) row = arow + k;
+            // (the swap depends on the row's low bits: a unit of four alternates between two places)
+            const int place = C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                         ::"r"(to + (uint32_t)(u * kUnit * C::kRow + place)), "l"(row) : "memory");
+            row += u < kUnitsA ? wstep : astep;
+          }
+        } else {
+          const int8_t* row = wrow;
+#pragma unroll
+          for (int u = 0; u < kUnits; ++u) {
+            if (u == kUnitsA) row = arow;
+            const bool live = u < kUnitsA ? ja + kUnit * u < A.N : ib + kUnit * (u - kUnitsA) < A.n;
+            const int shift = row_shift<kAlign>(row);
+            const uint32_t unit = to + (uint32_t)(u * kUnit * C::kRow);
+            copy_chunk(unit + (uint32_t)C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c), row, shift, k, live ? A.K : -16, any);
+            if (kAlign != 16 && c == 0)
+              copy_chunk(unit + (uint32_t)C::kStep, row, shift, k + C::kStep, live ? A.K : -16, any);
+            row += u < kUnitsA ? wstep : astep;
+          }
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) copy(grp + kGroups * d, d);
+    // reads: a lane per channel; of the activations a row rb of a unit and a chunk cb, eight
+    // lanes (which meet in shared memory) two rows and, of 128 codes, a half of each
+    const uint8_t* const read_w = mine + lane * C::kRow;
+    const int rb = kSub == 2 ? 2 * (lane >> 4) + ((lane >> 2) & 1) : r;
+    const int cb = kSub == 2 ? 4 * (((lane >> 3) ^ (lane >> 2)) & 1) + (lane & 3) : c;
+    const uint8_t* const read_a = mine + (32 + rb) * C::kRow;
+    const int wshift = row_shift<kAlign>(A.w + (int64_t)(j0 + 32 * q + lane) * A.ldw);
+    // 32 bytes of fp16 per piece: chunks 2 (cb % 4) and one more of the row, swizzled (the swizzle
+    // goes by the row's low three bits: a unit of four alternates, as above)
+    uint8_t* const at = base + (cb >> 2) * (NT * 128) + 128 * (NT / 4 * q + rb);
+    const int swz0 = (32 * (cb & 3)) ^ (16 * (rb & 7));
+    const uint32_t lanes = (uint32_t)(32 * q) << 16;
     constexpr int kCols = NT / 4;   // accumulator columns of this warp
     int acc[kCols];
 #pragma unroll
@@ -246,37 +352,57 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
       ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
       if (!ok) break;
       asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
-      const uint32_t to = at + s * (uint32_t)C::kStageBytes;
-      if (kAlign != 16) __syncwarp();   // (chunks that other lanes copied)
-      const uint32_t from = mine + (uint32_t)(slot * kUnits * C::kUnitBytes);
-      constexpr int kBatch = 4;   // units whose loads are in flight together
+      __syncwarp();   // (pieces that other lanes copied)
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int turn = slot * C::kTurnRows * C::kRow;
+      const uint32_t tw = tmem + lanes + (uint32_t)C::kAccCols + (uint32_t)C::kStageCols * s;
+      {
+        constexpr int kChunks = 4 * kSub;
+        uint4 v[kChunks + 1];
 #pragma unroll
-      for (int u0 = 0; u0 < kUnits; u0 += kBatch) {
-        uint32_t v[kBatch][4], h[4];
+        for (int i = 0; i < kChunks + (kAlign == 16 ? 0 : 1); ++i)
+          v[i] = *reinterpret_cast<const uint4*>(read_w + turn + C::chunk_at(lane, i));
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (u0 + u < kUnits) lds_chunk(v[u], from + (uint32_t)((u0 + u) * C::kUnitBytes));
+        for (int h = 0; h < kChunks / 2; ++h) {
+          uint32_t f[16];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          if (u0 + u < kUnits) {
+          for (int i = 0; i < 2; ++i) {
+            const uint4& lo = v[2 * h + i];
+            uint32_t x[4] = {lo.x, lo.y, lo.z, lo.w};
             if constexpr (kAlign != 16) {
-              uint32_t lo[4], hi[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) lo[i] = v[u][i];
-              lds_chunk(hi, from + (uint32_t)((u0 + u) * C::kUnitBytes) + 16u);
-              merge16(v[u], lo, hi,
-                      row_shift<kAlign>(u0 + u < CM / 32 ? wrow + (u0 + u) * wstep : arow + (u0 + u - CM / 32) * astep));
+              const uint4& hi = v[2 * h + i + 1];
+              const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, m[4] = {hi.x, hi.y, hi.z, hi.w};
+              merge16(x, l, m, wshift);
             }
-            const uint32_t dst = to + 4096u * (uint32_t)(u0 + u);
-            codes_f16(v[u][0], h[0], h[1]);
-            codes_f16(v[u][1], h[2], h[3]);
-            sts128(dst, h);
-            codes_f16(v[u][2], h[0], h[1]);
-            codes_f16(v[u][3], h[2], h[3]);
-            sts128(dst ^ 16u, h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) codes_f16(x[e], f[8 * i + 2 * e], f[8 * i + 2 * e + 1]);
           }
+          tmem_store16(tw + 16u * h, f);
         }
       }
+      uint8_t* const to = at + s * (uint32_t)C::kStageBytes;
+#pragma unroll
+      for (int u = 0; u < kUnitsB; ++u) {
+        const int high = kUnit == 4 ? 4 * (u & 1) : 0;   // of the row's low three bits
+        const uint8_t* from = read_a + turn + u * kUnit * C::kRow;
+        const uint4 lo = *reinterpret_cast<const uint4*>(from + C::chunk_at(rb + high, cb));
+        uint32_t x[4] = {lo.x, lo.y, lo.z, lo.w};
+        if constexpr (kAlign != 16) {
+          const uint4 hi = *reinterpret_cast<const uint4*>(from + 16 * cb + 16);
+          const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, m[4] = {hi.x, hi.y, hi.z, hi.w};
+          merge16(x, l, m, row_shift<kAlign>(A.a + (i0 + NT / 4 * q + rb + kUnit * u) * A.lda));
+        }
+        uint8_t* const row = to + 128 * kUnit * u;
+        uint4 h;
+        codes_f16(x[0], h.x, h.y);
+        codes_f16(x[1], h.z, h.w);
+        *reinterpret_cast<uint4*>(row + (swz0 ^ (16 * high))) = h;
+        codes_f16(x[2], h.x, h.y);
+        codes_f16(x[3], h.z, h.w);
+        *reinterpret_cast<uint4*>(row + (swz0 ^ (16 * high) ^ 16)) = h;
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->full[s]);
       copy(ks + kGroups * kDeep, slot);
@@ -287,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
     asm volatile("cp.async.wait_all;" ::: "memory");   // no copy outlives its thread
     while (ok && drained < chunks) drain();
     if (expire && threadIdx.x == 0) *failed = 1;
-    // every MMA has completed: the sums go where the stages were
+    // every MMA has completed, so every copy was read: the sums go where stages and ring were
     if (ok) {
       int* to = reinterpret_cast<int*>(base) + 32 * (warp & 3) + lane;
 #pragma unroll
@@ -297,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
     // ---------------- MMA issuers ----------------
     const int m = warp - kWorkers;
     const bool lead = elect_one();
-    const uint32_t d = uniform(tmem) + (uint32_t)(m * NT);
+    const uint32_t t0 = uniform(tmem), d = t0 + (uint32_t)(m * NT);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
     constexpr uint32_t kIdesc = idesc_f16(CM, NT);
     uint32_t s = (uint32_t)m, ph = 0;
@@ -318,12 +444,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
         // the workers' stores, acquired above, before the MMAs' reads
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(C::kStageBytes >> 4));
-        const uint64_t bd = ad + (uint64_t)(CM * 128 >> 4);
+        const uint64_t bd = desc0 + (uint64_t)(s * (uint32_t)(C::kStageBytes >> 4));
+        const uint32_t ta = t0 + (uint32_t)C::kAccCols + (uint32_t)C::kStageCols * s;
         if (lead) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mma_f16(d + (uint32_t)(kIssuers * b * NT), ad + 2 * e, bd + 2 * e, kIdesc, e > 0 ? 1u : accumulate);
+          for (int e = 0; e < 4 * kSub; ++e)
+            mma_f16_ts(d + (uint32_t)(kIssuers * b * NT), ta + 8 * e, bd + (uint64_t)((e >> 2) * (NT * 128 >> 4) + 2 * (e & 3)),
+                       kIdesc, e > 0 ? 1u : accumulate);
           mma_commit(&sh->empty[s]);
         }
         accumulate = 1u;
@@ -344,6 +471,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
     __syncwarp();
   }
   __syncwarp();
+  Factors F;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int j = j0 + 4 * lane + e;
+    F.sw[e] = j < A.N && A.w_scale ? A.w_scale[j] : 1.0f;
+    F.bias[e] = j < A.N && A.bias ? A.bias[j] : 0.0f;
+    F.thr[e] = j < A.N && A.thr ? A.thr[j] : 0;
+  }
+  {
+    // lane x: the warp's row x
+    const int t = (int)rank + split * (warp + kWorkers * lane);
+    F.sa = A.a_scale && t < NT && i0 + t < A.n ? A.a_scale[i0 + t] : 1.0f;
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -352,8 +492,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
   int* sums = reinterpret_cast<int*>(base);
   if (*failed) {
     // partial sums of this CTA's k range on CUDA cores
-    const int k0 = KS * first, k1 = min(A.K, KS * (first + steps));
-    for (int e = threadIdx.x; e < CM * NT; e += kThreads) {
+    const int k0 = C::kStep * first, k1 = min(A.K, C::kStep * (first + steps));
+    for (int e = threadIdx.x; e < CM * NT; e += C::kThreads) {
       const int j = e % CM, i = e / CM;
       const int sum = j0 + j < A.N && i0 + i < A.n ? plain_sum(A, i0 + i, j0 + j, k0, k1) : 0;
       sums[i * C::kSumPitch + j] = sum;
@@ -361,59 +501,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_int8_tile(const Int8Args A, int
     __syncthreads();
   }
   if (split > 1) cluster_sync();
-
-  // ---------------- output: rows rank, rank + split, ..., a warp per row ----------------
-  const int j = j0 + 4 * lane;
-  float sw[4], bias[4];
-  int thr[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const bool in = j + c < A.N;
-    sw[c] = in && A.w_scale ? A.w_scale[j + c] : 1.0f;
-    bias[c] = in && A.bias ? A.bias[j + c] : 0.0f;
-    thr[c] = in && A.thr ? A.thr[j + c] : 0;
-  }
-  const int size = A.type == BMLP_F32 || A.type == BMLP_I32 ? 4 : 2;
-  const bool vec = ((reinterpret_cast<uintptr_t>(A.out) | (uintptr_t)(A.ldo * size)) & (uintptr_t)(4 * size - 1)) == 0;
-  const int nw32 = 2 * ((A.N + 63) / 64);
-  for (int t = (int)rank + split * warp; t < NT; t += split * (kWorkers + kIssuers)) {
-    const int64_t i = i0 + t;
-    if (i >= A.n) break;
-    const uint32_t src = smem_u32(sums) + 4u * (uint32_t)(t * C::kSumPitch + 4 * lane);
-    int4 v;
-    if (split == 1) {
-      v = *reinterpret_cast<const int4*>(sums + t * C::kSumPitch + 4 * lane);
-    } else {
-      int4 p[kMaxSplit];
-#pragma unroll
-      for (int q = 0; q < kMaxSplit; ++q)
-        if (q < split) p[q] = ld_cluster(src, (uint32_t)q);
-      v = p[0];
-#pragma unroll
-      for (int q = 1; q < kMaxSplit; ++q)
-        if (q < split) {
-          v.x += p[q].x; v.y += p[q].y; v.z += p[q].z; v.w += p[q].w;
-        }
-    }
-    if (A.words) {
-      uint32_t bits = 0u;
-      bits |= (j + 0 < A.N && v.x >= thr[0]) ? 1u : 0u;
-      bits |= (j + 1 < A.N && v.y >= thr[1]) ? 2u : 0u;
-      bits |= (j + 2 < A.N && v.z >= thr[2]) ? 4u : 0u;
-      bits |= (j + 3 < A.N && v.w >= thr[3]) ? 8u : 0u;
-      bits <<= 4 * (lane & 7);
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(kFull, bits, o);
-      const int word = j0 / 32 + (lane >> 3);
-      if ((lane & 7) == 0 && word < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + word] = bits;
-    } else {
-      const float sa = A.a_scale ? A.a_scale[i] : 1.0f;
-      switch (A.type) {
-        case BMLP_F32: store4<float>(A, i, j, v, sa, sw, bias, vec); break;
-        case BMLP_F16: store4<__half>(A, i, j, v, sa, sw, bias, vec); break;
-        case BMLP_BF16: store4<__nv_bfloat16>(A, i, j, v, sa, sw, bias, vec); break;
-        default: store4<int32_t>(A, i, j, v, sa, sw, bias, vec);
-      }
+  if (warp < kWorkers) {
+    switch (split) {
+      case 1: write_rows<NT, 1>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
+      case 2: write_rows<NT, 2>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
+      case 4: write_rows<NT, 4>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
+      default: write_rows<NT, 8>(A, sums, C::kSumPitch, i0, j0, rank, F);
     }
   }
   if (split > 1) cluster_sync();   // no CTA leaves while its sums are read
@@ -427,7 +520,7 @@ cudaError_t launch_tile(const Int8Args& A, int split, int expire, cudaStream_t s
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((A.N + CM - 1) / CM * split), (unsigned)((A.n + NT - 1) / NT));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(C::kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -457,9 +550,9 @@ cudaError_t launch_int8_tile(const Int8Args& all, cudaStream_t st, int expire) {
   A.n = std::min<int64_t>(all.n, kMaxRows);
   const int nt = A.n <= 32 ? 32 : (A.n <= 64 ? 64 : (A.n <= 96 ? 96 : 128));
   const int64_t tiles = (int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt);
-  const int steps = (A.K + KS - 1) / KS;
+  const int steps = (A.K + 63) / 64;
   int split = 1;
-  while (split < kMaxSplit && tiles * (split + 1) <= sm_count() && steps >= 4 * (split + 1)) ++split;
+  while (split < kMaxSplit && tiles * (2 * split) <= sm_count() && steps >= 8 * split) split *= 2;
   const cudaError_t e =
       operand_align(A) == 16 ? launch_rows<16>(A, nt, split, expire, st) : launch_rows<1>(A, nt, split, expire, st);
   if (e != cudaSuccess || all.n <= kMaxRows) return e;
