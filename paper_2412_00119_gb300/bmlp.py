@@ -146,30 +146,40 @@ def _ptr(buf):
     raise TypeError("expected a torch tensor or a numpy array, got %r" % type(buf))
 
 
-_REAL_TYPES = {"torch.float32": BMLP_F32, "torch.float16": BMLP_F16, "torch.bfloat16": BMLP_BF16}
-_OUT_TYPES = dict(_REAL_TYPES, **{"torch.int32": BMLP_I32})
-_types = {}   # of the torch dtypes seen
+# -- tensors of the 8-bit front end (torch is imported when the first one comes) --
+_torch = _raw_stream = _get_device = None
+_real_types, _out_types = {}, {}      # torch dtype -> BMLP_* type
 
 
-def _type(t, of):
-    """BMLP_* type of a torch tensor's elements; `of`: the types allowed."""
-    name = _types.get(t.dtype)
-    if name is None:
-        name = _types[t.dtype] = str(t.dtype)
-    if name not in of:
-        raise TypeError("expected a tensor of %s, got %s" % (", ".join(of), name))
-    return of[name]
+def _use_torch():
+    global _torch, _raw_stream, _get_device
+    import torch
+    _real_types.update({torch.float32: BMLP_F32, torch.float16: BMLP_F16, torch.bfloat16: BMLP_BF16})
+    _out_types.update(_real_types)
+    _out_types[torch.int32] = BMLP_I32
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _get_device = getattr(torch._C, "_cuda_getDevice", None)
+    _torch = torch
+    return torch
 
 
-def _rows(t, n, K, what, dtype=None):
-    """(pointer, row stride in elements) of an n x K tensor whose rows are contiguous."""
-    if t.shape != (n, K):
-        raise ValueError("%s: expected shape %s, got %s" % (what, (n, K), tuple(t.shape)))
-    ld, step = t.stride()
-    if step != 1 and K > 1:
-        raise ValueError("%s: the elements of a row must be contiguous" % what)
-    if dtype is not None and t.dtype != dtype:
+def _type(t, of, what):
+    """BMLP_* type of a tensor's elements."""
+    code = of.get(t.dtype)
+    if code is None:
+        raise TypeError("%s: expected a tensor of %s, got %s" % (what, ", ".join(map(str, of)), t.dtype))
+    return code
+
+
+def _rows(t, shape, what, dtype):
+    """(pointer, row stride in elements) of a tensor of that shape whose rows are contiguous."""
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (what, shape, tuple(t.shape)))
+    if t.dtype is not dtype:
         raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % what)
     return t.data_ptr(), ld
 
 
@@ -177,10 +187,17 @@ def _vector(t, n, what, dtype):
     """Pointer of a contiguous vector of n elements (None: NULL)."""
     if t is None:
         return None
-    if t.shape != (n,) or (n > 1 and t.stride(0) != 1) or t.dtype != dtype:
+    if t.shape != (n,) or t.dtype is not dtype or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: expected %d contiguous values of %s, got %s of %s"
                          % (what, n, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
+
+
+def _tensor_stream(stream, t):
+    """_stream(stream), where a tensor on the device says that CUDA is initialised."""
+    if stream is None and _raw_stream is not None and _get_device is not None and t.is_cuda:
+        return _raw_stream(_get_device())
+    return _stream(stream)
 
 
 def _stream(stream):
@@ -279,27 +296,32 @@ def bmlp_expand_sign(x, E, K, out, stream=None):
 def bmlp_quantize_rows(x, q, scale, stream=None):
     """8-bit codes q (n x K int8) and scales (n fp32) of the rows of x (n x K
     fp32 / fp16 / bf16, on the device; row strides are kept)."""
-    import torch
-    n, K = x.shape
-    px, ldx = _rows(x, n, K, "x")
-    pq, ldq = _rows(q, n, K, "q", torch.int8)
-    _check(lib().bmlp_quantize_rows(px, _type(x, _REAL_TYPES), ldx, n, K, pq, ldq,
-                                    _vector(scale, n, "scale", torch.float32), _stream(stream)), None)
+    torch = _torch or _use_torch()
+    shape = n, K = x.shape
+    px, ldx = _rows(x, shape, "x", x.dtype)
+    pq, ldq = _rows(q, shape, "q", torch.int8)
+    rc = (_lib or lib()).bmlp_quantize_rows(px, _type(x, _real_types, "x"), ldx, n, K, pq, ldq,
+                                            _vector(scale, n, "scale", torch.float32), _tensor_stream(stream, x))
+    if rc:
+        _check(rc)
 
 
 def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stream=None):
     """RMS norm of the rows of x + res times gain as 8-bit codes q (n x K int8)
     and scales (n fp32); sum_out (may be x or res): x + res in their type.
     gain, res, sum_out: x's type, each may be None."""
-    import torch
-    n, K = x.shape
-    px, ldx = _rows(x, n, K, "x")
-    pr, ldr = (None, 0) if res is None else _rows(res, n, K, "res", x.dtype)
-    ps, lds = (None, 0) if sum_out is None else _rows(sum_out, n, K, "sum_out", x.dtype)
-    pq, ldq = _rows(q, n, K, "q", torch.int8)
-    _check(lib().bmlp_norm_quantize(px, ldx, pr, ldr, _vector(gain, K, "gain", x.dtype), _type(x, _REAL_TYPES),
-                                    n, K, eps, ps, lds, pq, ldq, _vector(scale, n, "scale", torch.float32),
-                                    _stream(stream)), None)
+    torch = _torch or _use_torch()
+    shape = n, K = x.shape
+    dtype = x.dtype
+    px, ldx = _rows(x, shape, "x", dtype)
+    pr, ldr = (None, 0) if res is None else _rows(res, shape, "res", dtype)
+    ps, lds = (None, 0) if sum_out is None else _rows(sum_out, shape, "sum_out", dtype)
+    pq, ldq = _rows(q, shape, "q", torch.int8)
+    rc = (_lib or lib()).bmlp_norm_quantize(px, ldx, pr, ldr, _vector(gain, K, "gain", dtype),
+                                            _type(x, _real_types, "x"), n, K, eps, ps, lds, pq, ldq,
+                                            _vector(scale, n, "scale", torch.float32), _tensor_stream(stream, x))
+    if rc:
+        _check(rc)
 
 
 def bmlp_int8_workspace(n, K, N):
@@ -307,18 +329,18 @@ def bmlp_int8_workspace(n, K, N):
     return int(lib().bmlp_int8_workspace(n, K, N))
 
 
-def _workspace(workspace, n, K, N, a, stream):
+def _workspace(L, workspace, n, K, N, a, stream):
     """(pointer, bytes, owner) of the given workspace, or of one from torch's
     allocator where the size wants it."""
     if workspace is None:
-        size = lib().bmlp_int8_workspace(n, K, N)
+        size = L.bmlp_int8_workspace(n, K, N)
         if size == 0 or not a.is_cuda:
             return None, 0, None
-        import torch
-        workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
-        raw = _stream(stream)
-        if raw != torch.cuda.current_stream(a.device).cuda_stream:
-            workspace.record_stream(torch.cuda.ExternalStream(raw, a.device))
+        workspace = _torch.empty(size, dtype=_torch.uint8, device=a.device)
+        if stream is not None:
+            raw = _stream(stream)
+            if raw != _torch.cuda.current_stream(a.device).cuda_stream:
+                workspace.record_stream(_torch.cuda.ExternalStream(raw, a.device))
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
@@ -327,33 +349,39 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     int8) times w (N x K int8) transposed, scaled per row and channel.
     workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: from
     torch's allocator)."""
-    import torch
-    n, K = a.shape
+    torch = _torch or _use_torch()
+    L = _lib or lib()
+    shape = n, K = a.shape
     N = w.shape[0]
-    pa, lda = _rows(a, n, K, "a", torch.int8)
-    pw, ldw = _rows(w, N, K, "w", torch.int8)
-    po, ldo = _rows(out, n, N, "out")
+    pa, lda = _rows(a, shape, "a", torch.int8)
+    pw, ldw = _rows(w, (N, K), "w", torch.int8)
+    po, ldo = _rows(out, (n, N), "out", out.dtype)
     f32 = torch.float32
-    ws, wsb, owner = _workspace(workspace, n, K, N, a, stream)
-    _check(lib().bmlp_int8_matmul(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw,
-                                  _vector(w_scale, N, "w_scale", f32), _vector(bias, N, "bias", f32), n, K, N,
-                                  po, _type(out, _OUT_TYPES), ldo, ws, wsb, _stream(stream)), None)
+    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 8 or workspace is not None else (None, 0, None)
+    rc = L.bmlp_int8_matmul(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw,
+                            _vector(w_scale, N, "w_scale", f32), _vector(bias, N, "bias", f32), n, K, N,
+                            po, _type(out, _out_types, "out"), ldo, ws, wsb, _tensor_stream(stream, a))
+    if rc:
+        _check(rc)
 
 
 def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     """Packed +-1 words (n x ceil(N/64) int64) of a (n x K int8) times w (N x K
     int8) transposed against threshold (N int32; None: 0).  workspace: as for
     bmlp_int8_matmul."""
-    import torch
-    n, K = a.shape
+    torch = _torch or _use_torch()
+    L = _lib or lib()
+    shape = n, K = a.shape
     N = w.shape[0]
-    pa, lda = _rows(a, n, K, "a", torch.int8)
-    pw, ldw = _rows(w, N, K, "w", torch.int8)
-    if out.shape != (n, (N + 63) // 64) or out.element_size() != 8:
-        raise ValueError("out: expected %d x %d 64-bit words" % (n, (N + 63) // 64))
-    ws, wsb, owner = _workspace(workspace, n, K, N, a, stream)
-    _check(lib().bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
-                                _ptr(out), ws, wsb, _stream(stream)), None)
+    pa, lda = _rows(a, shape, "a", torch.int8)
+    pw, ldw = _rows(w, (N, K), "w", torch.int8)
+    if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():
+        raise ValueError("out: expected %d x %d contiguous 64-bit words" % (n, (N + 63) // 64))
+    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 8 or workspace is not None else (None, 0, None)
+    rc = L.bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
+                          out.data_ptr(), ws, wsb, _tensor_stream(stream, a))
+    if rc:
+        _check(rc)
 
 
 def bmlp_debug_expand_sign(x, E, K, out, expired_tile, stream=None):

@@ -304,15 +304,22 @@ struct Int8Args {
   int64_t lda, ldw, ldo, n;
   int32_t K, N, type;
 };
-cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st);
+// expire != 0: the CTAs of the tensor-core kernels take a wait as expired (tests).
+cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st, int expire = 0);
 // Bytes of workspace with which the call is fastest; 0: none is used.
 int64_t int8_workspace(int64_t n, int K, int N);
-// At most kFewRows rows, on CUDA cores (kern_int8_few.cu).
+// At most kFewRows rows, on mma.sync (kern_int8_few.cu).
 constexpr int kFewRows = 8;
 cudaError_t launch_int8_few(const Int8Args& A, cudaStream_t st);
-// The tensor-core tiles of one CTA (kern_int8_tile.cu).  expire != 0: every CTA takes a
-// wait as expired.
-cudaError_t launch_int8_tile(const Int8Args& A, cudaStream_t st, int expire);
+// The tensor-core tiles of one CTA (kern_int8_tile.cu), nt rows wide (32, 64 or 128; with a
+// workspace 64 or 128: the activations then come from it as fp16 blocks, put there by a
+// launch before).  Rows in slabs of kTileSlab.
+constexpr int64_t kTileSlab = 65536;
+cudaError_t launch_int8_tile(const Int8Args& A, void* workspace, cudaStream_t st, int expire, int nt);
+int int8_tile_split(int64_t tiles, int K);
+// The rows as fp16 blocks (kern_int8_pair.cu), and their bytes.
+cudaError_t launch_int8_expand_rows(const Int8Args& A, void* workspace, cudaStream_t st);
+int64_t int8_rows_workspace(int64_t n, int K);
 // Both operands as fp16 in a workspace, then CTA pairs (kern_int8_pair.cu); rows in
 // slabs of kPairSlab.
 constexpr int64_t kPairSlab = 65536;

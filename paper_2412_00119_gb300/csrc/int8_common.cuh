@@ -21,58 +21,6 @@ template <> __device__ __forceinline__ float out_cast(float y) { return y; }
 template <> __device__ __forceinline__ __half out_cast(float y) { return __float2half_rn(y); }
 template <> __device__ __forceinline__ __nv_bfloat16 out_cast(float y) { return __float2bfloat16_rn(y); }
 
-__device__ __forceinline__ uint32_t skew_of(const int8_t* row) {
-  return (uint32_t)(reinterpret_cast<uintptr_t>(row) & 3);
-}
-
-// Bytes [k, k + 16) of a row that has them and (kAlign 1) four more after them (k a
-// multiple of 16).
-template <int kAlign>
-__device__ __forceinline__ void load16_inside(uint32_t (&v)[4], const int8_t* row, int k) {
-  if constexpr (kAlign == 16) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(row + k));
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-  } else {
-    const uint32_t skew = skew_of(row);
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(row + (k - (int)skew));
-    uint32_t w[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) w[i] = __ldg(p + i);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * skew);
-  }
-}
-
-// Bytes [k, k + 16) of the K codes at row, zeros from K on (k a multiple of 16).  What is
-// read around them: as below.
-template <int kAlign>
-__device__ __forceinline__ void load16(uint32_t (&v)[4], const int8_t* row, int k, int K) {
-  if constexpr (kAlign == 16) {
-    if (k + 16 <= K) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(row + k));
-      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-      return;
-    }
-  }
-  const int skew = (int)skew_of(row);
-  const int8_t* p = row + (k - skew);
-  uint32_t w[5];
-#pragma unroll
-  for (int i = 0; i < 5; ++i) {
-    const int size = K - k + skew - 4 * i;   // codes of the row from this word on
-    w[i] = 0u;
-    if (size >= 4) {
-      w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
-    } else {
-#pragma unroll
-      for (int b = 0; b < 3; ++b)
-        if (b < size && K > 0) w[i] |= (uint32_t)(uint8_t)__ldg(p + 4 * i + b) << (8 * b);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 8u * (uint32_t)skew);
-}
-
 // Rows that allow no 16-byte copies (kAlign 1) are copied as the aligned 16-byte chunks
 // around them: chunk i holds codes 16 i - s .. + 15, s the bytes between the row's start and
 // the aligned address before it, and the codes [16 i, 16 i + 16) are merged from chunks i and i + 1.
@@ -115,6 +63,56 @@ __device__ __forceinline__ void merge16(uint32_t (&v)[4], const uint32_t (&lo)[4
   for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(u[i], u[i + 1], 8u * (uint32_t)(shift & 3));
 }
 
+// Codes [k, k + 16) of a row straight to registers, zeros from K on (k a multiple of 16); what is
+// read around them: as by the copies above.
+__device__ __forceinline__ uint4 load_chunk(const int8_t* row, int shift, int k, int K) {
+  const int8_t* p = row + (k - shift);
+  const int size = K - k + shift;
+  if (size >= 16) return __ldg(reinterpret_cast<const uint4*>(p));
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = 0u;
+    if (size >= 4 * i + 4) {
+      w[i] = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 3; ++b)
+        if (size > 4 * i + b) w[i] |= (uint32_t)(uint8_t)__ldg(p + 4 * i + b) << (8 * b);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// shift: row_shift<kAlign>(row).
+template <int kAlign>
+__device__ __forceinline__ void load16(uint32_t (&v)[4], const int8_t* row, int shift, int k, int K) {
+  const uint4 a = load_chunk(row, shift, k, K);
+  const uint32_t lo[4] = {a.x, a.y, a.z, a.w};
+  if constexpr (kAlign == 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = lo[i];
+  } else {
+    const uint4 b = load_chunk(row, shift, k + 16, K);
+    const uint32_t hi[4] = {b.x, b.y, b.z, b.w};
+    merge16(v, lo, hi, shift);
+  }
+}
+// The same where every chunk read lies inside the row.
+template <int kAlign>
+__device__ __forceinline__ void load16_inside(uint32_t (&v)[4], const int8_t* row, int shift, int k) {
+  const uint4* p = reinterpret_cast<const uint4*>(row + (k - shift));
+  const uint4 a = __ldg(p);
+  const uint32_t lo[4] = {a.x, a.y, a.z, a.w};
+  if constexpr (kAlign == 16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = lo[i];
+  } else {
+    const uint4 b = __ldg(p + 1);
+    const uint32_t hi[4] = {b.x, b.y, b.z, b.w};
+    merge16(v, lo, hi, shift);
+  }
+}
+
 // Four codes as fp16: a code's byte with its sign bit flipped is code + 128, under the
 // exponent of 1024 in a half's low byte it is 1152 + code, exactly.
 __device__ __forceinline__ void codes_f16(uint32_t x, uint32_t& lo, uint32_t& hi) {
@@ -141,9 +139,8 @@ __device__ __forceinline__ void put_out(const Int8Args& A, int64_t i, int j, int
   else static_cast<__nv_bfloat16*>(A.out)[at] = out_cast<__nv_bfloat16>(y);
 }
 
-__device__ __forceinline__ int plain_sum(const Int8Args& A, int64_t i, int j, int k0, int k1) {
-  const int8_t* ar = A.a + i * A.lda;
-  const int8_t* wr = A.w + (int64_t)j * A.ldw;
+// Sum of products of the codes [k0, k1) of two rows.
+static __device__ __noinline__ int plain_sum(const int8_t* ar, const int8_t* wr, int k0, int k1) {
   int sum = 0;
   for (int k = k0; k < k1; ++k) sum += (int)ar[k] * (int)wr[k];
   return sum;
@@ -158,7 +155,7 @@ static __device__ __noinline__ void plain_tile(const Int8Args& A, int64_t i0, in
     const int64_t i = i0 + e / words;
     const int j = j0 + 32 * (e % words) + lane;
     if (i >= A.n) return;
-    const int s = j < A.N ? plain_sum(A, i, j, 0, A.K) : 0;
+    const int s = j < A.N ? plain_sum(A.a + i * A.lda, A.w + (int64_t)j * A.ldw, 0, A.K) : 0;
     if (A.words) {
       const uint32_t w = __ballot_sync(0xffffffffu, j < A.N && s >= (A.thr ? A.thr[j] : 0));
       if (lane == 0 && (j >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + (j >> 5)] = w;
@@ -179,11 +176,13 @@ inline Int8Args rest_of(Int8Args A, int64_t rows) {
   return A;
 }
 
-// 16: every row of both operands allows 16-byte loads; else 1.
+// 16: every row of the weights (of both operands) allows 16-byte loads; else 1.
+inline int operand_align_w(const Int8Args& A) {
+  return ((reinterpret_cast<uintptr_t>(A.w) | (A.N > 1 ? (uintptr_t)A.ldw : 0)) & 15) == 0 ? 16 : 1;
+}
 inline int operand_align(const Int8Args& A) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(A.a) | (A.n > 1 ? (uintptr_t)A.lda : 0) |
-                      reinterpret_cast<uintptr_t>(A.w) | (A.N > 1 ? (uintptr_t)A.ldw : 0);
-  return (a & 15) == 0 ? 16 : 1;
+  const bool a = ((reinterpret_cast<uintptr_t>(A.a) | (A.n > 1 ? (uintptr_t)A.lda : 0)) & 15) == 0;
+  return a ? operand_align_w(A) : 1;
 }
 
 }  // namespace i8

@@ -25,11 +25,12 @@ constexpr int kStep = 256;        // codes of a row per turn
 constexpr int kRing = 3;          // turns of the ring (four: fewer CTAs stay, 18.2 us)
 
 template <int kAlign> struct Few {
-  // bytes of a channel per turn: 16 chunks, or 17 at a pitch that, as the swap below, puts the
-  // 64 bytes of two channels that eight lanes read on different banks
-  static constexpr int kPitch = kAlign == 16 ? 256 : 320;
+  // bytes of a channel per turn: 16 chunks, or 17 (at a pitch of 320, without bank conflicts, fewer
+  // CTAs stay: 1 x 8191 -> 8192 28 us)
+  static constexpr int kPitch = kAlign == 16 ? 256 : 272;
   static constexpr int kTurnBytes = kChannels * kPitch;
-  // place of chunk c of channel r
+  // place of chunk c of channel r: of odd channels swapped by fours, which puts the 64 bytes of
+  // two channels that eight lanes read on different banks
   static __device__ __forceinline__ uint32_t at(int r, int c) {
     return (uint32_t)(r * kPitch + 16 * (kAlign == 16 ? c ^ ((r & 1) << 2) : c));
   }
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(32 * kWarps) k_int8_few(const Int8Args A) {
   for (int d = 0; d < kRing - 1; ++d) copy(first + d, d);
   // (rows past n read row 0: what comes of them is dropped)
   const int8_t* ar = A.a + (g < A.n ? g : 0) * A.lda;
+  const int ashift = row_shift<kAlign>(ar);
   const int shift0 = row_shift<kAlign>(A.w + (int64_t)(j0 + g) * A.ldw);
   const int shift1 = row_shift<kAlign>(A.w + (int64_t)(j0 + g + 8) * A.ldw);
   int acc[2][4] = {};
@@ -92,12 +94,12 @@ __global__ void __launch_bounds__(32 * kWarps) k_int8_few(const Int8Args A) {
 #pragma unroll 1
   for (int t = first; t < last; ++t) {
     uint32_t b[4][4];
-    if (kStep * (t + 1) + 4 <= A.K) {
+    if (kStep * (t + 1) + (kAlign == 16 ? 0 : 16) <= A.K) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) load16_inside<kAlign>(b[h], ar, kStep * t + 64 * h + 16 * q);
+      for (int h = 0; h < 4; ++h) load16_inside<kAlign>(b[h], ar, ashift, kStep * t + 64 * h + 16 * q);
     } else {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) load16<kAlign>(b[h], ar, kStep * t + 64 * h + 16 * q, A.K);
+      for (int h = 0; h < 4; ++h) load16<kAlign>(b[h], ar, ashift, kStep * t + 64 * h + 16 * q, A.K);
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
     __syncwarp();   // every lane's copies of this turn, and its reads of the turn before

@@ -63,9 +63,9 @@ struct ExpandArgs {
 };
 
 constexpr int kExpandThreads = 256;
-constexpr int kExpandSteps = 4;   // blocks along k per warp and turn
 
-template <int kAlign>
+// kExpandSteps: blocks along k per warp and turn.
+template <int kAlign, int kExpandSteps>
 __global__ void __launch_bounds__(kExpandThreads) k_int8_expand(const ExpandArgs E) {
   pdl_wait();
   pdl_trigger();
@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(kExpandThreads) k_int8_expand(const ExpandArgs
                   ((32 * c) ^ (16 * (r & 7)));
     uint32_t v[kExpandSteps][4];
 #pragma unroll
-    for (int i = 0; i < kExpandSteps; ++i) load16<kAlign>(v[i], src, kBlockK * (kb0 + i) + 16 * c, live ? E.K : 0);
+    for (int i = 0; i < kExpandSteps; ++i)
+      load16<kAlign>(v[i], src, row_shift<kAlign>(src), kBlockK * (kb0 + i) + 16 * c, live ? E.K : -16);
 #pragma unroll
     for (int i = 0; i < kExpandSteps; ++i) {
       if (kb0 + i < E.nkb) {
@@ -406,11 +407,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
 }
 
-template <int kAlign>
+template <int kAlign, int kSteps>
 cudaError_t expand(const ExpandArgs& E, cudaStream_t st) {
-  const int64_t turns = E.units * ((E.nkb + kExpandSteps - 1) / kExpandSteps);
+  const int64_t turns = E.units * ((E.nkb + kSteps - 1) / kSteps);
   const int64_t ctas = (turns + kExpandThreads / 32 - 1) / (kExpandThreads / 32);
-  return launch_kernel(k_int8_expand<kAlign>, dim3((unsigned)std::min<int64_t>(ctas, 8ll * sm_count())),
+  return launch_kernel(k_int8_expand<kAlign, kSteps>, dim3((unsigned)std::min<int64_t>(ctas, 8ll * sm_count())),
                        dim3(kExpandThreads), 0, st, true, E);
 }
 
@@ -418,6 +419,24 @@ int64_t padded(int64_t rows) { return (rows + TP - 1) / TP * TP; }
 int64_t row_bytes(int K) { return (int64_t)((K + kBlockK - 1) / kBlockK) * kBlockK * 2; }
 
 }  // namespace
+
+int64_t int8_rows_workspace(int64_t n, int K) {
+  n = std::min(n, kTileSlab);
+  return row_bytes(K) * ((n + kBlockRows - 1) / kBlockRows * kBlockRows);
+}
+
+cudaError_t launch_int8_expand_rows(const Int8Args& A, void* workspace, cudaStream_t st) {
+  ExpandArgs E = {};
+  E.x1 = A.a;
+  E.ld1 = A.lda;
+  E.rows1 = A.n;
+  E.units = (A.n + 7) / 8;   // (what the last block's other rows hold is dropped)
+  E.blocks1 = static_cast<uint8_t*>(workspace);
+  E.K = A.K;
+  E.nkb = (A.K + kBlockK - 1) / kBlockK;
+  const bool wide = ((reinterpret_cast<uintptr_t>(A.a) | (A.n > 1 ? (uintptr_t)A.lda : 0)) & 15) == 0;
+  return wide ? expand<16, 1>(E, st) : expand<1, 1>(E, st);
+}
 
 int64_t int8_pair_workspace(int64_t n, int K, int64_t N) {
   return row_bytes(K) * (padded(N) + std::min(padded(n), kPairSlab));
@@ -480,7 +499,7 @@ cudaError_t launch_int8_pair(const Int8Args& all, void* workspace, cudaStream_t 
     CUtensorMap wmap, amap;
     if (!block_map(&wmap, wblocks, padded(A.N) * nkb) || !block_map(&amap, ablocks, padded(A.n) * nkb))
       return cudaErrorNotSupported;
-    cudaError_t e = wide ? expand<16>(E, st) : expand<1>(E, st);
+    cudaError_t e = wide ? expand<16, 4>(E, st) : expand<1, 4>(E, st);
     if (e != cudaSuccess) return e;
     if (A.words) e = launch_out<Signs>(A, wmap, amap, nkb, st, expire);
     else if (A.type == BMLP_F32) e = launch_out<float>(A, wmap, amap, nkb, st, expire);

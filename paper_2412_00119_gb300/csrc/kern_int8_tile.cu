@@ -38,20 +38,19 @@ using namespace i8;
 
 constexpr int CM = 128;                 // channels of a tile
 constexpr int kWorkers = 16;
-constexpr int kMaxSplit = 8;
+constexpr int kMaxSplit = 4;             // CTAs that share K (of eight, few clusters find room at once)
 constexpr int kGroups = 4;              // worker groups, each a k-step of its own
 constexpr int kSmemBytes = 225 * 1024;  // for stages and copies in flight
-constexpr int64_t kMaxRows = 65535ll * 128;   // rows of a launch (the grid's y limit)
 
-template <int NT, int kAlign> struct Cfg {
-  static constexpr int kSub = NT <= 96 ? 2 : 1;                // 64 codes (a 128-byte row of fp16) each
+template <int NT, int kAlign, bool kReady> struct Cfg {
+  static constexpr int kSub = NT <= 64 || kReady ? 2 : 1;                // 64 codes (a 128-byte row of fp16) each
   static constexpr int kStep = 64 * kSub;                      // codes of a k-step
   static constexpr int kIssuers = NT <= 64 ? 2 : 1;
-  static constexpr int kThreads = 32 * (kWorkers + kIssuers);
+  static constexpr int kThreads = 32 * (kWorkers + kIssuers + (kReady ? 1 : 0));
   static constexpr int kChunk = 1024 / kStep * kIssuers;       // k-steps between drains: 1024 k per accumulator
   // a row of the ring: chunks of 16 codes, one more where they are merged (int8_common.cuh)
   static constexpr int kRow = kStep + (kAlign == 16 ? 0 : 16);
-  static constexpr int kTurnRows = 32 + NT / 4;                // rows of a warp: channels, activations
+  static constexpr int kTurnRows = 32 + (kReady ? 0 : NT / 4); // rows of a warp: channels, activations
   static constexpr int kTurnBytes = kWorkers * kTurnRows * kRow;
   static constexpr int kStageBytes = NT * 128 * kSub;          // activations
   static constexpr int kStageCols = 32 * kSub;                 // weights
@@ -67,9 +66,9 @@ template <int NT, int kAlign> struct Cfg {
   static constexpr int kRingBytes = kDeep * kTurnBytes;
   static constexpr int kStages = stages(kDeep);
   static constexpr int kTmemCols = kAccCols + kStageCols * kStages <= 256 ? 256 : 512;
-  static constexpr int kSumPitch = CM + 4;                     // int32 per row of the exchange
+  static constexpr int kCols = NT / 4;                         // accumulator columns (rows) of a worker
   static_assert(kAccCols + kStageCols * kStages <= 512, "tensor memory");
-  static_assert(4 * kSumPitch * NT <= kStages * kStageBytes + kRingBytes, "exchange fits");
+  static_assert(4 * CM * NT <= kStages * kStageBytes + kRingBytes, "exchange fits");
   static_assert(kStages >= kGroups && kStages <= kChunk, "a chunk is drained before the one after the next starts");
   // Place of chunk c of row r of the ring, from its row's start: swapped so that eight lanes
   // that read a chunk of eight rows are on different banks (rows of 80 and 144 bytes are by
@@ -82,7 +81,7 @@ template <int NT, int kAlign> struct Cfg {
 struct __align__(8) TileShared {
   unsigned long long full[8], empty[8];
   unsigned long long done[2], drained[2];
-  unsigned long long left;
+  unsigned long long left, never;
   uint32_t tmem_base;
   int failed, left_failed;
 };
@@ -92,113 +91,126 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ int4 ld_cluster(uint32_t addr, uint32_t rank) {
-  int4 v;
-  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n"
-               " ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [a];\n}"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr), "r"(rank) : "memory");
-  return v;
-}
-
-// Four neighbouring outputs of a row.
-template <typename T>
-__device__ __forceinline__ void store4(const Int8Args& A, int64_t i, int j, const int4& s, float sa, const float (&sw)[4],
-                                       const float (&bias)[4], bool vec) {
-  T* p = static_cast<T*>(A.out) + i * A.ldo + j;
-  const int v[4] = {s.x, s.y, s.z, s.w};
-  T y[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if constexpr (std::is_same<T, int32_t>::value) {
-      y[c] = v[c];
-    } else {
-      float f = scaled(v[c], sa, sw[c]);
-      if (A.bias) f = __fadd_rn(f, bias[c]);
-      y[c] = out_cast<T>(f);
-    }
-  }
-  if (vec && j + 4 <= A.N) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(y);
-    else *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(y);
-  } else {
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (j + c < A.N) p[c] = y[c];
-  }
-}
-
-// What a lane's outputs need from memory: asked for before the sums are there.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// What a thread's outputs need from memory: asked for before the sums are there.
 struct Factors {
-  float sw[4], bias[4], sa;
-  int thr[4];
+  float sw, bias, sa;
+  int thr;
 };
 
-// Outputs of a worker warp: rows rank + S (warp + 16 x) of the tile, a lane four channels, the
-// S partial sums of a row from the S CTAs' shared memory, all of them in flight together.
-template <int NT, int S>
-__device__ __forceinline__ void write_rows(const Int8Args& A, const int* sums, int pitch, int64_t i0, int j0, uint32_t rank,
-                                           const Factors& F) {
-  constexpr int kRows = (NT + kWorkers * S - 1) / (kWorkers * S);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = j0 + 4 * lane;
-  const int size = A.type == BMLP_F32 || A.type == BMLP_I32 ? 4 : 2;
-  const bool vec = ((reinterpret_cast<uintptr_t>(A.out) | (uintptr_t)(A.ldo * size)) & (uintptr_t)(4 * size - 1)) == 0;
-  const int nw32 = 2 * ((A.N + 63) / 64);
-  int4 p[kRows][S];
+// Outputs of a worker warp from its registers: kRows rows from i on of 32 channels from jw on,
+// a lane per channel.
+template <int kRows>
+__device__ __forceinline__ void write_rows(const Int8Args& A, const int (&v)[kRows], int64_t i, int jw, const Factors& F) {
+  const int lane = threadIdx.x & 31, j = jw + lane;
+  const int rows = (int)max((int64_t)0, min((int64_t)kRows, A.n - i));
+  if (A.words) {
+    const int nw32 = 2 * ((A.N + 63) / 64);
+    uint32_t mine = 0u;
 #pragma unroll
-  for (int x = 0; x < kRows; ++x) {
-    const int t = (int)rank + S * (warp + kWorkers * x);
-    if (t < NT && i0 + t < A.n) {
-      const int* row = sums + t * pitch + 4 * lane;
-#pragma unroll
-      for (int q = 0; q < S; ++q) {
-        if constexpr (S == 1) p[x][q] = *reinterpret_cast<const int4*>(row);
-        else p[x][q] = ld_cluster(smem_u32(row), (uint32_t)q);
-      }
+    for (int e = 0; e < kRows; ++e) {
+      const uint32_t w = __ballot_sync(kFull, j < A.N && v[e] >= F.thr);
+      if (lane == e) mine = w;
     }
+    if (lane < rows && (jw >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[(i + lane) * nw32 + (jw >> 5)] = mine;
+    return;
   }
+  auto store = [&](auto* out) {
+    using T = std::remove_pointer_t<decltype(out)>;
+    T* p = out + i * A.ldo + j;
+    const bool has_bias = A.bias != nullptr;
 #pragma unroll
-  for (int x = 0; x < kRows; ++x) {
-    const int t = (int)rank + S * (warp + kWorkers * x);
-    const int64_t i = i0 + t;
-    if (t >= NT || i >= A.n) continue;
-    int4 v = p[x][0];
-#pragma unroll
-    for (int q = 1; q < S; ++q) {
-      v.x += p[x][q].x; v.y += p[x][q].y; v.z += p[x][q].z; v.w += p[x][q].w;
-    }
-    if (A.words) {
-      uint32_t bits = 0u;
-      bits |= (j + 0 < A.N && v.x >= F.thr[0]) ? 1u : 0u;
-      bits |= (j + 1 < A.N && v.y >= F.thr[1]) ? 2u : 0u;
-      bits |= (j + 2 < A.N && v.z >= F.thr[2]) ? 4u : 0u;
-      bits |= (j + 3 < A.N && v.w >= F.thr[3]) ? 8u : 0u;
-      bits <<= 4 * (lane & 7);
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) bits |= __shfl_xor_sync(kFull, bits, o);
-      const int word = j0 / 32 + (lane >> 3);
-      if ((lane & 7) == 0 && word < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + word] = bits;
-    } else {
-      const float sa = __shfl_sync(kFull, F.sa, x);
-      switch (A.type) {
-        case BMLP_F32: store4<float>(A, i, j, v, sa, F.sw, F.bias, vec); break;
-        case BMLP_F16: store4<__half>(A, i, j, v, sa, F.sw, F.bias, vec); break;
-        case BMLP_BF16: store4<__nv_bfloat16>(A, i, j, v, sa, F.sw, F.bias, vec); break;
-        default: store4<int32_t>(A, i, j, v, sa, F.sw, F.bias, vec);
+    for (int e = 0; e < kRows; ++e, p += A.ldo) {
+      const float sa = __shfl_sync(kFull, F.sa, e);
+      T y;
+      if constexpr (std::is_same<T, int32_t>::value) {
+        y = v[e];
+      } else {
+        const float f = scaled(v[e], sa, F.sw);
+        y = out_cast<T>(has_bias ? __fadd_rn(f, F.bias) : f);
       }
+      if (e < rows && j < A.N) *p = y;
     }
+  };
+  switch (A.type) {
+    case BMLP_F32: store(static_cast<float*>(A.out)); break;
+    case BMLP_F16: store(static_cast<__half*>(A.out)); break;
+    case BMLP_BF16: store(static_cast<__nv_bfloat16*>(A.out)); break;
+    default: store(static_cast<int32_t*>(A.out));
   }
 }
 
-template <int NT, int kAlign>
-__global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(const Int8Args A, int split, int expire) {
-  using C = Cfg<NT, kAlign>;
+// The S CTAs of a cluster each finish kCols / S of every worker's columns: a thread sends the
+// partial sums of the others' columns to the same thread there (stores: nothing waits for
+// them), and adds what it was sent.  Slot of a sender: its distance from the receiver.
+template <int kCols, int S>
+__device__ __forceinline__ void exchange_and_write(const Int8Args& A, const int (&acc)[kCols], uint8_t* smem, uint32_t rank,
+                                                   int64_t i0, int jw, const Factors& F) {
+  constexpr int kOwn = kCols / S, kWide = kOwn % 4 == 0 ? 4 : (kOwn % 2 == 0 ? 2 : 1);
+  static_assert(kOwn * S == kCols, "columns are shared out evenly");
+  const int tid = (int)threadIdx.x, warp = tid >> 5;
+  int own[kOwn];
+  const bool worker = warp < kWorkers;
+  if constexpr (S == 1) {
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) own[e] = acc[e];
+  } else {
+    cluster_wait();   // every CTA of the cluster is done with its stages and ring
+    // kWide columns of a thread side by side, a row of threads, the next kWide
+    const uint32_t base = smem_u32(smem) + (uint32_t)(4 * kWide * tid);
+    if (worker) {
+#pragma unroll
+      for (int q = 0; q < S; ++q) {
+        if ((uint32_t)q != rank) {
+          const uint32_t slot = ((rank - (uint32_t)q) & (S - 1)) - 1u;
+          uint32_t to;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                       : "=r"(to) : "r"(base + slot * (uint32_t)(kOwn * 4 * 32 * kWorkers)), "r"(q));
+#pragma unroll
+          for (int e = 0; e < kOwn; e += kWide) {
+            const uint32_t at = to + (uint32_t)(e * 4 * 32 * kWorkers);
+            const int* v = acc + q * kOwn + e;
+            if constexpr (kWide == 4)
+              asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};"
+                           ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+            else if constexpr (kWide == 2)
+              asm volatile("st.shared::cluster.v2.s32 [%0], {%1, %2};" ::"r"(at), "r"(v[0]), "r"(v[1]) : "memory");
+            else
+              asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(at), "r"(v[0]) : "memory");
+          }
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < S; ++q)
+        if ((uint32_t)q == rank) {
+#pragma unroll
+          for (int e = 0; e < kOwn; ++e) own[e] = acc[q * kOwn + e];
+        }
+    }
+    cluster_arrive();
+    cluster_wait();   // what was sent is there; nobody writes to another CTA after this
+    if (worker) {
+#pragma unroll
+      for (int x = 0; x < S - 1; ++x)
+#pragma unroll
+        for (int e = 0; e < kOwn; ++e)
+          own[e] += reinterpret_cast<const int*>(smem)[(x * kOwn + e / kWide * kWide) * 32 * kWorkers + kWide * tid + e % kWide];
+    }
+  }
+  if (worker) write_rows<kOwn>(A, own, i0 + kCols * (warp >> 2) + kOwn * (int)rank, jw, F);
+}
+
+// kReady: the activations as fp16 blocks (kern_int8_pair.cu), written by the launch before
+// this one, which writes nothing else that is read here.
+template <int NT, int kAlign, bool kReady>
+__global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
+    k_int8_tile(const Int8Args A, const uint8_t* __restrict__ ablocks, int split, int expire) {
+  using C = Cfg<NT, kAlign, kReady>;
   constexpr int kStages = C::kStages, kDeep = C::kDeep, kIssuers = C::kIssuers, kChunk = C::kChunk;
   // a warp's copies: units of kUnit rows, 4 kSub lanes per row
   constexpr int kSub = C::kSub, kUnit = 8 / kSub;
-  constexpr int kUnitsA = 32 / kUnit, kUnitsB = NT / 4 / kUnit, kUnits = kUnitsA + kUnitsB;
+  constexpr int kUnitsA = 32 / kUnit, kUnitsB = kReady ? 0 : NT / 4 / kUnit, kUnits = kUnitsA + kUnitsB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* ring = base + kStages * C::kStageBytes;
@@ -215,7 +227,7 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&sh->full[s], kWorkers / kGroups);
+      mbar_init(&sh->full[s], kWorkers / kGroups + (kReady ? 1 : 0));
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -223,6 +235,7 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
       mbar_init(&sh->drained[b], kWorkers);
     }
     mbar_init(&sh->left, kIssuers);
+    mbar_init(&sh->never, 1);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -240,17 +253,26 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
   const int r = lane / (4 * kSub), c = lane % (4 * kSub);   // copies: row of a unit, 16 of its codes
   const int ja = j0 + 32 * q + r;                 // channel, + kUnit per unit
   const int64_t ib = i0 + NT / 4 * q + r;         // row, + kUnit per unit
-  if (warp < kWorkers && c == 0) {
-    // the first turn's weights on their way to L2 while the launch before this one ends
-    const int k = C::kStep * (first + grp);
+  if constexpr (!kReady) {
+    if (warp < kWorkers && c == 0) {
+      // the first turn's weights on their way to L2 while the launch before this one ends
+      const int k = C::kStep * (first + grp);
 #pragma unroll
-    for (int u = 0; u < kUnitsA; ++u)
-      if (ja + kUnit * u < A.N && k < A.K)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(A.w + (int64_t)(ja + kUnit * u) * A.ldw + k));
+      for (int u = 0; u < kUnitsA; ++u)
+        if (ja + kUnit * u < A.N && k < A.K)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(A.w + (int64_t)(ja + kUnit * u) * A.ldw + k));
+    }
+    pdl_wait();
+    pdl_trigger();
+  } else if (warp >= kWorkers) {
+    pdl_wait();   // (the workers' copies of the weights need not wait)
   }
-  pdl_wait();
-  pdl_trigger();
 
+  Factors F = {};
+  constexpr int kCols = C::kCols;
+  int acc[kCols];
+#pragma unroll
+  for (int e = 0; e < kCols; ++e) acc[e] = 0;
   if (warp < kWorkers) {
     // ---------------- workers ----------------
     const int8_t* wrow = A.w + (int64_t)ja * A.ldw;
@@ -258,21 +280,28 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
     const int8_t* any = aligned16(A.w);
     const int64_t wstep = kUnit * A.ldw, astep = kUnit * A.lda;
     uint8_t* const mine = ring + warp * kDeep * C::kTurnRows * C::kRow;
-    const bool whole = j0 + CM <= A.N && i0 + NT <= A.n;   // every row of the tile is one
     const uint32_t ring_to = smem_u32(mine) + (uint32_t)(r * C::kRow);
     auto copy = [&](int ks, int slot) {
       if (ks < steps) {
         const int k = C::kStep * (first + ks) + 16 * c;
         const uint32_t to = ring_to + (uint32_t)(slot * C::kTurnRows * C::kRow);
-        if (kAlign == 16 && whole && C::kStep * (first + ks + 1) <= A.K) {
+        // (a unit of four rows: the swap by the row's low bits alternates between two places)
+        if (C::kStep * (first + ks + 1) + (kAlign == 16 ? 0 : 16) <= A.K) {
+          // every code inside its row; channels past N and rows past n, whose sums are dropped, as
+          // the tile's first
           const int8_t* row = wrow + k;
 #pragma unroll
           for (int u = 0; u < kUnits; ++u) {
             if (u == kUnitsA) row = arow + k;
-            // (the swap depends on the row's low bits: a unit of four alternates between two places)
-            const int place = C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c);
+            const int8_t* p = row;
+            if (u < kUnitsA) p = ja + kUnit * u < A.N ? p : A.w + (int64_t)j0 * A.ldw + k;
+            else p = ib + kUnit * (u - kUnitsA) < A.n ? p : A.a + i0 * A.lda + k;
+            if constexpr (kAlign != 16) p = aligned16(p);
+            const uint32_t unit = to + (uint32_t)(u * kUnit * C::kRow);
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                         ::"r"(to + (uint32_t)(u * kUnit * C::kRow + place)), "l"(row) : "memory");
+                         ::"r"(unit + (uint32_t)C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c)), "l"(p) : "memory");
+            if (kAlign != 16 && c == 0)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(unit + (uint32_t)C::kStep), "l"(p + C::kStep) : "memory");
             row += u < kUnitsA ? wstep : astep;
           }
         } else {
@@ -306,16 +335,18 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
     uint8_t* const at = base + (cb >> 2) * (NT * 128) + 128 * (NT / 4 * q + rb);
     const int swz0 = (32 * (cb & 3)) ^ (16 * (rb & 7));
     const uint32_t lanes = (uint32_t)(32 * q) << 16;
-    constexpr int kCols = NT / 4;   // accumulator columns of this warp
-    int acc[kCols];
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) acc[e] = 0;
     const uint32_t tacc = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)(kCols * (warp >> 2));
     int drained = 0;   // chunks added to acc
+    bool arrived = false;
     bool ok = true;
     auto drain = [&]() {
       const int b = drained & 1;
       ok = __all_sync(kFull, mbar_wait(&sh->done[b], (uint32_t)(drained >> 1) & 1u, failed));
+      if (split > 1 && !arrived && (!ok || drained == chunks - 1)) {
+        // with the last MMAs stages and ring are done with: the others may write there
+        cluster_arrive();
+        arrived = true;
+      }
       if (!ok) return;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       // (the odd k-steps' accumulator has nothing in a chunk of one)
@@ -323,11 +354,19 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
 #pragma unroll 1
       for (int m = 0; m < both; ++m)
 #pragma unroll
-        for (int e = 0; e < kCols; e += 8) {
-          uint32_t v[8];
-          tmem_load8(v, tacc + (uint32_t)((kIssuers * b + m) * NT + e));
+        for (int e = 0; e < kCols; e += kCols % 16 == 0 ? 16 : 8) {
+          if constexpr (kCols % 16 == 0) {
+            uint32_t v[16];
+            tmem_load16(v, tacc + (uint32_t)((kIssuers * b + m) * NT + e));
+            tmem_wait_ld(v);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) acc[e + x] += __float2int_rn(__uint_as_float(v[x]));
+            for (int x = 0; x < 16; ++x) acc[e + x] += __float2int_rn(__uint_as_float(v[x]));
+          } else {
+            uint32_t v[8];
+            tmem_load8(v, tacc + (uint32_t)((kIssuers * b + m) * NT + e));
+#pragma unroll
+            for (int x = 0; x < 8; ++x) acc[e + x] += __float2int_rn(__uint_as_float(v[x]));
+          }
         }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -411,13 +450,46 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
       wrap();
     }
     asm volatile("cp.async.wait_all;" ::: "memory");   // no copy outlives its thread
+    if constexpr (kReady) {
+      pdl_wait();
+      pdl_trigger();
+    }
+    // what the outputs need, while the last MMAs run
+    const int j = j0 + 32 * q + lane;
+    F.sw = j < A.N && A.w_scale ? A.w_scale[j] : 1.0f;
+    F.bias = j < A.N && A.bias ? A.bias[j] : 0.0f;
+    F.thr = j < A.N && A.thr ? A.thr[j] : 0;
+    // (lane e: the warp's row e)
+    const int own = kCols / split;
+    const int64_t i = i0 + kCols * (warp >> 2) + own * (int)rank + lane;
+    F.sa = A.a_scale && lane < own && i < A.n ? A.a_scale[i] : 1.0f;
     while (ok && drained < chunks) drain();
+    if (split > 1 && !arrived) cluster_arrive();
     if (expire && threadIdx.x == 0) *failed = 1;
-    // every MMA has completed, so every copy was read: the sums go where stages and ring were
-    if (ok) {
-      int* to = reinterpret_cast<int*>(base) + 32 * (warp & 3) + lane;
-#pragma unroll
-      for (int e = 0; e < kCols; ++e) to[(kCols * (warp >> 2) + e) * C::kSumPitch] = acc[e];
+  } else if (kReady && warp == kWorkers + kIssuers) {
+    // ---------------- copies of the activations' blocks ----------------
+    if (lane == 0) {
+      const int nkb = (A.K + 63) / 64;
+      const uint8_t* src = ablocks + i0 / 128 * nkb * (int64_t)16384 + i0 % 128 * 128;
+      uint32_t s = 0, ph = 1;
+      bool ok = true;
+#pragma unroll 1
+      for (int ks = 0; ks < steps; ++ks) {
+        ok = mbar_wait(&sh->empty[s], ph, failed);
+        if (!ok) break;
+        const int kb = kSub * (first + ks), subs = min(kSub, nkb - kb);   // (a last k-step's second 64: none)
+        mbar_arrive_tx(&sh->full[s], (uint32_t)(subs * NT * 128));
+        for (int x = 0; x < subs; ++x)
+          bulk_g2s(base + s * C::kStageBytes + x * (NT * 128), src + (int64_t)(kb + x) * 16384, NT * 128, &sh->full[s]);
+        if (++s == (uint32_t)kStages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+      if (!ok) {
+        // no copy outlives the CTA: what was asked for lands long before this wait's limit
+        mbar_wait(&sh->never, 0, &sh->left_failed, 2000000ull);
+      }
     }
   } else {
     // ---------------- MMA issuers ----------------
@@ -441,16 +513,19 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
       for (int ks = ch * kChunk + m; ks < end && ok; ks += kIssuers) {
         ok = __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
         if (!ok) break;
-        // the workers' stores, acquired above, before the MMAs' reads
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        // the workers' stores to shared memory, acquired above, before the MMAs' reads
+        if constexpr (!kReady) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t bd = desc0 + (uint64_t)(s * (uint32_t)(C::kStageBytes >> 4));
         const uint32_t ta = t0 + (uint32_t)C::kAccCols + (uint32_t)C::kStageCols * s;
+        // (ready activations of a last k-step may end after its first 64)
+        const int mmas = kReady && kSub * (first + ks) + 1 >= (A.K + 63) / 64 ? 4 : 4 * kSub;
         if (lead) {
 #pragma unroll
           for (int e = 0; e < 4 * kSub; ++e)
-            mma_f16_ts(d + (uint32_t)(kIssuers * b * NT), ta + 8 * e, bd + (uint64_t)((e >> 2) * (NT * 128 >> 4) + 2 * (e & 3)),
-                       kIdesc, e > 0 ? 1u : accumulate);
+            if (e < 4 || e < mmas)
+              mma_f16_ts(d + (uint32_t)(kIssuers * b * NT), ta + 8 * e, bd + (uint64_t)((e >> 2) * (NT * 128 >> 4) + 2 * (e & 3)),
+                         kIdesc, e > 0 ? 1u : accumulate);
           mma_commit(&sh->empty[s]);
         }
         accumulate = 1u;
@@ -471,52 +546,34 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign>::kThreads, 1) k_int8_tile(cons
     __syncwarp();
   }
   __syncwarp();
-  Factors F;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int j = j0 + 4 * lane + e;
-    F.sw[e] = j < A.N && A.w_scale ? A.w_scale[j] : 1.0f;
-    F.bias[e] = j < A.N && A.bias ? A.bias[j] : 0.0f;
-    F.thr[e] = j < A.N && A.thr ? A.thr[j] : 0;
-  }
-  {
-    // lane x: the warp's row x
-    const int t = (int)rank + split * (warp + kWorkers * lane);
-    F.sa = A.a_scale && t < NT && i0 + t < A.n ? A.a_scale[i0 + t] : 1.0f;
-  }
+  if (split > 1 && warp >= kWorkers) cluster_arrive();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == kWorkers)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
-  int* sums = reinterpret_cast<int*>(base);
-  if (*failed) {
+  if (*failed && warp < kWorkers) {
     // partial sums of this CTA's k range on CUDA cores
-    const int k0 = C::kStep * first, k1 = min(A.K, C::kStep * (first + steps));
-    for (int e = threadIdx.x; e < CM * NT; e += C::kThreads) {
-      const int j = e % CM, i = e / CM;
-      const int sum = j0 + j < A.N && i0 + i < A.n ? plain_sum(A, i0 + i, j0 + j, k0, k1) : 0;
-      sums[i * C::kSumPitch + j] = sum;
-    }
-    __syncthreads();
-  }
-  if (split > 1) cluster_sync();
-  if (warp < kWorkers) {
-    switch (split) {
-      case 1: write_rows<NT, 1>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
-      case 2: write_rows<NT, 2>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
-      case 4: write_rows<NT, 4>(A, sums, C::kSumPitch, i0, j0, rank, F); break;
-      default: write_rows<NT, 8>(A, sums, C::kSumPitch, i0, j0, rank, F);
+    const int k0 = C::kStep * first, k1 = min(A.K, C::kStep * (first + steps)), j = j0 + 32 * q + lane;
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) {
+      const int64_t i = i0 + kCols * (warp >> 2) + e;
+      acc[e] = j < A.N && i < A.n ? plain_sum(A.a + i * A.lda, A.w + (int64_t)j * A.ldw, k0, k1) : 0;
     }
   }
-  if (split > 1) cluster_sync();   // no CTA leaves while its sums are read
+  const int jw = j0 + 32 * q;
+  switch (split) {
+    case 1: exchange_and_write<kCols, 1>(A, acc, base, rank, i0, jw, F); break;
+    case 2: exchange_and_write<kCols, 2>(A, acc, base, rank, i0, jw, F); break;
+    default: exchange_and_write<kCols, 4>(A, acc, base, rank, i0, jw, F);
+  }
 }
 
-template <int NT, int kAlign>
-cudaError_t launch_tile(const Int8Args& A, int split, int expire, cudaStream_t st) {
-  using C = Cfg<NT, kAlign>;
+template <int NT, int kAlign, bool kReady>
+cudaError_t launch_tile(const Int8Args& A, const uint8_t* ablocks, int split, int expire, cudaStream_t st) {
+  using C = Cfg<NT, kAlign, kReady>;
   constexpr int kSmem = 1024 + C::kStages * C::kStageBytes + C::kRingBytes + (int)sizeof(TileShared);
-  const cudaError_t e = cudaFuncSetAttribute(k_int8_tile<NT, kAlign>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(k_int8_tile<NT, kAlign, kReady>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((A.N + CM - 1) / CM * split), (unsigned)((A.n + NT - 1) / NT));
@@ -530,33 +587,42 @@ cudaError_t launch_tile(const Int8Args& A, int split, int expire, cudaStream_t s
   attr[1].val.clusterDim = {(unsigned)split, 1u, 1u};
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_int8_tile<NT, kAlign>, A, split, expire);
+  return cudaLaunchKernelEx(&cfg, k_int8_tile<NT, kAlign, kReady>, A, ablocks, split, expire);
 }
 
 template <int kAlign>
-cudaError_t launch_rows(const Int8Args& A, int nt, int split, int expire, cudaStream_t st) {
-  switch (nt) {
-    case 32: return launch_tile<32, kAlign>(A, split, expire, st);
-    case 64: return launch_tile<64, kAlign>(A, split, expire, st);
-    case 96: return launch_tile<96, kAlign>(A, split, expire, st);
-    default: return launch_tile<128, kAlign>(A, split, expire, st);
-  }
+cudaError_t launch_rows(const Int8Args& A, const uint8_t* ablocks, int nt, int split, int expire, cudaStream_t st) {
+  if (ablocks)
+    return nt == 64 ? launch_tile<64, kAlign, true>(A, ablocks, split, expire, st)
+                    : launch_tile<128, kAlign, true>(A, ablocks, split, expire, st);
+  return nt == 32   ? launch_tile<32, kAlign, false>(A, nullptr, split, expire, st)
+         : nt == 64 ? launch_tile<64, kAlign, false>(A, nullptr, split, expire, st)
+                    : launch_tile<128, kAlign, false>(A, nullptr, split, expire, st);
 }
 
 }  // namespace
 
-cudaError_t launch_int8_tile(const Int8Args& all, cudaStream_t st, int expire) {
-  Int8Args A = all;
-  A.n = std::min<int64_t>(all.n, kMaxRows);
-  const int nt = A.n <= 32 ? 32 : (A.n <= 64 ? 64 : (A.n <= 96 ? 96 : 128));
-  const int64_t tiles = (int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt);
-  const int steps = (A.K + 63) / 64;
+// CTAs that share K: as many as leave every SM at most one, with eight k-steps of 64 each.
+int int8_tile_split(int64_t tiles, int K) {
+  const int steps = (K + 63) / 64;
   int split = 1;
   while (split < kMaxSplit && tiles * (2 * split) <= sm_count() && steps >= 8 * split) split *= 2;
-  const cudaError_t e =
-      operand_align(A) == 16 ? launch_rows<16>(A, nt, split, expire, st) : launch_rows<1>(A, nt, split, expire, st);
-  if (e != cudaSuccess || all.n <= kMaxRows) return e;
-  return launch_int8_tile(rest_of(all, kMaxRows), st, expire);
+  return split;
+}
+
+cudaError_t launch_int8_tile(const Int8Args& all, void* workspace, cudaStream_t st, int expire, int nt) {
+  Int8Args A = all;
+  A.n = std::min<int64_t>(all.n, kTileSlab);
+  const int split = int8_tile_split((int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt), A.K);
+  if (workspace) {
+    const cudaError_t e = launch_int8_expand_rows(A, workspace, st);
+    if (e != cudaSuccess) return e;
+  }
+  const uint8_t* ablocks = static_cast<const uint8_t*>(workspace);
+  const bool wide = operand_align_w(A) == 16 && (workspace || operand_align(A) == 16);
+  const cudaError_t e = wide ? launch_rows<16>(A, ablocks, nt, split, expire, st) : launch_rows<1>(A, ablocks, nt, split, expire, st);
+  if (e != cudaSuccess || all.n <= kTileSlab) return e;
+  return launch_int8_tile(rest_of(all, kTileSlab), workspace, st, expire, nt);
 }
 
 }  // namespace bk
