@@ -282,10 +282,21 @@ int bmlp_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr,
  *   a: n x K, row stride lda.  w: N x K, row stride ldw.  All 256 values allowed.
  *   a_scale: n, w_scale: N, bias: N; each may be NULL (1, 1, 0).
  *   out: n x N of out_type, row stride ldo.
- * K in 1..BMLP_INT8_MAX_K, N >= 1. */
+ * K in 1..BMLP_INT8_MAX_K, N in 1..2^30.
+ * workspace, workspace_bytes: see bmlp_int8_workspace.  A bounded device-side wait that
+ * expires costs time only: the affected sums are made again without waits. */
 int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
                      const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
                      int32_t out_type, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* bmlp_int8_matmul with the path of an expired device-side wait forced, for tests:
+ * every CTA of its tensor-core kernels takes one as expired (up to 8 rows run
+ * without such waits).  The affected sums are made again on CUDA cores, so the
+ * output is whole, as it is where a bounded wait does expire. */
+int bmlp_debug_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
+                           const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
+                           int32_t out_type, int64_t ldo, void* workspace, int64_t workspace_bytes,
+                           void* cuda_stream);
 
 /* Signs of the same product, packed: bit j of row i is 1 (+1) iff
  * S_ij >= threshold_j (threshold: N int32, or NULL for 0: sign(0) = +1); exact.

@@ -95,6 +95,8 @@ SIGNATURES = [
                                      C.c_float, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp]),
     ("bmlp_int8_matmul", C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int32, C.c_int32,
                                    _vp, C.c_int32, C.c_int64, _vp, C.c_int64, _vp]),
+    ("bmlp_debug_int8_matmul", C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int32, C.c_int32,
+                                   _vp, C.c_int32, C.c_int64, _vp, C.c_int64, _vp]),
     ("bmlp_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp,
                                  C.c_int64, _vp]),
     ("bmlp_int8_workspace", C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
@@ -329,26 +331,50 @@ def bmlp_int8_workspace(n, K, N):
     return int(lib().bmlp_int8_workspace(n, K, N))
 
 
+_KEPT_WORKSPACE = 64 << 20     # bytes of the largest workspace that is kept for the next call
+_kept = threading.local()      # .at[device, stream]: this thread's, in the order of that stream
+
+
+def bmlp_release_workspaces():
+    """Give the workspaces that bmlp_int8_matmul and bmlp_int8_sign keep for the
+    calling thread back to torch's allocator."""
+    _kept.__dict__.clear()
+
+
 def _workspace(L, workspace, n, K, N, a, stream):
-    """(pointer, bytes, owner) of the given workspace, or of one from torch's
-    allocator where the size wants it."""
-    if workspace is None:
-        size = L.bmlp_int8_workspace(n, K, N)
-        if size == 0 or not a.is_cuda:
-            return None, 0, None
-        workspace = _torch.empty(size, dtype=_torch.uint8, device=a.device)
+    """(pointer, bytes) of the given workspace, or of one from torch's allocator where
+    the size wants it: kept for the thread's next call on the same stream if it is small
+    and the stream is torch's current one, not in a capture."""
+    if workspace is not None:
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    size = L.bmlp_int8_workspace(n, K, N)
+    if size == 0 or not a.is_cuda:
+        return None, 0, None
+    torch = _torch
+    keep = stream is None and size <= _KEPT_WORKSPACE and not torch.cuda.is_current_stream_capturing()
+    if keep:
+        at = _kept.__dict__.setdefault("at", {})
+        key = a.device, _tensor_stream(None, a)
+        workspace = at.get(key)
+        if workspace is not None and workspace.shape[0] >= size:
+            return workspace.data_ptr(), size, workspace
+        workspace = at[key] = None   # (the smaller one goes back first)
+        workspace = at[key] = torch.empty(size, dtype=torch.uint8, device=a.device)
+    else:
+        workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
         if stream is not None:
             raw = _stream(stream)
-            if raw != _torch.cuda.current_stream(a.device).cuda_stream:
-                workspace.record_stream(_torch.cuda.ExternalStream(raw, a.device))
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+            if raw != torch.cuda.current_stream(a.device).cuda_stream:
+                workspace.record_stream(torch.cuda.ExternalStream(raw, a.device))
+    return workspace.data_ptr(), size, workspace
 
 
-def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=None, workspace=None):
+def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=None, workspace=None, expired=False):
     """out (n x N fp32 / fp16 / bf16, or int32 without scales and bias) = a (n x K
     int8) times w (N x K int8) transposed, scaled per row and channel.
-    workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: from
-    torch's allocator)."""
+    workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: one from
+    torch's allocator; up to 64 MB of it stay with the thread for its next call on the
+    stream, until bmlp_release_workspaces).  expired: bmlp_debug_int8_matmul."""
     torch = _torch or _use_torch()
     L = _lib or lib()
     shape = n, K = a.shape
@@ -357,10 +383,11 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     po, ldo = _rows(out, (n, N), "out", out.dtype)
     f32 = torch.float32
-    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 8 or workspace is not None else (None, 0, None)
-    rc = L.bmlp_int8_matmul(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw,
-                            _vector(w_scale, N, "w_scale", f32), _vector(bias, N, "bias", f32), n, K, N,
-                            po, _type(out, _out_types, "out"), ldo, ws, wsb, _tensor_stream(stream, a))
+    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 32 or workspace is not None else (None, 0, None)
+    call = L.bmlp_debug_int8_matmul if expired else L.bmlp_int8_matmul
+    rc = call(pa, lda, _vector(a_scale, n, "a_scale", f32), pw, ldw, _vector(w_scale, N, "w_scale", f32),
+              _vector(bias, N, "bias", f32), n, K, N, po, _type(out, _out_types, "out"), ldo, ws, wsb,
+              _tensor_stream(stream, a))
     if rc:
         _check(rc)
 
@@ -377,7 +404,7 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():
         raise ValueError("out: expected %d x %d contiguous 64-bit words" % (n, (N + 63) // 64))
-    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 8 or workspace is not None else (None, 0, None)
+    ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 32 or workspace is not None else (None, 0, None)
     rc = L.bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
                           out.data_ptr(), ws, wsb, _tensor_stream(stream, a))
     if rc:

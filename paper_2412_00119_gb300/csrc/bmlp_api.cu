@@ -217,9 +217,10 @@ int quantize_call(const char* name, const QuantArgs& A, bool norm, void* cuda_st
 }
 
 // The same for bmlp_int8_matmul and bmlp_int8_sign (A.words set).
-int int8_call(const char* name, const Int8Args& A, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
-  if (A.n < 0 || A.K < 1 || A.K > BMLP_INT8_MAX_K || A.N < 1)
-    return fail(nullptr, BMLP_EINVAL, "%s: n < 0, N < 1, or K outside 1..%d", name, BMLP_INT8_MAX_K);
+int int8_call(const char* name, const Int8Args& A, void* workspace, int64_t workspace_bytes, void* cuda_stream,
+              int expire = 0) {
+  if (A.n < 0 || A.K < 1 || A.K > BMLP_INT8_MAX_K || A.N < 1 || A.N > (1 << 30))
+    return fail(nullptr, BMLP_EINVAL, "%s: n < 0, N < 1 or N > 2^30, or K outside 1..%d", name, BMLP_INT8_MAX_K);
   if (A.type < BMLP_F32 || A.type > BMLP_I32)
     return fail(nullptr, BMLP_EINVAL, "%s: unknown out_type", name);
   if (A.type == BMLP_I32 && (A.a_scale || A.w_scale || A.bias))
@@ -234,7 +235,7 @@ int int8_call(const char* name, const Int8Args& A, void* workspace, int64_t work
     return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
   if (workspace && (workspace_bytes < 0 || !usable(workspace, 4)))
     return fail(nullptr, BMLP_EINVAL, "%s: the workspace must be a device pointer, 16-byte aligned", name);
-  const cudaError_t e = launch_int8(A, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+  const cudaError_t e = launch_int8(A, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream), expire);
   if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
   return BMLP_OK;
 }
@@ -1008,6 +1009,15 @@ int bmlp_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const i
   return int8_call("bmlp_int8_matmul", A, workspace, workspace_bytes, cuda_stream);
 }
 
+int bmlp_debug_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, const int8_t* w, int64_t ldw,
+                           const float* w_scale, const float* bias, int64_t n, int32_t K, int32_t N, void* out,
+                           int32_t out_type, int64_t ldo, void* workspace, int64_t workspace_bytes,
+                           void* cuda_stream) {
+  TraceRange trace("bmlp_int8_matmul");
+  const Int8Args A = {a, w, a_scale, w_scale, bias, nullptr, out, nullptr, lda, ldw, ldo, n, K, N, out_type};
+  return int8_call("bmlp_debug_int8_matmul", A, workspace, workspace_bytes, cuda_stream, 1);
+}
+
 int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
                    int64_t n, int32_t K, int32_t N, uint64_t* out, void* workspace, int64_t workspace_bytes,
                    void* cuda_stream) {
@@ -1017,7 +1027,7 @@ int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, c
 }
 
 int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N) {
-  return n < 1 || K < 1 || K > BMLP_INT8_MAX_K || N < 1 ? 0 : int8_workspace(n, K, N);
+  return n < 1 || K < 1 || K > BMLP_INT8_MAX_K || N < 1 || N > (1 << 30) ? 0 : int8_workspace(n, K, N);
 }
 
 int bmlp_get_state(const bmlp_t* hc, int32_t layer, int16_t* H_out, uint64_t* W_out, int8_t* P_out,

@@ -2,6 +2,7 @@
 // BMLP library (fully binary training rule of arXiv 2412.00119, Alg. 1-3).
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -187,6 +188,20 @@ cudaError_t launch_kernel(void (*k)(KArgs...), dim3 grid, dim3 block, size_t sme
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, k, args...);
+}
+
+// Lets kernel k have `bytes` of dynamic shared memory, once per device (done: a static of the
+// caller's, one per kernel).
+template <typename K>
+cudaError_t allow_smem(std::atomic<uint64_t>& done, K k, int bytes) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  const cudaError_t es = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (es == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return es;
 }
 
 // ---------------------------------------------------------------------------

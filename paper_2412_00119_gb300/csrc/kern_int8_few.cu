@@ -151,8 +151,8 @@ __global__ void __launch_bounds__(32 * kWarps) k_int8_few(const Int8Args A) {
 template <int kWarps, int kAlign>
 cudaError_t launch_few(const Int8Args& A, int ctas, cudaStream_t st) {
   constexpr int kSmem = kWarps * kRing * Few<kAlign>::kTurnBytes;
-  const cudaError_t e =
-      cudaFuncSetAttribute(k_int8_few<kWarps, kAlign>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(done, k_int8_few<kWarps, kAlign>, kSmem);
   if (e != cudaSuccess) return e;
   return launch_kernel(k_int8_few<kWarps, kAlign>, dim3((unsigned)ctas), dim3(32 * kWarps), (size_t)kSmem, st, true, A);
 }

@@ -469,7 +469,8 @@ bool block_map(CUtensorMap* map, void* blocks, int64_t rows) {
 template <typename TOut>
 cudaError_t launch_out(const Int8Args& A, const CUtensorMap& wmap, const CUtensorMap& amap, int nkb, cudaStream_t st,
                        int expire) {
-  const cudaError_t e = cudaFuncSetAttribute(k_int8_pair<TOut>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(done, k_int8_pair<TOut>, kSmem);
   if (e != cudaSuccess) return e;
   const int ctiles = (int)(padded(A.N) / TP);
   const int64_t rtiles = padded(A.n) / TP;

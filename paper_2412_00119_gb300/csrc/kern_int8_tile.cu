@@ -573,7 +573,8 @@ template <int NT, int kAlign, bool kReady>
 cudaError_t launch_tile(const Int8Args& A, const uint8_t* ablocks, int split, int expire, cudaStream_t st) {
   using C = Cfg<NT, kAlign, kReady>;
   constexpr int kSmem = 1024 + C::kStages * C::kStageBytes + C::kRingBytes + (int)sizeof(TileShared);
-  const cudaError_t e = cudaFuncSetAttribute(k_int8_tile<NT, kAlign, kReady>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(done, k_int8_tile<NT, kAlign, kReady>, kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((A.N + CM - 1) / CM * split), (unsigned)((A.n + NT - 1) / NT));

@@ -399,6 +399,112 @@ def test_streams_and_capture():
         check()
 
 
+# sizes whose kernel is, in turn: the streamed one; 32-row tiles (K shared by four, one CTA);
+# 64- and 128-row tiles of ready activations (with and without sharing K; two rounds); pairs
+PLANS = [(5, 300, 100), (20, 2048, 300), (31, 100, 19500), (50, 8192, 8192), (64, 8000, 7000), (100, 4096, 8192),
+         (120, 8191, 4096), (300, 2300, 9000), (700, 4096, 4096), (1500, 1024, 8192), (2100, 1001, 6000)]
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", PLANS)
+def test_every_plan(n, K, N):
+    run_all(codes(n, K, n, "ends"), codes(N, K, K), K, N, n, 0, 0)
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(12, 200, 300), (20, 2048, 300), (50, 4096, 4000), (100, 2048, 4096), (300, 3000, 2000),
+                                   (1500, 1024, 8192)])
+def test_expired_waits_cost_time_only(n, K, N):
+    """With every CTA's wait taken as expired the sums are made again, whole; without a
+    workspace too."""
+    a, w = codes(n, K, n).to(DEV), codes(N, K, K).to(DEV)
+    S = sums64(a, w)
+    for ws in (None, torch.empty(16, dtype=torch.uint8, device=DEV)):
+        out = torch.full((n, N), -3, dtype=torch.int32, device=DEV)
+        B.bmlp_int8_matmul(a, w, out, workspace=ws, expired=True)
+        assert torch.equal(out.double(), S)
+        out.fill_(-3)
+        B.bmlp_int8_matmul(a, w, out, workspace=ws)     # the device is as it was
+        assert torch.equal(out.double(), S)
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(40, 3000, 5000), (100, 4096, 8192), (300, 2304, 4000), (1500, 1024, 8192)])
+def test_workspaces(n, K, N):
+    """Given, too small, misaligned, kept, on other streams: the same sums."""
+    a, w = codes(n, K, n).to(DEV), codes(N, K, K).to(DEV)
+    S = sums64(a, w)
+    size = B.bmlp_int8_workspace(n, K, N)
+    out = torch.empty((n, N), dtype=torch.int32, device=DEV)
+
+    def check():
+        torch.cuda.synchronize()
+        assert torch.equal(out.double(), S)
+        out.fill_(-3)
+
+    for bytes_ in (size, max(size - 1, 16), 16):
+        ws = torch.full((bytes_,), 0x7F, dtype=torch.uint8, device=DEV)     # (fp16 NaNs)
+        B.bmlp_int8_matmul(a, w, out, workspace=ws)
+        check()
+    if size:
+        with pytest.raises(B.BmlpError):
+            B.bmlp_int8_matmul(a, w, out, workspace=torch.empty(size + 16, dtype=torch.uint8, device=DEV)[1:])
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [torch.empty((n, N), dtype=torch.int32, device=DEV) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, o in zip(streams, outs):
+            with torch.cuda.stream(s):
+                B.bmlp_int8_matmul(a, w, o)
+        for s, o in zip(streams, outs):
+            B.bmlp_int8_matmul(a, w, o, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o.double(), S)
+    B.bmlp_int8_matmul(a, w, out)
+    check()
+    B.bmlp_release_workspaces()
+    B.bmlp_int8_matmul(a, w, out)
+    check()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.bmlp_int8_matmul(a, w, out)
+    B.bmlp_release_workspaces()
+    junk = torch.full((max(size, 16),), 0x7F, dtype=torch.uint8, device=DEV)
+    out.fill_(-3)
+    g.replay()
+    check()
+    del junk
+
+
+@gpu
+def test_back_to_back_calls_do_not_mix():
+    """Calls that depend on one another, with nothing between them: each kernel may start while
+    the one before it ends."""
+    n, K = 200, 512
+    a, w1, w2 = codes(n, K, 1).to(DEV), codes(K, K, 2).to(DEV), codes(96, K, 3).to(DEV)
+    y = torch.empty((n, K), dtype=torch.bfloat16, device=DEV)
+    q = torch.empty((n, K), dtype=torch.int8, device=DEV)
+    q2 = torch.empty((n, K), dtype=torch.int8, device=DEV)
+    s = torch.empty((n,), device=DEV)
+    out = torch.empty((n, 96), dtype=torch.int32, device=DEV)
+    want = None
+    for rep in range(30):
+        for rows in (n, 3, 20, 70):
+            B.bmlp_int8_matmul(a[:rows], w1, y[:rows], None, None)
+            B.bmlp_quantize_rows(y[:rows], q[:rows], s[:rows])
+            B.bmlp_int8_matmul(q[:rows], w1, y[:rows])
+            B.bmlp_norm_quantize(y[:rows], None, q2[:rows], s[:rows])
+            B.bmlp_int8_matmul(q2[:rows], w2, out[:rows])
+        torch.cuda.synchronize()
+        if want is None:
+            S1 = sums64(a, w1).float().bfloat16()
+            c1 = plain_codes(S1.cpu())[1]
+            c2 = plain_codes(sums64(c1, w1).float().bfloat16().cpu())[1]
+            want = sums64(c2, w2)
+        assert torch.equal(out.double(), want), rep
+
+
 @gpu
 def test_front_end_feeds_training():
     """Hidden states -> norm -> 8-bit product's signs -> training and prediction, equal to the
