@@ -632,3 +632,27 @@ def test_binding_refusals():
         B.bmlp_int8_sign(i8(2, 8), i8(4, 8), t((2, 2), dtype=torch.int64))
     with pytest.raises(B.BmlpError):
         B.bmlp_int8_sign(i8(2, 8), i8(4, 8), t((2, 1), dtype=torch.int64))   # host memory
+
+
+@gpu
+def test_example_runs():
+    """The example program: hidden states through the front end into training and prediction."""
+    import importlib.util
+    import os
+    from conftest import ROOT
+    spec = importlib.util.spec_from_file_location("hidden_states", os.path.join(ROOT, "examples", "hidden_states.py"))
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    got = ex.main(["--n", "3000", "--dim", "512", "--width", "512", "--epochs", "4"])
+    # codes of 8 bits are off by at most half a step of 1/127 of a row's largest value, here some
+    # 16 times the others' size: errors of that step's uniform distribution, 16 / 127 / sqrt(12) = 0.036
+    assert got["error"] < 0.1
+    assert got["same"]
+    # trained by the oracle on the same words
+    pm1 = lambda t: W.unpack(t.cpu().numpy().view(np.uint64), 512)   # noqa: E731
+    ref = O.OracleModel([512, 255, 255], 10, seed=5, bs=100)
+    x, y = pm1(got["words"]), got["y"].cpu().numpy()
+    for _ in range(4):
+        errors = ref.train(x, y, epoch_end=True)
+    assert errors == got["errors"]
+    assert np.array_equal(got["labels"].cpu().numpy(), ref.predict(pm1(got["test"])))
