@@ -103,11 +103,11 @@ __device__ __forceinline__ void row_reduce(float& sq, uint32_t& most, bool norm,
 template <typename T, int V> struct Pack {
   static constexpr int kBytes = V * (int)sizeof(T);
   uint32_t w[(kBytes + 3) / 4];
-  // `left` values of the row from p on, zeros after them
-  __device__ __forceinline__ void load(const T* p, int left) {
+  // values [skip, left) of those from p on, which are the row's; zeros in the others' place
+  __device__ __forceinline__ void load(const T* p, int skip, int left) {
 #pragma unroll
     for (int i = 0; i < (kBytes + 3) / 4; ++i) w[i] = 0u;
-    if (left >= V) {
+    if (skip <= 0 && left >= V) {
       if constexpr (kBytes == 16) {
         const uint4 v = *reinterpret_cast<const uint4*>(p);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
@@ -118,22 +118,22 @@ template <typename T, int V> struct Pack {
       }
     } else if constexpr (V > 1) {
 #pragma unroll
-      for (int i = 0; i < V - 1; ++i)
-        if (i < left) {
+      for (int i = 0; i < V; ++i)
+        if (i >= skip && i < left) {
           if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
           else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
         }
     }
   }
-  __device__ __forceinline__ void store(T* p, int left) const {
-    if (left >= V) {
+  __device__ __forceinline__ void store(T* p, int skip, int left) const {
+    if (skip <= 0 && left >= V) {
       if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
       else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
       else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     } else if constexpr (V > 1) {
 #pragma unroll
-      for (int i = 0; i < V - 1; ++i)
-        if (i < left) {
+      for (int i = 0; i < V; ++i)
+        if (i >= skip && i < left) {
           if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i) = w[i];
           else *reinterpret_cast<uint16_t*>(p + i) = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
         }
@@ -159,8 +159,7 @@ template <typename T, int V> struct Pack {
 };
 
 template <int V>
-__device__ __forceinline__ void store_codes(int8_t* p, const float (&u)[V], float inv, uint32_t live, int left) {
-  uint32_t w[(V + 3) / 4];
+__device__ __forceinline__ void make_codes(uint32_t (&w)[(V + 3) / 4], const float (&u)[V], float inv, uint32_t live) {
 #pragma unroll
   for (int i = 0; i < (V + 3) / 4; ++i) {
     uint32_t c[4];
@@ -169,6 +168,11 @@ __device__ __forceinline__ void store_codes(int8_t* p, const float (&u)[V], floa
     const uint32_t lo = V > 1 ? __byte_perm(c[0], c[1], 0x0040) : c[0];
     w[i] = (V > 2 ? __byte_perm(lo, __byte_perm(c[2], c[3], 0x0040), 0x5410) : lo) & live;
   }
+}
+
+// p aligned to V codes.
+template <int V>
+__device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&w)[(V + 3) / 4], int left) {
   if (left >= V) {
     if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
@@ -181,15 +185,49 @@ __device__ __forceinline__ void store_codes(int8_t* p, const float (&u)[V], floa
   }
 }
 
+// A row's K codes from shared memory, where code e is byte e + apart of buf (16-byte aligned, 16
+// bytes before it), to q, anywhere: a thread of `threads` takes aligned 16 bytes of q at a time.
+__device__ __forceinline__ void copy_codes(int8_t* q, const uint8_t* buf, int apart, int K, int tid, int threads) {
+  const int before = (int)(reinterpret_cast<uintptr_t>(q) & 15);
+  const int shift = apart - before;                       // byte of buf for the first of q's chunks
+  for (int e = 16 * tid - before; e < K; e += 16 * threads) {
+    const int at = e + before + shift;                    // (from -15 on)
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(buf + (at & ~3));
+    uint32_t v[4];
+    uint32_t x = w[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t y = w[i + 1];
+      v[i] = __funnelshift_r(x, y, 8u * (uint32_t)(at & 3));
+      x = y;
+    }
+    if (e >= 0 && e + 16 <= K) {
+      *reinterpret_cast<uint4*>(q + e) = make_uint4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (e + i >= 0 && e + i < K) q[e + i] = (int8_t)(v[i / 4] >> (8 * (i % 4)));
+    }
+  }
+}
+
 constexpr int kRowsPerCta = 8;   // rows of a CTA with a warp each
 // What is done to a row (residual: its registers are there only where it is).
 constexpr int kPlain = 0, kNormed = 1, kResidual = 2;
+
+// Shared memory of a row's codes: a vector per thread and turn, 16 bytes before and after.
+template <int V>
+__host__ __device__ constexpr int codes_bytes(int nv, int threads) { return nv * threads * V + 32; }
 
 // A row's T threads hold it: vector v of thread t is v T + t, NV vectors of V values
 // each.  The grid walks the rows; a row's values are loaded while the row before is
 // reduced and written, and the gain stays in registers (kAhead; without it neither,
 // where the registers do not hold both).
-template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead>
+// kApart: rows that do not start at multiples of 16 bytes, all buffers' equally far from one.
+// A thread's vectors are the aligned 16 bytes around the row; rows eight apart lie
+// alike, and a thread's rows are a multiple of eight apart.  The codes go through shared
+// memory, since theirs lie otherwise.
+template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead, bool kApart>
 __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize_regs(const QuantArgs A) {
   pdl_wait();
   pdl_trigger();
@@ -202,18 +240,37 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
   const T* res = static_cast<const T*>(A.res);
   T* sum = kNorm ? static_cast<T*>(A.sum) : nullptr;
   const T* gain = kNorm ? static_cast<const T*>(A.gain) : nullptr;
-  auto at = [&](int v) { return (v * threads + tid) * V; };
+  extern __shared__ uint4 smem_codes[];
+  uint8_t* codes = reinterpret_cast<uint8_t*>(smem_codes) + 16 + (kWarpRow ? (int)(threadIdx.x >> 5) * codes_bytes<V>(NV, 32) : 0);
+  const int apart = kApart ? (int)((reinterpret_cast<uintptr_t>(x + row * A.ldx) & 15) / sizeof(T)) : 0;
+  auto at = [&](int v) { return (v * threads + tid) * V - apart; };
+  auto skip = [&](int v) { return kApart ? -at(v) : 0; };
   Pack<T, V> px[NV], pr[kRes ? NV : 1], pg[kAhead ? NV : 1];
-  if (kAhead && gain) {
+  auto load_gain = [&](int v, Pack<T, V>& to) {
+    if constexpr (kApart) {
+      // (the gain lies otherwise than the rows: value by value)
 #pragma unroll
-    for (int v = 0; v < NV; ++v) pg[kAhead ? v : 0].load(gain + at(v), A.K - at(v));
+      for (int i = 0; i < (Pack<T, V>::kBytes + 3) / 4; ++i) to.w[i] = 0u;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (at(v) + i >= 0 && at(v) + i < A.K) {
+          if constexpr (sizeof(T) == 4) to.w[i] = reinterpret_cast<const uint32_t*>(gain)[at(v) + i];
+          else to.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(gain)[at(v) + i] << (16 * (i % 2));
+        }
+    } else {
+      to.load(gain + at(v), 0, A.K - at(v));
+    }
+  };
+  if (kAhead && gain && row < A.n) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load_gain(v, pg[kAhead ? v : 0]);
   }
   auto load = [&](int64_t i) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) px[v].load(x + i * A.ldx + at(v), A.K - at(v));
+    for (int v = 0; v < NV; ++v) px[v].load(x + i * A.ldx + at(v), skip(v), A.K - at(v));
     if constexpr (kRes) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) pr[v].load(res + i * A.ldr + at(v), A.K - at(v));
+      for (int v = 0; v < NV; ++v) pr[v].load(res + i * A.ldr + at(v), skip(v), A.K - at(v));
     }
   };
   if (kAhead && row < A.n) load(row);
@@ -235,12 +292,12 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
       for (int v = 0; v < NV; ++v) {
         Pack<T, V> ps;
         ps.set(u[v]);
-        ps.store(sum + row * A.lds + at(v), A.K - at(v));
+        ps.store(sum + row * A.lds + at(v), skip(v), A.K - at(v));
       }
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (!kAhead && gain) pg[0].load(gain + at(v), A.K - at(v));
+      if (!kAhead && gain) load_gain(v, pg[0]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         if (kNorm) sq += u[v][i] * u[v][i];
@@ -252,8 +309,26 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
     row_reduce<kWarpRow>(sq, mbits, kNorm, turn);
     const RowScale r = row_scale(mbits, sq, A.K, A.eps, kNorm);
     const uint32_t live = r.inv == 0.0f ? 0u : 0xFFFFFFFFu;
+    int8_t* q = A.q + row * A.ldq;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) store_codes<V>(A.q + row * A.ldq + at(v), u[v], r.inv, live, A.K - at(v));
+    for (int v = 0; v < NV; ++v) {
+      uint32_t w[(V + 3) / 4];
+      make_codes<V>(w, u[v], r.inv, live);
+      if constexpr (!kApart) {
+        store_codes<V>(q + at(v), w, A.K - at(v));
+      } else {
+        // (the row before was copied from there by threads that have since met in row_reduce)
+        uint8_t* to = codes + (v * threads + tid) * V;
+        if constexpr (V == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[(V + 3) / 4 - 1]);
+        else *reinterpret_cast<uint32_t*>(to) = w[0];
+      }
+    }
+    if constexpr (kApart) {
+      if constexpr (kWarpRow) __syncwarp();
+      else __syncthreads();
+      copy_codes(q, codes, apart, A.K, tid, threads);
+      if constexpr (kWarpRow) __syncwarp();
+    }
     if (tid == 0) A.scale[row] = r.scale;
   }
 }
@@ -296,22 +371,23 @@ __global__ void __launch_bounds__(kThreads) k_quantize_long(const QuantArgs A) {
 // norm is made (65,536 x 784 34 us on four CTAs per SM, without 42); fp32 rows and rows that
 // are only coded run faster from more warps (60,000 x 784 fp32 46, ahead 55; 60,000 x 1000
 // bf16 coded 28.6, ahead 32.5).
-template <typename T, int kMode, int V, int NV>
+template <typename T, int kMode, int V, int NV, bool kApart>
 cudaError_t launch_warp_rows(const QuantArgs& A, cudaStream_t st) {
-  constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain);
+  constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain) || kApart;
   const int64_t ctas = std::min((A.n + kRowsPerCta - 1) / kRowsPerCta, (int64_t)(kAhead && V * NV > 16 ? 4 : 8) * sm_count());
-  return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta), 0, st,
-                       true, A);
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead, kApart>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta),
+                       kApart ? (size_t)(kRowsPerCta * codes_bytes<V>(NV, 32)) : 0, st, true, A);
 }
 
 // A CTA per row: 1,024 threads an SM.
-template <typename T, int kMode, int V, int NV>
+template <typename T, int kMode, int V, int NV, bool kApart>
 cudaError_t launch_cta_rows(const QuantArgs& A, cudaStream_t st) {
-  const int threads = (A.K + 32 * V * NV - 1) / (32 * V * NV) * 32;
+  const int vecs = kApart ? (int)((A.K + 2ll * V - 2) / V) : A.K / V + (A.K % V != 0);
+  const int threads = (vecs + 32 * NV - 1) / (32 * NV) * 32;
   constexpr bool kAhead = !(kMode != kPlain && V * NV > (sizeof(T) == 2 ? 16 : 8));
-  const int64_t ctas = kAhead ? std::min(A.n, (int64_t)(1024 / threads) * sm_count()) : A.n;
-  return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead>, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st,
-                       true, A);
+  const int64_t ctas = kAhead ? std::min(A.n, (int64_t)(1024 / threads) * sm_count() / 8 * 8) : A.n;
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart>, dim3((unsigned)ctas), dim3((unsigned)threads),
+                       kApart ? (size_t)codes_bytes<V>(NV, threads) : 0, st, true, A);
 }
 
 // Which form (us, rows in bf16 unless said): rows that a warp holds in at most kWarpMost
@@ -319,33 +395,45 @@ cudaError_t launch_cta_rows(const QuantArgs& A, cudaStream_t st) {
 // 62).  Else a CTA per row, with one vector per thread for few rows (1 x 8192 2.5, two 2.8, four 4.1), and
 // for many as many as the registers hold beside the next row's: four without a norm
 // (8192 x 8192 30, two 34, one 44), two with it (8191 x 4096 with residual 40, four 57 for want of registers).
-template <typename T, int kMode, int V>
+template <typename T, int kMode, int V, bool kApart>
 cudaError_t launch_v(const QuantArgs& A, cudaStream_t st) {
-  constexpr int kWarpMost = V == 8 ? 4 : 8;
-  const int vecs = A.K / V + (A.K % V != 0);
-  if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1>(A, st);
-  if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2>(A, st);
-  if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4>(A, st);
-  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost>(A, st);
+  constexpr int kWarpMost = V == 8 ? 4 : (V == 4 ? 8 : 16);
+  const int64_t vecs = kApart ? (A.K + 2ll * V - 2) / V : A.K / V + (A.K % V != 0);
+  if constexpr (!kApart) {
+    if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1, false>(A, st);
+    if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2, false>(A, st);
+    if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4, false>(A, st);
+    if (V <= 2 && vecs <= 256) return launch_warp_rows<T, kMode, V, V <= 2 ? 8 : 4, false>(A, st);
+  }
+  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart>(A, st);
   if (vecs > 4096)
     return launch_kernel(k_quantize_long<T, kMode>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
   const bool few = A.n <= 2 * sm_count();
-  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4>(A, st);
-  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2>(A, st);
-  return launch_cta_rows<T, kMode, V, 1>(A, st);
+  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart>(A, st);
+  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart>(A, st);
+  return launch_cta_rows<T, kMode, V, 1, kApart>(A, st);
 }
 
+// Vectors of 16 bytes; also where rows start elsewhere but all buffers' alike, if they are long and
+// many (us, by single values after it: 8191 x 4095 bf16 with residual 68, 98; 60,000 x 1001 bf16
+// coded 51, 66; but 60,000 x 255 25, 13, and 100 x 1001 4.3, 2.1) or too long for single values;
+// else of 4 bytes or single values.
 template <typename T, int kMode>
 cudaError_t launch_type(const QuantArgs& A, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
   const bool many = A.n > 1;
-  const uintptr_t wide = reinterpret_cast<uintptr_t>(A.x) | reinterpret_cast<uintptr_t>(A.res) |
-                         reinterpret_cast<uintptr_t>(A.gain) | reinterpret_cast<uintptr_t>(A.sum) |
-                         (many ? (uintptr_t)((A.ldx | (A.res ? A.ldr : 0) | (A.sum ? A.lds : 0)) * (int64_t)sizeof(T)) : 0);
+  auto place = [&](const void* p, int64_t ld) {   // of a buffer's first rows, in 16 bytes
+    return (reinterpret_cast<uintptr_t>(p) & 15) | (many ? (uintptr_t)(ld * (int64_t)sizeof(T)) & 15 : 0) << 4;
+  };
+  const uintptr_t px = place(A.x, A.ldx);
+  const uintptr_t wide = px | (A.res ? place(A.res, A.ldr) : 0) | (A.sum ? place(A.sum, A.lds) : 0) |
+                         (reinterpret_cast<uintptr_t>(A.gain) & 15);
   const uintptr_t codes = reinterpret_cast<uintptr_t>(A.q) | (many ? (uintptr_t)A.ldq : 0);
-  if (wide % 16 == 0 && codes % V == 0) return launch_v<T, kMode, V>(A, st);
-  if (sizeof(T) == 2 && wide % 4 == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1>(A, st);
-  return launch_v<T, kMode, 1>(A, st);
+  if (wide == 0 && codes % V == 0) return launch_v<T, kMode, V, false>(A, st);
+  const bool alike = (!A.res || place(A.res, A.ldr) == px) && (!A.sum || place(A.sum, A.lds) == px);
+  if (alike && A.K > 512 && (A.n > 2 * sm_count() || A.K > 4096) && A.K <= 2048 * V - V) return launch_v<T, kMode, V, true>(A, st);
+  if (sizeof(T) == 2 && (wide & 0x33) == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1, false>(A, st);
+  return launch_v<T, kMode, 1, false>(A, st);
 }
 
 template <typename T>
