@@ -7,21 +7,26 @@
 // chunk's sums are added to int32 registers while the next chunk's MMAs run.
 //
 // A CTA computes 128 channels (MMA M; lanes of tensor memory) x NT rows (MMA N) over
-// its share of K; the CTAs of a cluster share K, and add their int32 sums through
-// distributed shared memory in a fixed order (integers: any order gives the same).
-// Channels on M: a narrow batch costs narrow MMAs, and a warp's lanes hold 32
-// neighbouring channels of a row, as the output wants them.  Warps of a CTA:
+// its share of K; the CTAs of a cluster share K, and send each other int32 sums through
+// distributed shared memory (integers: any order gives the same).  Channels on M: a
+// narrow batch costs narrow MMAs, and a warp's lanes hold 32 neighbouring channels of a row,
+// as the output wants them.  Warps of a CTA:
 //   - 16 workers in four groups that take the k-steps (128 codes of every row, or 64) in
 //     turn: a warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring
-//     of its own: more in flight than registers allow), turns them into fp16, the weights
-//     into tensor memory (a lane per channel) and the activations into shared memory (128B
-//     swizzle), and arrives on "full"; between them the workers drain finished chunks;
+//     of its own: with loads to registers, whose scoreboards are few, 26 us for 32 rows of
+//     8192 -> 8192, now 16.6), turns them into fp16, the weights into tensor memory (a lane per
+//     channel) and the activations into shared memory (128B swizzle), and arrives on "full";
+//     between them the workers drain finished chunks;
 //   - one or two warps issue the MMAs (two: of even and odd k-steps, each into accumulators
-//     of its own), committing to "empty" per k-step and "done" per chunk.
-// Bound: the workers' instructions (about 110 a warp for 64 codes of its rows, and 140 for
-// a turn whatever its length: k-steps of 128 where the ring has room), then the weights'
-// bytes.  With the fp16 weights in shared memory too, 60 KB moved through it per 64 codes at
-// NT = 32 and 96 KB at 128, in 570 and 750 clocks whatever the instructions.
+//     of its own), committing to "empty" per k-step and "done" per chunk;
+//   - with activations that are ready as fp16 blocks (more than 32 rows) one thread copies
+//     those, the workers start on the weights while the launch that writes the blocks runs,
+//     and 100 x 4096 -> 8192 takes 15.4 us (19.0 with the workers making them).
+// Bound, up to 32 rows: the workers' instructions, then the weights' bytes (a k-step of 128
+// 620 clocks, 8192 x 8192 weights 4.1 TB/s).  At 128 ready rows: shared memory's 128 bytes per
+// clock (96 KB per k-step of 128, 790 clocks where its MMAs need 512).  (With the fp16
+// weights in shared memory too a k-step of 64 took 570 clocks at 32 rows and 750 at 128.)  What
+// follows the last sum, the exchange between CTAs above all, takes 2 to 3 us of every call.
 // Every wait is bounded; if one expires the CTA's partial sums are made again on CUDA
 // cores, so the output is always whole.
 #include <algorithm>
@@ -43,7 +48,7 @@ constexpr int kGroups = 4;              // worker groups, each a k-step of its o
 constexpr int kSmemBytes = 225 * 1024;  // for stages and copies in flight
 
 template <int NT, int kAlign, bool kReady> struct Cfg {
-  static constexpr int kSub = NT <= 64 || kReady ? 2 : 1;                // 64 codes (a 128-byte row of fp16) each
+  static constexpr int kSub = NT <= 64 || kReady ? 2 : 1;      // 64 codes (a 128-byte row of fp16) each
   static constexpr int kStep = 64 * kSub;                      // codes of a k-step
   static constexpr int kIssuers = NT <= 64 ? 2 : 1;
   static constexpr int kThreads = 32 * (kWorkers + kIssuers + (kReady ? 1 : 0));
@@ -342,12 +347,12 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
     auto drain = [&]() {
       const int b = drained & 1;
       ok = __all_sync(kFull, mbar_wait(&sh->done[b], (uint32_t)(drained >> 1) & 1u, failed));
-      if (split > 1 && !arrived && (!ok || drained == chunks - 1)) {
+      if (!ok) return;
+      if (split > 1 && drained == chunks - 1) {
         // with the last MMAs stages and ring are done with: the others may write there
         cluster_arrive();
         arrived = true;
       }
-      if (!ok) return;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       // (the odd k-steps' accumulator has nothing in a chunk of one)
       const int both = min(kIssuers, steps - drained * kChunk);
@@ -464,7 +469,7 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
     const int64_t i = i0 + kCols * (warp >> 2) + own * (int)rank + lane;
     F.sa = A.a_scale && lane < own && i < A.n ? A.a_scale[i] : 1.0f;
     while (ok && drained < chunks) drain();
-    if (split > 1 && !arrived) cluster_arrive();
+    if (split > 1 && !arrived) cluster_arrive();   // (after a failure: no copy of this warp is in flight)
     if (expire && threadIdx.x == 0) *failed = 1;
   } else if (kReady && warp == kWorkers + kIssuers) {
     // ---------------- copies of the activations' blocks ----------------
