@@ -12,9 +12,7 @@ namespace i8 {
 
 // One scaled output before its bias, fp32 steps rounded one by one; sa, sw: 1 where
 // there is none.
-__device__ __forceinline__ float scaled(int s, float sa, float sw) {
-  return __fmul_rn(__fmul_rn((float)s, sa), sw);
-}
+__device__ __forceinline__ float scaled(float s, float sa, float sw) { return __fmul_rn(__fmul_rn(s, sa), sw); }
 
 template <typename T> __device__ __forceinline__ T out_cast(float y);
 template <> __device__ __forceinline__ float out_cast(float y) { return y; }
@@ -132,7 +130,7 @@ __device__ __forceinline__ void put_out(const Int8Args& A, int64_t i, int j, int
     static_cast<int32_t*>(A.out)[at] = s;
     return;
   }
-  float y = scaled(s, A.a_scale ? A.a_scale[i] : 1.0f, A.w_scale ? A.w_scale[j] : 1.0f);
+  float y = scaled((float)s, A.a_scale ? A.a_scale[i] : 1.0f, A.w_scale ? A.w_scale[j] : 1.0f);
   if (A.bias) y = __fadd_rn(y, A.bias[j]);
   if (A.type == BMLP_F32) static_cast<float*>(A.out)[at] = y;
   else if (A.type == BMLP_F16) static_cast<__half*>(A.out)[at] = out_cast<__half>(y);

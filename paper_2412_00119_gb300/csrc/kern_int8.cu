@@ -37,7 +37,7 @@ Plan plan_of(int64_t n, int K, int N) {
   };
   const double t32 = tiles(32, 4.6, 0.36, 2.5), t64 = tiles(64, 6.1, 0.44, 2.5), t128 = tiles(128, 7.4, 0.50, 1.5);
   const int64_t pairs = up(up(N, 256) * up(n, 256), sm_count() / 2);
-  const double tpair = 8.0 + 3.0 * codes / 4.5e6 + 3.5 + (double)pairs * std::max(4.5, (double)up(K, 64) * 0.27);
+  const double tpair = 8.0 + 3.0 * codes / 4.5e6 + 3.5 + (double)pairs * std::max(K <= 1024 ? 3.0 : 4.5, (double)up(K, 64) * 0.27);
   // (blocks are numbered in 31 bits)
   const bool blocks = ((int64_t)N + 256) * (K / 64 + 1) < (1ll << 31);
   Plan p = {Path::kTiles, 32};

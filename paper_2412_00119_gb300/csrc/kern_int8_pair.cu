@@ -20,12 +20,16 @@
 //   - on the even CTA one warp issues the MMAs.
 // Measured, both operands' expansion included: 16384 x 8192 -> 8192 1.15 to 1.19 ms = 1,850 to
 // 1,910 TFLOP/s, signs of 65536 x 4096 -> 8192 2.24 to 2.27 ms = 1,940 to 1,960 (bf16 by the
-// library 1,946).  A k-step takes 520 clocks where its MMAs take 512 (with forwarded completions
+// library 1,946).  Up to K = 1024 the one chunk's sums go from tensor memory to the outputs
+// in fp32 as they are read: 47,880 x 332 -> 14,928 signs 445 us (through int32 registers
+// 665).  A k-step takes 520 clocks where its MMAs take 512 (with forwarded completions
 // 730 to 790); a chunk's read-out takes 4,900 of the 8,200 of the next chunk's MMAs, a tile's
 // stores 4,900 (one instance per output type: with the types told apart inside the unrolled
 // stores 21,000).  The expansion runs at 4.1 TB/s.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include <cuda.h>
 
@@ -197,12 +201,49 @@ struct Signs {};
 template <typename T> struct IsSigns { static constexpr bool value = false; };
 template <> struct IsSigns<Signs> { static constexpr bool value = true; };
 
-template <typename T>
-__device__ __forceinline__ T out_of(int s, float sa, float sw, bool has_bias, float bias) {
-  const float y = scaled(s, sa, sw);
-  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
+// Bit e of lane l's word to bit l of lane e's.
+__device__ __forceinline__ uint32_t transpose_bits(uint32_t x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    const uint32_t low = s == 16 ? 0x0000FFFFu : (s == 8 ? 0x00FF00FFu : (s == 4 ? 0x0F0F0F0Fu : (s == 2 ? 0x33333333u : 0x55555555u)));
+    const uint32_t y = __shfl_xor_sync(kFull, x, s);
+    x = lane & s ? (x & ~low) | ((y >> s) & low) : (x & low) | ((y << s) & ~low);
+  }
+  return x;
 }
-template <> __device__ __forceinline__ int32_t out_of<int32_t>(int s, float, float, bool, float) { return s; }
+
+// A warp's outputs of 32 rows from i on (`rows` of them some), 32 channels from jw on, a lane per
+// channel; V: int32 sums, or the same as fp32 where they are exact.
+template <typename TOut, typename V>
+__device__ __forceinline__ void put_group(const Int8Args& A, const V (&v)[32], int64_t i, int rows, int jw, float sw,
+                                          float bias, V thr) {
+  const int lane = threadIdx.x & 31, j = jw + lane;
+  if constexpr (IsSigns<TOut>::value) {
+    const int nw32 = 2 * ((A.N + 63) / 64);
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) bits |= v[e] >= thr ? 1u << e : 0u;
+    bits = transpose_bits(j < A.N ? bits : 0u);
+    if (lane < rows && (jw >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[(i + lane) * nw32 + (jw >> 5)] = bits;
+  } else {
+    TOut* to = static_cast<TOut*>(A.out) + i * A.ldo + j;
+    const bool has_bias = A.bias != nullptr;
+    const float sal = A.a_scale && lane < rows ? A.a_scale[i + lane] : 1.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e, to += A.ldo) {
+      const float sa = __shfl_sync(kFull, sal, e);
+      TOut y;
+      if constexpr (std::is_same<TOut, int32_t>::value) {
+        y = (int32_t)v[e];
+      } else {
+        const float f = scaled((float)v[e], sa, sw);
+        y = out_cast<TOut>(has_bias ? __fadd_rn(f, bias) : f);
+      }
+      if (e < rows && j < A.N) *to = y;
+    }
+  }
+}
 
 template <typename TOut>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -247,7 +288,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // ---------------- epilogue ----------------
     const int quarter = warp & 3, half = warp >> 2;   // 32 channels; 128 of the tile's rows
     const uint32_t tacc = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(128 * half);
-    const int nw32 = 2 * ((A.N + 63) / 64);
     uint32_t seen = 0;   // chunks drained
     bool ok = true;
 #pragma unroll 1
@@ -260,6 +300,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const float sw = j < A.N && A.w_scale ? A.w_scale[j] : 1.0f;
       const float bias = j < A.N && A.bias ? A.bias[j] : 0.0f;
       const int thr = j < A.N && A.thr ? A.thr[j] : 0;
+      const int rows = (int)max((int64_t)0, min((int64_t)128, A.n - i0));
+      if (chunks == 1) {
+        // one chunk: the sums are in fp32 exactly, and go out as they are read
+        const uint32_t b = seen & 1u;
+        ok = __all_sync(kFull, mbar_wait_cluster(&sh->done[b], (seen >> 1) & 1u, failed));
+        if (!ok || expire) break;
+        ++seen;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        // (a threshold that no sum reaches, or every one, as an infinity: others are exact in fp32)
+        const float thrf = thr > 1 << 24 ? INFINITY : (thr < -(1 << 24) ? -INFINITY : (float)thr);
+#pragma unroll 1
+        for (int g = 0; g < 4; ++g) {
+          uint32_t v[2][16];
+          tmem_load16(v[0], tacc + 256u * b + 32u * (uint32_t)g);
+          tmem_load16(v[1], tacc + 256u * b + 32u * (uint32_t)g + 16u);
+          tmem_wait_ld(v[0]);
+          tmem_wait_ld(v[1]);
+          if (g == 3) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_rank0(&sh->drained[b]);
+          }
+          float f[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e >> 4][e & 15]);
+          put_group<TOut>(A, f, i0 + 32 * g, rows - 32 * g, jw, sw, bias, thrf);
+        }
+        continue;
+      }
       int acc[128];
 #pragma unroll
       for (int e = 0; e < 128; ++e) acc[e] = 0;
@@ -282,32 +351,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive_rank0(&sh->drained[b]);
       }
       if (!ok || expire) break;
-      if constexpr (IsSigns<TOut>::value) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int64_t i = i0 + 32 * g + lane;
-          uint32_t mine = 0u;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const uint32_t w = __ballot_sync(kFull, j < A.N && acc[32 * g + e] >= thr);
-            if (lane == e) mine = w;
-          }
-          if (i < A.n && (jw >> 5) < nw32) reinterpret_cast<uint32_t*>(A.words)[i * nw32 + (jw >> 5)] = mine;
-        }
-      } else {
-        TOut* to = static_cast<TOut*>(A.out) + i0 * A.ldo + j;
-        const int rows = (int)max((int64_t)0, min((int64_t)128, A.n - i0));
-        const bool has_bias = A.bias != nullptr;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float sal = A.a_scale && 32 * g + lane < rows ? A.a_scale[i0 + 32 * g + lane] : 1.0f;
-#pragma unroll
-          for (int e = 0; e < 32; ++e, to += A.ldo) {
-            const TOut y = out_of<TOut>(acc[32 * g + e], __shfl_sync(kFull, sal, e), sw, has_bias, bias);
-            if (32 * g + e < rows && j < A.N) *to = y;
-          }
-        }
-      }
+      for (int g = 0; g < 4; ++g)
+        put_group<TOut>(A, *reinterpret_cast<const int(*)[32]>(acc + 32 * g), i0 + 32 * g, rows - 32 * g, jw, sw, bias, thr);
     }
     if (expire && threadIdx.x == 0) *failed = 1;
   } else if (warp == kCopyWarp) {

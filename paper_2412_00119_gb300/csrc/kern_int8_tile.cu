@@ -132,7 +132,7 @@ __device__ __forceinline__ void write_rows(const Int8Args& A, const int (&v)[kRo
       if constexpr (std::is_same<T, int32_t>::value) {
         y = v[e];
       } else {
-        const float f = scaled(v[e], sa, F.sw);
+        const float f = scaled((float)v[e], sa, F.sw);
         y = out_cast<T>(has_bias ? __fadd_rn(f, F.bias) : f);
       }
       if (e < rows && j < A.N) *p = y;

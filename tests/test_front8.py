@@ -318,6 +318,21 @@ def test_thresholds_at_the_ends_of_int32():
 
 
 @gpu
+@pytest.mark.parametrize("n,K,N", [(2500, 1024, 4000), (3000, 1025, 4000), (5000, 1024, 60), (9000, 300, 100), (70, 1024, 300)])
+def test_thresholds_about_two_to_the_24(n, K, N):
+    """Sums up to 2^24 against thresholds at and past it, in every kernel: one compares them
+    in fp32."""
+    a, w = codes(n, K, 1, "ends"), codes(N, K, 2, "ends")
+    a[:5], w[:5] = -128, -128
+    a[5:8], w[5:8] = 127, -128
+    g = torch.Generator().manual_seed(3)
+    near = torch.tensor([0, 1, -1, 2 ** 24, 2 ** 24 - 1, 2 ** 24 + 1, 2 ** 24 + 2, -2 ** 24, -2 ** 24 - 1, -2 ** 24 + 1,
+                         2 ** 31 - 1, -2 ** 31, 127 * -128 * K, 128 * 128 * K])
+    thr = near[torch.randint(0, len(near), (N,), generator=g)].to(torch.int32).to(DEV)
+    run_all(a, w, K, N, 7, 0, 0, thr)
+
+
+@gpu
 @pytest.mark.parametrize("n", [1, 2, 20, 130, 400])
 def test_scales_that_are_not_finite(n):
     """A row's NaN scale (a row that could not be coded) reaches its outputs and no others;
