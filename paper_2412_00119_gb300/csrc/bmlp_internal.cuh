@@ -318,6 +318,7 @@ struct Int8Args {
   uint64_t* words;        // null: scaled output
   int64_t lda, ldw, ldo, n;
   int32_t K, N, type;
+  int32_t swapped;        // kern_int8_tile.cu: a and w (and their scales) have changed places
 };
 // expire != 0: the CTAs of the tensor-core kernels take a wait as expired (tests).
 cudaError_t launch_int8(const Int8Args& A, void* workspace, int64_t workspace_bytes, cudaStream_t st, int expire = 0);
@@ -328,10 +329,12 @@ constexpr int kFewRows = 8;
 cudaError_t launch_int8_few(const Int8Args& A, cudaStream_t st);
 // The tensor-core tiles of one CTA (kern_int8_tile.cu), nt rows wide (32, 64 or 128; with a
 // workspace 64 or 128: the activations then come from it as fp16 blocks, put there by a
-// launch before).  Rows in slabs of kTileSlab.
+// launch before).  Rows in slabs of kTileSlab.  swap: the tiles' lanes are the rows of a, their
+// rows the channels (n <= 2^30, N <= kTileSlab).
 constexpr int64_t kTileSlab = 65536;
-cudaError_t launch_int8_tile(const Int8Args& A, void* workspace, cudaStream_t st, int expire, int nt);
-int int8_tile_split(int64_t tiles, int K);
+cudaError_t launch_int8_tile(const Int8Args& A, void* workspace, cudaStream_t st, int expire, int nt, bool swap);
+// CTAs that share K, of that many tiles.
+int int8_tile_split(int64_t tiles, int K, int nt, bool swap);
 // The rows as fp16 blocks (kern_int8_pair.cu), and their bytes.
 cudaError_t launch_int8_expand_rows(const Int8Args& A, void* workspace, cudaStream_t st);
 int64_t int8_rows_workspace(int64_t n, int K);

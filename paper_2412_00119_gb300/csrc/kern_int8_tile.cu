@@ -10,7 +10,8 @@
 // its share of K; the CTAs of a cluster share K, and send each other int32 sums through
 // distributed shared memory (integers: any order gives the same).  Channels on M: a
 // narrow batch costs narrow MMAs, and a warp's lanes hold 32 neighbouring channels of a row,
-// as the output wants them.  Warps of a CTA:
+// as the output wants them; for many rows and few channels the two change places
+// (17,871 x 4646 -> 78 158 us, swapped 32).  Warps of a CTA:
 //   - 16 workers in four groups that take the k-steps (128 codes of every row, or 64) in
 //     turn: a warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring
 //     of its own: with loads to registers, whose scoreboards are few, 26 us for 32 rows of
@@ -31,6 +32,7 @@
 // cores, so the output is always whole.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "int8_common.cuh"
 #include "tc_common.cuh"
@@ -103,6 +105,69 @@ struct Factors {
   float sw, bias, sa;
   int thr;
 };
+
+// Outputs of a worker warp where the lanes are rows and a thread has kRows channels from i on
+// of its own (swapped operands); end: the tile's last channel + 1.
+template <int kRows>
+__device__ __forceinline__ void write_channels(const Int8Args& A, const int (&v)[kRows], int64_t i, int64_t end, int jw,
+                                               const Factors& F) {
+  const int j = jw + (int)(threadIdx.x & 31);
+  const int live = (int)max((int64_t)0, min((int64_t)kRows, A.n - i));   // channels that are some
+  if (A.words) {
+    if constexpr (kRows >= 8) {
+      const int64_t nw = (A.n + 63) / 64;
+      uint32_t bits = 0u;
+#pragma unroll
+      for (int e = 0; e < kRows; ++e) bits |= v[e] >= __shfl_sync(kFull, F.thr, e) ? 1u << e : 0u;
+      bits &= live >= 32 ? 0xFFFFFFFFu : (1u << live) - 1u;
+      if (j < A.N && i < 64 * nw) {
+        uint8_t* to = reinterpret_cast<uint8_t*>(A.words + j * nw) + (i >> 3);
+        if constexpr (kRows == 32) *reinterpret_cast<uint32_t*>(to) = bits;
+        else if constexpr (kRows == 16) *reinterpret_cast<uint16_t*>(to) = (uint16_t)bits;
+        else *to = (uint8_t)bits;
+        // (tiles of 32 may end in the middle of a row's last word: the rest is zero)
+        if (i + kRows == end && end >= A.n && end < 64 * nw) *reinterpret_cast<uint32_t*>(to + kRows / 8) = 0u;
+      }
+    }
+    return;
+  }
+  auto store = [&](auto* out) {
+    using T = std::remove_pointer_t<decltype(out)>;
+    constexpr int kVec = 16 / (int)sizeof(T);
+    T y[kRows];
+    const bool has_bias = A.bias != nullptr;
+#pragma unroll
+    for (int e = 0; e < kRows; ++e) {
+      if constexpr (std::is_same<T, int32_t>::value) {
+        y[e] = v[e];
+      } else {
+        const float f = scaled((float)v[e], F.sw, __shfl_sync(kFull, F.sa, e)), b = __shfl_sync(kFull, F.bias, e);
+        y[e] = out_cast<T>(has_bias ? __fadd_rn(f, b) : f);
+      }
+    }
+    if (j >= A.N) return;
+    T* p = out + (int64_t)j * A.ldo + i;
+    if (kRows % kVec == 0 && live == kRows && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+      for (int e = 0; e < kRows / kVec * kVec; e += kVec) {
+        union { uint4 w; T e[kVec]; } u;
+#pragma unroll
+        for (int x = 0; x < kVec; ++x) u.e[x] = y[e + x];
+        *reinterpret_cast<uint4*>(p + e) = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kRows; ++e)
+        if (e < live) p[e] = y[e];
+    }
+  };
+  switch (A.type) {
+    case BMLP_F32: store(static_cast<float*>(A.out)); break;
+    case BMLP_F16: store(static_cast<__half*>(A.out)); break;
+    case BMLP_BF16: store(static_cast<__nv_bfloat16*>(A.out)); break;
+    default: store(static_cast<int32_t*>(A.out));
+  }
+}
 
 // Outputs of a worker warp from its registers: kRows rows from i on of 32 channels from jw on,
 // a lane per channel.
@@ -203,7 +268,11 @@ __device__ __forceinline__ void exchange_and_write(const Int8Args& A, const int 
           own[e] += reinterpret_cast<const int*>(smem)[(x * kOwn + e / kWide * kWide) * 32 * kWorkers + kWide * tid + e % kWide];
     }
   }
-  if (worker) write_rows<kOwn>(A, own, i0 + kCols * (warp >> 2) + kOwn * (int)rank, jw, F);
+  if (worker) {
+    const int64_t i = i0 + kCols * (warp >> 2) + kOwn * (int)rank;
+    if (A.swapped) write_channels<kOwn>(A, own, i, i0 + 4 * kCols, jw, F);
+    else write_rows<kOwn>(A, own, i, jw, F);
+  }
 }
 
 // kReady: the activations as fp16 blocks (kern_int8_pair.cu), written by the launch before
@@ -462,12 +531,16 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
     // what the outputs need, while the last MMAs run
     const int j = j0 + 32 * q + lane;
     F.sw = j < A.N && A.w_scale ? A.w_scale[j] : 1.0f;
-    F.bias = j < A.N && A.bias ? A.bias[j] : 0.0f;
-    F.thr = j < A.N && A.thr ? A.thr[j] : 0;
     // (lane e: the warp's row e)
     const int own = kCols / split;
     const int64_t i = i0 + kCols * (warp >> 2) + own * (int)rank + lane;
-    F.sa = A.a_scale && lane < own && i < A.n ? A.a_scale[i] : 1.0f;
+    const bool row = lane < own && i < A.n;
+    F.sa = A.a_scale && row ? A.a_scale[i] : 1.0f;
+    // (bias and thresholds go with the call's channels)
+    const int64_t channel = A.swapped ? i : (int64_t)j;
+    const bool some = A.swapped ? row : j < A.N;
+    F.bias = some && A.bias ? A.bias[channel] : 0.0f;
+    F.thr = some && A.thr ? A.thr[channel] : 0;
     while (ok && drained < chunks) drain();
     if (split > 1 && !arrived) cluster_arrive();   // (after a failure: no copy of this warp is in flight)
     if (expire && threadIdx.x == 0) *failed = 1;
@@ -608,18 +681,27 @@ cudaError_t launch_rows(const Int8Args& A, const uint8_t* ablocks, int nt, int s
 
 }  // namespace
 
-// CTAs that share K: as many as leave every SM at most one, with eight k-steps of 64 each.
-int int8_tile_split(int64_t tiles, int K) {
-  const int steps = (K + 63) / 64;
+// As many as leave every SM at most one, with eight k-steps of 64 each; of swapped operands a
+// thread keeps eight channels (a byte of signs).
+int int8_tile_split(int64_t tiles, int K, int nt, bool swap) {
+  const int steps = (K + 63) / 64, most = swap ? std::min(kMaxSplit, nt / 32) : kMaxSplit;
   int split = 1;
-  while (split < kMaxSplit && tiles * (2 * split) <= sm_count() && steps >= 8 * split) split *= 2;
+  while (split < most && tiles * (2 * split) <= sm_count() && steps >= 8 * split) split *= 2;
   return split;
 }
 
-cudaError_t launch_int8_tile(const Int8Args& all, void* workspace, cudaStream_t st, int expire, int nt) {
+cudaError_t launch_int8_tile(const Int8Args& all, void* workspace, cudaStream_t st, int expire, int nt, bool swap) {
   Int8Args A = all;
   A.n = std::min<int64_t>(all.n, kTileSlab);
-  const int split = int8_tile_split((int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt), A.K);
+  if (swap) {
+    A.n = all.N;
+    A.N = (int32_t)all.n;
+    std::swap(A.a, A.w);
+    std::swap(A.lda, A.ldw);
+    std::swap(A.a_scale, A.w_scale);
+    A.swapped = 1;
+  }
+  const int split = int8_tile_split((int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt), A.K, nt, swap);
   if (workspace) {
     const cudaError_t e = launch_int8_expand_rows(A, workspace, st);
     if (e != cudaSuccess) return e;
@@ -627,8 +709,8 @@ cudaError_t launch_int8_tile(const Int8Args& all, void* workspace, cudaStream_t 
   const uint8_t* ablocks = static_cast<const uint8_t*>(workspace);
   const bool wide = operand_align_w(A) == 16 && (workspace || operand_align(A) == 16);
   const cudaError_t e = wide ? launch_rows<16>(A, ablocks, nt, split, expire, st) : launch_rows<1>(A, ablocks, nt, split, expire, st);
-  if (e != cudaSuccess || all.n <= kTileSlab) return e;
-  return launch_int8_tile(rest_of(all, kTileSlab), workspace, st, expire, nt);
+  if (e != cudaSuccess || swap || all.n <= kTileSlab) return e;
+  return launch_int8_tile(rest_of(all, kTileSlab), workspace, st, expire, nt, false);
 }
 
 }  // namespace bk

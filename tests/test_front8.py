@@ -320,8 +320,8 @@ def test_thresholds_at_the_ends_of_int32():
 @gpu
 @pytest.mark.parametrize("n,K,N", [(2500, 1024, 4000), (3000, 1025, 4000), (5000, 1024, 60), (9000, 300, 100), (70, 1024, 300)])
 def test_thresholds_about_two_to_the_24(n, K, N):
-    """Sums up to 2^24 against thresholds at and past it, in every kernel: one compares them
-    in fp32."""
+    """Sums up to 2^24 against thresholds at and past it, in every kernel that compares them in
+    fp32 or whose lanes are rows."""
     a, w = codes(n, K, 1, "ends"), codes(N, K, 2, "ends")
     a[:5], w[:5] = -128, -128
     a[5:8], w[5:8] = 127, -128
@@ -330,6 +330,15 @@ def test_thresholds_about_two_to_the_24(n, K, N):
                          2 ** 31 - 1, -2 ** 31, 127 * -128 * K, 128 * 128 * K])
     thr = near[torch.randint(0, len(near), (N,), generator=g)].to(torch.int32).to(DEV)
     run_all(a, w, K, N, 7, 0, 0, thr)
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(1000, 64, 20), (3000, 200, 31), (17871, 646, 78), (5000, 1100, 100), (9000, 79, 129),
+                                   (40000, 88, 105), (2615, 3000, 42), (700, 4096, 64), (3333, 4100, 33)])
+def test_many_rows_and_few_channels(n, K, N):
+    """Where rows and channels change places inside: strides, biases and thresholds too."""
+    for pad, off in [(0, 0), (16, 16), (3, 1)]:
+        run_all(codes(n, K, n, "ends"), codes(N, K, K), K, N, n, pad, off)
 
 
 @gpu
@@ -428,7 +437,7 @@ def test_every_plan(n, K, N):
 
 @gpu
 @pytest.mark.parametrize("n,K,N", [(12, 200, 300), (20, 2048, 300), (50, 4096, 4000), (100, 2048, 4096), (300, 3000, 2000),
-                                   (1500, 1024, 8192)])
+                                   (1500, 1024, 8192), (4000, 1500, 50), (4000, 3000, 120)])
 def test_expired_waits_cost_time_only(n, K, N):
     """With every CTA's wait taken as expired the sums are made again, whole; without a
     workspace too."""
@@ -444,7 +453,7 @@ def test_expired_waits_cost_time_only(n, K, N):
 
 
 @gpu
-@pytest.mark.parametrize("n,K,N", [(40, 3000, 5000), (100, 4096, 8192), (300, 2304, 4000), (1500, 1024, 8192)])
+@pytest.mark.parametrize("n,K,N", [(40, 3000, 5000), (100, 4096, 8192), (300, 2304, 4000), (1500, 1024, 8192), (4000, 1500, 100)])
 def test_workspaces(n, K, N):
     """Given, too small, misaligned, kept, on other streams: the same sums."""
     a, w = codes(n, K, n).to(DEV), codes(N, K, K).to(DEV)
