@@ -185,13 +185,15 @@ __device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&w)[(V + 
   }
 }
 
-// A row's K codes from shared memory, where code e is byte e + apart of buf (16-byte aligned, 16
-// bytes before it), to q, anywhere: a thread of `threads` takes aligned 16 bytes of q at a time.
-__device__ __forceinline__ void copy_codes(int8_t* q, const uint8_t* buf, int apart, int K, int tid, int threads) {
-  const int before = (int)(reinterpret_cast<uintptr_t>(q) & 15);
-  const int shift = apart - before;                       // byte of buf for the first of q's chunks
-  for (int e = 16 * tid - before; e < K; e += 16 * threads) {
-    const int at = e + before + shift;                    // (from -15 on)
+// `count` values of a row (U: their bits) from shared memory, where value e begins at byte e sizeof(U) + apart of buf
+// (16-byte aligned, 16 bytes before it and after its last), to `to`, anywhere: a thread of
+// `threads` takes aligned 16 bytes of it at a time.
+template <typename U>
+__device__ __forceinline__ void copy_row(U* to, const uint8_t* buf, int apart, int count, int tid, int threads) {
+  constexpr int kEach = 16 / (int)sizeof(U);
+  const int before = (int)(reinterpret_cast<uintptr_t>(to) & 15) / (int)sizeof(U);
+  for (int e = kEach * tid - before; e < count; e += kEach * threads) {
+    const int at = e * (int)sizeof(U) + apart;            // (from -15 on)
     const uint32_t* w = reinterpret_cast<const uint32_t*>(buf + (at & ~3));
     uint32_t v[4];
     uint32_t x = w[0];
@@ -201,12 +203,12 @@ __device__ __forceinline__ void copy_codes(int8_t* q, const uint8_t* buf, int ap
       v[i] = __funnelshift_r(x, y, 8u * (uint32_t)(at & 3));
       x = y;
     }
-    if (e >= 0 && e + 16 <= K) {
-      *reinterpret_cast<uint4*>(q + e) = make_uint4(v[0], v[1], v[2], v[3]);
+    if (e >= 0 && e + kEach <= count) {
+      *reinterpret_cast<uint4*>(to + e) = make_uint4(v[0], v[1], v[2], v[3]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (e + i >= 0 && e + i < K) q[e + i] = (int8_t)(v[i / 4] >> (8 * (i % 4)));
+      for (int i = 0; i < kEach; ++i)
+        if (e + i >= 0 && e + i < count) to[e + i] = (U)(v[i * (int)sizeof(U) / 4] >> (8 * (i * (int)sizeof(U) % 4)));
     }
   }
 }
@@ -215,20 +217,20 @@ constexpr int kRowsPerCta = 8;   // rows of a CTA with a warp each
 // What is done to a row (residual: its registers are there only where it is).
 constexpr int kPlain = 0, kNormed = 1, kResidual = 2;
 
-// Shared memory of a row's codes: a vector per thread and turn, 16 bytes before and after.
-template <int V>
-__host__ __device__ constexpr int codes_bytes(int nv, int threads) { return nv * threads * V + 32; }
+// Shared memory of a row's codes, or of its sums: a vector per thread and turn, 16 bytes before
+// and after.
+__host__ __device__ constexpr int row_bytes(int nv, int threads, int vector) { return nv * threads * vector + 32; }
 
 // A row's T threads hold it: vector v of thread t is v T + t, NV vectors of V values
 // each.  The grid walks the rows; a row's values are loaded while the row before is
 // reduced and written, and the gain stays in registers (kAhead; without it neither,
 // where the registers do not hold both).
-// kApart: rows that do not start at multiples of 16 bytes, all buffers' equally far from one.
+// kApart: rows that do not start at multiples of 16 bytes, the inputs' equally far from one.
 // A thread's vectors are the aligned 16 bytes around the row; rows eight apart lie
 // alike, and a thread's rows are a multiple of eight apart.  The codes go through shared
-// memory, since theirs lie otherwise.
+// memory, since theirs lie otherwise, and the sums where theirs do (apart_sum).
 template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead, bool kApart>
-__global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize_regs(const QuantArgs A) {
+__global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize_regs(const QuantArgs A, bool apart_sum) {
   pdl_wait();
   pdl_trigger();
   const int threads = kWarpRow ? 32 : (int)blockDim.x;
@@ -241,7 +243,9 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
   T* sum = kNorm ? static_cast<T*>(A.sum) : nullptr;
   const T* gain = kNorm ? static_cast<const T*>(A.gain) : nullptr;
   extern __shared__ uint4 smem_codes[];
-  uint8_t* codes = reinterpret_cast<uint8_t*>(smem_codes) + 16 + (kWarpRow ? (int)(threadIdx.x >> 5) * codes_bytes<V>(NV, 32) : 0);
+  uint8_t* codes = reinterpret_cast<uint8_t*>(smem_codes) + 16 + (kWarpRow ? (int)(threadIdx.x >> 5) * row_bytes(NV, 32, V) : 0);
+  uint8_t* sums = reinterpret_cast<uint8_t*>(smem_codes) + 16 + (kWarpRow ? kRowsPerCta : 1) * row_bytes(NV, threads, V) +
+                  (kWarpRow ? (int)(threadIdx.x >> 5) * row_bytes(NV, 32, 16) : 0);
   const int apart = kApart ? (int)((reinterpret_cast<uintptr_t>(x + row * A.ldx) & 15) / sizeof(T)) : 0;
   auto at = [&](int v) { return (v * threads + tid) * V - apart; };
   auto skip = [&](int v) { return kApart ? -at(v) : 0; };
@@ -292,7 +296,11 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
       for (int v = 0; v < NV; ++v) {
         Pack<T, V> ps;
         ps.set(u[v]);
-        ps.store(sum + row * A.lds + at(v), skip(v), A.K - at(v));
+        // (the row before was copied from there before its codes were)
+        if constexpr (kApart) {
+          if (apart_sum) *reinterpret_cast<uint4*>(sums + 16 * (v * threads + tid)) = make_uint4(ps.w[0], ps.w[1], ps.w[2], ps.w[3]);
+        }
+        if (!kApart || !apart_sum) ps.store(sum + row * A.lds + at(v), skip(v), A.K - at(v));
       }
     }
 #pragma unroll
@@ -307,6 +315,11 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
     }
     uint32_t mbits = __float_as_uint(most);
     row_reduce<kWarpRow>(sq, mbits, kNorm, turn);
+    if (kApart && apart_sum) {   // (only where there are sums)
+      if constexpr (kWarpRow) __syncwarp();   // (a CTA's threads have met in row_reduce)
+      using Bits = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+      copy_row(reinterpret_cast<Bits*>(sum + row * A.lds), sums, apart * (int)sizeof(T), A.K, tid, threads);
+    }
     const RowScale r = row_scale(mbits, sq, A.K, A.eps, kNorm);
     const uint32_t live = r.inv == 0.0f ? 0u : 0xFFFFFFFFu;
     int8_t* q = A.q + row * A.ldq;
@@ -326,7 +339,7 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
     if constexpr (kApart) {
       if constexpr (kWarpRow) __syncwarp();
       else __syncthreads();
-      copy_codes(q, codes, apart, A.K, tid, threads);
+      copy_row(q, codes, apart, A.K, tid, threads);
       if constexpr (kWarpRow) __syncwarp();
     }
     if (tid == 0) A.scale[row] = r.scale;
@@ -372,22 +385,30 @@ __global__ void __launch_bounds__(kThreads) k_quantize_long(const QuantArgs A) {
 // are only coded run faster from more warps (60,000 x 784 fp32 46, ahead 55; 60,000 x 1000
 // bf16 coded 28.6, ahead 32.5).
 template <typename T, int kMode, int V, int NV, bool kApart>
-cudaError_t launch_warp_rows(const QuantArgs& A, cudaStream_t st) {
+cudaError_t launch_warp_rows(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain) || kApart;
   const int64_t ctas = std::min((A.n + kRowsPerCta - 1) / kRowsPerCta, (int64_t)(kAhead && V * NV > 16 ? 4 : 8) * sm_count());
   return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead, kApart>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta),
-                       kApart ? (size_t)(kRowsPerCta * codes_bytes<V>(NV, 32)) : 0, st, true, A);
+                       kApart ? (size_t)kRowsPerCta * (row_bytes(NV, 32, V) + (apart_sum ? row_bytes(NV, 32, 16) : 0)) : 0, st, true,
+                       A, apart_sum);
 }
 
 // A CTA per row: 1,024 threads an SM.
 template <typename T, int kMode, int V, int NV, bool kApart>
-cudaError_t launch_cta_rows(const QuantArgs& A, cudaStream_t st) {
+cudaError_t launch_cta_rows(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   const int vecs = kApart ? (int)((A.K + 2ll * V - 2) / V) : A.K / V + (A.K % V != 0);
   const int threads = (vecs + 32 * NV - 1) / (32 * NV) * 32;
   constexpr bool kAhead = !(kMode != kPlain && V * NV > (sizeof(T) == 2 ? 16 : 8));
   const int64_t ctas = kAhead ? std::min(A.n, (int64_t)(1024 / threads) * sm_count() / 8 * 8) : A.n;
+  if (kApart && apart_sum) {
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(done, k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart>,
+                                     row_bytes(NV, 1024, V) + row_bytes(NV, 1024, 16));
+    if (e != cudaSuccess) return e;
+  }
   return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart>, dim3((unsigned)ctas), dim3((unsigned)threads),
-                       kApart ? (size_t)codes_bytes<V>(NV, threads) : 0, st, true, A);
+                       kApart ? (size_t)row_bytes(NV, threads, V) + (apart_sum ? row_bytes(NV, threads, 16) : 0) : 0, st, true, A,
+                       apart_sum);
 }
 
 // Which form (us, rows in bf16 unless said): rows that a warp holds in at most kWarpMost
@@ -396,25 +417,25 @@ cudaError_t launch_cta_rows(const QuantArgs& A, cudaStream_t st) {
 // for many as many as the registers hold beside the next row's: four without a norm
 // (8192 x 8192 30, two 34, one 44), two with it (8191 x 4096 with residual 40, four 57 for want of registers).
 template <typename T, int kMode, int V, bool kApart>
-cudaError_t launch_v(const QuantArgs& A, cudaStream_t st) {
+cudaError_t launch_v(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   constexpr int kWarpMost = V == 8 ? 4 : (V == 4 ? 8 : 16);
   const int64_t vecs = kApart ? (A.K + 2ll * V - 2) / V : A.K / V + (A.K % V != 0);
   if constexpr (!kApart) {
-    if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1, false>(A, st);
-    if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2, false>(A, st);
-    if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4, false>(A, st);
-    if (V <= 2 && vecs <= 256) return launch_warp_rows<T, kMode, V, V <= 2 ? 8 : 4, false>(A, st);
+    if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1, false>(A, apart_sum, st);
+    if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2, false>(A, apart_sum, st);
+    if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4, false>(A, apart_sum, st);
+    if (V <= 2 && vecs <= 256) return launch_warp_rows<T, kMode, V, V <= 2 ? 8 : 4, false>(A, apart_sum, st);
   }
-  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart>(A, st);
+  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart>(A, apart_sum, st);
   if (vecs > 4096)
     return launch_kernel(k_quantize_long<T, kMode>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
   const bool few = A.n <= 2 * sm_count();
-  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart>(A, st);
-  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart>(A, st);
-  return launch_cta_rows<T, kMode, V, 1, kApart>(A, st);
+  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart>(A, apart_sum, st);
+  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart>(A, apart_sum, st);
+  return launch_cta_rows<T, kMode, V, 1, kApart>(A, apart_sum, st);
 }
 
-// Vectors of 16 bytes; also where rows start elsewhere but all buffers' alike, if they are long and
+// Vectors of 16 bytes; also where rows start elsewhere but the inputs' alike, if they are long and
 // many (us, by single values after it: 8191 x 4095 bf16 with residual 68, 98; 60,000 x 1001 bf16
 // coded 51, 66; but 60,000 x 255 25, 13, and 100 x 1001 4.3, 2.1) or too long for single values;
 // else of 4 bytes or single values.
@@ -429,11 +450,12 @@ cudaError_t launch_type(const QuantArgs& A, cudaStream_t st) {
   const uintptr_t wide = px | (A.res ? place(A.res, A.ldr) : 0) | (A.sum ? place(A.sum, A.lds) : 0) |
                          (reinterpret_cast<uintptr_t>(A.gain) & 15);
   const uintptr_t codes = reinterpret_cast<uintptr_t>(A.q) | (many ? (uintptr_t)A.ldq : 0);
-  if (wide == 0 && codes % V == 0) return launch_v<T, kMode, V, false>(A, st);
-  const bool alike = (!A.res || place(A.res, A.ldr) == px) && (!A.sum || place(A.sum, A.lds) == px);
-  if (alike && A.K > 512 && (A.n > 2 * sm_count() || A.K > 4096) && A.K <= 2048 * V - V) return launch_v<T, kMode, V, true>(A, st);
-  if (sizeof(T) == 2 && (wide & 0x33) == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1, false>(A, st);
-  return launch_v<T, kMode, 1, false>(A, st);
+  if (wide == 0 && codes % V == 0) return launch_v<T, kMode, V, false>(A, false, st);
+  const bool apart_sum = A.sum && place(A.sum, A.lds) != px;
+  if ((!A.res || place(A.res, A.ldr) == px) && A.K > 512 && (A.n > 2 * sm_count() || A.K > 4096) && A.K <= 2048 * V - V)
+    return launch_v<T, kMode, V, true>(A, apart_sum, st);
+  if (sizeof(T) == 2 && (wide & 0x33) == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1, false>(A, false, st);
+  return launch_v<T, kMode, 1, false>(A, false, st);
 }
 
 template <typename T>

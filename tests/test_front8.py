@@ -192,6 +192,30 @@ def test_quantize_special_rows(K, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,K", [(1, 4097), (3, 8184), (330, 513), (2500, 517), (611, 784), (400, 1001), (701, 2047), (330, 4096),
+                                 (311, 8180), (5, 16376)])
+def test_norm_with_sums_that_lie_elsewhere(n, K, dtype):
+    """Inputs whose rows start alike, sums that start otherwise, in some rows or in all."""
+    for pad, off, spad, soff in [(1, 0, 0, 0), (3, 5, 0, 0), (0, 0, 1, 0), (0, 0, 0, 1), (7, 2, 16, 2), (2, 8, 5, 3)]:
+        x, res = hidden(n, K, n + K, dtype), hidden(n, K, n + 5 * K, dtype)
+        xd, rd = (rows(n, K, dtype, pad, off)[1] for _ in range(2))
+        sb, sd = rows(n, K, dtype, spad, soff, fill=7)
+        qb, qd = rows(n, K, torch.int8, spad, soff, fill=99)
+        xd.copy_(x)
+        rd.copy_(res)
+        scale = torch.full((n,), -1.0, device=DEV)
+        B.bmlp_norm_quantize(xd, None, qd, scale, res=rd, sum_out=sd, eps=EPS)
+        h, want = plain_codes(x, res)
+        assert torch.equal(qd.cpu(), want)
+        check_codes(qd.cpu(), scale.cpu(), x, res, None, True, K)
+        assert torch.equal(sd.cpu(), h.to(dtype))
+        for b, fill in ((sb, 7), (qb, 99)):
+            assert (b[:soff] == fill).all() and (b[soff + n * (K + spad):] == fill).all()
+            assert (b[soff:soff + n * (K + spad)].view(n, -1)[:, K:] == fill).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("K", [96, 1001, 8192, 40000])
 def test_norm_in_place(K, dtype):
     n = 5
