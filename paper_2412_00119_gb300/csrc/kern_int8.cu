@@ -16,21 +16,24 @@ struct Plan {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Which kernel: the least of the times that a line through measurements gives each (us; with
-// what was measured beside it).  Tiles: a launch and what follows the last sum, and per k-step of
-// 128 codes; the tiles' rows made ready; more tiles than SMs run in rounds.  Rows at odd places: K not a multiple of 16 stands
-// for them (the size of the workspace goes by the sizes alone).
-//   32-row tiles      32 x 8192 -> 8192 16.6, 32 x 4096 -> 4096 7.8, 200 x 1024 -> 1024 6.0
-//   64, ready rows    64 x 8192 -> 8192 20.1 (32-row 26.5, 128-row 22.6), 500 x 1000 -> 1000 9.0 (9.6, 9.7)
-//   128, ready rows   100 x 4096 -> 8192 15.5 (31, 18.3; pairs 46), 300 x 8192 -> 8192 61 (132, 86; 88),
-//                     700 x 4096 -> 4096 36 (78, 50; 38.5)
-//   pairs             1500 x 1024 -> 8192 36 (128-row 46), 2000 x 4096 -> 4096 63 (73)
-//   swapped           17871 x 4646 -> 78 32 (158), 33078 x 2816 -> 448 94 (154), 1000 x 1000 -> 525 11.2 (14.2);
-//                     47454 x 119 -> 35 25 (20.5), the line's worst here
+// Which kernel: the least of the times that lines give each, fitted to measurements of every plan
+// at 290 sizes (the chosen plan's times are 1.2% above the best's in the mean, 67% at worst; some of
+// them below, in us).  Tiles: a launch and what follows the last sum; per k-step of 128 codes; per
+// further round where there are more tiles than SMs; the tiles' rows made ready.  Rows at odd places:
+// K not a multiple of 16 stands for them (the size of the workspace goes by the sizes alone).
+//                         32-row tiles  64, ready  128, ready  pairs  swapped 32, 64, 128
+//   200 x 1024 -> 1024 and smaller: 32-row tiles (172 x 208 -> 224 3.6, 5.3, 6.0, 9.7)
+//   46 x 4320 -> 7472             16.6       14.2           -      -
+//   100 x 4096 -> 8192            30.2       18.8        15.6      -
+//   300 x 12144 -> 8208            198        127          89    140
+//   2478 x 1600 -> 8415            287        156          91     67
+//   13230 x 1696 -> 272             92         69          49     46     62, 41, 34
+//   36560 x 12548 -> 35            980        907         716    528     307, 119, -
+//   16084 x 128 -> 2192 signs      205        105          67     30     221, 111, 63
 // Up to 8 rows the streamed kernel: 8 x 8192 -> 8192 14.8 (32-row 17.0), 1 x 784 -> 2048 2.8 (5.3).
 Plan plan_of(int64_t n, int K, int N) {
   if (n <= 8) return {Path::kFew, 0, false};
-  const double odd = K % 16 ? 1.0 : 0.0;
+  const bool odd = K % 16 != 0;
   Plan p = {Path::kTiles, 32, false};
   double best = 1e30;
   for (int swap = 0; swap < 2; ++swap) {
@@ -41,17 +44,16 @@ Plan plan_of(int64_t n, int K, int N) {
       const int split = int8_tile_split(t, K, nt, swap);
       const double steps = (double)up(K, 128) / split, rounds = (double)up(t * split, sm_count());
       const double ready = path == Path::kReadyTiles ? 3.0 * (double)rows * K / 4.5e6 : 0;
-      const double us = start + 1.5 * odd + ready + rounds * steps * per_step * (1 + 0.3 * odd) + (rounds - 1) * per_round;
+      const double us = start + ready + rounds * steps * per_step + (rounds - 1) * per_round + 0.3 * swap * rounds;
       if (us < best) p = {path, nt, swap != 0}, best = us;
     };
-    tiles(Path::kTiles, 32, 4.6, 0.36, 2.5);
-    if (rows > 32) tiles(Path::kReadyTiles, 64, 6.1, 0.44, 2.5);
-    if (rows > 64) tiles(Path::kReadyTiles, 128, 7.4, 0.50, 1.5);
+    tiles(Path::kTiles, 32, 3.1, odd ? 1.03 : 0.46, 3.3);
+    if (rows > 32) tiles(Path::kReadyTiles, 64, odd ? 5.5 : 5.1, odd ? 0.60 : 0.43, 3.9);
+    if (rows > 64) tiles(Path::kReadyTiles, 128, 6.7, odd ? 0.59 : 0.42, 5.1);
   }
   // pairs; up to K = 1024 a tile's outputs go out as they are read
   const int64_t pairs = up(up(N, 256) * up(n, 256), sm_count() / 2);
-  const double tile = std::max(K <= 1024 ? 3.0 : 4.5, (double)up(K, 64) * 0.27);
-  const double us = 8.0 + 3.0 * ((double)n + N) * K / 4.5e6 + 3.5 + (double)pairs * tile;
+  const double us = 10.8 + 3.0 * ((double)n + N) * K / 4.5e6 + (double)pairs * std::max(K <= 1024 ? 3.3 : 10.0, (double)up(K, 64) * 0.27);
   // (blocks are numbered in 31 bits)
   if (((int64_t)N + 256) * (K / 64 + 1) < (1ll << 31) && n > 128 && us < best) p = {Path::kPairs, 0, false};
   return p;
