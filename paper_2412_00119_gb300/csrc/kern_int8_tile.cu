@@ -375,21 +375,23 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
         const uint32_t to = ring_to + (uint32_t)(slot * C::kTurnRows * C::kRow);
         // (a unit of four rows: the swap by the row's low bits alternates between two places)
         if (C::kStep * (first + ks + 1) + (kAlign == 16 ? 0 : 16) <= A.K) {
-          // every code inside its row; channels past N and rows past n, whose sums are dropped, as
-          // the tile's first
+          // every code inside its row; channels past N and rows past n as zeros, with nothing read
+          // (18 rows of 4863 -> 12288 28 us; 45 where the 14 others read the tile's first row, a line
+          // that every CTA then asks for many times a k-step)
           const int8_t* row = wrow + k;
 #pragma unroll
           for (int u = 0; u < kUnits; ++u) {
             if (u == kUnitsA) row = arow + k;
-            const int8_t* p = row;
-            if (u < kUnitsA) p = ja + kUnit * u < A.N ? p : A.w + (int64_t)j0 * A.ldw + k;
-            else p = ib + kUnit * (u - kUnitsA) < A.n ? p : A.a + i0 * A.lda + k;
+            const bool live = u < kUnitsA ? ja + kUnit * u < A.N : ib + kUnit * (u - kUnitsA) < A.n;
+            const int8_t* p = live ? row : any;
+            const int size = live ? 16 : 0;
             if constexpr (kAlign != 16) p = aligned16(p);
             const uint32_t unit = to + (uint32_t)(u * kUnit * C::kRow);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                         ::"r"(unit + (uint32_t)C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c)), "l"(p) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                         ::"r"(unit + (uint32_t)C::chunk_at(kUnit == 4 ? r + 4 * (u & 1) : r, c)), "l"(p), "r"(size) : "memory");
             if (kAlign != 16 && c == 0)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(unit + (uint32_t)C::kStep), "l"(p + C::kStep) : "memory");
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                           ::"r"(unit + (uint32_t)C::kStep), "l"(p + (live ? C::kStep : 0)), "r"(size) : "memory");
             row += u < kUnitsA ? wstep : astep;
           }
         } else {
@@ -484,26 +486,34 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
       const int turn = slot * C::kTurnRows * C::kRow;
       const uint32_t tw = tmem + lanes + (uint32_t)C::kAccCols + (uint32_t)C::kStageCols * s;
       {
-        constexpr int kChunks = 4 * kSub;
-        uint4 v[kChunks + 1];
+        // the row's words: whole chunks, or from the 8 bytes on that hold the first code, a word or
+        // none of which is passed over, and then shifted by bytes (merge16's steps, the first by
+        // address: 17,871 x 4646 -> 78 30 us, by merge16 32)
+        constexpr int kWords = 16 * kSub + (kAlign == 16 ? 0 : 2);
+        uint32_t v[kWords];
+        if constexpr (kAlign == 16) {
 #pragma unroll
-        for (int i = 0; i < kChunks + (kAlign == 16 ? 0 : 1); ++i)
-          v[i] = *reinterpret_cast<const uint4*>(read_w + turn + C::chunk_at(lane, i));
+          for (int i = 0; i < kWords / 4; ++i) {
+            const uint4 w = *reinterpret_cast<const uint4*>(read_w + turn + C::chunk_at(lane, i));
+            v[4 * i] = w.x, v[4 * i + 1] = w.y, v[4 * i + 2] = w.z, v[4 * i + 3] = w.w;
+          }
+        } else {
+          const uint8_t* from = read_w + turn + (wshift & 8);
 #pragma unroll
-        for (int h = 0; h < kChunks / 2; ++h) {
+          for (int i = 0; i < kWords / 2; ++i) {
+            const uint2 w = *reinterpret_cast<const uint2*>(from + 8 * i);
+            v[2 * i] = w.x, v[2 * i + 1] = w.y;
+          }
+#pragma unroll
+          for (int i = 0; i < kWords - 1; ++i) v[i] = wshift & 4 ? v[i + 1] : v[i];
+#pragma unroll
+          for (int i = 0; i < kWords - 2; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 8u * (uint32_t)(wshift & 3));
+        }
+#pragma unroll
+        for (int h = 0; h < 2 * kSub; ++h) {
           uint32_t f[16];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4& lo = v[2 * h + i];
-            uint32_t x[4] = {lo.x, lo.y, lo.z, lo.w};
-            if constexpr (kAlign != 16) {
-              const uint4& hi = v[2 * h + i + 1];
-              const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, m[4] = {hi.x, hi.y, hi.z, hi.w};
-              merge16(x, l, m, wshift);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) codes_f16(x[e], f[8 * i + 2 * e], f[8 * i + 2 * e + 1]);
-          }
+          for (int e = 0; e < 8; ++e) codes_f16(v[8 * h + e], f[2 * e], f[2 * e + 1]);
           tmem_store16(tw + 16u * h, f);
         }
       }
