@@ -25,7 +25,8 @@
 // 665).  A k-step takes 520 clocks where its MMAs take 512 (with forwarded completions
 // 730 to 790); a chunk's read-out takes 4,900 of the 8,200 of the next chunk's MMAs, a tile's
 // stores 4,900 (one instance per output type: with the types told apart inside the unrolled
-// stores 21,000).  The expansion runs at 4.1 TB/s.
+// stores 21,000).  The expansion of 16384 and 8192 rows
+// of 8192 takes 161 us (3.8 TB/s), of rows of 8191 195.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 #include <cmath>
@@ -95,9 +96,15 @@ __global__ void __launch_bounds__(kExpandThreads) k_int8_expand(const ExpandArgs
     uint8_t* to = (second ? E.blocks1 : E.blocks0) + (row / kBlockRows * E.nkb + kb0) * (int64_t)kBlockBytes + 128 * r +
                   ((32 * c) ^ (16 * (r & 7)));
     uint32_t v[kExpandSteps][4];
+    const int shift = row_shift<kAlign>(src);
+    if (live && kBlockK * (kb0 + kExpandSteps) + (kAlign == 16 ? 0 : 16) <= E.K) {
 #pragma unroll
-    for (int i = 0; i < kExpandSteps; ++i)
-      load16<kAlign>(v[i], src, row_shift<kAlign>(src), kBlockK * (kb0 + i) + 16 * c, live ? E.K : -16);
+      for (int i = 0; i < kExpandSteps; ++i) load16_inside<kAlign>(v[i], src, shift, kBlockK * (kb0 + i) + 16 * c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kExpandSteps; ++i)
+        load16<kAlign>(v[i], src, shift, kBlockK * (kb0 + i) + 16 * c, live ? E.K : -16);
+    }
 #pragma unroll
     for (int i = 0; i < kExpandSteps; ++i) {
       if (kb0 + i < E.nkb) {
