@@ -104,6 +104,8 @@ template <typename T, int V> struct Pack {
   static constexpr int kBytes = V * (int)sizeof(T);
   uint32_t w[(kBytes + 3) / 4];
   // values [skip, left) of those from p on, which are the row's; zeros in the others' place
+  // (kWhole: all or none are)
+  template <bool kWhole>
   __device__ __forceinline__ void load(const T* p, int skip, int left) {
 #pragma unroll
     for (int i = 0; i < (kBytes + 3) / 4; ++i) w[i] = 0u;
@@ -116,7 +118,7 @@ template <typename T, int V> struct Pack {
       } else {
         w[0] = *reinterpret_cast<const uint16_t*>(p);
       }
-    } else if constexpr (V > 1) {
+    } else if constexpr (V > 1 && !kWhole) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (i >= skip && i < left) {
@@ -125,12 +127,13 @@ template <typename T, int V> struct Pack {
         }
     }
   }
+  template <bool kWhole>
   __device__ __forceinline__ void store(T* p, int skip, int left) const {
     if (skip <= 0 && left >= V) {
       if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
       else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
       else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
-    } else if constexpr (V > 1) {
+    } else if constexpr (V > 1 && !kWhole) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (i >= skip && i < left) {
@@ -171,14 +174,14 @@ __device__ __forceinline__ void make_codes(uint32_t (&w)[(V + 3) / 4], const flo
 }
 
 // p aligned to V codes.
-template <int V>
+template <int V, bool kWhole>
 __device__ __forceinline__ void store_codes(int8_t* p, const uint32_t (&w)[(V + 3) / 4], int left) {
   if (left >= V) {
     if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
     else if constexpr (V == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     else *p = (int8_t)w[0];
-  } else if constexpr (V > 1) {
+  } else if constexpr (V > 1 && !kWhole) {
 #pragma unroll
     for (int i = 0; i < V - 1; ++i)
       if (i < left) p[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
@@ -221,6 +224,18 @@ constexpr int kPlain = 0, kNormed = 1, kResidual = 2;
 // and after.
 __host__ __device__ constexpr int row_bytes(int nv, int threads, int vector) { return nv * threads * vector + 32; }
 
+// CTAs that an SM holds at least, by the registers each may have, where a warp's norm of a row has
+// 32 values per lane (us; without a bound the compiler takes more than help): 60,000 x 784 fp32 38
+// with four, 41 without; with residual 65,536 x 784 bf16 59 with three, 69; rows at odd places
+// 60,000 x 785 bf16 57 with two, 70 with three, 93, but 60,000 x 1001 fp32
+// with residual 125 without, 137 with two.
+template <typename T, int kMode, int kValues, bool kWarpRow, bool kWhole>
+__host__ __device__ constexpr int least_ctas() {
+  if (!kWarpRow || kValues <= 16 || kMode == kPlain) return 1;
+  if (!kWhole) return kMode == kResidual && sizeof(T) == 4 ? 1 : 2;
+  return kMode == kNormed ? 4 : 3;
+}
+
 // A row's T threads hold it: vector v of thread t is v T + t, NV vectors of V values
 // each.  The grid walks the rows; a row's values are loaded while the row before is
 // reduced and written, and the gain stays in registers (kAhead; without it neither,
@@ -229,8 +244,10 @@ __host__ __device__ constexpr int row_bytes(int nv, int threads, int vector) { r
 // A thread's vectors are the aligned 16 bytes around the row; rows eight apart lie
 // alike, and a thread's rows are a multiple of eight apart.  The codes go through shared
 // memory, since theirs lie otherwise, and the sums where theirs do (apart_sum).
-template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead, bool kApart>
-__global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize_regs(const QuantArgs A, bool apart_sum) {
+// kWhole: K is a multiple of V, and no vector is partly the row's.
+template <typename T, int kMode, int V, int NV, bool kWarpRow, bool kAhead, bool kApart, bool kWhole>
+__global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024, (least_ctas<T, kMode, V * NV, kWarpRow, kWhole>()))
+    k_quantize_regs(const QuantArgs A, bool apart_sum) {
   pdl_wait();
   pdl_trigger();
   const int threads = kWarpRow ? 32 : (int)blockDim.x;
@@ -262,7 +279,7 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
           else to.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(gain)[at(v) + i] << (16 * (i % 2));
         }
     } else {
-      to.load(gain + at(v), 0, A.K - at(v));
+      to.template load<kWhole>(gain + at(v), 0, A.K - at(v));
     }
   };
   if (kAhead && gain && row < A.n) {
@@ -271,10 +288,10 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
   }
   auto load = [&](int64_t i) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) px[v].load(x + i * A.ldx + at(v), skip(v), A.K - at(v));
+    for (int v = 0; v < NV; ++v) px[v].template load<kWhole>(x + i * A.ldx + at(v), skip(v), A.K - at(v));
     if constexpr (kRes) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) pr[v].load(res + i * A.ldr + at(v), skip(v), A.K - at(v));
+      for (int v = 0; v < NV; ++v) pr[v].template load<kWhole>(res + i * A.ldr + at(v), skip(v), A.K - at(v));
     }
   };
   if (kAhead && row < A.n) load(row);
@@ -300,7 +317,7 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
         if constexpr (kApart) {
           if (apart_sum) *reinterpret_cast<uint4*>(sums + 16 * (v * threads + tid)) = make_uint4(ps.w[0], ps.w[1], ps.w[2], ps.w[3]);
         }
-        if (!kApart || !apart_sum) ps.store(sum + row * A.lds + at(v), skip(v), A.K - at(v));
+        if (!kApart || !apart_sum) ps.template store<kWhole>(sum + row * A.lds + at(v), skip(v), A.K - at(v));
       }
     }
 #pragma unroll
@@ -328,7 +345,7 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024) k_quantize
       uint32_t w[(V + 3) / 4];
       make_codes<V>(w, u[v], r.inv, live);
       if constexpr (!kApart) {
-        store_codes<V>(q + at(v), w, A.K - at(v));
+        store_codes<V, kWhole>(q + at(v), w, A.K - at(v));
       } else {
         // (the row before was copied from there by threads that have since met in row_reduce)
         uint8_t* to = codes + (v * threads + tid) * V;
@@ -380,21 +397,20 @@ __global__ void __launch_bounds__(kThreads) k_quantize_long(const QuantArgs A) {
   if (threadIdx.x == 0) A.scale[row] = r.scale;
 }
 
-// A warp per row.  With 32 values per lane the next row is loaded ahead where a 16-bit row's
-// norm is made (65,536 x 784 34 us on four CTAs per SM, without 42); fp32 rows and rows that
-// are only coded run faster from more warps (60,000 x 784 fp32 46, ahead 55; 60,000 x 1000
-// bf16 coded 28.6, ahead 32.5).
-template <typename T, int kMode, int V, int NV, bool kApart>
+// A warp per row.  With 32 values per lane whole rows run faster from more warps than with the next
+// row loaded ahead (65,536 x 784 bf16 31 us, ahead 40; 60,000 x 784 fp32 38, ahead 55;
+// 60,000 x 1000 bf16 coded 28.6, ahead 32.5), rows with a ragged end in 16 bits or at odd places not.
+template <typename T, int kMode, int V, int NV, bool kApart, bool kWhole>
 cudaError_t launch_warp_rows(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
-  constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain) || kApart;
+    constexpr bool kAhead = V * NV <= 16 || (sizeof(T) == 2 && kMode != kPlain && !kWhole) || kApart;
   const int64_t ctas = std::min((A.n + kRowsPerCta - 1) / kRowsPerCta, (int64_t)(kAhead && V * NV > 16 ? 4 : 8) * sm_count());
-  return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead, kApart>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta),
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, true, kAhead, kApart, kWhole>, dim3((unsigned)ctas), dim3(32 * kRowsPerCta),
                        kApart ? (size_t)kRowsPerCta * (row_bytes(NV, 32, V) + (apart_sum ? row_bytes(NV, 32, 16) : 0)) : 0, st, true,
                        A, apart_sum);
 }
 
 // A CTA per row: 1,024 threads an SM.
-template <typename T, int kMode, int V, int NV, bool kApart>
+template <typename T, int kMode, int V, int NV, bool kApart, bool kWhole>
 cudaError_t launch_cta_rows(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   const int vecs = kApart ? (int)((A.K + 2ll * V - 2) / V) : A.K / V + (A.K % V != 0);
   const int threads = (vecs + 32 * NV - 1) / (32 * NV) * 32;
@@ -402,37 +418,37 @@ cudaError_t launch_cta_rows(const QuantArgs& A, bool apart_sum, cudaStream_t st)
   const int64_t ctas = kAhead ? std::min(A.n, (int64_t)(1024 / threads) * sm_count() / 8 * 8) : A.n;
   if (kApart && apart_sum) {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = allow_smem(done, k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart>,
+    const cudaError_t e = allow_smem(done, k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart, kWhole>,
                                      row_bytes(NV, 1024, V) + row_bytes(NV, 1024, 16));
     if (e != cudaSuccess) return e;
   }
-  return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart>, dim3((unsigned)ctas), dim3((unsigned)threads),
+  return launch_kernel(k_quantize_regs<T, kMode, V, NV, false, kAhead, kApart, kWhole>, dim3((unsigned)ctas), dim3((unsigned)threads),
                        kApart ? (size_t)row_bytes(NV, threads, V) + (apart_sum ? row_bytes(NV, threads, 16) : 0) : 0, st, true, A,
                        apart_sum);
 }
 
 // Which form (us, rows in bf16 unless said): rows that a warp holds in at most kWarpMost
-// vectors per lane get a warp each (65,536 x 784 34, by CTAs 58; 60,000 x 784 fp32 46, by CTAs
+// vectors per lane get a warp each (65,536 x 784 31, by CTAs 58; 60,000 x 784 fp32 38, by CTAs
 // 62).  Else a CTA per row, with one vector per thread for few rows (1 x 8192 2.5, two 2.8, four 4.1), and
 // for many as many as the registers hold beside the next row's: four without a norm
 // (8192 x 8192 30, two 34, one 44), two with it (8191 x 4096 with residual 40, four 57 for want of registers).
-template <typename T, int kMode, int V, bool kApart>
+template <typename T, int kMode, int V, bool kApart, bool kWhole>
 cudaError_t launch_v(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   constexpr int kWarpMost = V == 8 ? 4 : (V == 4 ? 8 : 16);
   const int64_t vecs = kApart ? (A.K + 2ll * V - 2) / V : A.K / V + (A.K % V != 0);
   if constexpr (!kApart) {
-    if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1, false>(A, apart_sum, st);
-    if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2, false>(A, apart_sum, st);
-    if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4, false>(A, apart_sum, st);
-    if (V <= 2 && vecs <= 256) return launch_warp_rows<T, kMode, V, V <= 2 ? 8 : 4, false>(A, apart_sum, st);
+    if (vecs <= 32) return launch_warp_rows<T, kMode, V, 1, false, kWhole>(A, apart_sum, st);
+    if (vecs <= 64) return launch_warp_rows<T, kMode, V, 2, false, kWhole>(A, apart_sum, st);
+    if (vecs <= 128) return launch_warp_rows<T, kMode, V, 4, false, kWhole>(A, apart_sum, st);
+    if (V <= 2 && vecs <= 256) return launch_warp_rows<T, kMode, V, V <= 2 ? 8 : 4, false, kWhole>(A, apart_sum, st);
   }
-  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart>(A, apart_sum, st);
+  if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart, kWhole>(A, apart_sum, st);
   if (vecs > 4096)
     return launch_kernel(k_quantize_long<T, kMode>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
   const bool few = A.n <= 2 * sm_count();
-  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart>(A, apart_sum, st);
-  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart>(A, apart_sum, st);
-  return launch_cta_rows<T, kMode, V, 1, kApart>(A, apart_sum, st);
+  if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart, kWhole>(A, apart_sum, st);
+  if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart, kWhole>(A, apart_sum, st);
+  return launch_cta_rows<T, kMode, V, 1, kApart, kWhole>(A, apart_sum, st);
 }
 
 // Vectors of 16 bytes; also where rows start elsewhere but the inputs' alike, if they are long and
@@ -450,12 +466,13 @@ cudaError_t launch_type(const QuantArgs& A, cudaStream_t st) {
   const uintptr_t wide = px | (A.res ? place(A.res, A.ldr) : 0) | (A.sum ? place(A.sum, A.lds) : 0) |
                          (reinterpret_cast<uintptr_t>(A.gain) & 15);
   const uintptr_t codes = reinterpret_cast<uintptr_t>(A.q) | (many ? (uintptr_t)A.ldq : 0);
-  if (wide == 0 && codes % V == 0) return launch_v<T, kMode, V, false>(A, false, st);
+  if (wide == 0 && codes % V == 0)
+    return A.K % V ? launch_v<T, kMode, V, false, false>(A, false, st) : launch_v<T, kMode, V, false, true>(A, false, st);
   const bool apart_sum = A.sum && place(A.sum, A.lds) != px;
   if ((!A.res || place(A.res, A.ldr) == px) && A.K > 512 && (A.n > 2 * sm_count() || A.K > 4096) && A.K <= 2048 * V - V)
-    return launch_v<T, kMode, V, true>(A, apart_sum, st);
-  if (sizeof(T) == 2 && (wide & 0x33) == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1, false>(A, false, st);
-  return launch_v<T, kMode, 1, false>(A, false, st);
+    return launch_v<T, kMode, V, true, false>(A, apart_sum, st);
+  if (sizeof(T) == 2 && (wide & 0x33) == 0 && codes % 2 == 0) return launch_v<T, kMode, sizeof(T) == 2 ? 2 : 1, false, false>(A, false, st);
+  return launch_v<T, kMode, 1, false, false>(A, false, st);
 }
 
 template <typename T>
