@@ -414,6 +414,30 @@ def test_offsets_past_32_bits(n):
 
 
 @gpu
+@pytest.mark.parametrize("n,K,N", [(9000, 512, 128), (5000, 640, 96), (20000, 300, 64), (6000, 304, 48), (30000, 130, 256)])
+def test_many_rows_and_few_channels_in_whole_vectors(n, K, N):
+    run_all(codes(n, K, n, "ends"), codes(N, K, K), K, N, n, 0, 0)
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(5000, 300, 60), (4500, 1500, 120)])
+def test_offsets_past_32_bits_of_many_rows(n, K, N):
+    """Few channels: rows and channels change places; the last rows lie past 2^32 elements."""
+    far = 2 ** 32 // (n - 1) + 5
+    abuf = torch.zeros(far * (n - 1) + K, dtype=torch.int8, device=DEV)
+    a = abuf.as_strided((n, K), (far, 1))
+    a.copy_(codes(n, K, 9))
+    w = codes(N, K, 8).to(DEV)
+    obuf = torch.zeros(far * (n - 1) + N, dtype=torch.float16, device=DEV)
+    out = obuf.as_strided((n, N), (far, 1))
+    B.bmlp_int8_matmul(a, w, out, torch.full((n,), 2.0 ** -16, device=DEV))
+    assert torch.equal(out, (sums64(a, w).float() * 2.0 ** -16).half())
+    words = torch.zeros((n, W.words(N)), dtype=torch.int64, device=DEV)
+    B.bmlp_int8_sign(a, w, words)
+    assert np.array_equal(words.cpu().numpy().view(np.uint64), W.pack(np.where(sums64(a, w).cpu().numpy() >= 0, 1, -1)))
+
+
+@gpu
 def test_streams_and_capture():
     """On a stream of its own, and replayed from a graph on new inputs."""
     n, K, N = 37, 512, 200
