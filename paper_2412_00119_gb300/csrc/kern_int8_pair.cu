@@ -21,7 +21,7 @@
 // Measured, both operands' expansion included: 16384 x 8192 -> 8192 1.15 to 1.19 ms = 1,850 to
 // 1,910 TFLOP/s, signs of 65536 x 4096 -> 8192 2.24 to 2.27 ms = 1,940 to 1,960 (bf16 by the
 // library 1,946).  Up to K = 1024 the one chunk's sums go from tensor memory to the outputs
-// in fp32 as they are read: 47,880 x 332 -> 14,928 signs 445 us (through int32 registers
+// in fp32 as they are read: 47,880 x 332 -> 14,928 signs 420 us (through int32 registers
 // 665).  A k-step takes 520 clocks where its MMAs take 512 (with forwarded completions
 // 730 to 790); a chunk's read-out takes 4,900 of the 8,200 of the next chunk's MMAs, a tile's
 // stores 4,900 (one instance per output type: with the types told apart inside the unrolled
@@ -317,21 +317,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         // (a threshold that no sum reaches, or every one, as an infinity: others are exact in fp32)
         const float thrf = thr > 1 << 24 ? INFINITY : (thr < -(1 << 24) ? -INFINITY : (float)thr);
-#pragma unroll 1
+        // (all are read before the arrival and stored after it, since its release waits for stores under
+        // way: 37,155 x 55 -> 13,908 signs 242 us, read and stored by quarters 290)
+        uint32_t v[8][16];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tmem_load16(v[e], tacc + 256u * b + 16u * (uint32_t)e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tmem_wait_ld(v[e]);
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive_rank0(&sh->drained[b]);
+#pragma unroll
         for (int g = 0; g < 4; ++g) {
-          uint32_t v[2][16];
-          tmem_load16(v[0], tacc + 256u * b + 32u * (uint32_t)g);
-          tmem_load16(v[1], tacc + 256u * b + 32u * (uint32_t)g + 16u);
-          tmem_wait_ld(v[0]);
-          tmem_wait_ld(v[1]);
-          if (g == 3) {
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive_rank0(&sh->drained[b]);
-          }
           float f[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e >> 4][e & 15]);
+          for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[2 * g + (e >> 4)][e & 15]);
           put_group<TOut>(A, f, i0 + 32 * g, rows - 32 * g, jw, sw, bias, thrf);
         }
         continue;
