@@ -45,7 +45,7 @@ using namespace i8;
 
 constexpr int CM = 128;                 // channels of a tile
 constexpr int kWorkers = 16;
-constexpr int kMaxSplit = 4;             // CTAs that share K (of eight, few clusters find room at once)
+constexpr int kFewTiles = 12;           // tiles at most whose K eight CTAs share (more clusters of eight find no room at once)
 constexpr int kGroups = 4;              // worker groups, each a k-step of its own
 constexpr int kSmemBytes = 225 * 1024;  // for stages and copies in flight
 
@@ -667,6 +667,7 @@ __global__ void __launch_bounds__(Cfg<NT, kAlign, kReady>::kThreads, 1)
   switch (split) {
     case 1: exchange_and_write<kCols, 1>(A, acc, base, rank, i0, jw, F); break;
     case 2: exchange_and_write<kCols, 2>(A, acc, base, rank, i0, jw, F); break;
+    case 8: exchange_and_write<kCols, 8>(A, acc, base, rank, i0, jw, F); break;
     default: exchange_and_write<kCols, 4>(A, acc, base, rank, i0, jw, F);
   }
 }
@@ -705,12 +706,14 @@ cudaError_t launch_rows(const Int8Args& A, const uint8_t* ablocks, int nt, int s
 
 }  // namespace
 
-// As many as leave every SM at most one, with eight k-steps of 64 each; of swapped operands a
-// thread keeps eight channels (a byte of signs).
+// Up to four: as many as leave every SM at most one, with eight k-steps of 64 each; of swapped
+// operands a thread keeps eight channels (a byte of signs).  Eight for a few tiles (us: 20 rows of
+// 8192 -> 512 6.5, by four 9.2, -> 1536 7.4, 9.3; but 16384 -> 2048, 16 tiles, 19.4, 15.0).
 int int8_tile_split(int64_t tiles, int K, int nt, bool swap) {
-  const int steps = (K + 63) / 64, most = swap ? std::min(kMaxSplit, nt / 32) : kMaxSplit;
+  const int steps = (K + 63) / 64, most = swap ? nt / 32 : 4;
   int split = 1;
   while (split < most && tiles * (2 * split) <= sm_count() && steps >= 8 * split) split *= 2;
+  if (!swap && split == 4 && tiles <= kFewTiles && steps >= 32) split = 8;
   return split;
 }
 

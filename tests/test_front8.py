@@ -471,7 +471,7 @@ def test_streams_and_capture():
         check()
 
 
-# sizes whose kernel is, in turn: the streamed one; 32-row tiles (K shared by four, one CTA);
+# sizes whose kernel is, in turn: the streamed one; 32-row tiles (K shared by eight, one CTA);
 # 64- and 128-row tiles of ready activations (with and without sharing K; two rounds); pairs
 PLANS = [(5, 300, 100), (20, 2048, 300), (31, 100, 19500), (50, 8192, 8192), (64, 8000, 7000), (100, 4096, 8192),
          (120, 8191, 4096), (300, 2300, 9000), (700, 4096, 4096), (1500, 1024, 8192), (2100, 1001, 6000)]
@@ -498,6 +498,21 @@ def test_expired_waits_cost_time_only(n, K, N):
         out.fill_(-3)
         B.bmlp_int8_matmul(a, w, out, workspace=ws)     # the device is as it was
         assert torch.equal(out.double(), S)
+
+
+# a few tiles, whose K eight CTAs share, and one tile more
+SHARED = [(20, 2048, 1536), (20, 2047, 1537), (12, 9000, 40), (21, 14142, 384), (60, 4096, 700), (100, 5000, 200), (200, 8192, 128)]
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", SHARED)
+def test_depth_shared_by_eight(n, K, N):
+    run_all(codes(n, K, n, "ends"), codes(N, K, K), K, N, n, 0, 0)
+    a, w = codes(n, K, n).to(DEV), codes(N, K, K).to(DEV)
+    out = torch.full((n, N), -3, dtype=torch.int32, device=DEV)
+    for expired in (True, False):
+        B.bmlp_int8_matmul(a, w, out, expired=expired)
+        assert torch.equal(out.double(), sums64(a, w))
 
 
 @gpu
