@@ -12,6 +12,7 @@ default stream).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import sys
@@ -341,6 +342,19 @@ def bmlp_release_workspaces():
     _kept.__dict__.clear()
 
 
+def _on_stream(stream, a):
+    """torch's current stream is the call's: a block that was freed on a stream is given out
+    again at once, in the order of that stream alone."""
+    if stream is None:
+        return contextlib.nullcontext()
+    raw = _stream(stream)
+    if raw == _tensor_stream(None, a):
+        return contextlib.nullcontext()
+    cuda = _torch.cuda
+    # (0 and 1: the legacy default stream)
+    return cuda.stream(cuda.ExternalStream(raw, a.device) if raw > 1 else cuda.default_stream(a.device))
+
+
 def _workspace(L, workspace, n, K, N, a, stream):
     """(pointer, bytes) of the given workspace, or of one from torch's allocator where
     the size wants it: kept for the thread's next call on the same stream if it is small
@@ -361,11 +375,8 @@ def _workspace(L, workspace, n, K, N, a, stream):
         workspace = at[key] = None   # (the smaller one goes back first)
         workspace = at[key] = torch.empty(size, dtype=torch.uint8, device=a.device)
     else:
-        workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
-        if stream is not None:
-            raw = _stream(stream)
-            if raw != torch.cuda.current_stream(a.device).cuda_stream:
-                workspace.record_stream(torch.cuda.ExternalStream(raw, a.device))
+        with _on_stream(stream, a):
+            workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
     return workspace.data_ptr(), size, workspace
 
 

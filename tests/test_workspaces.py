@@ -1,0 +1,179 @@
+"""Where the binding takes the 8-bit product's workspace from: on which stream, in
+which capture, how much of it stays, and which tensors a caller may give.
+
+The rules are tested without a GPU on a recording stand-in for torch's allocator and
+for the library; what they are for, memory that other work still uses, on the GPU."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+from paper_2412_00119_gb300 import bmlp as B
+
+DEV = "cuda:0"
+gpu = pytest.mark.gpu
+SIZE = 4096
+
+
+class Tensor:
+    """What the binding asks of a tensor on the device."""
+
+    def __init__(self, shape, dtype, device=0, ptr=4096):
+        self.shape, self.dtype, self.ptr = torch.Size(shape), dtype, ptr
+        self.device = torch.device("cuda", device)
+        self.is_cuda = True
+
+    def stride(self, dim=None):
+        s = [1] * len(self.shape)
+        for i in range(len(s) - 2, -1, -1):
+            s[i] = s[i + 1] * self.shape[i + 1]
+        return tuple(s) if dim is None else s[dim]
+
+    def data_ptr(self):
+        return self.ptr
+
+    def get_device(self):
+        return self.device.index
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def record_stream(self, stream):
+        pass
+
+
+class Device:
+    """torch's streams and allocator, and the library, as far as the binding sees them."""
+
+    def __init__(self):
+        self.current, self.capturing, self.device = 100, set(), 0
+        self.allocated = []          # (stream, bytes) of every block
+        self.calls = []              # (stream, workspace, bytes) of every product
+        self.room = 1 << 40
+        self.size = SIZE             # that the library asks for
+        self.pools = {}              # block -> id of the pool it lies in
+
+    def empty(self, size, dtype, device):
+        if size > self.room:
+            raise torch.cuda.OutOfMemoryError("no room")
+        self.allocated.append((self.current, size))
+        t = Tensor((size,), dtype, torch.device(device).index or 0, ptr=1 << 20 | len(self.allocated) << 8)
+        self.pools[t.ptr] = (0, 1) if self.current in self.capturing and self.graph else (0, 0)
+        return t
+
+    graph = True                     # captures are torch's own
+
+    @contextlib.contextmanager
+    def stream(self, s):
+        before, self.current = self.current, s.cuda_stream
+        yield
+        self.current = before
+
+    def snapshot(self):
+        return [dict(address=p, total_size=256, segment_pool_id=i) for p, i in self.pools.items()]
+
+    def product(self, *args):
+        # (workspace, bytes, stream: the last three)
+        self.calls.append((args[-1], args[-3], args[-2]))
+        return 0
+
+
+@pytest.fixture
+def dev(monkeypatch):
+    d = Device()
+    B.bmlp_release_workspaces()
+    B._use_torch()
+    stream = lambda raw=0, device=None: types.SimpleNamespace(cuda_stream=raw)   # noqa: E731
+    cuda = types.SimpleNamespace(
+        stream=d.stream, ExternalStream=stream, default_stream=lambda device=None: stream(0),
+        current_stream=lambda device=None: stream(d.current), is_current_stream_capturing=lambda: d.current in d.capturing,
+        OutOfMemoryError=torch.cuda.OutOfMemoryError, memory_snapshot=d.snapshot)
+    fake = types.SimpleNamespace(cuda=cuda, empty=d.empty, **{t: getattr(torch, t) for t in
+                                 ("int8", "uint8", "int32", "int64", "float32", "float16", "bfloat16")})
+    library = types.SimpleNamespace(bmlp_int8_workspace=lambda n, K, N: d.size, bmlp_int8_matmul=d.product,
+                                    bmlp_debug_int8_matmul=d.product, bmlp_int8_sign=d.product)
+    monkeypatch.setattr(B, "_torch", fake)
+    monkeypatch.setattr(B, "_raw_stream", lambda device: d.current)
+    monkeypatch.setattr(B, "_get_device", lambda: d.device)
+    monkeypatch.setattr(B, "_lib", library)
+    yield d
+    B.bmlp_release_workspaces()
+
+
+def product(n=64, K=128, N=256, device=0, out_device=0, **kw):
+    a, w = Tensor((n, K), torch.int8, device), Tensor((N, K), torch.int8, device)
+    B.bmlp_int8_matmul(a, w, Tensor((n, N), torch.float32, out_device), **kw)
+
+
+def signs(n=64, K=128, N=256, **kw):
+    a, w = Tensor((n, K), torch.int8), Tensor((N, K), torch.int8)
+    B.bmlp_int8_sign(a, w, Tensor((n, (N + 63) // 64), torch.int64), **kw)
+
+
+@pytest.mark.parametrize("call", [product, signs])
+def test_workspace_belongs_to_the_calls_stream(dev, call):
+    """torch hands a block that was freed on a stream out again at once, in the order of that
+    stream alone: the block has to be one of the stream that the kernels run on."""
+    for stream in (None, 100, 42, types.SimpleNamespace(cuda_stream=43), 0):
+        del dev.allocated[:], dev.calls[:]
+        B.bmlp_release_workspaces()
+        call(stream=stream)
+        (on, workspace, size), = dev.calls
+        assert size == SIZE and workspace
+        assert dev.allocated == [(on, SIZE)], stream
+        assert dev.current == 100
+
+
+@gpu
+def test_workspace_beside_work_on_the_current_stream():
+    """A block of the workspace's size that was freed on the current stream while kernels that
+    write and read it are still queued there; then a product on another stream."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    torch.cuda.set_device(DEV)
+    n, K, N = 300, 2304, 4000
+    g = torch.Generator().manual_seed(1)
+    a, w = (torch.randint(-128, 128, s, generator=g).to(torch.int8).to(DEV) for s in ((n, K), (N, K)))
+    S = (a.double() @ w.double().t()).to(torch.int32)
+    size = B.bmlp_int8_workspace(n, K, N)
+    assert size > 0
+    s = torch.cuda.Stream()
+    busy = torch.randn((2048, 2048), device=DEV)
+    out = torch.empty((n, N), dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for _ in range(20):
+            busy = busy @ busy
+            busy /= busy.abs().amax()
+        block = torch.full((size,), 7, dtype=torch.uint8, device=DEV)
+        busy = busy @ busy
+        busy /= busy.abs().amax()
+        seen = block.clone()
+        del block
+        out.fill_(-3)
+        done = torch.cuda.Event()
+        done.record()
+        # (the outputs' filling ends before the product begins; the current stream then has more work)
+        s.wait_event(done)
+        B.bmlp_int8_matmul(a, w, out, stream=s)
+        torch.cuda.synchronize()
+        assert (seen == 7).all() and torch.equal(out, S)
+        # without that wait: the block's writer and reader are pending while the product runs
+        for _ in range(20):
+            busy = busy @ busy
+            busy /= busy.abs().amax()
+        block = torch.full((size,), 9, dtype=torch.uint8, device=DEV)
+        busy = busy @ busy
+        busy /= busy.abs().amax()
+        seen = block.clone()
+        del block
+        B.bmlp_int8_matmul(a, w, out, stream=s)
+        torch.cuda.synchronize()
+        assert (seen == 9).all() and torch.equal(out, S)
