@@ -351,14 +351,40 @@ def _on_stream(stream, a):
     if raw == _tensor_stream(None, a):
         return contextlib.nullcontext()
     cuda = _torch.cuda
+    if isinstance(stream, cuda.Stream):
+        return cuda.stream(stream)
     # (0 and 1: the legacy default stream)
     return cuda.stream(cuda.ExternalStream(raw, a.device) if raw > 1 else cuda.default_stream(a.device))
+
+
+def _in_graph_pool(block):
+    """Whether a block that was allocated in a capture stays the graph's."""
+    cuda = _torch.cuda
+    if cuda.get_allocator_backend() != "native":
+        return True     # (an allocation of the graph's own)
+    at = block.data_ptr()
+    return any(s["address"] <= at < s["address"] + s["total_size"] and tuple(s.get("segment_pool_id", (0, 0))) != (0, 0)
+               for s in cuda.memory_snapshot())
+
+
+def _block(size, a, stream):
+    """A block of the call's stream.  None in a capture that is not torch's own: the block would
+    be given to others while the graph still writes it."""
+    torch = _torch
+    captured = torch.cuda.is_current_stream_capturing()
+    with _on_stream(stream, a):
+        capturing = torch.cuda.is_current_stream_capturing()
+        if capturing and not captured:
+            return None
+        block = torch.empty(size, dtype=torch.uint8, device=a.device)
+        return None if capturing and not _in_graph_pool(block) else block
 
 
 def _workspace(L, workspace, n, K, N, a, stream):
     """(pointer, bytes) of the given workspace, or of one from torch's allocator where
     the size wants it: kept for the thread's next call on the same stream if it is small
-    and the stream is torch's current one, not in a capture."""
+    and the stream is torch's current one, not in a capture.  None where there is none to
+    be had: the product runs without."""
     if workspace is not None:
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     size = L.bmlp_int8_workspace(n, K, N)
@@ -375,8 +401,9 @@ def _workspace(L, workspace, n, K, N, a, stream):
         workspace = at[key] = None   # (the smaller one goes back first)
         workspace = at[key] = torch.empty(size, dtype=torch.uint8, device=a.device)
     else:
-        with _on_stream(stream, a):
-            workspace = torch.empty(size, dtype=torch.uint8, device=a.device)
+        workspace = _block(size, a, stream)
+        if workspace is None:
+            return None, 0, None
     return workspace.data_ptr(), size, workspace
 
 
@@ -385,7 +412,8 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     int8) times w (N x K int8) transposed, scaled per row and channel.
     workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: one from
     torch's allocator; up to 64 MB of it stay with the thread for its next call on the
-    stream, until bmlp_release_workspaces).  expired: bmlp_debug_int8_matmul."""
+    stream, until bmlp_release_workspaces; a capture that torch does not make takes none,
+    which is slower: give it one).  expired: bmlp_debug_int8_matmul."""
     torch = _torch or _use_torch()
     L = _lib or lib()
     shape = n, K = a.shape

@@ -92,9 +92,9 @@ def dev(monkeypatch):
     B._use_torch()
     stream = lambda raw=0, device=None: types.SimpleNamespace(cuda_stream=raw)   # noqa: E731
     cuda = types.SimpleNamespace(
-        stream=d.stream, ExternalStream=stream, default_stream=lambda device=None: stream(0),
+        stream=d.stream, Stream=torch.cuda.Stream, ExternalStream=stream, default_stream=lambda device=None: stream(0),
         current_stream=lambda device=None: stream(d.current), is_current_stream_capturing=lambda: d.current in d.capturing,
-        OutOfMemoryError=torch.cuda.OutOfMemoryError, memory_snapshot=d.snapshot)
+        OutOfMemoryError=torch.cuda.OutOfMemoryError, memory_snapshot=d.snapshot, get_allocator_backend=lambda: "native")
     fake = types.SimpleNamespace(cuda=cuda, empty=d.empty, **{t: getattr(torch, t) for t in
                                  ("int8", "uint8", "int32", "int64", "float32", "float16", "bfloat16")})
     library = types.SimpleNamespace(bmlp_int8_workspace=lambda n, K, N: d.size, bmlp_int8_matmul=d.product,
@@ -129,6 +129,113 @@ def test_workspace_belongs_to_the_calls_stream(dev, call):
         assert size == SIZE and workspace
         assert dev.allocated == [(on, SIZE)], stream
         assert dev.current == 100
+
+
+def test_workspace_in_captures(dev):
+    """The address of a captured call's workspace stays in the graph: it has to be a block that
+    torch keeps for the graph, or none."""
+    def run(stream, capturing, graph, want):
+        del dev.allocated[:], dev.calls[:]
+        dev.capturing, dev.graph = capturing, graph
+        product(stream=stream)
+        (on, workspace, size), = dev.calls
+        assert on == (100 if stream is None else stream)
+        if want:
+            assert dev.allocated == [(on, SIZE)] and size == SIZE and dev.pools[workspace] == (0, 1)
+        else:
+            assert not workspace and size == 0
+            # no allocation in a capture that torch knows nothing of, where it may not be allowed
+            assert not dev.allocated or 100 in capturing
+        given = Tensor((SIZE,), torch.uint8, ptr=1 << 40)
+        product(stream=stream, workspace=given)
+        assert dev.calls[1] == (on, 1 << 40, SIZE)
+
+    for stream in (None, 100, 42):
+        run(stream, {100, 42}, True, True)      # torch's capture, and a stream forked from it
+        run(stream, {100, 42}, False, False)    # another runtime's capture
+    run(42, {42}, False, False)                 # of a stream that is not the current one
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(300, 2304, 4000), (100, 4096, 8192), (4000, 1500, 100)])
+def test_captures_by_the_driver(n, K, N):
+    """Captures that torch does not make, of the current stream and of another: the graph uses no
+    memory that torch gives to others."""
+    import ctypes as C
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    torch.cuda.set_device(DEV)
+    cu = C.CDLL("libcuda.so.1")
+
+    def ok(rc):
+        assert rc == 0, rc
+    g = torch.Generator().manual_seed(1)
+    a, w = (torch.randint(-128, 128, s, generator=g).to(torch.int8).to(DEV) for s in ((n, K), (N, K)))
+    S = (a.double() @ w.double().t()).to(torch.int32)
+    size = B.bmlp_int8_workspace(n, K, N)
+    out = torch.empty((n, N), dtype=torch.int32, device=DEV)
+    given = torch.empty((size,), dtype=torch.uint8, device=DEV)
+    s = torch.cuda.Stream()
+    B.bmlp_int8_matmul(a, w, out)
+    for how in ("another", "current", "given"):
+        with torch.cuda.stream(s):
+            blocks = [torch.empty((size,), dtype=torch.uint8, device=DEV) for _ in range(2)]
+            del blocks              # (of which torch may take one in the capture)
+        torch.cuda.synchronize()
+        raw, graph, exe = C.c_void_p(s.cuda_stream), C.c_void_p(), C.c_void_p()
+        ok(cu.cuStreamBeginCapture_v2(raw, 1))
+        try:
+            if how == "another":
+                B.bmlp_int8_matmul(a, w, out, stream=s)
+            elif how == "given":
+                B.bmlp_int8_matmul(a, w, out, stream=s, workspace=given)
+            else:
+                with torch.cuda.stream(s):
+                    B.bmlp_int8_matmul(a, w, out)
+        finally:
+            ok(cu.cuStreamEndCapture(raw, C.byref(graph)))
+        ok(cu.cuGraphInstantiateWithFlags(C.byref(exe), graph, C.c_ulonglong(0)))
+        with torch.cuda.stream(s):
+            others = [torch.full((size,), 0x7F, dtype=torch.uint8, device=DEV) for _ in range(3)]
+            out.fill_(-3)
+            ok(cu.cuGraphLaunch(exe, raw))
+        torch.cuda.synchronize()
+        assert torch.equal(out, S), how
+        assert all((t == 0x7F).all() for t in others), how
+        ok(cu.cuGraphExecDestroy(exe))
+        ok(cu.cuGraphDestroy(graph))
+
+
+@gpu
+def test_workspace_in_a_forked_capture():
+    """torch's capture with a second stream: the block is the graph's, and that stream's."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    torch.cuda.set_device(DEV)
+    n, K, N = 300, 2304, 4000
+    g = torch.Generator().manual_seed(1)
+    a, w = (torch.randint(-128, 128, s, generator=g).to(torch.int8).to(DEV) for s in ((n, K), (N, K)))
+    S = (a.double() @ w.double().t()).to(torch.int32)
+    outs = [torch.empty((n, N), dtype=torch.int32, device=DEV) for _ in range(3)]
+    s = torch.cuda.Stream()
+    B.bmlp_int8_matmul(a, w, outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        current = torch.cuda.current_stream()
+        s.wait_stream(current)
+        B.bmlp_int8_matmul(a, w, outs[0])
+        B.bmlp_int8_matmul(a, w, outs[1], stream=s)
+        B.bmlp_int8_matmul(a, w, outs[2], stream=s)
+        current.wait_stream(s)
+    junk = [torch.full((B.bmlp_int8_workspace(n, K, N),), 0x7F, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    for _ in range(3):
+        for o in outs:
+            o.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, S) for o in outs)
+        assert all((t == 0x7F).all() for t in junk)
 
 
 @gpu
