@@ -386,6 +386,8 @@ def _workspace(L, workspace, n, K, N, a, stream):
     and the stream is torch's current one, not in a capture.  None where there is none to
     be had: the product runs without."""
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace: its bytes must be contiguous")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     size = L.bmlp_int8_workspace(n, K, N)
     if size == 0 or not a.is_cuda:

@@ -131,6 +131,19 @@ def test_workspace_belongs_to_the_calls_stream(dev, call):
         assert dev.current == 100
 
 
+def test_workspace_of_any_layout_is_refused():
+    """An expanded or strided tensor has fewer bytes of its own from its pointer on than it has
+    elements: the kernels would write past them."""
+    a, w = torch.zeros((64, 128), dtype=torch.int8), torch.zeros((256, 128), dtype=torch.int8)
+    out, words = torch.zeros((64, 256)), torch.zeros((64, 4), dtype=torch.int64)
+    for ws in (torch.zeros((1,), dtype=torch.uint8).expand(1 << 24), torch.zeros((4096,), dtype=torch.uint8)[::2],
+               torch.zeros((64, 64), dtype=torch.uint8)[:, :32], torch.zeros((8, 4), dtype=torch.float32).t()):
+        with pytest.raises(ValueError, match="workspace"):
+            B.bmlp_int8_matmul(a, w, out, workspace=ws)
+        with pytest.raises(ValueError, match="workspace"):
+            B.bmlp_int8_sign(a, w, words, workspace=ws)
+
+
 def test_workspace_in_captures(dev):
     """The address of a captured call's workspace stays in the graph: it has to be a block that
     torch keeps for the graph, or none."""
