@@ -186,6 +186,12 @@ def _rows(t, shape, what, dtype):
     return t.data_ptr(), ld
 
 
+def _int32(K, N=1):
+    """ctypes would cut a K or N of more than 32 bits without a word."""
+    if (K | N) >> 31:
+        raise BmlpError(BMLP_EINVAL, "K = %d or N = %d past 31 bits" % (K, N))
+
+
 def _vector(t, n, what, dtype):
     """Pointer of a contiguous vector of n elements (None: NULL)."""
     if t is None:
@@ -301,6 +307,7 @@ def bmlp_quantize_rows(x, q, scale, stream=None):
     fp32 / fp16 / bf16, on the device; row strides are kept)."""
     torch = _torch or _use_torch()
     shape = n, K = x.shape
+    _int32(K)
     px, ldx = _rows(x, shape, "x", x.dtype)
     pq, ldq = _rows(q, shape, "q", torch.int8)
     rc = (_lib or lib()).bmlp_quantize_rows(px, _type(x, _real_types, "x"), ldx, n, K, pq, ldq,
@@ -315,6 +322,7 @@ def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stre
     gain, res, sum_out: x's type, each may be None."""
     torch = _torch or _use_torch()
     shape = n, K = x.shape
+    _int32(K)
     dtype = x.dtype
     px, ldx = _rows(x, shape, "x", dtype)
     pr, ldr = (None, 0) if res is None else _rows(res, shape, "res", dtype)
@@ -329,7 +337,7 @@ def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stre
 
 def bmlp_int8_workspace(n, K, N):
     """Bytes of workspace with which the product of this size runs fastest."""
-    return int(lib().bmlp_int8_workspace(n, K, N))
+    return 0 if (K | N) >> 31 else int(lib().bmlp_int8_workspace(n, K, N))   # (0: refused)
 
 
 _KEPT_WORKSPACE = 64 << 20     # bytes of the largest workspace that is kept for the next call
@@ -420,6 +428,7 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     L = _lib or lib()
     shape = n, K = a.shape
     N = w.shape[0]
+    _int32(K, N)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     po, ldo = _rows(out, (n, N), "out", out.dtype)
@@ -441,6 +450,7 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     L = _lib or lib()
     shape = n, K = a.shape
     N = w.shape[0]
+    _int32(K, N)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():
