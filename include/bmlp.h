@@ -235,7 +235,7 @@ int bmlp_debug_expand_sign(const uint8_t* x, int64_t n, int32_t D, const uint64_
  * four has a backward form.
  *
  * Common to the four: no handle (errors: bmlp_last_error(NULL)); every pointer
- * is a device pointer, caller-owned; asynchronous on cuda_stream, nothing is
+ * is memory of the current device (or managed), caller-owned; asynchronous on cuda_stream, nothing is
  * allocated; may be captured.  Row strides (ld...) are in elements and at
  * least the row's length where there is more than one row; rows may start at
  * any element.  n == 0 is a no-op.  Outputs may not overlap inputs except where

@@ -202,6 +202,17 @@ def _vector(t, n, what, dtype):
     return t.data_ptr()
 
 
+def _one_device(x, *others):
+    """Refuses tensors of another device than the current one, where the kernels run.  (Host
+    memory is the library's to refuse.)"""
+    here = x.get_device()
+    if here >= 0 and here != (_get_device or _torch.cuda.current_device)():
+        raise ValueError("tensors on cuda:%d, which is not the current device" % here)
+    for t in others:
+        if t is not None and t.get_device() not in (here, -1):
+            raise ValueError("tensors on different devices: cuda:%d and %s" % (t.get_device(), x.device))
+
+
 def _tensor_stream(stream, t):
     """_stream(stream), where a tensor on the device says that CUDA is initialised."""
     if stream is None and _raw_stream is not None and _get_device is not None and t.is_cuda:
@@ -308,6 +319,7 @@ def bmlp_quantize_rows(x, q, scale, stream=None):
     torch = _torch or _use_torch()
     shape = n, K = x.shape
     _int32(K)
+    _one_device(x, q, scale)
     px, ldx = _rows(x, shape, "x", x.dtype)
     pq, ldq = _rows(q, shape, "q", torch.int8)
     rc = (_lib or lib()).bmlp_quantize_rows(px, _type(x, _real_types, "x"), ldx, n, K, pq, ldq,
@@ -324,6 +336,7 @@ def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stre
     shape = n, K = x.shape
     _int32(K)
     dtype = x.dtype
+    _one_device(x, gain, q, scale, res, sum_out)
     px, ldx = _rows(x, shape, "x", dtype)
     pr, ldr = (None, 0) if res is None else _rows(res, shape, "res", dtype)
     ps, lds = (None, 0) if sum_out is None else _rows(sum_out, shape, "sum_out", dtype)
@@ -429,6 +442,7 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     shape = n, K = a.shape
     N = w.shape[0]
     _int32(K, N)
+    _one_device(a, w, out, a_scale, w_scale, bias, workspace)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     po, ldo = _rows(out, (n, N), "out", out.dtype)
@@ -451,6 +465,7 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     shape = n, K = a.shape
     N = w.shape[0]
     _int32(K, N)
+    _one_device(a, w, out, threshold, workspace)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():

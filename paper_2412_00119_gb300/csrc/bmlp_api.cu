@@ -192,9 +192,18 @@ void block_tables(double q, int n, unsigned long long* any, unsigned long long* 
 
 double reinforce_q(double p_r, int K) { return p_r * std::sqrt(2.0 / (M_PI * (double)K)); }
 
-// Whether an optional buffer of 2^shift-byte elements is a device buffer, aligned.
+// Whether an optional buffer of 2^shift-byte elements is aligned memory of the current device
+// (another one's would fault in the kernels where the two are not peers).
 bool usable(const void* p, int shift) {
-  return !p || ((reinterpret_cast<uintptr_t>(p) & ((1u << shift) - 1)) == 0 && is_device_ptr(p));
+  if (!p) return true;
+  if ((reinterpret_cast<uintptr_t>(p) & ((1u << shift) - 1)) != 0) return false;
+  cudaPointerAttributes a;
+  int here = 0;
+  if (cudaPointerGetAttributes(&a, p) != cudaSuccess || cudaGetDevice(&here) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  return a.type == cudaMemoryTypeManaged || (a.type == cudaMemoryTypeDevice && a.device == here);
 }
 
 // The checks and the launch that bmlp_quantize_rows and bmlp_norm_quantize share.

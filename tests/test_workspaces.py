@@ -144,6 +144,46 @@ def test_workspace_of_any_layout_is_refused():
             B.bmlp_int8_sign(a, w, words, workspace=ws)
 
 
+def test_tensors_of_another_device_are_refused(dev):
+    """The kernels run on the current device, where another one's memory would be a fault."""
+    i8, f32 = torch.int8, torch.float32
+    reached = []
+    B._lib.bmlp_quantize_rows = B._lib.bmlp_norm_quantize = lambda *a: reached.append(a) or 0
+
+    def quantize(*where):
+        x, q, s = (Tensor(*t, d) for t, d in zip([((4, 8), f32), ((4, 8), i8), ((4,), f32)], where))
+        B.bmlp_quantize_rows(x, q, s)
+
+    def norm(*where):
+        x, g, q, s, r, t = (Tensor(*t, d) for t, d in zip(
+            [((4, 8), f32), ((8,), f32), ((4, 8), i8), ((4,), f32), ((4, 8), f32), ((4, 8), f32)], where))
+        B.bmlp_norm_quantize(x, g, q, s, res=r, sum_out=t)
+
+    def matmul(*where):
+        a, w, o, sa, sw, b, ws = (Tensor(*t, d) for t, d in zip(
+            [((64, 8), i8), ((4, 8), i8), ((64, 4), f32), ((64,), f32), ((4,), f32), ((4,), f32), ((64,), torch.uint8)], where))
+        B.bmlp_int8_matmul(a, w, o, sa, sw, b, workspace=ws)
+
+    def sign(*where):
+        a, w, o, t, ws = (Tensor(*t, d) for t, d in zip(
+            [((64, 8), i8), ((4, 8), i8), ((64, 1), torch.int64), ((4,), torch.int32), ((64,), torch.uint8)], where))
+        B.bmlp_int8_sign(a, w, o, t, workspace=ws)
+
+    for call, count in ((quantize, 3), (norm, 6), (matmul, 7), (sign, 5)):
+        for wrong in range(count):
+            with pytest.raises(ValueError, match="device"):
+                call(*[int(i == wrong) for i in range(count)])
+        with pytest.raises(ValueError, match="device"):
+            call(*[1] * count)
+        assert not reached and not dev.calls
+        dev.device = 1
+        call(*[1] * count)
+        dev.device = 0
+        call(*[0] * count)
+        assert len(reached) + len(dev.calls) == 2
+        del reached[:], dev.calls[:]
+
+
 def test_workspace_in_captures(dev):
     """The address of a captured call's workspace stays in the graph: it has to be a block that
     torch keeps for the graph, or none."""
