@@ -380,22 +380,20 @@ def _on_stream(stream, a):
 
 def _in_graph_pool(block):
     """Whether a block that was allocated in a capture stays the graph's."""
-    cuda = _torch.cuda
-    if cuda.get_allocator_backend() != "native":
-        return True     # (an allocation of the graph's own)
     at = block.data_ptr()
     return any(s["address"] <= at < s["address"] + s["total_size"] and tuple(s.get("segment_pool_id", (0, 0))) != (0, 0)
-               for s in cuda.memory_snapshot())
+               for s in _torch.cuda.memory_snapshot())
 
 
 def _block(size, a, stream):
     """A block of the call's stream.  None in a capture that is not torch's own: the block would
-    be given to others while the graph still writes it."""
+    be given to others while the graph still writes it.  None too in a capture with another
+    allocator than torch's native one: what those allocate there is no device memory yet."""
     torch = _torch
     captured = torch.cuda.is_current_stream_capturing()
     with _on_stream(stream, a):
         capturing = torch.cuda.is_current_stream_capturing()
-        if capturing and not captured:
+        if capturing and not (captured and torch.cuda.get_allocator_backend() == "native"):
             return None
         block = torch.empty(size, dtype=torch.uint8, device=a.device)
         return None if capturing and not _in_graph_pool(block) else block

@@ -69,6 +69,7 @@ class Device:
         return t
 
     graph = True                     # captures are torch's own
+    backend = "native"
 
     @contextlib.contextmanager
     def stream(self, s):
@@ -94,7 +95,7 @@ def dev(monkeypatch):
     cuda = types.SimpleNamespace(
         stream=d.stream, Stream=torch.cuda.Stream, ExternalStream=stream, default_stream=lambda device=None: stream(0),
         current_stream=lambda device=None: stream(d.current), is_current_stream_capturing=lambda: d.current in d.capturing,
-        OutOfMemoryError=torch.cuda.OutOfMemoryError, memory_snapshot=d.snapshot, get_allocator_backend=lambda: "native")
+        OutOfMemoryError=torch.cuda.OutOfMemoryError, memory_snapshot=d.snapshot, get_allocator_backend=lambda: d.backend)
     fake = types.SimpleNamespace(cuda=cuda, empty=d.empty, **{t: getattr(torch, t) for t in
                                  ("int8", "uint8", "int32", "int64", "float32", "float16", "bfloat16")})
     library = types.SimpleNamespace(bmlp_int8_workspace=lambda n, K, N: d.size, bmlp_int8_matmul=d.product,
@@ -207,6 +208,9 @@ def test_workspace_in_captures(dev):
         run(stream, {100, 42}, True, True)      # torch's capture, and a stream forked from it
         run(stream, {100, 42}, False, False)    # another runtime's capture
     run(42, {42}, False, False)                 # of a stream that is not the current one
+    dev.backend = "cudaMallocAsync"             # whose blocks are no device memory in a capture
+    for stream in (None, 42):
+        run(stream, {100, 42}, True, False)
 
 
 @gpu
