@@ -386,16 +386,19 @@ def _in_graph_pool(block):
 
 
 def _block(size, a, stream):
-    """A block of the call's stream.  None in a capture that is not torch's own: the block would
-    be given to others while the graph still writes it.  None too in a capture with another
-    allocator than torch's native one: what those allocate there is no device memory yet."""
+    """A block of the call's stream.  None where there is no room for it; in a capture that is
+    not torch's own, whose graph would write it while others have it; and in a capture with
+    another allocator than torch's native one: what those allocate there is no device memory yet."""
     torch = _torch
     captured = torch.cuda.is_current_stream_capturing()
     with _on_stream(stream, a):
         capturing = torch.cuda.is_current_stream_capturing()
         if capturing and not (captured and torch.cuda.get_allocator_backend() == "native"):
             return None
-        block = torch.empty(size, dtype=torch.uint8, device=a.device)
+        try:
+            block = torch.empty(size, dtype=torch.uint8, device=a.device)
+        except torch.cuda.OutOfMemoryError:
+            return None
         return None if capturing and not _in_graph_pool(block) else block
 
 
@@ -420,11 +423,11 @@ def _workspace(L, workspace, n, K, N, a, stream):
         if workspace is not None and workspace.shape[0] >= size:
             return workspace.data_ptr(), size, workspace
         workspace = at[key] = None   # (the smaller one goes back first)
-        workspace = at[key] = torch.empty(size, dtype=torch.uint8, device=a.device)
+        workspace = at[key] = _block(size, a, None)
     else:
         workspace = _block(size, a, stream)
-        if workspace is None:
-            return None, 0, None
+    if workspace is None:
+        return None, 0, None
     return workspace.data_ptr(), size, workspace
 
 
@@ -433,8 +436,8 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     int8) times w (N x K int8) transposed, scaled per row and channel.
     workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: one from
     torch's allocator; up to 64 MB of it stay with the thread for its next call on the
-    stream, until bmlp_release_workspaces; a capture that torch does not make takes none,
-    which is slower: give it one).  expired: bmlp_debug_int8_matmul."""
+    stream, until bmlp_release_workspaces; where there is no room for it, and in a capture
+    that torch does not make, the call runs without, slower).  expired: bmlp_debug_int8_matmul."""
     torch = _torch or _use_torch()
     L = _lib or lib()
     shape = n, K = a.shape

@@ -213,6 +213,51 @@ def test_workspace_in_captures(dev):
         run(stream, {100, 42}, True, False)
 
 
+def test_without_room_for_a_workspace(dev):
+    """The product has kernels that need none; a later call may find room again."""
+    dev.room = SIZE - 1
+    for call in (product, signs):
+        for stream in (None, 42):
+            del dev.calls[:]
+            dev.room = SIZE - 1
+            call(stream=stream)
+            call(stream=stream)
+            assert [c[1:] for c in dev.calls] == [(None, 0)] * 2
+            dev.room = SIZE
+            call(stream=stream)
+            assert dev.calls[2][1] and dev.calls[2][2] == SIZE
+        B.bmlp_release_workspaces()
+
+
+@gpu
+def test_product_without_room_on_the_device():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    torch.cuda.set_device(DEV)
+    n, K, N = 1500, 4096, 4096
+    g = torch.Generator().manual_seed(1)
+    a, w = (torch.randint(-128, 128, s, generator=g).to(torch.int8).to(DEV) for s in ((n, K), (N, K)))
+    S = (a.double() @ w.double().t()).to(torch.int32)
+    out = torch.full((n, N), -3, dtype=torch.int32, device=DEV)
+    B.bmlp_release_workspaces()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    size = B.bmlp_int8_workspace(n, K, N)
+    assert size > 40 << 20          # (more than is left over in a segment of torch's)
+    total = torch.cuda.get_device_properties(DEV).total_memory
+    try:
+        # a limit of torch's own allocator
+        torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (1 << 20)) / total)
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            torch.empty((size,), dtype=torch.uint8, device=DEV)
+        B.bmlp_int8_matmul(a, w, out)
+        B.bmlp_int8_matmul(a, w, out, stream=torch.cuda.Stream())
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    torch.cuda.synchronize()
+    assert torch.equal(out, S)
+
+
 @gpu
 @pytest.mark.parametrize("n,K,N", [(300, 2304, 4000), (100, 4096, 8192), (4000, 1500, 100)])
 def test_captures_by_the_driver(n, K, N):
