@@ -354,6 +354,7 @@ def bmlp_int8_workspace(n, K, N):
 
 
 _KEPT_WORKSPACE = 64 << 20     # bytes of the largest workspace that is kept for the next call
+_KEPT_STREAMS = 4              # of the streams used last
 _kept = threading.local()      # .at[device, stream]: this thread's, in the order of that stream
 
 
@@ -419,10 +420,13 @@ def _workspace(L, workspace, n, K, N, a, stream):
     if keep:
         at = _kept.__dict__.setdefault("at", {})
         key = a.device, _tensor_stream(None, a)
-        workspace = at.get(key)
+        workspace = at.pop(key, None)
         if workspace is not None and workspace.shape[0] >= size:
+            at[key] = workspace      # (the last in the order of use)
             return workspace.data_ptr(), size, workspace
         workspace = at[key] = None   # (the smaller one goes back first)
+        while len(at) > _KEPT_STREAMS:
+            del at[next(iter(at))]
         workspace = at[key] = _block(size, a, None)
     else:
         workspace = _block(size, a, stream)
@@ -436,7 +440,7 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     int8) times w (N x K int8) transposed, scaled per row and channel.
     workspace: a device tensor of bmlp_int8_workspace(n, K, N) bytes (None: one from
     torch's allocator; up to 64 MB of it stay with the thread for its next call on the
-    stream, until bmlp_release_workspaces; where there is no room for it, and in a capture
+    stream, for the four streams used last, until bmlp_release_workspaces; where there is no room for it, and in a capture
     that torch does not make, the call runs without, slower).  expired: bmlp_debug_int8_matmul."""
     torch = _torch or _use_torch()
     L = _lib or lib()

@@ -5,6 +5,7 @@ The rules are tested without a GPU on a recording stand-in for torch's allocator
 for the library; what they are for, memory that other work still uses, on the GPU."""
 import contextlib
 import types
+import weakref
 
 import pytest
 import torch
@@ -58,6 +59,7 @@ class Device:
         self.calls = []              # (stream, workspace, bytes) of every product
         self.room = 1 << 40
         self.size = SIZE             # that the library asks for
+        self.live = weakref.WeakSet()
         self.pools = {}              # block -> id of the pool it lies in
 
     def empty(self, size, dtype, device):
@@ -65,6 +67,7 @@ class Device:
             raise torch.cuda.OutOfMemoryError("no room")
         self.allocated.append((self.current, size))
         t = Tensor((size,), dtype, torch.device(device).index or 0, ptr=1 << 20 | len(self.allocated) << 8)
+        self.live.add(t)
         self.pools[t.ptr] = (0, 1) if self.current in self.capturing and self.graph else (0, 0)
         return t
 
@@ -211,6 +214,34 @@ def test_workspace_in_captures(dev):
     dev.backend = "cudaMallocAsync"             # whose blocks are no device memory in a capture
     for stream in (None, 42):
         run(stream, {100, 42}, True, False)
+
+
+def test_workspaces_kept_for_few_streams(dev):
+    """What stays with the thread is bounded, however many streams it uses; the last used stay."""
+    for stream in range(200, 230):
+        dev.current = stream
+        for _ in range(3):
+            product()
+        assert len(dev.live) <= 4
+    assert len(dev.allocated) == 30
+    for stream in (226, 227, 228, 229, 226, 227):
+        dev.current = stream
+        product()
+    assert len(dev.allocated) == 30
+    dev.current = 230                # takes the place of the one unused the longest
+    product()
+    dev.current = 226
+    product()
+    assert len(dev.allocated) == 31
+    dev.current = 228
+    product()
+    assert len(dev.allocated) == 32 and len(dev.live) == 4
+    dev.size = 2 * SIZE              # a larger one takes a smaller one's place
+    product()
+    product()
+    assert len(dev.allocated) == 33 and len(dev.live) == 4
+    B.bmlp_release_workspaces()
+    assert len(dev.live) == 0
 
 
 def test_without_room_for_a_workspace(dev):
