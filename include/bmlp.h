@@ -269,7 +269,9 @@ int bmlp_quantize_rows(const void* x, int32_t x_type, int64_t ldx, int64_t n, in
  * scale = 0; a row whose A or sum of squares is not finite: q = 0, scale = NaN.
  *   x, res, sum_out: n x K of x_type, row strides ldx, ldr, lds; res and sum_out
  *     may be NULL.  sum_out may be x or res itself (same pointer and stride).
- *   gain: K values of x_type, or NULL (1).  eps >= 0 and finite.
+ *   gain: K values of x_type, or NULL (1).  eps >= 0 and finite (below 2^-80, where a
+ *     row's squares may be too small for fp32 beside it, fp32 and bf16 rows take a
+ *     slower kernel).
  *   q: n x K, row stride ldq.  scale: n. */
 int bmlp_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr, const void* gain,
                        int32_t x_type, int64_t n, int32_t K, float eps, void* sum_out, int64_t lds,

@@ -14,7 +14,8 @@
 // registers, so memory is read and written once.  Vectors of 16 bytes where the rows
 // of every buffer allow them, else of 4 bytes or single values.  Bound: memory.
 //
-// k_quantize_long: rows too long for that, read twice.
+// k_quantize_long: rows too long for that, read twice.  Also rows of any length where eps
+// does not hold up squares that leave fp32 (kSmallEps).
 #include <algorithm>
 #include <type_traits>
 
@@ -39,11 +40,19 @@ template <> __device__ __forceinline__ float from_f32(float v) { return v; }
 template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
 
-// The row's code factor and scale from the bits of A and (norm) its sum of squares.
+// Below this eps (2^-80) a row's scale may hang on squares that are lost in fp32, those of
+// |h| < 2^-63.  Such rows have a sum below kSmallSum (2^-90: what a greater one has lost is
+// less than 2^-60 of it for each value), every |h| below 2^-45, and squares of h kUp (2^85)
+// that are inside fp32's range down to its least subnormal.
+constexpr float kSmallEps = 8.27180613e-25f, kSmallSum = 8.07793566e-28f;
+constexpr float kUpA = 4398046511104.0f, kUpB = 2.0f * kUpA, kUp = kUpA * kUpB;   // 2^42, 2^43
+
+// The row's code factor and scale from the bits of A and (norm) its sum of squares; small: of
+// squares of h kUp.
 struct RowScale {
   float inv, scale;
 };
-__device__ __forceinline__ RowScale row_scale(uint32_t abits, float sumsq, int K, float eps, bool norm) {
+__device__ __forceinline__ RowScale row_scale(uint32_t abits, float sumsq, int K, float eps, bool norm, bool small = false) {
   RowScale r = {0.0f, __uint_as_float(0x7FFFFFFFu)};
   if (abits >= kInfBits || (norm && !(sumsq < __uint_as_float(kInfBits)))) return r;
   const float A = __uint_as_float(abits);
@@ -51,7 +60,10 @@ __device__ __forceinline__ RowScale row_scale(uint32_t abits, float sumsq, int K
   if (A < kLeast) return r;
   r.inv = 127.0f / A;
   r.scale = A / 127.0f;
-  if (norm) r.scale = __fmul_rn(r.scale, 1.0f / sqrtf(__fadd_rn(sumsq / (float)K, eps)));
+  if (norm) {
+    const float rstd = 1.0f / sqrtf(__fadd_rn(sumsq / (float)K, small ? eps * kUp * kUp : eps));
+    r.scale = small ? (r.scale * kUpA) * (rstd * kUpB) : __fmul_rn(r.scale, rstd);
+  }
   return r;
 }
 
@@ -365,36 +377,45 @@ __global__ void __launch_bounds__(kWarpRow ? 32 * kRowsPerCta : 1024, (least_cta
 
 constexpr int kThreads = 1024;
 
-template <typename T, int kMode>
+// A CTA per row; a warp where rows are short (only with kSmall: 60,000 x 784 fp32 83 us, by CTAs 574;
+// in registers, at other eps, 38.  The two sums there cost every call 6%, at any eps).
+// kSmall: eps < kSmallEps.
+template <typename T, int kMode, bool kSmall, bool kWarpRow>
 __global__ void __launch_bounds__(kThreads) k_quantize_long(const QuantArgs A) {
   constexpr bool kNorm = kMode != kPlain;
+  constexpr uint32_t kStep = kWarpRow ? 32 : kThreads;
   pdl_wait();
   pdl_trigger();
   const T* gain = static_cast<const T*>(A.gain);
-  const int64_t row = blockIdx.x;
+  const uint32_t tid = threadIdx.x % kStep;
+  const int64_t row = kWarpRow ? (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
+  if (kWarpRow && row >= A.n) return;
   const T* x = static_cast<const T*>(A.x) + row * A.ldx;
   const T* res = kNorm && A.res ? static_cast<const T*>(A.res) + row * A.ldr : nullptr;
   T* sum = kNorm && A.sum ? static_cast<T*>(A.sum) + row * A.lds : nullptr;
   auto h_of = [&](uint32_t i) { return res ? __fadd_rn(to_f32(x[i]), to_f32(res[i])) : to_f32(x[i]); };
   auto u_of = [&](float h, uint32_t i) { return kNorm && gain ? __fmul_rn(h, to_f32(gain[i])) : h; };
-  float sq = 0.0f, most = 0.0f;
-  for (uint32_t i = threadIdx.x; i < (uint32_t)A.K; i += kThreads) {
+  float sq = 0.0f, sq_up = 0.0f, most = 0.0f;
+  for (uint32_t i = tid; i < (uint32_t)A.K; i += kStep) {
     const float h = h_of(i);
     sq += h * h;
+    if (kSmall) sq_up += (h * kUp) * (h * kUp);
     most = max_nan(most, u_of(h, i));
   }
   uint32_t mbits = __float_as_uint(most);
-  row_reduce<false>(sq, mbits, kNorm, 0);
-  const RowScale r = row_scale(mbits, sq, A.K, A.eps, kNorm);
+  row_reduce<kWarpRow>(sq, mbits, kNorm, 0);
+  const bool small = kSmall && sq < kSmallSum;
+  if (kSmall) row_reduce<kWarpRow>(sq_up, mbits, kNorm, 1);
+  const RowScale r = row_scale(mbits, small ? sq_up : sq, A.K, A.eps, kNorm, small);
   const uint32_t live = r.inv == 0.0f ? 0u : 0xFFFFFFFFu;
   // the row's values again: a thread writes its own elements of sum_out only after
   // it has read them (sum_out may be x or res)
-  for (uint32_t i = threadIdx.x; i < (uint32_t)A.K; i += kThreads) {
+  for (uint32_t i = tid; i < (uint32_t)A.K; i += kStep) {
     const float h = h_of(i);
     if (sum) sum[i] = from_f32<T>(h);
     A.q[row * A.ldq + i] = (int8_t)(code(u_of(h, i), r.inv) & live);
   }
-  if (threadIdx.x == 0) A.scale[row] = r.scale;
+  if (tid == 0) A.scale[row] = r.scale;
 }
 
 // A warp per row.  With 32 values per lane whole rows run faster from more warps than with the next
@@ -444,7 +465,7 @@ cudaError_t launch_v(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
   }
   if (vecs <= 32 * kWarpMost) return launch_warp_rows<T, kMode, V, kWarpMost, kApart, kWhole>(A, apart_sum, st);
   if (vecs > 4096)
-    return launch_kernel(k_quantize_long<T, kMode>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
+    return launch_kernel(k_quantize_long<T, kMode, false, false>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
   const bool few = A.n <= 2 * sm_count();
   if (vecs > 2048 || (!few && (V <= 2 || kMode == kPlain))) return launch_cta_rows<T, kMode, V, 4, kApart, kWhole>(A, apart_sum, st);
   if (vecs > 1024 || !few) return launch_cta_rows<T, kMode, V, 2, kApart, kWhole>(A, apart_sum, st);
@@ -458,6 +479,14 @@ cudaError_t launch_v(const QuantArgs& A, bool apart_sum, cudaStream_t st) {
 template <typename T, int kMode>
 cudaError_t launch_type(const QuantArgs& A, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
+  // (the squares of fp16 values do not leave fp32)
+  if constexpr (kMode != kPlain && !std::is_same<T, __half>::value)
+    if (A.eps < kSmallEps) {
+      constexpr int kEach = kThreads / 32;
+      if (A.K > 2048) return launch_kernel(k_quantize_long<T, kMode, true, false>, dim3((unsigned)A.n), dim3(kThreads), 0, st, true, A);
+      return launch_kernel(k_quantize_long<T, kMode, true, true>, dim3((unsigned)((A.n + kEach - 1) / kEach)), dim3(kThreads), 0, st,
+                           true, A);
+    }
   const bool many = A.n > 1;
   auto place = [&](const void* p, int64_t ld) {   // of a buffer's first rows, in 16 bytes
     return (reinterpret_cast<uintptr_t>(p) & 15) | (many ? (uintptr_t)(ld * (int64_t)sizeof(T)) & 15 : 0) << 4;

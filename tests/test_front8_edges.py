@@ -39,3 +39,52 @@ def test_sizes_past_31_bits_are_refused():
         assert B.bmlp_int8_workspace(300, big, 4000) == 0
         assert B.bmlp_int8_workspace(300, 2304, big) == 0
     assert B.bmlp_int8_workspace(300, 2 - 2 ** 32, 4000) == 0
+
+
+# -- rows whose squares leave fp32 -----------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("K", [1, 7, 64, 257, 784, 4096, 8191, 40000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
+def test_norm_of_small_rows_at_small_eps(K, dtype):
+    """The scale of rows down to the type's least values, where eps does not hold their mean
+    square up: finite, and as the formula in 64 bits has it."""
+    sizes = [1.0, 1e-5, 1e-12, 1e-14, 1e-18, 3e-20, 1e-21, 1e-23, 1e-25, 1e-30, 1e-35, 1e-37, 1e-42, 0.0]
+    if dtype == torch.float16:
+        sizes = [1.0, 1e-3, 1e-6, 6e-8, 0.0]
+    n = len(sizes)
+    g = torch.Generator().manual_seed(K)
+    size = torch.tensor(sizes, dtype=torch.float64)[:, None]
+    x = (torch.randn((n, K), generator=g, dtype=torch.float64) * size).to(dtype)
+    res = (torch.randn((n, K), generator=g, dtype=torch.float64) * size).to(dtype)
+    x[:, 0] = size[:, 0].to(dtype)      # (no row of a size is 0)
+    res[:, 0] = 0
+    for gain_size in (None, 1.0, 1e20):
+        if gain_size == 1e20 and dtype == torch.float16:
+            continue
+        gain = None if gain_size is None else ((1 + 0.3 * torch.rand((K,), generator=g)) * gain_size).to(dtype)
+        for eps in (0.0, 1e-45, 1e-38, 1e-30, 7e-25, 9e-25, 1e-12):
+            for use_res, place in ((False, None), (True, None), (True, "x"), (True, "res"), (False, "x")):
+                xd, rd = x.to(DEV), res.to(DEV) if use_res else None
+                q = torch.full((n, K), 99, dtype=torch.int8, device=DEV)
+                scale = torch.full((n,), -1.0, device=DEV)
+                out = {"x": xd, "res": rd, None: None}[place]
+                B.bmlp_norm_quantize(xd, None if gain is None else gain.to(DEV), q, scale, res=rd, sum_out=out, eps=eps)
+                h = x.float() + res.float() if use_res else x.float()
+                u = h if gain is None else h * gain.float()
+                A = u.abs().amax(1)
+                coded = A >= 127 * 2.0 ** -126
+                inv = torch.full_like(A, 127.0) / torch.where(coded, A, 1)
+                want_q = torch.round(torch.where(coded[:, None], u * inv[:, None], 0)).to(torch.int8)
+                assert torch.equal(q.cpu(), want_q)
+                if place:
+                    assert torch.equal(out.cpu(), h.to(dtype))
+                # h and A as they are in fp32, everything after them in 64 bits, with eps as the call has it
+                eps32 = torch.tensor(eps, dtype=torch.float32).double()
+                want = torch.where(coded, A.double() / 127 / torch.sqrt(h.double().square().mean(1) + eps32), 0)
+                # roundings: A / 127, mean, eps, the addition, root, 1 / it, product; h^2 and its sum of at
+                # most K / 256 + 16 additions in sequence, halved by the root; a subnormal result's last place
+                tol = (8 + (K / 256 + 20) / 2) * 2.0 ** -24 * want + 2.0 ** -149
+                got = scale.cpu().double()
+                assert torch.isfinite(got).all(), (eps, gain_size, got)
+                assert ((got - want).abs() <= tol).all(), (eps, gain_size, got, want)
