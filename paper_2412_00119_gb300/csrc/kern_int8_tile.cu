@@ -718,26 +718,27 @@ int int8_tile_split(int64_t tiles, int K, int nt, bool swap) {
 }
 
 cudaError_t launch_int8_tile(const Int8Args& all, void* workspace, cudaStream_t st, int expire, int nt, bool swap) {
-  Int8Args A = all;
-  A.n = std::min<int64_t>(all.n, kTileSlab);
-  if (swap) {
-    A.n = all.N;
-    A.N = (int32_t)all.n;
-    std::swap(A.a, A.w);
-    std::swap(A.lda, A.ldw);
-    std::swap(A.a_scale, A.w_scale);
-    A.swapped = 1;
-  }
-  const int split = int8_tile_split((int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt), A.K, nt, swap);
-  if (workspace) {
-    const cudaError_t e = launch_int8_expand_rows(A, workspace, st);
+  const int64_t slab = swap ? all.n : kTileSlab;
+  for (int64_t off = 0; off < all.n; off += slab) {
+    Int8Args A = off ? rest_of(all, off) : all;
+    A.n = std::min(A.n, slab);
+    if (swap) {
+      A.n = all.N;
+      A.N = (int32_t)all.n;
+      std::swap(A.a, A.w);
+      std::swap(A.lda, A.ldw);
+      std::swap(A.a_scale, A.w_scale);
+      A.swapped = 1;
+    }
+    const int split = int8_tile_split((int64_t)((A.N + CM - 1) / CM) * ((A.n + nt - 1) / nt), A.K, nt, swap);
+    cudaError_t e = cudaSuccess;
+    if (workspace && (e = launch_int8_expand_rows(A, workspace, st)) != cudaSuccess) return e;
+    const uint8_t* ablocks = static_cast<const uint8_t*>(workspace);
+    const bool wide = operand_align_w(A) == 16 && (workspace || operand_align(A) == 16);
+    e = wide ? launch_rows<16>(A, ablocks, nt, split, expire, st) : launch_rows<1>(A, ablocks, nt, split, expire, st);
     if (e != cudaSuccess) return e;
   }
-  const uint8_t* ablocks = static_cast<const uint8_t*>(workspace);
-  const bool wide = operand_align_w(A) == 16 && (workspace || operand_align(A) == 16);
-  const cudaError_t e = wide ? launch_rows<16>(A, ablocks, nt, split, expire, st) : launch_rows<1>(A, ablocks, nt, split, expire, st);
-  if (e != cudaSuccess || swap || all.n <= kTileSlab) return e;
-  return launch_int8_tile(rest_of(all, kTileSlab), workspace, st, expire, nt, false);
+  return cudaSuccess;
 }
 
 }  // namespace bk

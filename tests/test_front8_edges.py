@@ -1,6 +1,8 @@
 """The 8-bit front end past the sizes of its other tests: rows and channels that leave 31
 bits or a slab, second turns of persistent kernels, rows whose squares leave fp32, and
 tensors that do not belong to the call."""
+import threading
+
 import pytest
 import torch
 
@@ -39,6 +41,55 @@ def test_sizes_past_31_bits_are_refused():
         assert B.bmlp_int8_workspace(300, big, 4000) == 0
         assert B.bmlp_int8_workspace(300, 2304, big) == 0
     assert B.bmlp_int8_workspace(300, 2 - 2 ** 32, 4000) == 0
+
+
+# -- many rows -------------------------------------------------------------------------
+
+def few_workspaces(n, K, N):
+    """A workspace as the size wants it, and one that is too small for any."""
+    size = B.bmlp_int8_workspace(n, K, N)
+    assert size > 16
+    return torch.empty((size,), dtype=torch.uint8, device=DEV), torch.empty((16,), dtype=torch.uint8, device=DEV)
+
+
+@gpu
+def test_rows_of_thousands_of_slabs():
+    """157 M rows without a workspace, 2,400 launches, from a thread with a small stack: the host
+    side needs no more of it than for one."""
+    n, N = 65536 * 2400 + 77, 130
+    g = torch.Generator(device=DEV).manual_seed(1)
+    a = torch.randint(-128, 128, (n, 1), generator=g, device=DEV).to(torch.int8)
+    w = torch.randint(-128, 128, (N, 1), generator=g, device=DEV).to(torch.int8)
+    thr = torch.randint(-9000, 9000, (N,), generator=g, device=DEV, dtype=torch.int32)
+    out = torch.full((n, 3), -1, dtype=torch.int64, device=DEV)
+    _, small = few_workspaces(n, 1, N)
+    torch.cuda.synchronize()
+    failed = []
+
+    def call():
+        try:
+            B.bmlp_int8_sign(a, w, out, thr, workspace=small)
+            torch.cuda.synchronize()
+        except Exception as e:      # (to be raised below)
+            failed.append(e)
+
+    B.bmlp_int8_sign(a[:70000], w, out[:70000], thr, workspace=small)
+    before = threading.stack_size(512 * 1024)
+    try:
+        t = threading.Thread(target=call)
+        t.start()
+        t.join()
+    finally:
+        threading.stack_size(before)
+    assert not failed, failed
+    # the words of each of the 256 codes
+    values = torch.arange(-128, 128, device=DEV)
+    bits = torch.zeros((256, 192), dtype=torch.bool, device=DEV)
+    bits[:, :N] = values[:, None] * w[:, 0].long() >= thr.long()
+    table = (bits.view(256, 3, 64).long() << torch.arange(64, device=DEV)).sum(2)
+    for first in range(0, n, 1 << 24):
+        rows = slice(first, min(n, first + (1 << 24)))
+        assert torch.equal(out[rows], table[a[rows, 0].long() + 128])
 
 
 # -- rows whose squares leave fp32 -----------------------------------------------------
