@@ -6,7 +6,9 @@ import threading
 import pytest
 import torch
 
+import workloads as W
 from paper_2412_00119_gb300 import bmlp as B
+from test_front8 import TYPES, check_codes, codes, hidden, plain_codes, rows
 
 DEV = "cuda:0"
 gpu = pytest.mark.gpu
@@ -50,6 +52,98 @@ def few_workspaces(n, K, N):
     size = B.bmlp_int8_workspace(n, K, N)
     assert size > 16
     return torch.empty((size,), dtype=torch.uint8, device=DEV), torch.empty((16,), dtype=torch.uint8, device=DEV)
+
+
+# (n, K, N): the pairs of both operands' blocks, whose rows come in slabs of 65,536: two and
+# three slabs, the last of one row and of some; one chunk of K and two
+SLABS = [(65537, 64, 700), (65536 + 300, 1100, 515), (131100, 200, 515), (131073, 64, 1024), (196608, 40, 300)]
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N", SLABS)
+def test_rows_past_a_slab(n, K, N):
+    """Every output type and the signs, in rows at even and odd places, with the workspace of the
+    pairs and with none, which leaves the tiles' slabs."""
+    a, w = codes(n, K, n, "ends").to(DEV), codes(N, K, K).to(DEV)
+    whole, small = few_workspaces(n, K, N)
+    assert whole.numel() == 128 * ((K + 63) // 64) * ((N + 255) // 256 * 256 + 65536)   # (the pairs')
+    S = a.double() @ w.double().t()
+    g = torch.Generator(device=DEV).manual_seed(5)
+    # scales of two rows a slab apart differ, as do biases and thresholds of channels
+    sa = torch.exp(torch.randn((n,), generator=g, device=DEV)) / 100
+    sw = torch.exp(torch.randn((N,), generator=g, device=DEV)) / 100
+    bias = torch.randn((N,), generator=g, device=DEV) * 10
+    thr = torch.randint(-3000, 3000, (N,), generator=g, device=DEV, dtype=torch.int32)
+    y = S.float() * sa[:, None] * sw + bias
+    bits = torch.zeros((n, 64 * W.words(N)), dtype=torch.bool, device=DEV)
+    bits[:, :N] = S >= thr.double()
+    words = (bits.view(n, -1, 64).long() << torch.arange(64, device=DEV)).sum(2)
+    for pad in (0, 3):
+        _, ad = rows(n, K, torch.int8, pad, pad, fill=-77)
+        ad.copy_(a)
+        for ws in (whole, small):
+            whole.fill_(0x7F)
+            for dtype in [torch.int32] + TYPES:
+                buf, out = rows(n, N, dtype, pad, pad, fill=-5)
+                if dtype == torch.int32:
+                    B.bmlp_int8_matmul(ad, w, out, workspace=ws)
+                    assert torch.equal(out.double(), S), (pad, ws.numel())
+                else:
+                    B.bmlp_int8_matmul(ad, w, out, sa, sw, bias, workspace=ws)
+                    assert torch.equal(out, y.to(dtype)), (pad, ws.numel(), dtype)
+                assert (buf[:pad] == -5).all() and (buf[pad + n * (N + pad):] == -5).all()
+                if pad:
+                    assert (buf[pad:pad + n * (N + pad)].view(n, -1)[:, N:] == -5).all()
+            got = torch.full((n, W.words(N)), -1, dtype=torch.int64, device=DEV)
+            B.bmlp_int8_sign(ad, w, got, thr, workspace=ws)
+            assert torch.equal(got, words), (pad, ws.numel())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,K", [(20011, 40), (20011, 100), (10007, 255), (20011, 784), (10007, 785), (10007, 1001), (1500, 4096),
+                                 (1500, 4095), (1500, 8184)])
+def test_norm_of_rows_past_a_turn(n, K, dtype):
+    """More rows than the kernel's warps or CTAs take at once: those that follow, with the rows loaded
+    ahead of an in-place sum and the places that rows keep from turn to turn."""
+    x, res = hidden(n, K, n + K, dtype), hidden(n, K, n + 5 * K, dtype)
+    gain = (1 + 0.3 * torch.randn(K, generator=torch.Generator().manual_seed(K))).to(dtype)
+    for use_res in (False, True):
+        r = res if use_res else None
+        for use_gain in (False, True):
+            gn = gain if use_gain else None
+            h, want = plain_codes(x, r, gn)
+            # (pad and start of the inputs, of the sums; in place)
+            for pad, off, spad, soff, place in [(0, 0, 0, 0, None), (0, 0, 0, 0, "x"), (0, 0, 0, 0, "res"), (3, 1, 0, 0, None),
+                                                (3, 1, 0, 0, "x"), (1, 0, 1, 0, "res"), (0, 0, 5, 3, None), (7, 2, 2, 1, None)]:
+                if place == "res" and not use_res:
+                    continue
+                xd, rd = rows(n, K, dtype, pad, off)[1], rows(n, K, dtype, pad, off)[1]
+                sb, sd = rows(n, K, dtype, spad, soff, fill=7)
+                qb, qd = rows(n, K, torch.int8, spad, soff, fill=99)
+                xd.copy_(x)
+                rd.copy_(res)
+                scale = torch.full((n,), -1.0, device=DEV)
+                out = {"x": xd, "res": rd, None: sd}[place]
+                B.bmlp_norm_quantize(xd, None if gn is None else gn.to(DEV), qd, scale, res=rd if use_res else None, sum_out=out,
+                                     eps=1e-6)
+                assert torch.equal(qd.cpu(), want), (use_res, use_gain, pad, place)
+                assert torch.equal(out.cpu(), h.to(dtype)), (use_res, use_gain, pad, place)
+                assert (qb[:soff] == 99).all() and (qb[soff + n * (K + spad):] == 99).all()
+                if place is None:
+                    assert (sb[:soff] == 7).all() and (sb[soff + n * (K + spad):] == 7).all()
+                    if spad:
+                        assert (sb[soff:soff + n * (K + spad)].view(n, -1)[:, K:] == 7).all()
+            check_codes(qd.cpu(), scale.cpu(), x, r, gn, True, K)
+    want = plain_codes(x)[1]
+    for pad, off in [(0, 0), (3, 1)]:
+        xd = rows(n, K, dtype, pad, off)[1]
+        xd.copy_(x)
+        _, qd = rows(n, K, torch.int8, pad, off, fill=99)
+        scale = torch.full((n,), -1.0, device=DEV)
+        B.bmlp_quantize_rows(xd, qd, scale)
+        assert torch.equal(qd.cpu(), want)
+        check_codes(qd.cpu(), scale.cpu(), x, None, None, False, K)
 
 
 @gpu
