@@ -309,6 +309,12 @@ int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, c
                    int64_t n, int32_t K, int32_t N, uint64_t* out, void* workspace, int64_t workspace_bytes,
                    void* cuda_stream);
 
+/* bmlp_int8_sign with the path of an expired device-side wait forced, as
+ * bmlp_debug_int8_matmul, for tests. */
+int bmlp_debug_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
+                         int64_t n, int32_t K, int32_t N, uint64_t* out, void* workspace, int64_t workspace_bytes,
+                         void* cuda_stream);
+
 /* Workspace with which bmlp_int8_matmul and bmlp_int8_sign run fastest for this
  * size, in bytes: 0 for few rows, else room for both operands in fp16 (rows in
  * slabs, so it does not grow past 65,536 of them).  The two calls take a device

@@ -100,6 +100,8 @@ SIGNATURES = [
                                    _vp, C.c_int32, C.c_int64, _vp, C.c_int64, _vp]),
     ("bmlp_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp,
                                  C.c_int64, _vp]),
+    ("bmlp_debug_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp,
+                                       C.c_int64, _vp]),
     ("bmlp_int8_workspace", C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
     ("bmlp_layer_forward_engine", C.c_int, [_vp, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp]),
 ]
@@ -461,10 +463,10 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
         _check(rc)
 
 
-def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
+def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None, expired=False):
     """Packed +-1 words (n x ceil(N/64) int64) of a (n x K int8) times w (N x K
     int8) transposed against threshold (N int32; None: 0).  workspace: as for
-    bmlp_int8_matmul."""
+    bmlp_int8_matmul.  expired: bmlp_debug_int8_sign."""
     torch = _torch or _use_torch()
     L = _lib or lib()
     shape = n, K = a.shape
@@ -476,8 +478,9 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None):
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():
         raise ValueError("out: expected %d x %d contiguous 64-bit words" % (n, (N + 63) // 64))
     ws, wsb, owner = _workspace(L, workspace, n, K, N, a, stream) if n > 32 or workspace is not None else (None, 0, None)
-    rc = L.bmlp_int8_sign(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
-                          out.data_ptr(), ws, wsb, _tensor_stream(stream, a))
+    call = L.bmlp_debug_int8_sign if expired else L.bmlp_int8_sign
+    rc = call(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
+              out.data_ptr(), ws, wsb, _tensor_stream(stream, a))
     if rc:
         _check(rc)
 

@@ -1035,6 +1035,14 @@ int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, c
   return int8_call("bmlp_int8_sign", A, workspace, workspace_bytes, cuda_stream);
 }
 
+int bmlp_debug_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,
+                         int64_t n, int32_t K, int32_t N, uint64_t* out, void* workspace, int64_t workspace_bytes,
+                         void* cuda_stream) {
+  TraceRange trace("bmlp_int8_sign");
+  const Int8Args A = {a, w, nullptr, nullptr, nullptr, threshold, nullptr, out, lda, ldw, 0, n, K, N, BMLP_I32};
+  return int8_call("bmlp_debug_int8_sign", A, workspace, workspace_bytes, cuda_stream, 1);
+}
+
 int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N) {
   return n < 1 || K < 1 || K > BMLP_INT8_MAX_K || N < 1 || N > (1 << 30) ? 0 : int8_workspace(n, K, N);
 }

@@ -100,6 +100,26 @@ def test_rows_past_a_slab(n, K, N):
 
 
 @gpu
+@pytest.mark.parametrize("n,K,N", [(12, 200, 300), (20, 2048, 300), (33, 1000, 100), (50, 4096, 4000), (100, 2048, 4096),
+                                   (300, 3000, 2000), (1500, 1024, 8130), (1500, 1030, 4001), (4000, 1500, 50), (4000, 3000, 120),
+                                   (1000, 64, 20)])
+def test_signs_after_expired_waits(n, K, N):
+    """With every CTA's wait taken as expired the words are whole, their pad bits zero; with a
+    workspace and without one that suffices."""
+    a, w = codes(n, K, n, "ends").to(DEV), codes(N, K, K).to(DEV)
+    S = a.double() @ w.double().t()
+    for thr in (None, S[0].to(torch.int32)):
+        bits = torch.zeros((n, 64 * W.words(N)), dtype=torch.bool, device=DEV)
+        bits[:, :N] = S >= (0 if thr is None else thr.double())
+        want = (bits.view(n, -1, 64).long() << torch.arange(64, device=DEV)).sum(2)
+        for ws in (None, torch.empty(16, dtype=torch.uint8, device=DEV)):
+            for expired in (True, False):      # (and the device is as it was)
+                out = torch.full((n, W.words(N)), -1, dtype=torch.int64, device=DEV)
+                B.bmlp_int8_sign(a, w, out, thr, workspace=ws, expired=expired)
+                assert torch.equal(out, want), (ws is None, expired)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("n,K", [(20011, 40), (20011, 100), (10007, 255), (20011, 784), (10007, 785), (10007, 1001), (1500, 4096),
                                  (1500, 4095), (1500, 8184)])

@@ -102,7 +102,8 @@ def dev(monkeypatch):
     fake = types.SimpleNamespace(cuda=cuda, empty=d.empty, **{t: getattr(torch, t) for t in
                                  ("int8", "uint8", "int32", "int64", "float32", "float16", "bfloat16")})
     library = types.SimpleNamespace(bmlp_int8_workspace=lambda n, K, N: d.size, bmlp_int8_matmul=d.product,
-                                    bmlp_debug_int8_matmul=d.product, bmlp_int8_sign=d.product)
+                                    bmlp_debug_int8_matmul=d.product, bmlp_int8_sign=d.product,
+                                    bmlp_debug_int8_sign=d.product)
     monkeypatch.setattr(B, "_torch", fake)
     monkeypatch.setattr(B, "_raw_stream", lambda device: d.current)
     monkeypatch.setattr(B, "_get_device", lambda: d.device)
