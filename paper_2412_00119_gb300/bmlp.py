@@ -153,17 +153,19 @@ def _ptr(buf):
 
 # -- tensors of the 8-bit front end (torch is imported when the first one comes) --
 _torch = _raw_stream = _get_device = None
+_devices = 0                          # that torch sees
 _real_types, _out_types = {}, {}      # torch dtype -> BMLP_* type
 
 
 def _use_torch():
-    global _torch, _raw_stream, _get_device
+    global _torch, _raw_stream, _get_device, _devices
     import torch
     _real_types.update({torch.float32: BMLP_F32, torch.float16: BMLP_F16, torch.bfloat16: BMLP_BF16})
     _out_types.update(_real_types)
     _out_types[torch.int32] = BMLP_I32
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _get_device = getattr(torch._C, "_cuda_getDevice", None)
+    _devices = torch.cuda.device_count()
     _torch = torch
     return torch
 
@@ -190,8 +192,7 @@ def _rows(t, shape, what, dtype):
 
 def _int32(K, N=1):
     """ctypes would cut a K or N of more than 32 bits without a word."""
-    if (K | N) >> 31:
-        raise BmlpError(BMLP_EINVAL, "K = %d or N = %d past 31 bits" % (K, N))
+    raise BmlpError(BMLP_EINVAL, "K = %d or N = %d past 31 bits" % (K, N))
 
 
 def _vector(t, n, what, dtype):
@@ -205,8 +206,8 @@ def _vector(t, n, what, dtype):
 
 
 def _one_device(x, *others):
-    """Refuses tensors of another device than the current one, where the kernels run.  (Host
-    memory is the library's to refuse.)"""
+    """Refuses tensors of another device than the current one, where the kernels run.  (The
+    library does too, by its pointers, and refuses host memory.)"""
     here = x.get_device()
     if here >= 0 and here != (_get_device or _torch.cuda.current_device)():
         raise ValueError("tensors on cuda:%d, which is not the current device" % here)
@@ -320,8 +321,10 @@ def bmlp_quantize_rows(x, q, scale, stream=None):
     fp32 / fp16 / bf16, on the device; row strides are kept)."""
     torch = _torch or _use_torch()
     shape = n, K = x.shape
-    _int32(K)
-    _one_device(x, q, scale)
+    if K >> 31:
+        _int32(K)
+    if _devices > 1:
+        _one_device(x, q, scale)
     px, ldx = _rows(x, shape, "x", x.dtype)
     pq, ldq = _rows(q, shape, "q", torch.int8)
     rc = (_lib or lib()).bmlp_quantize_rows(px, _type(x, _real_types, "x"), ldx, n, K, pq, ldq,
@@ -336,9 +339,11 @@ def bmlp_norm_quantize(x, gain, q, scale, res=None, sum_out=None, eps=1e-6, stre
     gain, res, sum_out: x's type, each may be None."""
     torch = _torch or _use_torch()
     shape = n, K = x.shape
-    _int32(K)
+    if K >> 31:
+        _int32(K)
     dtype = x.dtype
-    _one_device(x, gain, q, scale, res, sum_out)
+    if _devices > 1:
+        _one_device(x, gain, q, scale, res, sum_out)
     px, ldx = _rows(x, shape, "x", dtype)
     pr, ldr = (None, 0) if res is None else _rows(res, shape, "res", dtype)
     ps, lds = (None, 0) if sum_out is None else _rows(sum_out, shape, "sum_out", dtype)
@@ -448,8 +453,10 @@ def bmlp_int8_matmul(a, w, out, a_scale=None, w_scale=None, bias=None, stream=No
     L = _lib or lib()
     shape = n, K = a.shape
     N = w.shape[0]
-    _int32(K, N)
-    _one_device(a, w, out, a_scale, w_scale, bias, workspace)
+    if (K | N) >> 31:
+        _int32(K, N)
+    if _devices > 1:
+        _one_device(a, w, out, a_scale, w_scale, bias, workspace)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     po, ldo = _rows(out, (n, N), "out", out.dtype)
@@ -471,8 +478,10 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None, expir
     L = _lib or lib()
     shape = n, K = a.shape
     N = w.shape[0]
-    _int32(K, N)
-    _one_device(a, w, out, threshold, workspace)
+    if (K | N) >> 31:
+        _int32(K, N)
+    if _devices > 1:
+        _one_device(a, w, out, threshold, workspace)
     pa, lda = _rows(a, shape, "a", torch.int8)
     pw, ldw = _rows(w, (N, K), "w", torch.int8)
     if out.shape != (n, (N + 63) // 64) or out.element_size() != 8 or not out.is_contiguous():

@@ -192,14 +192,21 @@ void block_tables(double q, int n, unsigned long long* any, unsigned long long* 
 
 double reinforce_q(double p_r, int K) { return p_r * std::sqrt(2.0 / (M_PI * (double)K)); }
 
-// Whether an optional buffer of 2^shift-byte elements is aligned memory of the current device
-// (another one's would fault in the kernels where the two are not peers).
-bool usable(const void* p, int shift) {
+// The current device; -1: none.
+int current_device() {
+  int here = -1;
+  if (cudaGetDevice(&here) == cudaSuccess) return here;
+  (void)cudaGetLastError();
+  return -1;
+}
+
+// Whether an optional buffer of 2^shift-byte elements is aligned memory of this device (another
+// one's would fault in the kernels where the two are not peers).
+bool usable(const void* p, int shift, int here) {
   if (!p) return true;
   if ((reinterpret_cast<uintptr_t>(p) & ((1u << shift) - 1)) != 0) return false;
   cudaPointerAttributes a;
-  int here = 0;
-  if (cudaPointerGetAttributes(&a, p) != cudaSuccess || cudaGetDevice(&here) != cudaSuccess) {
+  if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
     (void)cudaGetLastError();
     return false;
   }
@@ -216,9 +223,9 @@ int quantize_call(const char* name, const QuantArgs& A, bool norm, void* cuda_st
     return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below K", name);
   if (A.sum && ((A.sum == A.x && A.lds != A.ldx) || (A.sum == A.res && A.lds != A.ldr)) && A.n > 1)
     return fail(nullptr, BMLP_EINVAL, "%s: sum_out in place needs its input's row stride", name);
-  const int shift = A.type == BMLP_F32 ? 2 : 1;
-  if (!A.x || !A.q || !A.scale || !usable(A.x, shift) || !usable(A.res, shift) || !usable(A.gain, shift) ||
-      !usable(A.sum, shift) || !usable(A.q, 0) || !usable(A.scale, 2))
+  const int shift = A.type == BMLP_F32 ? 2 : 1, here = current_device();
+  if (!A.x || !A.q || !A.scale || !usable(A.x, shift, here) || !usable(A.res, shift, here) || !usable(A.gain, shift, here) ||
+      !usable(A.sum, shift, here) || !usable(A.q, 0, here) || !usable(A.scale, 2, here))
     return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
   const cudaError_t e = launch_quantize(A, norm, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
@@ -237,12 +244,12 @@ int int8_call(const char* name, const Int8Args& A, void* workspace, int64_t work
   if (A.n == 0) return BMLP_OK;
   if ((A.n > 1 && (A.lda < A.K || (A.out && A.ldo < A.N))) || (A.N > 1 && A.ldw < A.K))
     return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below its row's length", name);
-  const int shift = A.type == BMLP_F32 || A.type == BMLP_I32 ? 2 : 1;
-  if (!A.a || !A.w || (!A.out && !A.words) || !usable(A.a, 0) || !usable(A.w, 0) || !usable(A.a_scale, 2) ||
-      !usable(A.w_scale, 2) || !usable(A.bias, 2) || !usable(A.thr, 2) || !usable(A.out, shift) ||
-      !usable(A.words, 3))
+  const int shift = A.type == BMLP_F32 || A.type == BMLP_I32 ? 2 : 1, here = current_device();
+  if (!A.a || !A.w || (!A.out && !A.words) || !usable(A.a, 0, here) || !usable(A.w, 0, here) || !usable(A.a_scale, 2, here) ||
+      !usable(A.w_scale, 2, here) || !usable(A.bias, 2, here) || !usable(A.thr, 2, here) || !usable(A.out, shift, here) ||
+      !usable(A.words, 3, here))
     return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
-  if (workspace && (workspace_bytes < 0 || !usable(workspace, 4)))
+  if (workspace && (workspace_bytes < 0 || !usable(workspace, 4, here)))
     return fail(nullptr, BMLP_EINVAL, "%s: the workspace must be a device pointer, 16-byte aligned", name);
   const cudaError_t e = launch_int8(A, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream), expire);
   if (e != cudaSuccess) return cuda_fail(nullptr, e, name);

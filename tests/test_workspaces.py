@@ -107,6 +107,7 @@ def dev(monkeypatch):
     monkeypatch.setattr(B, "_torch", fake)
     monkeypatch.setattr(B, "_raw_stream", lambda device: d.current)
     monkeypatch.setattr(B, "_get_device", lambda: d.device)
+    monkeypatch.setattr(B, "_devices", 2)
     monkeypatch.setattr(B, "_lib", library)
     yield d
     B.bmlp_release_workspaces()
