@@ -302,7 +302,8 @@ int bmlp_debug_int8_matmul(const int8_t* a, int64_t lda, const float* a_scale, c
 
 /* Signs of the same product, packed: bit j of row i is 1 (+1) iff
  * S_ij >= threshold_j (threshold: N int32, or NULL for 0: sign(0) = +1); exact.
- * Scales are positive, so they do not matter here.  out: n rows of ceil(N/64)
+ * Scales are positive, so they do not matter here; a row that was not finite has
+ * codes of 0 and with them sums of 0 (its NaN scale tells it).  out: n rows of ceil(N/64)
  * words, 8-byte aligned, pad bits 0: bmlp_train / bmlp_predict input for
  * K_0 = N. */
 int bmlp_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t ldw, const int32_t* threshold,

@@ -17,10 +17,13 @@ struct Plan {
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Which kernel: the least of the times that lines give each, fitted to measurements of every plan
-// at 290 sizes (the chosen plan's times are 1.2% above the best's in the mean, 67% at worst; some of
-// them below, in us).  Tiles: a launch and what follows the last sum; per k-step of 128 codes; per
+// at 290 sizes; at 290 others the chosen plan's times are 0.8% above the best's in the mean, 27% at
+// worst (some of the first below, in us).  The lines know nothing of what eight CTAs that share K gain and
+// how many clusters run at once (kern_int8_tile.cu): 300 x 16384 -> 384 17.7, 32-row tiles 15.9;
+// 50 x 1243 -> 2331 11.9, 64-row tiles 7.9.  Tiles: a launch and what follows the last sum; per k-step of 128 codes; per
 // further round where there are more tiles than SMs; the tiles' rows made ready.  Rows at odd places:
-// K not a multiple of 16 stands for them (the size of the workspace goes by the sizes alone).
+// K not a multiple of 16 stands for them (the size of the workspace goes by the sizes alone; at 13
+// sizes of whole K in rows at odd places the chosen plan was the best of all).
 //                         32-row tiles  64, ready  128, ready  pairs  swapped 32, 64, 128
 //   200 x 1024 -> 1024 and smaller: 32-row tiles (172 x 208 -> 224 3.6, 5.3, 6.0, 9.7)
 //   46 x 4320 -> 7472             16.6       14.2           -      -

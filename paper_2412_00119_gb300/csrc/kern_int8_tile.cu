@@ -15,7 +15,7 @@
 //   - 16 workers in four groups that take the k-steps (128 codes of every row, or 64) in
 //     turn: a warp copies its rows' codes kDeep turns ahead (asynchronous copies to a ring
 //     of its own: with loads to registers, whose scoreboards are few, 26 us for 32 rows of
-//     8192 -> 8192, now 16.6), turns them into fp16, the weights into tensor memory (a lane per
+//     8192 -> 8192, now 16.7), turns them into fp16, the weights into tensor memory (a lane per
 //     channel) and the activations into shared memory (128B swizzle), and arrives on "full";
 //     between them the workers drain finished chunks;
 //   - one or two warps issue the MMAs (two: of even and odd k-steps, each into accumulators
@@ -708,7 +708,8 @@ cudaError_t launch_rows(const Int8Args& A, const uint8_t* ablocks, int nt, int s
 
 // Up to four: as many as leave every SM at most one, with eight k-steps of 64 each; of swapped
 // operands a thread keeps eight channels (a byte of signs).  Eight for a few tiles (us: 20 rows of
-// 8192 -> 512 6.5, by four 9.2, -> 1536 7.4, 9.3; but 16384 -> 2048, 16 tiles, 19.4, 15.0).
+// 8192 -> 512 6.5, by four 9.2, -> 1536 7.4, 9.3; but 16384 -> 2048, 16 tiles, 19.4, 15.0).  No more than
+// 36 clusters of four run at once: 30 rows of 1243 in 36 tiles 7.1, in 37 or 38 12.7.
 int int8_tile_split(int64_t tiles, int K, int nt, bool swap) {
   const int steps = (K + 63) / 64, most = swap ? nt / 32 : 4;
   int split = 1;
