@@ -18,7 +18,7 @@
 //     even one's barriers (tensor copies of a CTA pair may: forwarding the odd CTA's
 //     completions by a thread there cost 700 clocks of a k-step's round trip);
 //   - on the even CTA one warp issues the MMAs.
-// Measured, both operands' expansion included: 16384 x 8192 -> 8192 1.17 to 1.21 ms = 1,820 to
+// Measured, both operands' expansion included: 16384 x 8192 -> 8192 1.17 to 1.22 ms = 1,800 to
 // 1,880 TFLOP/s, signs of 65536 x 4096 -> 8192 2.21 to 2.27 ms = 1,940 to 1,990 (bf16 by the
 // library 1,946).  Up to K = 1024 the one chunk's sums go from tensor memory to the outputs
 // in fp32 as they are read: 47,880 x 332 -> 14,928 signs 420 us (through int32 registers
