@@ -324,6 +324,109 @@ int bmlp_debug_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t 
  * without it, slower.  Host only; 0 for sizes that the calls refuse. */
 int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit front end (no counterpart in the paper): the real-valued rows
+ * of the 8-bit front end at half the bytes, by the 4-bit kind of the tensor cores.
+ * bmlp_mx4_norm_quantize takes hidden states, bmlp_mx4_quantize a weight matrix or
+ * rows that are normed already, and bmlp_mx4_matmul gives their product (whose
+ * fp32 rows bmlp_binarize_median takes to bmlp_train / bmlp_predict input),
+ * bmlp_mx4_matmul_grouped that with a weight matrix for each group of rows, such as
+ * the tokens of each expert.  bmlp_mx4_dequantize gives the values that codes
+ * stand for.
+ *
+ * Format (the microscaling format MXFP4 of the Open Compute Project): a row of K
+ * values is ceil(K/2) bytes of codes, value 2 i in the low four bits of byte i,
+ * and ceil(K/32) scale bytes, one for each 32 values.  A code is e2m1: bit 3 the
+ * sign, bits 2..0 = 0..7 the size 0, 1/2, 1, 3/2, 2, 3, 4, 6.  Scale byte s is
+ * 2^(s - 127); 255 is NaN, and so is every value and sum that it scales.  For odd K
+ * the high bits of a row's last byte are 0.
+ *
+ * Common to the five: no handle (errors: bmlp_last_error(NULL)); every pointer is
+ * memory of the current device (or managed), caller-owned; asynchronous on
+ * cuda_stream, nothing is allocated and no workspace needed; may be captured.
+ * Row strides are in elements for real values and in bytes for codes and scales,
+ * and at least the row's length where there is more than one row; rows may start
+ * anywhere (codes and scales in rows at multiples of 16 bytes run fastest, as
+ * bmlp_mx4_matmul says).  n in 0..BMLP_MX4_MAX_ROWS, 0 is a no-op.  Outputs may not
+ * overlap inputs except where said.  BMLP_EINVAL for bad arguments, BMLP_ECUDA if a
+ * launch fails.  None has a backward form, as the 8-bit front end.
+ * ------------------------------------------------------------------------- */
+#define BMLP_MX4_MAX_ROWS (1 << 30)
+#define BMLP_MX4_MAX_GROUPS 4096
+
+/* Rows to codes and scales.  Of each 32 values of a row (the last block may have fewer),
+ * with m = max |x_i|:
+ *   s = max(0, floor(log2 m) - 2 + 127),   code_i = e2m1(x_i 2^(127 - s))
+ * where e2m1 rounds to the nearest (ties to the even code) and what is above 6
+ * becomes 6; m = 0 gives s = 0.  A block with an infinity or a NaN: codes 0, s = 255.
+ *   x: n x K of x_type, row stride ldx.  q: n x ceil(K/2), row stride ldq.
+ *   scale: n x ceil(K/32), row stride lds. */
+int bmlp_mx4_quantize(const void* x, int32_t x_type, int64_t ldx, int64_t n, int32_t K, uint8_t* q,
+                      int64_t ldq, uint8_t* scale, int64_t lds, void* cuda_stream);
+
+/* Root-mean-square norm of rows with the residual's addition, to the same codes:
+ *   h = x + res (fp32; h = x where res is NULL),  sum_out = h (rounded to x_type),
+ *   u_i = h_i * gain_i,   codes and scales of u as above,
+ *   row_scale = 1 / sqrt(mean_i h_i^2 + eps)
+ * so h_i row_scale gain_i is about code_i 2^(s - 127) row_scale: the factor that is
+ * common to the row stays outside of the codes (bmlp_mx4_matmul takes it).  Sums are
+ * held in fp32; a row whose sum of squares is not finite: row_scale = NaN; a row of
+ * zeros with eps = 0: row_scale = 0.
+ *   x, res, sum_out: n x K of x_type, row strides ldx, ldr, ldsum; res and sum_out
+ *     may be NULL.  sum_out may be x or res itself (same pointer and stride).
+ *   gain: K values of x_type, or NULL (1).  eps >= 0 and finite.
+ *   q, scale: as for bmlp_mx4_quantize.  row_scale: n. */
+int bmlp_mx4_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr, const void* gain,
+                           int32_t x_type, int64_t n, int32_t K, float eps, void* sum_out, int64_t ldsum,
+                           uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds, float* row_scale,
+                           void* cuda_stream);
+
+/* Values of codes: out = code 2^(s - 127), times row_scale where it is not NULL (fp32, one
+ * rounding), rounded to out_type (without row_scale exact in fp32 and bf16, but for values of 2^128
+ * on, which become infinite).
+ *   q, scale: n rows of K codes and their scales.  row_scale: n, or NULL.
+ *   out: n x K of out_type (BMLP_F32, BMLP_F16 or BMLP_BF16), row stride ldo. */
+int bmlp_mx4_dequantize(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, const float* row_scale,
+                        int64_t n, int32_t K, void* out, int32_t out_type, int64_t ldo, void* cuda_stream);
+
+/* Product of such rows:
+ *   S_ij = sum_b 2^(sa_ib - 127) 2^(sw_jb - 127) sum_{k in block b} a_ik w_jk
+ *   out_ij = S_ij * row_scale_i + bias_j
+ * with sums in fp32, the last two operations rounded one by one, and rounded to out_type.
+ *   a, a_scale: n rows of K codes and their scales, row strides lda and ldas.
+ *   w, w_scale: N rows (channels), row strides ldw and ldws.
+ *   row_scale: n, bias: N (fp32); each may be NULL (1, 0).
+ *   out: n x N of out_type (BMLP_F32, BMLP_F16 or BMLP_BF16), row stride ldo.
+ * K in 1..2^31 - 1, N in 1..2^30; for odd K the unused four bits of a row of a or of w may
+ * be anything if the other's are 0. */
+int bmlp_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas, const float* row_scale,
+                    const uint8_t* w, int64_t ldw, const uint8_t* w_scale, int64_t ldws, const float* bias,
+                    int64_t n, int32_t K, int32_t N, void* out, int32_t out_type, int64_t ldo, void* cuda_stream);
+
+/* The same with E matrices of weights, rows offsets[e] <= i < offsets[e + 1] by the e-th.
+ *   w, w_scale: E groups of N rows, group strides gw and gws (bytes).
+ *   bias: E groups of N, group stride gb (elements), or NULL.
+ *   offsets: E + 1 device integers, 0 <= offsets[0] <= .. <= offsets[E] <= n; read when the
+ *     call runs, so they may be computed on the device.  Groups may be empty.  One that
+ *     decreases or leaves 0..n is taken as the nearest value that does not.
+ * Rows of no group (before offsets[0], from offsets[E] on) are left as they are, and
+ * of their inputs nothing matters.  E in 1..BMLP_MX4_MAX_GROUPS. */
+int bmlp_mx4_matmul_grouped(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                            const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                            const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                            const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                            int32_t out_type, int64_t ldo, void* cuda_stream);
+
+/* bmlp_mx4_matmul_grouped (offsets NULL: bmlp_mx4_matmul, E = 1) with the path of an expired
+ * device-side wait forced, for tests: every CTA of its tensor-core kernels takes one as
+ * expired.  The affected sums are made again on CUDA cores, so the output is whole,
+ * as it is where a bounded wait does expire. */
+int bmlp_debug_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                          const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                          const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                          const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                          int32_t out_type, int64_t ldo, void* cuda_stream);
+
 /* One layer of forward-only evaluation (Sec. 3.1; Alg. 1 l.8-9):
  * a_out = sign(a_in W_l), sign(0) = +1, for n packed rows.  a_in: n rows of
  * ceil(K_{l-1}/64) words (pad bits 0); a_out: n rows of ceil(K_l/64) words,

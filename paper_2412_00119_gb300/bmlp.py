@@ -34,6 +34,8 @@ BMLP_FWD_AUTO, BMLP_FWD_POPC, BMLP_FWD_TCGEN05, BMLP_FWD_B1MMA, BMLP_FWD_S8MMA =
 BMLP_GROUPS_CONTIGUOUS, BMLP_GROUPS_FIXED, BMLP_GROUPS_RESHUFFLED = 0, 1, 2
 BMLP_F32, BMLP_F16, BMLP_BF16, BMLP_I32 = 0, 1, 2, 3
 BMLP_INT8_MAX_K = 131071
+BMLP_MX4_MAX_ROWS = 1 << 30
+BMLP_MX4_MAX_GROUPS = 4096
 PROFILE_KINDS = ("train_forward", "cls_select", "update", "eval_forward", "eval_out", "copy",
                  "r_events")
 
@@ -103,6 +105,20 @@ SIGNATURES = [
     ("bmlp_debug_int8_sign", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp,
                                        C.c_int64, _vp]),
     ("bmlp_int8_workspace", C.c_int64, [C.c_int64, C.c_int32, C.c_int32]),
+    ("bmlp_mx4_quantize", C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int64,
+                                    _vp]),
+    ("bmlp_mx4_norm_quantize", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
+                                         C.c_float, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp]),
+    ("bmlp_mx4_dequantize", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int32, _vp, C.c_int32,
+                                      C.c_int64, _vp]),
+    ("bmlp_mx4_matmul", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, C.c_int64, _vp,
+                                  C.c_int64, C.c_int32, C.c_int32, _vp, C.c_int32, C.c_int64, _vp]),
+    ("bmlp_mx4_matmul_grouped", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, _vp,
+                                          C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
+                                          C.c_int32, _vp, C.c_int32, C.c_int64, _vp]),
+    ("bmlp_debug_mx4_matmul", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, _vp,
+                                        C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
+                                        C.c_int32, _vp, C.c_int32, C.c_int64, _vp]),
     ("bmlp_layer_forward_engine", C.c_int, [_vp, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp]),
 ]
 
@@ -490,6 +506,148 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None, expir
     call = L.bmlp_debug_int8_sign if expired else L.bmlp_int8_sign
     rc = call(pa, lda, pw, ldw, _vector(threshold, N, "threshold", torch.int32), n, K, N,
               out.data_ptr(), ws, wsb, _tensor_stream(stream, a))
+    if rc:
+        _check(rc)
+
+
+# -- microscaled 4-bit front end ---------------------------------------------------
+
+def bmlp_mx4_empty(n, K, device="cuda"):
+    """(codes, scales) for n rows of K values: n x ceil(K/2) and n x ceil(K/32) bytes
+    (torch.uint8) in buffers whose rows start at multiples of 16 bytes, which the
+    products read fastest.  n may be a tuple: (E, N) for the weights of E groups."""
+    torch = _torch or _use_torch()
+    lead = (n,) if isinstance(n, int) else tuple(n)
+    return tuple(torch.empty((*lead, (size + 15) // 16 * 16), dtype=torch.uint8, device=device)[..., :size]
+                 for size in ((K + 1) // 2, (K + 31) // 32))
+
+
+def _codes(q, scale, n, K, what):
+    """(pointer, row stride) of n rows of K codes and of their scales."""
+    u8 = _torch.uint8
+    return (*_rows(q, (n, (K + 1) // 2), what, u8), *_rows(scale, (n, (K + 31) // 32), what + "'s scales", u8))
+
+
+def bmlp_mx4_quantize(x, q, scale, stream=None):
+    """4-bit codes q (n x ceil(K/2) uint8) and scales (n x ceil(K/32) uint8) of the rows
+    of x (n x K fp32 / fp16 / bf16, on the device; row strides are kept)."""
+    torch = _torch or _use_torch()
+    shape = n, K = x.shape
+    if K >> 31:
+        _int32(K)
+    if _devices > 1:
+        _one_device(x, q, scale)
+    px, ldx = _rows(x, shape, "x", x.dtype)
+    pq, ldq, ps, lds = _codes(q, scale, n, K, "q")
+    rc = (_lib or lib()).bmlp_mx4_quantize(px, _type(x, _real_types, "x"), ldx, n, K, pq, ldq, ps, lds,
+                                           _tensor_stream(stream, x))
+    if rc:
+        _check(rc)
+
+
+def bmlp_mx4_norm_quantize(x, gain, q, scale, row_scale, res=None, sum_out=None, eps=1e-6, stream=None):
+    """RMS norm of the rows of x + res times gain as 4-bit codes q (n x ceil(K/2)
+    uint8), scales (n x ceil(K/32) uint8) and a factor per row (row_scale, n fp32);
+    sum_out (may be x or res): x + res in their type.  gain, res, sum_out: x's type,
+    each may be None."""
+    torch = _torch or _use_torch()
+    shape = n, K = x.shape
+    if K >> 31:
+        _int32(K)
+    dtype = x.dtype
+    if _devices > 1:
+        _one_device(x, gain, q, scale, row_scale, res, sum_out)
+    px, ldx = _rows(x, shape, "x", dtype)
+    pr, ldr = (None, 0) if res is None else _rows(res, shape, "res", dtype)
+    po, ldo = (None, 0) if sum_out is None else _rows(sum_out, shape, "sum_out", dtype)
+    pq, ldq, ps, lds = _codes(q, scale, n, K, "q")
+    rc = (_lib or lib()).bmlp_mx4_norm_quantize(px, ldx, pr, ldr, _vector(gain, K, "gain", dtype),
+                                                _type(x, _real_types, "x"), n, K, eps, po, ldo, pq, ldq, ps, lds,
+                                                _vector(row_scale, n, "row_scale", torch.float32),
+                                                _tensor_stream(stream, x))
+    if rc:
+        _check(rc)
+
+
+def bmlp_mx4_dequantize(q, scale, out, row_scale=None, stream=None):
+    """out (n x K fp32 / fp16 / bf16) = the values of codes q and scales, times row_scale
+    (n fp32) where it is given."""
+    torch = _torch or _use_torch()
+    shape = n, K = out.shape
+    if K >> 31:
+        _int32(K)
+    if _devices > 1:
+        _one_device(out, q, scale, row_scale)
+    po, ldo = _rows(out, shape, "out", out.dtype)
+    pq, ldq, ps, lds = _codes(q, scale, n, K, "q")
+    rc = (_lib or lib()).bmlp_mx4_dequantize(pq, ldq, ps, lds, _vector(row_scale, n, "row_scale", torch.float32),
+                                             n, K, po, _type(out, _real_types, "out"), ldo,
+                                             _tensor_stream(stream, out))
+    if rc:
+        _check(rc)
+
+
+def bmlp_mx4_matmul(a, a_scale, w, w_scale, out, row_scale=None, bias=None, stream=None, expired=False):
+    """out (n x N fp32 / fp16 / bf16) = the rows of a (n x ceil(K/2) uint8 codes and
+    n x ceil(K/32) uint8 scales) times those of w (N of them) transposed, times row_scale
+    (n fp32) plus bias (N fp32).  For odd K the last byte's high bits are 0.  expired:
+    bmlp_debug_mx4_matmul."""
+    torch = _torch or _use_torch()
+    n, K = a.shape[0], 2 * a.shape[1]
+    N = w.shape[0]
+    if (K | N) >> 31:
+        _int32(K, N)
+    if _devices > 1:
+        _one_device(a, a_scale, w, w_scale, out, row_scale, bias)
+    pa, lda, pas, ldas = _codes(a, a_scale, n, K, "a")
+    pw, ldw, pws, ldws = _codes(w, w_scale, N, K, "w")
+    po, ldo = _rows(out, (n, N), "out", out.dtype)
+    f32, L = torch.float32, _lib or lib()
+    prs, pb = _vector(row_scale, n, "row_scale", f32), _vector(bias, N, "bias", f32)
+    code, st = _type(out, _real_types, "out"), _tensor_stream(stream, a)
+    if expired:
+        rc = L.bmlp_debug_mx4_matmul(pa, lda, pas, ldas, prs, pw, ldw, 0, pws, ldws, 0, pb, 0, None, 1, n, K, N, po, code,
+                                     ldo, st)
+    else:
+        rc = L.bmlp_mx4_matmul(pa, lda, pas, ldas, prs, pw, ldw, pws, ldws, pb, n, K, N, po, code, ldo, st)
+    if rc:
+        _check(rc)
+
+
+def _groups(t, shape, what, dtype):
+    """(pointer, row stride, group stride) of a tensor of that shape whose rows are contiguous."""
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (what, shape, tuple(t.shape)))
+    if t.dtype is not dtype:
+        raise TypeError("%s: expected %s, got %s" % (what, dtype, t.dtype))
+    group, ld, step = t.stride()
+    if step != 1 and shape[2] > 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % what)
+    return t.data_ptr(), ld, group
+
+
+def bmlp_mx4_matmul_grouped(a, a_scale, w, w_scale, offsets, out, row_scale=None, bias=None, stream=None,
+                            expired=False):
+    """bmlp_mx4_matmul with E matrices of weights: w (E x N x ceil(K/2) uint8), w_scale
+    (E x N x ceil(K/32) uint8), bias (E x N fp32); rows offsets[e] <= i < offsets[e + 1] of a
+    by the e-th (offsets: E + 1 int32 on the device).  Rows of no group stay as they are."""
+    torch = _torch or _use_torch()
+    n, K = a.shape[0], 2 * a.shape[1]
+    E, N = w.shape[0], w.shape[1]
+    if (K | N) >> 31:
+        _int32(K, N)
+    if _devices > 1:
+        _one_device(a, a_scale, w, w_scale, offsets, out, row_scale, bias)
+    u8, f32, L = torch.uint8, torch.float32, _lib or lib()
+    pa, lda, pas, ldas = _codes(a, a_scale, n, K, "a")
+    pw, ldw, gw = _groups(w, (E, N, K // 2), "w", u8)
+    pws, ldws, gws = _groups(w_scale, (E, N, (K + 31) // 32), "w's scales", u8)
+    po, ldo = _rows(out, (n, N), "out", out.dtype)
+    pb, gb = (None, 0) if bias is None else _rows(bias, (E, N), "bias", f32)
+    call = L.bmlp_debug_mx4_matmul if expired else L.bmlp_mx4_matmul_grouped
+    rc = call(pa, lda, pas, ldas, _vector(row_scale, n, "row_scale", f32), pw, ldw, gw, pws, ldws, gws, pb, gb,
+              _vector(offsets, E + 1, "offsets", torch.int32), E, n, K, N, po, _type(out, _real_types, "out"), ldo,
+              _tensor_stream(stream, a))
     if rc:
         _check(rc)
 

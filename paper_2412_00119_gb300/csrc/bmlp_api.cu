@@ -256,6 +256,55 @@ int int8_call(const char* name, const Int8Args& A, void* workspace, int64_t work
   return BMLP_OK;
 }
 
+// Whether rows of `need` elements do not fit their stride.
+bool short_rows(int64_t rows, int64_t ld, int64_t need) { return rows > 1 && ld < need; }
+int64_t code_bytes(int32_t K) { return ((int64_t)K + 1) / 2; }
+int64_t scale_bytes(int32_t K) { return ((int64_t)K + 31) / 32; }
+bool real_type(int32_t t) { return t == BMLP_F32 || t == BMLP_F16 || t == BMLP_BF16; }
+
+// The checks and the launch that bmlp_mx4_quantize and bmlp_mx4_norm_quantize share.
+int mx4_quantize_call(const char* name, const Mx4QuantArgs& A, bool norm, void* cuda_stream) {
+  if (A.n < 0 || A.n > BMLP_MX4_MAX_ROWS || A.K < 1)
+    return fail(nullptr, BMLP_EINVAL, "%s: n outside 0..%d or K < 1", name, BMLP_MX4_MAX_ROWS);
+  if (!real_type(A.type)) return fail(nullptr, BMLP_EINVAL, "%s: x_type must be BMLP_F32, BMLP_F16 or BMLP_BF16", name);
+  if (A.n == 0) return BMLP_OK;
+  if (short_rows(A.n, A.ldx, A.K) || (A.res && short_rows(A.n, A.ldr, A.K)) || (A.sum && short_rows(A.n, A.lds, A.K)) ||
+      short_rows(A.n, A.ldq, code_bytes(A.K)) || short_rows(A.n, A.ldc, scale_bytes(A.K)))
+    return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below its row's length", name);
+  if (A.sum && ((A.sum == A.x && A.lds != A.ldx) || (A.sum == A.res && A.lds != A.ldr)) && A.n > 1)
+    return fail(nullptr, BMLP_EINVAL, "%s: sum_out in place needs its input's row stride", name);
+  const int shift = A.type == BMLP_F32 ? 2 : 1, here = current_device();
+  if (!A.x || !A.q || !A.scale || (norm && !A.row_scale) || !usable(A.x, shift, here) || !usable(A.res, shift, here) ||
+      !usable(A.gain, shift, here) || !usable(A.sum, shift, here) || !usable(A.q, 0, here) || !usable(A.scale, 0, here) ||
+      !usable(A.row_scale, 2, here))
+    return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
+  const cudaError_t e = launch_mx4_quantize(A, norm, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
+  return BMLP_OK;
+}
+
+// The same for the products.
+int mx4_call(const char* name, const Mx4Args& A, bool grouped, void* cuda_stream, int expire = 0) {
+  if (A.n < 0 || A.n > BMLP_MX4_MAX_ROWS || A.K < 1 || A.N < 1 || A.N > (1 << 30))
+    return fail(nullptr, BMLP_EINVAL, "%s: n outside 0..%d, K < 1 or N outside 1..2^30", name, BMLP_MX4_MAX_ROWS);
+  if (A.E < 1 || A.E > BMLP_MX4_MAX_GROUPS)
+    return fail(nullptr, BMLP_EINVAL, "%s: E outside 1..%d", name, BMLP_MX4_MAX_GROUPS);
+  if (!real_type(A.type)) return fail(nullptr, BMLP_EINVAL, "%s: out_type must be BMLP_F32, BMLP_F16 or BMLP_BF16", name);
+  if (A.n == 0) return BMLP_OK;
+  if (short_rows(A.n, A.lda, code_bytes(A.K)) || short_rows(A.n, A.ldas, scale_bytes(A.K)) || short_rows(A.n, A.ldo, A.N) ||
+      short_rows(A.N, A.ldw, code_bytes(A.K)) || short_rows(A.N, A.ldws, scale_bytes(A.K)))
+    return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below its row's length", name);
+  if (A.gw < 0 || A.gws < 0 || A.ldb < 0) return fail(nullptr, BMLP_EINVAL, "%s: a group stride is negative", name);
+  const int shift = A.type == BMLP_F32 ? 2 : 1, here = current_device();
+  if (!A.a || !A.as || !A.w || !A.ws || !A.out || (grouped && !A.offsets) || !usable(A.a, 0, here) || !usable(A.as, 0, here) ||
+      !usable(A.w, 0, here) || !usable(A.ws, 0, here) || !usable(A.row_scale, 2, here) || !usable(A.bias, 2, here) ||
+      !usable(A.offsets, 2, here) || !usable(A.out, shift, here))
+    return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
+  const cudaError_t e = launch_mx4(A, static_cast<cudaStream_t>(cuda_stream), expire);
+  if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
+  return BMLP_OK;
+}
+
 int upload_thresholds(bmlp_t* h, cudaStream_t st) {
   std::vector<RTables> rt((size_t)h->L);
   for (int l = 1; l <= h->L; ++l) {
@@ -1052,6 +1101,75 @@ int bmlp_debug_int8_sign(const int8_t* a, int64_t lda, const int8_t* w, int64_t 
 
 int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N) {
   return n < 1 || K < 1 || K > BMLP_INT8_MAX_K || N < 1 || N > (1 << 30) ? 0 : int8_workspace(n, K, N);
+}
+
+int bmlp_mx4_quantize(const void* x, int32_t x_type, int64_t ldx, int64_t n, int32_t K, uint8_t* q,
+                      int64_t ldq, uint8_t* scale, int64_t lds, void* cuda_stream) {
+  TraceRange trace("bmlp_mx4_quantize");
+  Mx4QuantArgs A = {};
+  A.x = x; A.q = q; A.scale = scale;
+  A.ldx = ldx; A.ldq = ldq; A.ldc = lds; A.n = n;
+  A.K = K; A.type = x_type;
+  return mx4_quantize_call("bmlp_mx4_quantize", A, false, cuda_stream);
+}
+
+int bmlp_mx4_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t ldr, const void* gain,
+                           int32_t x_type, int64_t n, int32_t K, float eps, void* sum_out, int64_t ldsum,
+                           uint8_t* q, int64_t ldq, uint8_t* scale, int64_t lds, float* row_scale,
+                           void* cuda_stream) {
+  TraceRange trace("bmlp_mx4_norm_quantize");
+  if (!(eps >= 0.0f) || std::isinf(eps))
+    return fail(nullptr, BMLP_EINVAL, "bmlp_mx4_norm_quantize: eps must be finite and >= 0");
+  const Mx4QuantArgs A = {x, res, gain, sum_out, q, scale, row_scale, ldx, ldr, ldsum, ldq, lds, n, K, x_type, eps};
+  return mx4_quantize_call("bmlp_mx4_norm_quantize", A, true, cuda_stream);
+}
+
+int bmlp_mx4_dequantize(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, const float* row_scale,
+                        int64_t n, int32_t K, void* out, int32_t out_type, int64_t ldo, void* cuda_stream) {
+  TraceRange trace("bmlp_mx4_dequantize");
+  const char* name = "bmlp_mx4_dequantize";
+  if (n < 0 || n > BMLP_MX4_MAX_ROWS || K < 1)
+    return fail(nullptr, BMLP_EINVAL, "%s: n outside 0..%d or K < 1", name, BMLP_MX4_MAX_ROWS);
+  if (!real_type(out_type)) return fail(nullptr, BMLP_EINVAL, "%s: out_type must be BMLP_F32, BMLP_F16 or BMLP_BF16", name);
+  if (n == 0) return BMLP_OK;
+  if (short_rows(n, ldq, code_bytes(K)) || short_rows(n, lds, scale_bytes(K)) || short_rows(n, ldo, K))
+    return fail(nullptr, BMLP_EINVAL, "%s: a row stride is below its row's length", name);
+  const int here = current_device();
+  if (!q || !scale || !out || !usable(q, 0, here) || !usable(scale, 0, here) || !usable(row_scale, 2, here) ||
+      !usable(out, out_type == BMLP_F32 ? 2 : 1, here))
+    return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
+  const Mx4DequantArgs A = {q, scale, row_scale, out, ldq, lds, ldo, n, K, out_type};
+  const cudaError_t e = launch_mx4_dequantize(A, static_cast<cudaStream_t>(cuda_stream));
+  if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
+  return BMLP_OK;
+}
+
+int bmlp_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas, const float* row_scale,
+                    const uint8_t* w, int64_t ldw, const uint8_t* w_scale, int64_t ldws, const float* bias,
+                    int64_t n, int32_t K, int32_t N, void* out, int32_t out_type, int64_t ldo, void* cuda_stream) {
+  TraceRange trace("bmlp_mx4_matmul");
+  const Mx4Args A = {a, a_scale, row_scale, w, w_scale, bias, nullptr, out, lda, ldas, ldw, 0, ldws, 0, 0, ldo, n, K, N, 1, out_type};
+  return mx4_call("bmlp_mx4_matmul", A, false, cuda_stream);
+}
+
+int bmlp_mx4_matmul_grouped(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                            const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                            const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                            const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                            int32_t out_type, int64_t ldo, void* cuda_stream) {
+  TraceRange trace("bmlp_mx4_matmul_grouped");
+  const Mx4Args A = {a, a_scale, row_scale, w, w_scale, bias, offsets, out, lda, ldas, ldw, gw, ldws, gws, gb, ldo, n, K, N, E, out_type};
+  return mx4_call("bmlp_mx4_matmul_grouped", A, true, cuda_stream);
+}
+
+int bmlp_debug_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                          const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                          const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                          const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                          int32_t out_type, int64_t ldo, void* cuda_stream) {
+  TraceRange trace("bmlp_debug_mx4_matmul");
+  const Mx4Args A = {a, a_scale, row_scale, w, w_scale, bias, offsets, out, lda, ldas, ldw, gw, ldws, gws, gb, ldo, n, K, N, E, out_type};
+  return mx4_call("bmlp_debug_mx4_matmul", A, E > 1, cuda_stream, 1);
 }
 
 int bmlp_get_state(const bmlp_t* hc, int32_t layer, int16_t* H_out, uint64_t* W_out, int8_t* P_out,

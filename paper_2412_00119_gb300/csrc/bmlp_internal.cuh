@@ -343,6 +343,46 @@ int64_t int8_rows_workspace(int64_t n, int K);
 constexpr int64_t kPairSlab = 65536;
 int64_t int8_pair_workspace(int64_t n, int K, int64_t N);
 cudaError_t launch_int8_pair(const Int8Args& A, void* workspace, cudaStream_t st, int expire);
+// Microscaled 4-bit front end: rows to codes and scales, with a norm (row_scale) or without,
+// and back (kern_mx4_quantize.cu).  ldq, ldc: row strides of codes and scales in bytes.
+struct Mx4QuantArgs {
+  const void* x;
+  const void* res;      // or null
+  const void* gain;     // or null
+  void* sum;            // or null
+  uint8_t* q;
+  uint8_t* scale;
+  float* row_scale;     // with a norm
+  int64_t ldx, ldr, lds, ldq, ldc, n;
+  int32_t K, type;      // BMLP_F32 / F16 / BF16
+  float eps;
+};
+cudaError_t launch_mx4_quantize(const Mx4QuantArgs& A, bool norm, cudaStream_t st);
+struct Mx4DequantArgs {
+  const uint8_t* q;
+  const uint8_t* scale;
+  const float* row_scale;   // or null
+  void* out;
+  int64_t ldq, ldc, ldo, n;
+  int32_t K, type;
+};
+cudaError_t launch_mx4_dequantize(const Mx4DequantArgs& A, cudaStream_t st);
+// Product of such rows (kern_mx4_product.cu), by one matrix of weights (E = 1, offsets null)
+// or by that of each row's group.  Strides of codes and scales (ld..: rows, g..: groups) in bytes.
+struct Mx4Args {
+  const uint8_t* a;
+  const uint8_t* as;
+  const float* row_scale;   // or null
+  const uint8_t* w;
+  const uint8_t* ws;
+  const float* bias;        // or null; ldb: group stride
+  const int32_t* offsets;   // E + 1, or null: every row is in group 0
+  void* out;
+  int64_t lda, ldas, ldw, gw, ldws, gws, ldb, ldo, n;
+  int32_t K, N, E, type;
+};
+// expire != 0: the CTAs take a wait as expired (tests).
+cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

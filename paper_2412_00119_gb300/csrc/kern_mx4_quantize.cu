@@ -1,0 +1,382 @@
+// kern_mx4_quantize.cu -- rows of real values to microscaled 4-bit codes (e2m1, two to a
+// byte, with a power-of-two scale per 32), with or without the root-mean-square norm
+// and the residual's addition before them, and codes back to real values.
+//
+//   h = x + res,  u = h gain,  of each 32 u: m = max |u|,
+//   s = max(0, floor(log2 m) - 2 + 127),  code = e2m1(u 2^(127-s)),  row_scale = 1 / sqrt(mean h^2 + eps)
+//
+// 2^(127-s) is a normal fp32 number for every finite m, and the product with it exact, so a
+// code has one rounding (and u at most two).  The norm's factor stays outside of the
+// codes: they need their own 32 values alone, and a row passes through once, whatever its
+// length, with the sum of squares running beside.  The maximum is taken on the bits of |u| as
+// unsigned integers, whose order is the values' order with infinities and NaNs on top.
+// Bound: memory.
+#include <algorithm>
+#include <type_traits>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "bmlp_internal.cuh"
+
+namespace bk {
+namespace {
+
+constexpr unsigned kFullMask = 0xffffffffu;
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
+
+// Below this eps (2^-80) a row's factor may hang on squares that are lost in fp32, those of
+// |h| < 2^-63.  Such rows have a sum below kSmallSum (2^-90: what a greater one has lost is
+// less than 2^-60 of it for each value), every |h| below 2^-45, and squares of h kUp (2^85)
+// that are inside fp32's range down to its least subnormal.
+constexpr float kSmallEps = 8.27180613e-25f, kSmallSum = 8.07793566e-28f;
+constexpr float kUp = 3.86856262e25f;   // 2^85
+
+__device__ __forceinline__ float row_factor(float sumsq, float sumsq_up, int K, float eps, bool small) {
+  if (!(sumsq < __uint_as_float(kInfBits))) return __uint_as_float(0x7FFFFFFFu);
+  const bool up = small && sumsq < kSmallSum;
+  const float root = up ? sqrtf(sumsq_up / (float)K + eps * kUp * kUp) : sqrtf(sumsq / (float)K + eps);
+  return root > 0.0f ? (up ? (1.0f / root) * kUp : 1.0f / root) : 0.0f;
+}
+
+// V values as they lie in memory (V > 1: 16 bytes, aligned).
+template <typename T, int V> struct Values {
+  static constexpr int kWords = V > 1 ? 4 : 1;
+  uint32_t w[kWords];
+  // the first `left` of those at p; zeros in the others' place
+  __device__ __forceinline__ void load(const T* p, int64_t left) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    if (left >= V) {
+      if constexpr (V > 1) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else if constexpr (sizeof(T) == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else {
+        w[0] = *reinterpret_cast<const uint16_t*>(p);
+      }
+    } else if constexpr (V > 1) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < left) {
+          if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+          else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
+        }
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[i]);
+    else if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (16 * (i % 2)))));
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void store_values(T* p, const float (&f)[V], int64_t left) {
+  if constexpr (V > 1) {
+    if (left >= V) {
+      constexpr int kEach = 16 / (int)sizeof(T);
+#pragma unroll
+      for (int h = 0; h < V; h += kEach) {
+        union { uint4 w; T e[kEach]; } u;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) u.e[i] = from_f32<T>(f[h + i]);
+        *reinterpret_cast<uint4*>(p + h) = u.w;
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < left) p[i] = from_f32<T>(f[i]);
+}
+
+// Two codes in a byte, ties to the even code.
+__device__ __forceinline__ uint32_t code_pair(float lo, float hi) {
+  uint32_t r;
+  asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n cvt.u32.u8 %0, b;\n}" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Codes of a lane's V values u and their block's scale byte.  Blocks of 32 are 32 / V
+// neighbouring lanes'; every lane of the warp calls.
+template <int V>
+__device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t& s) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(u[i]) & 0x7FFFFFFFu);
+  if constexpr (V == 1) {
+    m = __reduce_max_sync(kFullMask, m);
+  } else {
+#pragma unroll
+    for (int o = 1; o < 32 / V; o *= 2) m = max(m, __shfl_xor_sync(kFullMask, m, o));
+  }
+  const bool finite = m < kInfBits;
+  const uint32_t e = m >> 23;
+  s = finite ? (e > 2u ? e - 2u : 0u) : 255u;
+  const float up = __uint_as_float(finite ? (254u - s) << 23 : 0u);
+  uint32_t c = 0u;
+  if constexpr (V == 1) {
+    const float t = u[0] * up, next = __shfl_down_sync(kFullMask, t, 1);
+    c = code_pair(t, next);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) c |= code_pair(u[i] * up, u[i + 1] * up) << (4 * i);
+  }
+  return finite ? c : 0u;
+}
+
+// Codes and scale of a lane's V values from element e of a row on, `left` of which are the row's.
+template <int V>
+__device__ __forceinline__ void store_codes(uint8_t* q, uint8_t* scale, int64_t e, int64_t left, uint32_t c, uint32_t s) {
+  const int lane = threadIdx.x & 31;
+  if constexpr (V == 1) {
+    if ((lane & 1) == 0 && left > 0) q[e >> 1] = (uint8_t)c;   // (past the row: zeros)
+  } else if (left >= V) {
+    if constexpr (V == 8) *reinterpret_cast<uint32_t*>(q + (e >> 1)) = c;
+    else *reinterpret_cast<uint16_t*>(q + (e >> 1)) = (uint16_t)c;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i)
+      if (2 * i < left) q[(e >> 1) + i] = (uint8_t)(c >> (8 * i));
+  }
+  if (lane % (32 / V) == 0 && left > 0) scale[e >> 5] = (uint8_t)s;
+}
+
+// ---------------------------------------------------------------------------
+// Without a norm: a warp takes kAhead times 32 V neighbouring values of a row at a time.
+// ---------------------------------------------------------------------------
+constexpr int kThreads = 256;
+
+template <typename T, int V, int kAhead>
+__global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int kPart = 32 * V * kAhead;
+  const int lane = threadIdx.x & 31;
+  const int64_t parts = ((int64_t)A.K + kPart - 1) / kPart, total = A.n * parts;
+  for (int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < total;
+       t += (int64_t)gridDim.x * (kThreads / 32)) {
+    const int64_t row = t / parts, e0 = (t % parts) * kPart + V * lane;
+    const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+    Values<T, V> v[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) v[a].load(x + e0 + 32 * V * a, A.K - (e0 + 32 * V * a));
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t e = e0 + 32 * V * a;
+      float u[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) u[i] = v[a].get(i);
+      uint32_t s;
+      const uint32_t c = make_codes<V>(u, s);
+      store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, A.K - e, c, s);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// With it: a row's threads are a warp (kWarpRow) or a CTA.
+// ---------------------------------------------------------------------------
+template <typename T, bool kRes, bool kSmall, int V, int kAhead, bool kWarpRow>
+__global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const Mx4QuantArgs A) {
+  pdl_wait();
+  pdl_trigger();
+  const int threads = kWarpRow ? 32 : (int)blockDim.x, lane = threadIdx.x & 31;
+  const int tid = kWarpRow ? lane : (int)threadIdx.x;
+  const int64_t row = kWarpRow ? (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
+  if (kWarpRow && row >= A.n) return;
+  const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+  const T* res = kRes ? static_cast<const T*>(A.res) + row * A.ldr : nullptr;
+  T* sum = A.sum ? static_cast<T*>(A.sum) + row * A.lds : nullptr;
+  const T* gain = static_cast<const T*>(A.gain);
+  float sq = 0.0f, sq_up = 0.0f;
+  const int64_t step = (int64_t)threads * V;
+  // (whole warps: the lanes of one meet in make_codes)
+  for (int64_t e0 = V * tid; e0 - V * lane < A.K; e0 += kAhead * step) {
+    Values<T, V> v[kAhead], r[kRes ? kAhead : 1], g[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) v[a].load(x + e0 + a * step, A.K - (e0 + a * step));
+    if constexpr (kRes) {
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) r[a].load(res + e0 + a * step, A.K - (e0 + a * step));
+    }
+    if (gain) {
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) g[a].load(gain + e0 + a * step, A.K - (e0 + a * step));
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t e = e0 + a * step, left = A.K - e;
+      float u[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        u[i] = v[a].get(i);
+        if constexpr (kRes) u[i] = __fadd_rn(u[i], r[a].get(i));
+        sq += u[i] * u[i];
+        if constexpr (kSmall) sq_up += (u[i] * kUp) * (u[i] * kUp);
+      }
+      // (these values of x and res are read: sum_out may be one of them)
+      if (sum) store_values<T, V>(sum + e, u, left);
+      if (gain) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) u[i] = __fmul_rn(u[i], g[a].get(i));
+      }
+      uint32_t s;
+      const uint32_t c = make_codes<V>(u, s);
+      store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, left, c, s);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sq += __shfl_xor_sync(kFullMask, sq, o);
+    if constexpr (kSmall) sq_up += __shfl_xor_sync(kFullMask, sq_up, o);
+  }
+  if constexpr (!kWarpRow) {
+    __shared__ float part[2][32];
+    const int warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    if (lane == 0) {
+      part[0][warp] = sq;
+      part[1][warp] = sq_up;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    sq = lane < warps ? part[0][lane] : 0.0f;
+    sq_up = lane < warps ? part[1][lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      sq += __shfl_xor_sync(kFullMask, sq, o);
+      if constexpr (kSmall) sq_up += __shfl_xor_sync(kFullMask, sq_up, o);
+    }
+  }
+  if (tid == 0) A.row_scale[row] = row_factor(sq, sq_up, A.K, A.eps, kSmall);
+}
+
+// ---------------------------------------------------------------------------
+// Codes to values: a lane takes V codes at a time.
+// ---------------------------------------------------------------------------
+// The two values of a byte of codes.
+__device__ __forceinline__ float2 pair_values(uint32_t byte) {
+  uint32_t h;
+  asm("{\n .reg .b8 b;\n cvt.u8.u32 b, %1;\n cvt.rn.f16x2.e2m1x2 %0, b;\n}" : "=r"(h) : "r"(byte));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArgs A) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t parts = ((int64_t)A.K + V - 1) / V, total = A.n * parts;
+  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < total; t += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = t / parts, e = (t % parts) * V, left = A.K - e;
+    const uint8_t* q = A.q + row * A.ldq + (e >> 1);
+    uint32_t c = 0u;
+    if constexpr (V == 8) {
+      if (left >= V - 1) {
+        c = *reinterpret_cast<const uint32_t*>(q);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+          if (2 * i < left) c |= (uint32_t)q[i] << (8 * i);
+      }
+    } else {
+      c = *q;
+    }
+    const uint32_t s = A.scale[row * A.ldc + (e >> 5)];
+    // 2^(s-127): below 2^-126 a subnormal number; 255 is NaN
+    const float unit = __uint_as_float(s == 0u ? 0x00400000u : (s == 255u ? 0x7FFFFFFFu : s << 23));
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const float2 two = pair_values((c >> (4 * i)) & 255u);
+      f[i] = two.x * unit;
+      f[i + 1] = two.y * unit;
+    }
+    if (A.row_scale) {
+      const float by = A.row_scale[row];
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] *= by;
+    }
+    T* out = static_cast<T*>(A.out) + row * A.ldo + e;
+    if constexpr (V == 8) {
+      store_values<T, V>(out, f, left);
+    } else {
+      out[0] = from_f32<T>(f[0]);
+      if (left > 1) out[1] = from_f32<T>(f[1]);
+    }
+  }
+}
+
+// Whether rows of a buffer start at multiples of `bytes` (a power of two).
+bool rows_at(const void* p, int64_t ld_bytes, int64_t n, int bytes) {
+  return ((reinterpret_cast<uintptr_t>(p) | (n > 1 ? (uintptr_t)ld_bytes : 0)) & (uintptr_t)(bytes - 1)) == 0;
+}
+
+unsigned grid_of(int64_t units, int per_cta) {
+  return (unsigned)std::min<int64_t>((units + per_cta - 1) / per_cta, 64ll * sm_count());
+}
+
+template <typename T, int V>
+cudaError_t launch_plain(const Mx4QuantArgs& A, cudaStream_t st) {
+  constexpr int kAhead = 4;
+  const int64_t parts = ((int64_t)A.K + 32 * V * kAhead - 1) / (32 * V * kAhead);
+  return launch_kernel(k_mx4_quantize<T, V, kAhead>, dim3(grid_of(A.n * parts, kThreads / 32)), dim3(kThreads), 0, st, true, A);
+}
+
+template <typename T, bool kRes, bool kSmall, int V>
+cudaError_t launch_norm(const Mx4QuantArgs& A, cudaStream_t st) {
+  constexpr int kAhead = V > 1 ? 2 : 4;
+  const int64_t vecs = ((int64_t)A.K + V - 1) / V;
+  if (vecs <= 128)
+    return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kAhead, true>, dim3((unsigned)((A.n + kThreads / 32 - 1) / (kThreads / 32))),
+                         dim3(kThreads), 0, st, true, A);
+  const int64_t want = A.n <= 2 * sm_count() ? vecs : (vecs + kAhead - 1) / kAhead;
+  const int threads = (int)std::min<int64_t>(1024, (want + 31) / 32 * 32);
+  return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kAhead, false>, dim3((unsigned)A.n), dim3((unsigned)threads), 0, st, true, A);
+}
+
+template <typename T, int V>
+cudaError_t launch_v(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
+  if (!norm) return launch_plain<T, V>(A, st);
+  // (the squares of fp16 values do not leave fp32)
+  if constexpr (!std::is_same<T, __half>::value)
+    if (A.eps < kSmallEps) return A.res ? launch_norm<T, true, true, V>(A, st) : launch_norm<T, false, true, V>(A, st);
+  return A.res ? launch_norm<T, true, false, V>(A, st) : launch_norm<T, false, false, V>(A, st);
+}
+
+template <typename T>
+cudaError_t launch_type(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  constexpr int64_t kSize = (int64_t)sizeof(T);
+  const bool wide = rows_at(A.x, A.ldx * kSize, A.n, 16) && (!A.res || rows_at(A.res, A.ldr * kSize, A.n, 16)) &&
+                    (!A.sum || rows_at(A.sum, A.lds * kSize, A.n, 16)) && rows_at(A.gain, 0, 1, 16) && rows_at(A.q, A.ldq, A.n, V / 2);
+  return wide ? launch_v<T, V>(A, norm, st) : launch_v<T, 1>(A, norm, st);
+}
+
+template <typename T>
+cudaError_t launch_dequant(const Mx4DequantArgs& A, cudaStream_t st) {
+  const bool wide = rows_at(A.out, A.ldo * (int64_t)sizeof(T), A.n, 16) && rows_at(A.q, A.ldq, A.n, 4);
+  const int64_t units = A.n * (((int64_t)A.K + (wide ? 7 : 1)) / (wide ? 8 : 2));
+  return wide ? launch_kernel(k_mx4_dequantize<T, 8>, dim3(grid_of(units, kThreads)), dim3(kThreads), 0, st, true, A)
+              : launch_kernel(k_mx4_dequantize<T, 2>, dim3(grid_of(units, kThreads)), dim3(kThreads), 0, st, true, A);
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_quantize(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
+  if (A.type == BMLP_F32) return launch_type<float>(A, norm, st);
+  return A.type == BMLP_F16 ? launch_type<__half>(A, norm, st) : launch_type<__nv_bfloat16>(A, norm, st);
+}
+
+cudaError_t launch_mx4_dequantize(const Mx4DequantArgs& A, cudaStream_t st) {
+  if (A.type == BMLP_F32) return launch_dequant<float>(A, st);
+  return A.type == BMLP_F16 ? launch_dequant<__half>(A, st) : launch_dequant<__nv_bfloat16>(A, st);
+}
+
+}  // namespace bk
