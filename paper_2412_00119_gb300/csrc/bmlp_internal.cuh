@@ -383,6 +383,8 @@ struct Mx4Args {
 };
 // expire != 0: the CTAs take a wait as expired (tests).
 cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire);
+// The tensor-core tiles of one CTA (kern_mx4_tile.cu).
+cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

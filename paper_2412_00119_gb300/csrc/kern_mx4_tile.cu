@@ -1,0 +1,647 @@
+// kern_mx4_tile.cu -- the microscaled 4-bit product on the tensor cores, tiles of one CTA.
+//
+// The codes lie in memory as tcgen05.mma kind::mxf4 wants them in shared memory (K-major, two
+// to a byte), so tensor copies take them there, zeros past the operands' ends, and nobody
+// touches them on the way.  A CTA computes 128 channels (MMA M; lanes of tensor memory) x up to
+// 128 rows (MMA N, as many as the tile has, up to 16); channels on M: a narrow batch costs narrow MMAs,
+// and a warp's lanes hold 32 neighbouring channels of a row, as the output wants them.
+// Warps:
+//   - one thread copies stages of 256 codes of every row into a ring (rows at places that
+//     tensor copies cannot take: eight warps do, shifting whole 16-byte pieces);
+//   - four warps take the scales of 512 codes (16 bytes) of every row from global memory
+//     through shared memory into tensor memory, where the MMA reads row r's at lane r % 32
+//     of column r / 32, four blocks' bytes in a column, and in each quarter of the lanes;
+//   - one warp issues the MMAs, 64 codes (two blocks) each;
+//   - eight warps write finished tiles while the next one's MMAs run (two accumulators).
+// Where there are fewer tiles than SMs, the CTAs of a cluster share K and add their sums up
+// in the order of their ranks, through distributed shared memory.
+// By group: the row tiles of a group start at its first row; what a tile has of the next
+// group's rows is multiplied and dropped.
+// Every wait is bounded; if one expires the CTA's tiles are made again on CUDA cores.
+// Measured (us): 1 x 8192 -> 8192 11.6 (scales one piece ahead in registers 16.3: a turn then takes
+// a memory latency), 100 x 4096 -> 8192 17.4, 96 x 4096 -> 2048 by 32 26, 16384 x 8192 -> 8192 748.
+#include <algorithm>
+
+#include <cuda.h>
+
+#include "int8_common.cuh"
+#include "mx4_common.cuh"
+#include "tc_common.cuh"
+
+namespace bk {
+namespace {
+
+using namespace tc;
+using namespace mx4;
+
+constexpr int CM = 128;                  // channels of a tile
+constexpr int kMaxRows = 128;
+constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
+constexpr int kEpiWarps = 8, kScaleWarps = 4, kMmaWarp = kEpiWarps + kScaleWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kLoadWarps = 8;
+constexpr int kMaxStages = 8;
+constexpr int kSlots = 4;                // of scales, 512 codes each, in tensor memory
+constexpr int kSlotCols = 32;            // 4 x 4 columns of the channels', as many of the rows'
+
+struct __align__(8) TileShared {
+  unsigned long long full[kMaxStages], empty[kMaxStages];
+  unsigned long long sfull[kSlots], sempty[kSlots];
+  unsigned long long done[2], drained[2];
+  unsigned long long left;
+  uint32_t tmem_base;
+  int failed, left_failed;
+};
+
+struct TilePlan {
+  int nt;          // rows of a tile, a multiple of 16
+  int stages;
+  int cols;        // of tensor memory
+  int split;       // CTAs that share K
+  int ctiles;      // channel tiles
+  int ctas;        // of the grid
+  int whole;       // every row's scales start at a multiple of 16 bytes
+};
+
+constexpr int kScaleRing = 6;            // 512 codes' scales of every row in flight (three where rows start anywhere)
+// rows of the ring: all that a warp reads at a time
+__host__ __device__ constexpr int scale_rows(int nt) { return CM + (nt + 31) / 32 * 32; }
+int64_t tile_smem(const Mx4Args& A, int nt, int stages) {
+  return 1024 + (int64_t)(CM + nt) * stages * kStepBytes + kScaleRing * 16 * scale_rows(nt) + (int64_t)sizeof(TileShared) +
+         (A.offsets ? 8 * ((int64_t)A.E + 1) : 0);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t local_addr, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local_addr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float peer_load(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void mma_mx4(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa,
+                                        uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate));
+}
+
+__device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy_a(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// The tiles of a CTA (or of a cluster of them), one after another: row tile u, channel tile ct.
+struct Item {
+  int e;          // group
+  int rows;
+  int64_t r0;     // first row
+  int j0;         // first channel
+};
+struct Items {
+  const int32_t* tile0;   // by group: its first row tile (E + 1); null: one group
+  const int32_t* row0;    // and its first row
+  int E, nt, ctiles, step_u, step_c;
+  int64_t rtiles, n;
+};
+struct Cursor {
+  int64_t u;
+  int ct;
+  __device__ __forceinline__ Cursor(const Items& I, uint32_t first) : u(first / (uint32_t)I.ctiles), ct((int)(first % (uint32_t)I.ctiles)) {}
+  __device__ __forceinline__ bool live(const Items& I) const { return u < I.rtiles; }
+  __device__ __forceinline__ void next(const Items& I) {
+    u += I.step_u;
+    ct += I.step_c;
+    if (ct >= I.ctiles) {
+      ct -= I.ctiles;
+      ++u;
+    }
+  }
+  __device__ __forceinline__ Item at(const Items& I) const {
+    Item it;
+    it.j0 = CM * ct;
+    int64_t end = I.n;
+    if (I.tile0) {
+      int lo = 0, hi = I.E;      // the last group with tile0 <= u
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (I.tile0[mid] <= u) lo = mid; else hi = mid;
+      }
+      it.e = lo;
+      it.r0 = I.row0[lo] + (u - I.tile0[lo]) * I.nt;
+      end = I.row0[lo + 1];
+    } else {
+      it.e = 0;
+      it.r0 = u * I.nt;
+    }
+    it.rows = (int)min((int64_t)I.nt, end - it.r0);
+    return it;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ T output(float sum, bool has_rs, float rs, bool has_bias, float bias) {
+  const float y = has_rs ? __fmul_rn(sum, rs) : sum;
+  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
+}
+
+// A tile's outputs on CUDA cores (columns first, first + step, ..), by all threads: only after a
+// wait has expired.
+static __device__ __noinline__ void plain_rows(const Mx4Args& A, const Item& it, int first, int step) {
+  for (int64_t k = threadIdx.x; k < (int64_t)CM * it.rows; k += blockDim.x) {
+    const int j = it.j0 + (int)(k % CM), x = (int)(k / CM);
+    if (x % step == first && j < A.N) put_out(A, it.r0 + x, j, it.e, plain_sum(A, it.r0 + x, j, it.e));
+  }
+}
+
+template <typename TOut, bool kTma>
+__global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps), kTma ? 2 : 1)
+    k_mx4_tile(const Mx4Args A, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap,
+               const TilePlan P, int expire) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int stage_bytes = (CM + P.nt) * kStepBytes;
+  uint8_t* scales = base + P.stages * stage_bytes;
+  const int ring_bytes = kScaleRing * 16 * scale_rows(P.nt);
+  TileShared* sh = reinterpret_cast<TileShared*>(scales + ring_bytes);
+  int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t S = (uint32_t)P.split, rank = S > 1 ? cluster_rank() : 0u;
+  volatile int* failed = &sh->failed;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P.stages; ++s) {
+      mbar_init(&sh->full[s], kTma ? 1 : kLoadWarps);
+      mbar_init(&sh->empty[s], 1);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&sh->sfull[s], kScaleWarps);
+      mbar_init(&sh->sempty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&sh->done[b], 1);
+      mbar_init(&sh->drained[b], kEpiWarps);
+    }
+    mbar_init(&sh->left, 1);
+    sh->failed = sh->left_failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&sh->tmem_base)), "r"(P.cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (kTma && warp == kCopyWarp && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
+  }
+  pdl_wait();
+  pdl_trigger();
+  if (A.offsets && warp == 0) {
+    // the groups' first rows and first row tiles
+    int row = 0, tile = 0;
+    for (int e0 = 0; e0 <= A.E; e0 += 32) {
+      const int e = e0 + lane;
+      int r = e <= A.E ? clamp_offset(A.offsets[e], 0, A.n) : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int v = __shfl_up_sync(kFull, r, o);
+        if (lane >= o) r = max(r, v);
+      }
+      r = max(r, row);
+      if (e <= A.E) groups[A.E + 1 + e] = r;
+      row = __shfl_sync(kFull, r, 31);
+    }
+    __syncwarp();
+    for (int e0 = 0; e0 <= A.E; e0 += 32) {
+      const int e = e0 + lane;
+      const int mine = e < A.E ? (groups[A.E + 2 + e] - groups[A.E + 1 + e] + P.nt - 1) / P.nt : 0;
+      int t = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int v = __shfl_up_sync(kFull, t, o);
+        if (lane >= o) t += v;
+      }
+      if (e <= A.E) groups[e] = tile + t - mine;
+      tile += __shfl_sync(kFull, t, 31);
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = sh->tmem_base;
+  const uint32_t first = blockIdx.x / S, step = gridDim.x / S;
+  const Items items = {A.offsets ? groups : nullptr, A.offsets ? groups + A.E + 1 : nullptr, A.E, P.nt, P.ctiles,
+                       (int)(step / (uint32_t)P.ctiles), (int)(step % (uint32_t)P.ctiles),
+                       A.offsets ? (int64_t)groups[A.E] : (A.n + P.nt - 1) / P.nt, A.n};
+  // this CTA's k-steps [k0, k1): whole chunks of two
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+  const int steps = (int)((bytes + kStepBytes - 1) / kStepBytes), chunks = (steps + 1) / 2;
+  const int c0 = (int)((int64_t)chunks * rank / S), c1 = (int)((int64_t)chunks * (rank + 1) / S);
+  const int k0 = 2 * c0, k1 = min(2 * c1, steps);
+
+  if (warp < kEpiWarps) {
+    // ---------------- outputs ----------------
+    const int quarter = warp & 3, half = warp >> 2;
+    const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
+    bool ok = true;
+    uint32_t seen = 0;
+#pragma unroll 1
+    for (Cursor at(items, first); at.live(items) && ok; at.next(items), ++seen) {
+      const Item it = at.at(items);
+      const int j = it.j0 + 32 * quarter + lane;
+      const bool live = j < A.N;
+      // what the outputs need from memory, asked for before the sums are there
+      const float bias = has_bias && live ? A.bias[it.e * A.ldb + j] : 0.0f;
+      float rs[kMaxRows / 32];   // of 16 rows each, every other 16 of the tile
+#pragma unroll
+      for (int c = 0; c < kMaxRows / 32; ++c) {
+        const int x = 16 * (2 * c + half) + (lane & 15);
+        rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
+      }
+      const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)P.nt;
+      ok = __all_sync(kFull, mbar_wait(&sh->done[b], (seen >> 1) & 1u, failed));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+      for (int c = 0; c < kMaxRows / 32; ++c) {
+        const int x0 = 16 * (2 * c + half);
+        if (x0 >= it.rows) break;
+        uint32_t v[16];
+        tmem_load16(v, tacc + (uint32_t)x0);
+        tmem_wait_ld(v);
+        if (S > 1) {
+          float* to = reinterpret_cast<float*>(base) + x0 * CM + 32 * quarter + lane;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) to[x * CM] = __uint_as_float(v[x]);
+        } else if (!expire) {
+          const int left = it.rows - x0;
+          TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j;
+#pragma unroll
+          for (int x = 0; x < 16; ++x, to += A.ldo) {
+            const TOut y = output<TOut>(__uint_as_float(v[x]), has_rs, __shfl_sync(kFull, rs[c], x), has_bias, bias);
+            if (x < left && live) *to = y;
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->drained[b]);
+    }
+    if (expire && threadIdx.x == 0) *failed = 1;
+  } else if (warp < kMmaWarp) {
+    // ---------------- scales ----------------
+    const int q = warp - kEpiWarps;      // (a multiple of four before it: its quarter of the lanes)
+    const int len = (int)(((int64_t)A.K + 31) / 32);
+    const int r = 32 * q + lane;         // the channel and the row that this lane copies
+    const bool whole = P.whole != 0;
+    const int depth = whole ? kScaleRing : kScaleRing / 2, pitch = whole ? 16 : 32;
+    const uint32_t slot_bytes = (uint32_t)(pitch * scale_rows(P.nt));
+    const uint32_t buf = smem_u32(scales);
+    const uint32_t slots = tmem + ((uint32_t)(32 * q) << 16) + 2u * (uint32_t)P.nt;
+    const int8_t *wrow = nullptr, *arow = nullptr;
+    const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.as));
+    int wlen = 0, alen = 0, nc = c0;     // (nc: the chunk that is copied next)
+    Cursor ahead(items, first);
+    auto rows_of = [&]() {
+      const Item it = ahead.at(items);
+      wlen = it.j0 + r < A.N ? len : -16;
+      alen = r < it.rows ? len : -16;
+      wrow = reinterpret_cast<const int8_t*>(A.ws) + (wlen > 0 ? it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws : 0);
+      arow = reinterpret_cast<const int8_t*>(A.as) + (alen > 0 ? (it.r0 + r) * A.ldas : 0);
+    };
+    auto copy = [&](uint32_t slot) {
+      if (ahead.live(items)) {
+        const uint32_t to = buf + slot * slot_bytes + (uint32_t)(pitch * r);
+        const int ws = i8::row_shift<1>(wrow), as = i8::row_shift<1>(arow);
+        i8::copy_chunk(to, wrow, ws, 16 * nc, wlen, any);
+        if (!whole) i8::copy_chunk(to + 16u, wrow, ws, 16 * nc + 16, wlen, any);
+        if (r < P.nt) {
+          i8::copy_chunk(to + (uint32_t)(pitch * CM), arow, as, 16 * nc, alen, any);
+          if (!whole) i8::copy_chunk(to + (uint32_t)(pitch * CM) + 16u, arow, as, 16 * nc + 16, alen, any);
+        }
+        if (++nc == c1) {
+          nc = c0;
+          ahead.next(items);
+          if (ahead.live(items)) rows_of();
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (ahead.live(items)) rows_of();
+    for (int d = 0; d < depth - 1; ++d) copy((uint32_t)d);
+    uint32_t slot = 0, ph = 1, from = 0;
+    bool ok = true;
+    // (to the end even after an expired wait: the four warps meet in every turn)
+#pragma unroll 1
+    for (Cursor at(items, first); at.live(items); at.next(items)) {
+      // the shifts of the rows that this lane reads
+      int shift[8] = {};
+      const int words = (P.nt + 31) >> 5;
+      if (!whole) {
+        const Item it = at.at(items);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          shift[x] = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.ws + it.e * A.gws + (int64_t)(it.j0 + 32 * x + lane) * A.ldws));
+          shift[4 + x] = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.as + (it.r0 + 32 * x + lane) * A.ldas));
+        }
+      }
+#pragma unroll 1
+      for (int c = c0; c < c1; ++c) {
+        if (whole) asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing - 2) : "memory");
+        else asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing / 2 - 2) : "memory");
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kScaleWarps) : "memory");   // all copies of this chunk, all reads of the last
+        copy(from == 0 ? (uint32_t)depth - 1 : from - 1);
+        const uint32_t row = buf + from * slot_bytes + (uint32_t)(pitch * lane);
+        if (++from == (uint32_t)depth) from = 0;
+        ok = __all_sync(kFull, ok && mbar_wait(&sh->sempty[slot], ph, failed));
+        if (ok) {
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t v[16];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              uint32_t s[4] = {0u, 0u, 0u, 0u};
+              if (h == 0 || x < words) {
+                // (what lies behind the tile's rows scales no output)
+                const uint32_t p = row + (uint32_t)(pitch * (CM * h + 32 * x));
+                i8::lds_chunk(s, p);
+                if (!whole) {
+                  uint32_t hi[4], m[4];
+                  i8::lds_chunk(hi, p + 16u);
+                  i8::merge16(m, s, hi, shift[4 * h + x]);
+#pragma unroll
+                  for (int y = 0; y < 4; ++y) s[y] = m[y];
+                }
+              }
+#pragma unroll
+              for (int y = 0; y < 4; ++y) v[4 * y + x] = s[y];
+            }
+            tmem_store16(slots + (uint32_t)kSlotCols * slot + 16u * (uint32_t)h, v);
+          }
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh->sfull[slot]);
+        }
+        if (++slot == kSlots) {
+          slot = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    cp_async_wait_all();
+  } else if (warp == kMmaWarp) {
+    // ---------------- MMAs ----------------
+    const bool lead = elect_one();
+    const uint32_t d = uniform(tmem);
+    const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
+    uint32_t s = 0, ph = 0, slot = 0, sph = 0, made = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (Cursor at(items, first); at.live(items) && ok; at.next(items), ++made) {
+      const Item it = at.at(items);
+      const uint32_t b = made & 1u, acc = d + b * (uint32_t)P.nt;
+      const uint32_t idesc = uniform(idesc_f4(CM, (it.rows + 15) & ~15));
+      ok = __all_sync(kFull, mbar_wait(&sh->drained[b], ((made >> 1) & 1u) ^ 1u, failed));
+      if (!ok) break;
+#pragma unroll 1
+      for (int k = k0; k < k1; ++k) {
+        if ((k & 1) == 0) ok = __all_sync(kFull, mbar_wait(&sh->sfull[slot], sph, failed));
+        ok = ok && __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
+        const uint64_t bd = ad + (uint64_t)(CM * kStepBytes >> 4);
+        const uint32_t sf = d + 2u * (uint32_t)P.nt + (uint32_t)kSlotCols * slot + 8u * (uint32_t)(k & 1);
+        const int64_t left = bytes - (int64_t)k * kStepBytes;
+        if (lead) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e == 0 || left > 32 * e)
+              mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
+                      sf + 4 * (e >> 1), sf + 16 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
+          mma_commit(&sh->empty[s]);
+          if ((k & 1) || k + 1 == k1) mma_commit(&sh->sempty[slot]);
+        }
+        __syncwarp();
+        if ((k & 1) || k + 1 == k1) {
+          if (++slot == kSlots) {
+            slot = 0;
+            sph ^= 1u;
+          }
+        }
+        if (++s == (uint32_t)P.stages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+      if (ok && lead) mma_commit(&sh->done[b]);
+      __syncwarp();
+    }
+    if (lead) {
+      // no MMA outlives its operands and its tensor memory
+      mma_commit(&sh->left);
+      mbar_wait(&sh->left, 0, &sh->left_failed);
+    }
+    __syncwarp();
+  } else if constexpr (kTma) {
+    // ---------------- copies ----------------
+    if (lane == 0) {
+      uint32_t s = 0, ph = 1;
+      int64_t copied = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (Cursor at(items, first); at.live(items) && ok; at.next(items)) {
+        const Item it = at.at(items);
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k) {
+          ok = mbar_wait(&sh->empty[s], ph, failed);
+          if (!ok) break;
+          const uint32_t to = smem_u32(base + s * stage_bytes), bar = smem_u32(&sh->full[s]);
+          mbar_arrive_tx(&sh->full[s], (uint32_t)stage_bytes);
+          copy_w(to, &wmap, k * kStepBytes, it.j0, it.e, bar);
+          copy_a(to + CM * kStepBytes, &amap, k * kStepBytes, (int)it.r0, bar);
+          ++copied;
+          if (++s == (uint32_t)P.stages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      if (!ok)
+        // no copy outlives its CTA
+        for (int64_t k = copied > P.stages ? copied - P.stages : 0; k < copied; ++k)
+          mbar_wait(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed);
+    }
+  } else {
+    // ---------------- loads ----------------
+    // A lane takes 16-byte pieces; a row's start may be anywhere.
+    const int l = (int)threadIdx.x - 32 * kCopyWarp;
+    const int c = l & 7;
+    uint32_t s = 0, ph = 1;
+    bool ok = true;
+#pragma unroll 1
+    for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
+      const Item it = cur.at(items);
+#pragma unroll 1
+      for (int k = k0; k < k1; ++k) {
+        ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
+        if (!ok) break;
+        const uint32_t to = smem_u32(base + s * stage_bytes);
+        const int at = k * kStepBytes + 16 * c;
+        const int rows = CM + ((it.rows + 15) & ~15);
+#pragma unroll 1
+        for (int r0 = l >> 3; r0 < rows; r0 += 4 * kLoadWarps * 4) {
+          uint32_t v[4][4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = r0 + u * 4 * kLoadWarps;
+            const bool chan = r < CM;
+            const bool live = r < rows && (chan ? it.j0 + r < A.N : r - CM < it.rows);
+            const int8_t* row = reinterpret_cast<const int8_t*>(
+                !live ? A.a : (chan ? A.w + it.e * A.gw + (int64_t)(it.j0 + r) * A.ldw : A.a + (it.r0 + r - CM) * A.lda));
+            i8::load16<1>(v[u], row, i8::row_shift<1>(row), at, live ? (int)bytes : -16);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = r0 + u * 4 * kLoadWarps;
+            if (r < rows) sts128(to + 128u * (uint32_t)r + 16u * (uint32_t)(c ^ (r & 7)), v[u]);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->full[s]);
+        if (++s == (uint32_t)P.stages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.cols) : "memory");
+  if (S > 1) {
+    cluster_sync();   // every CTA's sums are in its shared memory
+    bool redo = false;
+    for (uint32_t p = 0; p < S; ++p) redo |= __float_as_int(peer_load(peer_addr(smem_u32(&sh->failed), p))) != 0;
+    const Cursor at(items, first);   // (one tile)
+    if (at.live(items)) {
+      const Item it = at.at(items);
+      if (redo) {
+        plain_rows(A, it, (int)rank, (int)S);
+      } else if (threadIdx.x < 2 * CM) {
+        const int j = it.j0 + (int)(threadIdx.x & (CM - 1));
+        const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
+        if (j < A.N) {
+          const float bias = has_bias ? A.bias[it.e * A.ldb + j] : 0.0f;
+          uint32_t from[8];
+#pragma unroll
+          for (uint32_t p = 0; p < 8; ++p) from[p] = peer_addr(smem_u32(base) + 4u * (threadIdx.x & (CM - 1)), p < S ? p : 0);
+#pragma unroll 1
+          for (int x = (int)rank + (int)S * (int)(threadIdx.x / CM); x < it.rows; x += 2 * (int)S) {
+            const float rs = has_rs ? A.row_scale[it.r0 + x] : 1.0f;
+            float f[8];
+#pragma unroll
+            for (uint32_t p = 0; p < 8; ++p) f[p] = p < S ? peer_load(from[p] + 4u * CM * (uint32_t)x) : 0.0f;
+            float sum = f[0];
+#pragma unroll
+            for (uint32_t p = 1; p < 8; ++p)
+              if (p < S) sum = __fadd_rn(sum, f[p]);
+            static_cast<TOut*>(A.out)[(it.r0 + x) * A.ldo + j] = output<TOut>(sum, has_rs, rs, has_bias, bias);
+          }
+        }
+      }
+    }
+    cluster_sync();   // no CTA leaves while its sums are read
+  } else if (*failed) {
+    for (Cursor at(items, first); at.live(items); at.next(items)) plain_rows(A, at.at(items), 0, 1);
+  }
+}
+
+template <typename TOut, bool kTma>
+cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const CUtensorMap& wmap, const CUtensorMap& amap, cudaStream_t st,
+                        int expire) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(done, k_mx4_tile<TOut, kTma>, 227 * 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)P.ctas);
+  cfg.blockDim = dim3(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps));
+  cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)P.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = P.split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k_mx4_tile<TOut, kTma>, A, wmap, amap, P, expire);
+}
+
+// Whether rows start at multiples of 16 bytes.
+bool rows_whole(const uint8_t* p, int64_t ld, int64_t rows) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(rows > 1 ? ld : 0)) & 15) == 0;
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
+  const int sms = sm_count();
+  TilePlan P = {};
+  P.ctiles = (int)(((int64_t)A.N + CM - 1) / CM);
+  // rows of a tile: the rows, or a group's on average, in equal parts
+  const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = (A.n + some - 1) / some;
+  const int64_t parts = (mean + kMaxRows - 1) / kMaxRows;
+  P.nt = (int)std::min<int64_t>(kMaxRows, ((mean + parts - 1) / parts + 15) / 16 * 16);
+  const int64_t rtiles = A.offsets ? some + (A.n - some) / P.nt : (A.n + P.nt - 1) / P.nt;   // at most
+  const int64_t tiles = rtiles * P.ctiles;
+  const int64_t chunks = ((int64_t)A.K + 511) / 512;
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+  CUtensorMap wmap, amap;
+  const bool tma = code_map(&wmap, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) && code_map(&amap, A.a, bytes, A.n, A.lda, 0, 0, P.nt);
+  // two CTAs of an SM where their tensor memory and registers have room
+  const bool two = tma && 2 * P.nt + kSlots * kSlotCols <= 256;
+  P.cols = two ? 256 : 512;
+  const int64_t room = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0);
+  P.stages = (int)std::min<int64_t>(kMaxStages, room / ((CM + P.nt) * kStepBytes));
+  const int64_t slots = (two ? 2 : 1) * (int64_t)sms;
+  P.split = 1;
+  while (P.split < 8 && 2 * P.split <= chunks && tiles * P.split * 2 <= slots) P.split *= 2;
+  P.ctas = (int)(P.split > 1 ? tiles * P.split : std::min(tiles, slots));
+  P.whole = rows_whole(A.as, A.ldas, A.n) && rows_whole(A.ws, A.ldws, A.N) && (A.E == 1 || (A.gws & 15) == 0);
+  if (tma) {
+    if (A.type == BMLP_F32) return launch_tile<float, true>(A, P, wmap, amap, st, expire);
+    if (A.type == BMLP_F16) return launch_tile<__half, true>(A, P, wmap, amap, st, expire);
+    return launch_tile<__nv_bfloat16, true>(A, P, wmap, amap, st, expire);
+  }
+  if (A.type == BMLP_F32) return launch_tile<float, false>(A, P, wmap, amap, st, expire);
+  if (A.type == BMLP_F16) return launch_tile<__half, false>(A, P, wmap, amap, st, expire);
+  return launch_tile<__nv_bfloat16, false>(A, P, wmap, amap, st, expire);
+}
+
+}  // namespace bk
