@@ -8,18 +8,22 @@
 // Warps:
 //   - one thread copies stages of 256 codes of every row into a ring (rows at places that
 //     tensor copies cannot take: eight warps do, shifting whole 16-byte pieces);
-//   - four warps take the scales of 512 codes (16 bytes) of every row from global memory
-//     through shared memory into tensor memory, where the MMA reads row r's at lane r % 32
-//     of column r / 32, four blocks' bytes in a column, and in each quarter of the lanes;
-//   - one warp issues the MMAs, 64 codes (two blocks) each;
+//   - four warps take the scales of 512 codes (16 bytes) of every row, a row each lane's own,
+//     through a ring into the stages, as cells of 128 rows x 128 codes: the four bytes
+//     of row r at 16 (r % 32) + 4 (r / 32), which is how the MMA wants them in the lanes and
+//     columns of tensor memory;
+//   - one warp copies a stage's cells there (to all four quarters of the lanes) and issues the
+//     MMAs, 64 codes (two blocks) each;
 //   - eight warps write finished tiles while the next one's MMAs run (two accumulators).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share K and add their sums up
 // in the order of their ranks, through distributed shared memory.
 // By group: the row tiles of a group start at its first row; what a tile has of the next
 // group's rows is multiplied and dropped.
 // Every wait is bounded; if one expires the CTA's tiles are made again on CUDA cores.
-// Measured (us): 1 x 8192 -> 8192 11.6 (scales one piece ahead in registers 16.3: a turn then takes
-// a memory latency), 100 x 4096 -> 8192 17.4, 96 x 4096 -> 2048 by 32 26, 16384 x 8192 -> 8192 748.
+// Measured (us): 1 x 8192 -> 8192 11.0, 100 x 4096 -> 8192 10.3, 96 x 4096 -> 2048 by 32 24.9, 16384 x 8192 ->
+// 8192 619.  (Scales one piece ahead in registers: 16.3, 19.3, 41, 1182, a turn then takes a
+// memory latency.  Stored to tensor memory by four warps, each with all rows': 11.6, 17.4, 26.4,
+// 748, 1,550 clocks of theirs per 512 codes.)
 #include <algorithm>
 
 #include <cuda.h>
@@ -39,13 +43,15 @@ constexpr int kMaxRows = 128;
 constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
 constexpr int kEpiWarps = 8, kScaleWarps = 4, kMmaWarp = kEpiWarps + kScaleWarps, kCopyWarp = kMmaWarp + 1;
 constexpr int kLoadWarps = 8;
+constexpr int kRawRow = kStepBytes + 16; // of a row at any place: the chunks around 128 bytes
+constexpr int kDeep = 3;                 // steps of them in flight, and the one that is read
 constexpr int kMaxStages = 8;
-constexpr int kSlots = 4;                // of scales, 512 codes each, in tensor memory
-constexpr int kSlotCols = 32;            // 4 x 4 columns of the channels', as many of the rows'
+constexpr int kCell = 512;               // bytes of the scales of 128 rows x 128 codes
+constexpr int kCells = 4 * kCell;        // of a stage: two of the channels, two of the rows
+constexpr int kSlotCols = 16;            // of tensor memory for them
 
 struct __align__(8) TileShared {
   unsigned long long full[kMaxStages], empty[kMaxStages];
-  unsigned long long sfull[kSlots], sempty[kSlots];
   unsigned long long done[2], drained[2];
   unsigned long long left;
   uint32_t tmem_base;
@@ -63,10 +69,9 @@ struct TilePlan {
 };
 
 constexpr int kScaleRing = 6;            // 512 codes' scales of every row in flight (three where rows start anywhere)
-// rows of the ring: all that a warp reads at a time
-__host__ __device__ constexpr int scale_rows(int nt) { return CM + (nt + 31) / 32 * 32; }
-int64_t tile_smem(const Mx4Args& A, int nt, int stages) {
-  return 1024 + (int64_t)(CM + nt) * stages * kStepBytes + kScaleRing * 16 * scale_rows(nt) + (int64_t)sizeof(TileShared) +
+__host__ __device__ constexpr int stage_size(int nt) { return (CM + nt) * kStepBytes + kCells; }
+int64_t tile_smem(const Mx4Args& A, int nt, int stages, bool tma) {
+  return 1024 + (tma ? 0 : (int64_t)kDeep * kRawRow * (CM + nt)) + (int64_t)stages * stage_size(nt) + kScaleRing * 16 * (CM + nt) + (int64_t)sizeof(TileShared) +
          (A.offsets ? 8 * ((int64_t)A.E + 1) : 0);
 }
 
@@ -83,9 +88,14 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t local_addr, uint32_t rank
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local_addr), "r"(rank));
   return a;
 }
-__device__ __forceinline__ float peer_load(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+__device__ __forceinline__ uint32_t peer_load(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 peer_load4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
 
@@ -95,6 +105,22 @@ __device__ __forceinline__ void mma_mx4(uint32_t tmem_d, uint64_t adesc, uint64_
       "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
       " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
       ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate));
+}
+
+// Descriptor of a cell: 32 rows of 16 bytes one after another, no swizzle.
+__device__ __forceinline__ uint64_t cell_desc(uint32_t saddr) {
+  uint64_t d = (saddr & 0x3FFFFu) >> 4;
+  d |= (uint64_t)(128 >> 4) << 16;   // from 8 rows to the next, in either sense
+  d |= (uint64_t)(128 >> 4) << 32;
+  d |= (uint64_t)1 << 46;            // descriptor version (sm_100 family)
+  return d;
+}
+// A cell to four columns of tensor memory, 32 lanes in each quarter.
+__device__ __forceinline__ void copy_cell(uint32_t tmem_to, uint64_t cell) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem_to), "l"(cell) : "memory");
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 
 __device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -171,16 +197,68 @@ static __device__ __noinline__ void plain_rows(const Mx4Args& A, const Item& it,
   }
 }
 
+// Outputs of rows rank, rank + S, .. of a tile from the S CTAs' sums ([row][channel] at `sums` of each
+// one's shared memory), added in the order of their ranks: a warp takes a row, a lane four channels.
+// rs: of the warp's l-th row in lane l.  Eight loads are under way at a time.
+template <typename TOut, int S>
+__device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint32_t rank, uint32_t sums, float rs,
+                                          const float (&bias)[4]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+  constexpr int kRows = 8 / S;
+  uint32_t from[S];
+#pragma unroll
+  for (int p = 0; p < S; ++p) from[p] = peer_addr(sums + 16u * (uint32_t)lane, (uint32_t)p);
+  const int j = it.j0 + 4 * lane;
+  const bool vec = j + 4 <= A.N && ((A.ldo | it.j0) & 3) == 0 && (reinterpret_cast<uintptr_t>(A.out) & (4 * sizeof(TOut) - 1)) == 0;
+  int l = 0;
+#pragma unroll 1
+  for (int x0 = (int)rank + S * warp; x0 < it.rows; x0 += kRows * S * warps) {
+    float4 f[kRows][S];
+#pragma unroll
+    for (int y = 0; y < kRows; ++y)
+#pragma unroll
+      for (int p = 0; p < S; ++p)
+        if (y == 0 || x0 + y * S * warps < it.rows) f[y][p] = peer_load4(from[p] + 4u * CM * (uint32_t)(x0 + y * S * warps));
+#pragma unroll
+    for (int y = 0; y < kRows; ++y, ++l) {
+      const int x = x0 + y * S * warps;
+      const float by = __shfl_sync(kFull, rs, l);
+      if (x >= it.rows) break;
+      float4 sum = f[y][0];
+#pragma unroll
+      for (int p = 1; p < S; ++p) {
+        sum.x = __fadd_rn(sum.x, f[y][p].x);
+        sum.y = __fadd_rn(sum.y, f[y][p].y);
+        sum.z = __fadd_rn(sum.z, f[y][p].z);
+        sum.w = __fadd_rn(sum.w, f[y][p].w);
+      }
+      union { TOut e[4]; uint2 two; uint4 four; } out;
+      const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out.e[e] = output<TOut>(v[e], A.row_scale != nullptr, by, A.bias != nullptr, bias[e]);
+      TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x) * A.ldo + j;
+      if (vec) {
+        if constexpr (sizeof(TOut) == 4) *reinterpret_cast<uint4*>(to) = out.four;
+        else *reinterpret_cast<uint2*>(to) = out.two;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < A.N) to[e] = out.e[e];
+      }
+    }
+  }
+}
+
 template <typename TOut, bool kTma>
 __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps), kTma ? 2 : 1)
     k_mx4_tile(const Mx4Args A, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap,
                const TilePlan P, int expire) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const int stage_bytes = (CM + P.nt) * kStepBytes;
+  const int stage_bytes = stage_size(P.nt);
   uint8_t* scales = base + P.stages * stage_bytes;
-  const int ring_bytes = kScaleRing * 16 * scale_rows(P.nt);
-  TileShared* sh = reinterpret_cast<TileShared*>(scales + ring_bytes);
+  const int ring_bytes = kScaleRing * 16 * (CM + P.nt);
+  TileShared* sh = reinterpret_cast<TileShared*>(scales + ring_bytes + (kTma ? 0 : kDeep * kRawRow * (CM + P.nt)));
   int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t S = (uint32_t)P.split, rank = S > 1 ? cluster_rank() : 0u;
@@ -188,12 +266,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P.stages; ++s) {
-      mbar_init(&sh->full[s], kTma ? 1 : kLoadWarps);
+      mbar_init(&sh->full[s], kScaleWarps + (kTma ? 1 : kLoadWarps));
       mbar_init(&sh->empty[s], 1);
-    }
-    for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&sh->sfull[s], kScaleWarps);
-      mbar_init(&sh->sempty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sh->done[b], 1);
@@ -308,35 +382,47 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     if (expire && threadIdx.x == 0) *failed = 1;
   } else if (warp < kMmaWarp) {
     // ---------------- scales ----------------
-    const int q = warp - kEpiWarps;      // (a multiple of four before it: its quarter of the lanes)
+    const int q = warp - kEpiWarps;
     const int len = (int)(((int64_t)A.K + 31) / 32);
-    const int r = 32 * q + lane;         // the channel and the row that this lane copies
-    const bool whole = P.whole != 0;
+    const int r = 32 * q + lane;         // this lane's channel and row
+    const bool whole = P.whole != 0, has_row = r < P.nt;
     const int depth = whole ? kScaleRing : kScaleRing / 2, pitch = whole ? 16 : 32;
-    const uint32_t slot_bytes = (uint32_t)(pitch * scale_rows(P.nt));
-    const uint32_t buf = smem_u32(scales);
-    const uint32_t slots = tmem + ((uint32_t)(32 * q) << 16) + 2u * (uint32_t)P.nt;
-    const int8_t *wrow = nullptr, *arow = nullptr;
+    const uint32_t slot_bytes = (uint32_t)(pitch * (CM + P.nt));
+    const uint32_t ring = smem_u32(scales) + (uint32_t)(pitch * r);
+    const uint32_t cells = smem_u32(base) + (uint32_t)(stage_bytes - kCells) + 16u * (uint32_t)lane + 4u * (uint32_t)q;
     const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.as));
-    int wlen = 0, alen = 0, nc = c0;     // (nc: the chunk that is copied next)
+    // the chunks that are copied next, and what is left of their rows from there on
+    const int8_t *wfrom = any, *afrom = any;
+    int wleft = 0, aleft = 0, nc = c0;
     Cursor ahead(items, first);
     auto rows_of = [&]() {
       const Item it = ahead.at(items);
-      wlen = it.j0 + r < A.N ? len : -16;
-      alen = r < it.rows ? len : -16;
-      wrow = reinterpret_cast<const int8_t*>(A.ws) + (wlen > 0 ? it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws : 0);
-      arow = reinterpret_cast<const int8_t*>(A.as) + (alen > 0 ? (it.r0 + r) * A.ldas : 0);
+      const bool wlive = it.j0 + r < A.N, alive = r < it.rows;
+      const int8_t* w = reinterpret_cast<const int8_t*>(A.ws) + it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws;
+      const int8_t* a = reinterpret_cast<const int8_t*>(A.as) + (it.r0 + r) * A.ldas;
+      const int ws = i8::row_shift<1>(w), as = i8::row_shift<1>(a);
+      wfrom = wlive ? w - ws + 16 * c0 : any;
+      afrom = alive ? a - as + 16 * c0 : any;
+      wleft = wlive ? len + ws - 16 * c0 : 0;
+      aleft = alive ? len + as - 16 * c0 : 0;
+    };
+    auto chunk = [&](uint32_t to, const int8_t* from, int left) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"(to), "l"(left > 0 ? from : any), "r"(min(16, max(0, left))) : "memory");
     };
     auto copy = [&](uint32_t slot) {
       if (ahead.live(items)) {
-        const uint32_t to = buf + slot * slot_bytes + (uint32_t)(pitch * r);
-        const int ws = i8::row_shift<1>(wrow), as = i8::row_shift<1>(arow);
-        i8::copy_chunk(to, wrow, ws, 16 * nc, wlen, any);
-        if (!whole) i8::copy_chunk(to + 16u, wrow, ws, 16 * nc + 16, wlen, any);
-        if (r < P.nt) {
-          i8::copy_chunk(to + (uint32_t)(pitch * CM), arow, as, 16 * nc, alen, any);
-          if (!whole) i8::copy_chunk(to + (uint32_t)(pitch * CM) + 16u, arow, as, 16 * nc + 16, alen, any);
+        const uint32_t to = ring + slot * slot_bytes;
+        chunk(to, wfrom, wleft);
+        if (!whole) chunk(to + 16u, wfrom + 16, wleft - 16);
+        if (has_row) {
+          chunk(to + (uint32_t)(pitch * CM), afrom, aleft);
+          if (!whole) chunk(to + (uint32_t)(pitch * CM) + 16u, afrom + 16, aleft - 16);
         }
+        wfrom += 16;
+        afrom += 16;
+        wleft -= 16;
+        aleft -= 16;
         if (++nc == c1) {
           nc = c0;
           ahead.next(items);
@@ -346,65 +432,60 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
     if (ahead.live(items)) rows_of();
-    for (int d = 0; d < depth - 1; ++d) copy((uint32_t)d);
-    uint32_t slot = 0, ph = 1, from = 0;
-    bool ok = true;
-    // (to the end even after an expired wait: the four warps meet in every turn)
 #pragma unroll 1
-    for (Cursor at(items, first); at.live(items); at.next(items)) {
-      // the shifts of the rows that this lane reads
-      int shift[8] = {};
-      const int words = (P.nt + 31) >> 5;
+    for (int d = 0; d < depth - 1; ++d) copy((uint32_t)d);
+    uint32_t s = 0, ph = 1, from = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (Cursor at(items, first); at.live(items) && ok; at.next(items)) {
+      int wshift = 0, ashift = 0;
       if (!whole) {
         const Item it = at.at(items);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          shift[x] = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.ws + it.e * A.gws + (int64_t)(it.j0 + 32 * x + lane) * A.ldws));
-          shift[4 + x] = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.as + (it.r0 + 32 * x + lane) * A.ldas));
-        }
+        wshift = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.ws + it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws));
+        ashift = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.as + (it.r0 + r) * A.ldas));
       }
 #pragma unroll 1
-      for (int c = c0; c < c1; ++c) {
+      for (int c = c0; c < c1 && ok; ++c) {
         if (whole) asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing - 2) : "memory");
         else asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing / 2 - 2) : "memory");
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * kScaleWarps) : "memory");   // all copies of this chunk, all reads of the last
-        copy(from == 0 ? (uint32_t)depth - 1 : from - 1);
-        const uint32_t row = buf + from * slot_bytes + (uint32_t)(pitch * lane);
-        if (++from == (uint32_t)depth) from = 0;
-        ok = __all_sync(kFull, ok && mbar_wait(&sh->sempty[slot], ph, failed));
-        if (ok) {
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        // (a lane reads what it copied itself)
+        uint32_t w[4], a[4] = {0u, 0u, 0u, 0u};
+        const uint32_t src = ring + from * slot_bytes;
+        i8::lds_chunk(w, src);
+        if (has_row) i8::lds_chunk(a, src + (uint32_t)(pitch * CM));
+        if (!whole) {
+          uint32_t hi[4], m[4];
+          i8::lds_chunk(hi, src + 16u);
+          i8::merge16(m, w, hi, wshift);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t v[16];
+          for (int y = 0; y < 4; ++y) w[y] = m[y];
+          if (has_row) {
+            i8::lds_chunk(hi, src + (uint32_t)(pitch * CM) + 16u);
+            i8::merge16(m, a, hi, ashift);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              uint32_t s[4] = {0u, 0u, 0u, 0u};
-              if (h == 0 || x < words) {
-                // (what lies behind the tile's rows scales no output)
-                const uint32_t p = row + (uint32_t)(pitch * (CM * h + 32 * x));
-                i8::lds_chunk(s, p);
-                if (!whole) {
-                  uint32_t hi[4], m[4];
-                  i8::lds_chunk(hi, p + 16u);
-                  i8::merge16(m, s, hi, shift[4 * h + x]);
-#pragma unroll
-                  for (int y = 0; y < 4; ++y) s[y] = m[y];
-                }
-              }
-#pragma unroll
-              for (int y = 0; y < 4; ++y) v[4 * y + x] = s[y];
-            }
-            tmem_store16(slots + (uint32_t)kSlotCols * slot + 16u * (uint32_t)h, v);
+            for (int y = 0; y < 4; ++y) a[y] = m[y];
           }
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh->sfull[slot]);
         }
-        if (++slot == kSlots) {
-          slot = 0;
-          ph ^= 1u;
+        copy(from == 0 ? (uint32_t)depth - 1 : from - 1);
+        if (++from == (uint32_t)depth) from = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (2 * c + h >= k1) break;
+          ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
+          if (!ok) break;
+          const uint32_t to = cells + s * (uint32_t)stage_bytes;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            sts32(to + (uint32_t)(kCell * y), w[2 * h + y]);
+            if (has_row) sts32(to + (uint32_t)(kCell * (2 + y)), a[2 * h + y]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh->full[s]);
+          if (++s == (uint32_t)P.stages) {
+            s = 0;
+            ph ^= 1u;
+          }
         }
       }
     }
@@ -414,7 +495,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     const bool lead = elect_one();
     const uint32_t d = uniform(tmem);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
-    uint32_t s = 0, ph = 0, slot = 0, sph = 0, made = 0;
+    const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + (uint32_t)(stage_bytes - kCells)));
+    uint32_t s = 0, ph = 0, made = 0;
     bool ok = true;
 #pragma unroll 1
     for (Cursor at(items, first); at.live(items) && ok; at.next(items), ++made) {
@@ -425,30 +507,25 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       if (!ok) break;
 #pragma unroll 1
       for (int k = k0; k < k1; ++k) {
-        if ((k & 1) == 0) ok = __all_sync(kFull, mbar_wait(&sh->sfull[slot], sph, failed));
-        ok = ok && __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
+        ok = __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
-        const uint64_t bd = ad + (uint64_t)(CM * kStepBytes >> 4);
-        const uint32_t sf = d + 2u * (uint32_t)P.nt + (uint32_t)kSlotCols * slot + 8u * (uint32_t)(k & 1);
-        const int64_t left = bytes - (int64_t)k * kStepBytes;
+        const uint64_t off = (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
+        const uint64_t ad = desc0 + off, bd = ad + (uint64_t)(CM * kStepBytes >> 4), cd = cells0 + off;
+        const uint32_t sf = d + 2u * (uint32_t)P.nt + (uint32_t)kSlotCols * s;
+        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
         if (lead) {
+          // (copies and MMAs of a thread run in their order)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) copy_cell(sf + 4 * e, cd + (uint64_t)(e * (kCell >> 4)));
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (e == 0 || left > 32 * e)
               mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
-                      sf + 4 * (e >> 1), sf + 16 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
+                      sf + 4 * (e >> 1), sf + 8 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
           mma_commit(&sh->empty[s]);
-          if ((k & 1) || k + 1 == k1) mma_commit(&sh->sempty[slot]);
         }
         __syncwarp();
-        if ((k & 1) || k + 1 == k1) {
-          if (++slot == kSlots) {
-            slot = 0;
-            sph ^= 1u;
-          }
-        }
         if (++s == (uint32_t)P.stages) {
           s = 0;
           ph ^= 1u;
@@ -477,7 +554,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
           ok = mbar_wait(&sh->empty[s], ph, failed);
           if (!ok) break;
           const uint32_t to = smem_u32(base + s * stage_bytes), bar = smem_u32(&sh->full[s]);
-          mbar_arrive_tx(&sh->full[s], (uint32_t)stage_bytes);
+          mbar_arrive_tx(&sh->full[s], (uint32_t)(stage_bytes - kCells));
           copy_w(to, &wmap, k * kStepBytes, it.j0, it.e, bar);
           copy_a(to + CM * kStepBytes, &amap, k * kStepBytes, (int)it.r0, bar);
           ++copied;
@@ -494,48 +571,87 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     }
   } else {
     // ---------------- loads ----------------
-    // A lane takes 16-byte pieces; a row's start may be anywhere.
-    const int l = (int)threadIdx.x - 32 * kCopyWarp;
-    const int c = l & 7;
-    uint32_t s = 0, ph = 1;
+    // Each warp for itself: the aligned 16-byte chunks around 16 channels' and nt / 8 rows' codes
+    // to a ring, kDeep steps ahead, and from there, shifted to their places, to the stage.
+    const int w = warp - kCopyWarp, c = lane & 7, sub = lane >> 3, mine = P.nt / kLoadWarps;
+    const int len = (int)bytes;
+    const uint32_t raw_bytes = (uint32_t)(kRawRow * (CM + P.nt));
+    const uint32_t raw = smem_u32(base + P.stages * stage_bytes + ring_bytes) + (uint32_t)(kRawRow * 16 * w);
+    const uint32_t raw_a = raw + (uint32_t)(kRawRow * (CM - 16 * w + mine * w));
+    const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.a));
+    const int8_t *wrow = any, *arow = any;   // the warp's first
+    int wlive = 0, alive = 0, nk = k0;       // how many of its rows there are
+    Cursor ahead(items, first);
+    auto rows_of = [&](const Item& it) {
+      const int j = it.j0 + 16 * w, i = mine * w;
+      wlive = min(16, A.N - j);
+      alive = min(mine, it.rows - i);
+      wrow = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)j * A.ldw;
+      arow = reinterpret_cast<const int8_t*>(A.a) + (it.r0 + i) * A.lda;
+    };
+    auto copy = [&](uint32_t slot) {
+      if (ahead.live(items)) {
+        const int k = nk * kStepBytes;
+        auto part = [&](const int8_t* rows, int64_t ld, int all, int live, uint32_t to) {
+          const int8_t* row = rows + sub * ld;
+          for (int r = sub; r < all; r += 4, row += 4 * ld)
+            i8::copy_chunk(to + (uint32_t)(kRawRow * r + 16 * c), row, i8::row_shift<1>(row), k + 16 * c, r < live ? len : -16, any);
+          if (lane < all) {
+            row = rows + lane * ld;
+            i8::copy_chunk(to + (uint32_t)(kRawRow * lane + 128), row, i8::row_shift<1>(row), k + 128, lane < live ? len : -16, any);
+          }
+        };
+        part(wrow, A.ldw, 16, wlive, raw + slot * raw_bytes);
+        part(arow, A.lda, mine, alive, raw_a + slot * raw_bytes);
+        if (++nk == k1) {
+          nk = k0;
+          ahead.next(items);
+          if (ahead.live(items)) rows_of(ahead.at(items));
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (ahead.live(items)) rows_of(ahead.at(items));
+#pragma unroll 1
+    for (int d = 0; d < kDeep - 1; ++d) copy((uint32_t)d);
+    uint32_t s = 0, ph = 1, from = 0;
     bool ok = true;
 #pragma unroll 1
     for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
       const Item it = cur.at(items);
+      const int8_t* w0 = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)(it.j0 + 16 * w + sub) * A.ldw;
+      const int8_t* a0 = reinterpret_cast<const int8_t*>(A.a) + (it.r0 + mine * w + sub) * A.lda;
 #pragma unroll 1
       for (int k = k0; k < k1; ++k) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 2) : "memory");
+        __syncwarp();   // every lane's copies of this step, and its reads of the step before
+        copy(from == 0 ? kDeep - 1 : from - 1);
         ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
         if (!ok) break;
         const uint32_t to = smem_u32(base + s * stage_bytes);
-        const int at = k * kStepBytes + 16 * c;
-        const int rows = CM + ((it.rows + 15) & ~15);
-#pragma unroll 1
-        for (int r0 = l >> 3; r0 < rows; r0 += 4 * kLoadWarps * 4) {
-          uint32_t v[4][4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int r = r0 + u * 4 * kLoadWarps;
-            const bool chan = r < CM;
-            const bool live = r < rows && (chan ? it.j0 + r < A.N : r - CM < it.rows);
-            const int8_t* row = reinterpret_cast<const int8_t*>(
-                !live ? A.a : (chan ? A.w + it.e * A.gw + (int64_t)(it.j0 + r) * A.ldw : A.a + (it.r0 + r - CM) * A.lda));
-            i8::load16<1>(v[u], row, i8::row_shift<1>(row), at, live ? (int)bytes : -16);
+        auto part = [&](const int8_t* row, int64_t ld, int all, uint32_t src, int r0) {
+#pragma unroll 2
+          for (int r = sub; r < all; r += 4, row += 4 * ld) {
+            uint32_t lo[4], hi[4], v[4];
+            i8::lds_chunk(lo, src + (uint32_t)(kRawRow * r + 16 * c));
+            i8::lds_chunk(hi, src + (uint32_t)(kRawRow * r + 16 * c + 16));
+            i8::merge16(v, lo, hi, i8::row_shift<1>(row));
+            sts128(to + 128u * (uint32_t)(r0 + r) + 16u * (uint32_t)(c ^ ((r0 + r) & 7)), v);
           }
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int r = r0 + u * 4 * kLoadWarps;
-            if (r < rows) sts128(to + 128u * (uint32_t)r + 16u * (uint32_t)(c ^ (r & 7)), v[u]);
-          }
-        }
+        };
+        part(w0, A.ldw, 16, raw + from * raw_bytes, 16 * w);
+        part(a0, A.lda, mine, raw_a + from * raw_bytes, CM + mine * w);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh->full[s]);
+        if (++from == kDeep) from = 0;
         if (++s == (uint32_t)P.stages) {
           s = 0;
           ph ^= 1u;
         }
       }
     }
+    cp_async_wait_all();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -544,36 +660,28 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.cols) : "memory");
   if (S > 1) {
+    const Cursor at(items, first);   // (one tile)
+    const bool some = at.live(items);
+    const Item it = some ? at.at(items) : Item{};
+    const int warps = (int)blockDim.x >> 5;
+    // this rank's rows are rank, rank + S, ..; lane l keeps the factor of the warp's l-th
+    const int own = (int)rank + (int)S * (warp + warps * lane);
+    const float rs = A.row_scale && own < it.rows ? A.row_scale[it.r0 + own] : 1.0f;
+    const int j = it.j0 + 4 * lane;
+    float bias[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) bias[y] = A.bias && some && j + y < A.N ? A.bias[it.e * A.ldb + j + y] : 0.0f;
     cluster_sync();   // every CTA's sums are in its shared memory
     bool redo = false;
-    for (uint32_t p = 0; p < S; ++p) redo |= __float_as_int(peer_load(peer_addr(smem_u32(&sh->failed), p))) != 0;
-    const Cursor at(items, first);   // (one tile)
-    if (at.live(items)) {
-      const Item it = at.at(items);
-      if (redo) {
-        plain_rows(A, it, (int)rank, (int)S);
-      } else if (threadIdx.x < 2 * CM) {
-        const int j = it.j0 + (int)(threadIdx.x & (CM - 1));
-        const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
-        if (j < A.N) {
-          const float bias = has_bias ? A.bias[it.e * A.ldb + j] : 0.0f;
-          uint32_t from[8];
-#pragma unroll
-          for (uint32_t p = 0; p < 8; ++p) from[p] = peer_addr(smem_u32(base) + 4u * (threadIdx.x & (CM - 1)), p < S ? p : 0);
-#pragma unroll 1
-          for (int x = (int)rank + (int)S * (int)(threadIdx.x / CM); x < it.rows; x += 2 * (int)S) {
-            const float rs = has_rs ? A.row_scale[it.r0 + x] : 1.0f;
-            float f[8];
-#pragma unroll
-            for (uint32_t p = 0; p < 8; ++p) f[p] = p < S ? peer_load(from[p] + 4u * CM * (uint32_t)x) : 0.0f;
-            float sum = f[0];
-#pragma unroll
-            for (uint32_t p = 1; p < 8; ++p)
-              if (p < S) sum = __fadd_rn(sum, f[p]);
-            static_cast<TOut*>(A.out)[(it.r0 + x) * A.ldo + j] = output<TOut>(sum, has_rs, rs, has_bias, bias);
-          }
-        }
-      }
+    for (uint32_t p = 0; p < S; ++p) redo |= peer_load(peer_addr(smem_u32(&sh->failed), p)) != 0u;
+    if (redo) {
+      if (some) plain_rows(A, it, (int)rank, (int)S);
+    } else if (S == 2) {
+      join_sums<TOut, 2>(A, it, rank, smem_u32(base), rs, bias);
+    } else if (S == 4) {
+      join_sums<TOut, 4>(A, it, rank, smem_u32(base), rs, bias);
+    } else {
+      join_sums<TOut, 8>(A, it, rank, smem_u32(base), rs, bias);
     }
     cluster_sync();   // no CTA leaves while its sums are read
   } else if (*failed) {
@@ -590,7 +698,7 @@ cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const CUtensorMap& 
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.ctas);
   cfg.blockDim = dim3(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps));
-  cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages);
+  cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages, kTma);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -625,10 +733,10 @@ cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
   CUtensorMap wmap, amap;
   const bool tma = code_map(&wmap, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) && code_map(&amap, A.a, bytes, A.n, A.lda, 0, 0, P.nt);
   // two CTAs of an SM where their tensor memory and registers have room
-  const bool two = tma && 2 * P.nt + kSlots * kSlotCols <= 256;
+  const bool two = tma && P.nt <= 64;
   P.cols = two ? 256 : 512;
-  const int64_t room = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0);
-  P.stages = (int)std::min<int64_t>(kMaxStages, room / ((CM + P.nt) * kStepBytes));
+  const int64_t room = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0, tma);
+  P.stages = (int)std::min<int64_t>(two ? (256 - 2 * P.nt) / kSlotCols : kMaxStages, room / stage_size(P.nt));
   const int64_t slots = (two ? 2 : 1) * (int64_t)sms;
   P.split = 1;
   while (P.split < 8 && 2 * P.split <= chunks && tiles * P.split * 2 <= slots) P.split *= 2;
