@@ -1,0 +1,474 @@
+// kern_mx4_pair.cu -- the microscaled 4-bit product of many rows: 256 x 256 tiles by pairs of CTAs,
+// for operands that tensor copies can take (kern_mx4_tile.cu has the formats in shared and
+// tensor memory).
+//
+// A cluster of two CTAs computes 256 channels (MMA M) x up to 256 rows (N, as many as the tile
+// has, up to 32) with tcgen05.mma.cta_group::2.  CTA r copies channels 128 r .. + 127 and the r-th half
+// of the rows: 32 KB per 256 codes, in 512 clocks of MMA; its tensor memory receives the sums of
+// its channels and all rows, and it needs the scales of its channels and of all rows there.
+// The grid is persistent, a pair per two SMs.  Two accumulators of 256 columns and the scales
+// do not fit tensor memory side by side: the accumulators share 80 columns, which the epilogue
+// reads first.  Warps of a CTA: eight write outputs, eight bring scales, one thread copies codes
+// (both CTAs' copies complete on the even one's barriers), and on the even CTA one warp issues
+// the copies of scales to tensor memory and the MMAs.
+// Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
+#include <algorithm>
+
+#include "mx4_common.cuh"
+#include "tc_common.cuh"
+
+namespace bk {
+namespace {
+
+using namespace tc;
+using namespace mx4;
+
+constexpr int TP = 256;                  // channels, and rows at most, of a tile
+constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
+constexpr int kBlockBytes = 128 * kStepBytes;
+constexpr int kCells = 6 * kCell;        // of a stage: two of the channels, four of the rows (two halves of 128, twice)
+constexpr int kStageBytes = 2 * kBlockBytes + kCells;
+constexpr int kStages = 6;
+constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
+constexpr int kEpiWarps = 8, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kThreads = 32 * (kCopyWarp + 1);
+constexpr int kShared = 80;              // columns of both accumulators
+constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
+constexpr int kSlots = 3, kSlotCols = 24;
+static_assert(kSfCol + kSlots * kSlotCols <= 512 && kStageBytes % 1024 == 0, "tensor memory, swizzle atoms");
+// A wait tells a phase from the next by its parity, so the phase two before the one that is waited for must be
+// known to be over.  The last wait of a scale warp's unit before tells that of the MMAs up to kUnit + 1 +
+// kStages steps back, and the next asks for 2 kStages - 1 (the second of two stages).
+static_assert(kStages >= kUnit + 2, "phases");
+constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
+
+struct __align__(8) PairShared {
+  unsigned long long full[kStages], empty[kStages];
+  unsigned long long done[2], drained;
+  unsigned long long left;
+  uint32_t tmem_base;
+  int failed, left_failed;
+};
+constexpr int64_t pair_smem(int E) {
+  return 1024 + (int64_t)kStages * kStageBytes + (int64_t)sizeof(PairShared) + 8 * (int64_t)(E + 1);
+}
+
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Bounded wait with cluster-scope acquire (the barrier collects arrivals of the peer).
+__device__ __forceinline__ bool mbar_wait_cluster(unsigned long long* bar, uint32_t parity, volatile int* failed) {
+  const uint32_t a = smem_u32(bar);
+  uint32_t ok;
+  auto try_wait = [&]() {
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(a), "r"(parity) : "memory");
+  };
+  try_wait();
+  if (ok) return true;
+  const unsigned long long t0 = clock64();
+  while (true) {
+    try_wait();
+    if (ok) return true;
+    if (*failed) return false;
+    if (clock64() - t0 > kWaitCycles) {
+      *failed = 1;
+      return false;
+    }
+  }
+}
+// The barrier at this offset in CTA 0 of the cluster, and an arrival on it.  Its release is the CTA's own: what
+// the arrivals here tell of lies in this CTA's shared memory (cells, through the fence of the proxies) or tensor
+// memory (columns that were read), where the pair's copies and MMAs meet it.  (A release for the
+// cluster waits for every load and store under way, 1,500 clocks each.)
+__device__ __forceinline__ uint32_t rank0_address(unsigned long long* bar) {
+  uint32_t remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(smem_u32(bar)));
+  return remote;
+}
+__device__ __forceinline__ void mbar_arrive_rank0(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
+}
+
+__device__ __forceinline__ void mma_mx4_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa,
+                                             uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate));
+}
+// A cell of each CTA to four columns of its tensor memory, 32 lanes in each quarter.
+__device__ __forceinline__ void copy_cell_pair(uint32_t tmem_to, uint64_t cell) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem_to), "l"(cell) : "memory");
+}
+// Arrive once on the barrier at this offset in both CTAs of the pair when what was issued so far completes.
+__device__ __forceinline__ void mma_commit_pair(unsigned long long* bar) {
+  const uint16_t mask = 0x3;
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+      ::"r"(smem_u32(bar)), "h"(mask) : "memory");
+}
+// Tensor copies to this CTA's shared memory, completing on a barrier of either CTA of the pair.
+__device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy_a(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// Tile t: bands of kBand row tiles, inside a band channel by channel.
+__device__ __forceinline__ Item tile_at(const Items& I, int64_t t) {
+  const int64_t per = (int64_t)kBand * I.ctiles;
+  const int64_t band = (t | per) >> 31 == 0 ? (int64_t)((uint32_t)t / (uint32_t)per) : t / per;
+  const int64_t left = I.rtiles - band * kBand;
+  const uint32_t wide = left < kBand ? (uint32_t)left : (uint32_t)kBand;
+  const int64_t in = t - band * per;
+  const int64_t ct = in >> 31 == 0 ? (int64_t)((uint32_t)in / wide) : in / wide;
+  return I.at(band * kBand + (in - ct * wide), TP * (int)ct);
+}
+
+template <typename TOut>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    k_mx4_pair(const Mx4Args A, const __grid_constant__ Maps maps, int ctiles, int whole, int expire) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  PairShared* sh = reinterpret_cast<PairShared*>(base + kStages * kStageBytes);
+  int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = pair_rank();
+  volatile int* failed = &sh->failed;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&sh->full[s], 1 + 2 * kScaleWarps);
+      mbar_init(&sh->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) mbar_init(&sh->done[b], 1);
+    mbar_init(&sh->drained, 2 * kEpiWarps);
+    mbar_init(&sh->left, 1);
+    sh->failed = sh->left_failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&sh->tmem_base)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  if (warp == kCopyWarp && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.w) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+  }
+  pdl_wait();
+  pdl_trigger();
+  if (A.offsets && warp == 0) group_tiles(A, TP, groups);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  pair_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = sh->tmem_base;
+  const Items items = {A.offsets ? groups : nullptr, A.offsets ? groups + A.E + 1 : nullptr, A.E, TP, ctiles, 0, 0,
+                       A.offsets ? (int64_t)groups[A.E] : (A.n + TP - 1) / TP, A.n};
+  const int64_t tiles = items.rtiles * ctiles, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+  const int steps = (int)((bytes + kStepBytes - 1) / kStepBytes);
+
+  if (warp < kEpiWarps) {
+    // ---------------- outputs ----------------
+    const int quarter = warp & 3, half = warp >> 2;
+    const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
+    uint32_t seen = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int64_t t = pair; t < tiles && ok; t += pairs, ++seen) {
+      const Item it = tile_at(items, t);
+      const int j = it.j0 + 128 * (int)rank + 32 * quarter + lane;
+      const bool live = j < A.N;
+      // what the outputs need from memory, asked for before the sums are there
+      const float bias = has_bias && live ? A.bias[it.e * A.ldb + j] : 0.0f;
+      float rs[TP / 32];   // of 16 rows each, every other 16 of the tile
+#pragma unroll
+      for (int c = 0; c < TP / 32; ++c) {
+        const int x = 16 * (2 * c + half) + (lane & 15);
+        rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
+      }
+      const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)(TP - kShared);
+      ok = __all_sync(kFull, mbar_wait_cluster(&sh->done[b], (seen >> 1) & 1u, failed));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      // the columns that the accumulators share: the second one's first five blocks of 16, the first one's last
+      constexpr int kFirst = kShared / 16;
+      static_assert(kShared == 80 && TP == 256, "blocks 0 to 4 and 11 to 15");
+      const int lo = b ? 0 : TP / 16 - kFirst, hi = lo + kFirst;
+      const int c0 = (lo - half + 1) / 2, some = (hi - half + 1) / 2 - c0;   // this warp's: 2 c + half in lo .. hi - 1
+      uint32_t v[3][16];
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < some) tmem_load16(v[i], tacc + 16u * (uint32_t)(2 * (c0 + i) + half));
+#pragma unroll
+      for (int i = 0; i < 3; ++i) tmem_wait_ld(v[i]);
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_rank0(&sh->drained);
+      auto put = [&](const uint32_t (&f)[16], int c) {
+        const int x0 = 16 * (2 * c + half), left = it.rows - x0;
+        if (left <= 0 || expire) return;
+        float by = rs[0];
+#pragma unroll
+        for (int i = 1; i < TP / 32; ++i)
+          if (c == i) by = rs[i];
+        TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j;
+#pragma unroll
+        for (int x = 0; x < 16; ++x, to += A.ldo) {
+          const TOut y = output<TOut>(__uint_as_float(f[x]), has_rs, __shfl_sync(kFull, by, x), has_bias, bias);
+          if (x < left && live) *to = y;
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < some) put(v[i], c0 + i);
+      // (read before the next tile's arrival: after that this accumulator may be written again)
+#pragma unroll 1
+      for (int i = some; i < TP / 32; ++i) {
+        const int c = (c0 + i) & (TP / 32 - 1);
+        if (16 * (2 * c + half) >= it.rows) continue;
+        uint32_t f[16];
+        tmem_load16(f, tacc + 16u * (uint32_t)(2 * c + half));
+        tmem_wait_ld(f);
+        put(f, c);
+      }
+    }
+    if (expire && threadIdx.x == 0) *failed = 1;
+  } else if (warp < kMmaWarp) {
+    // ---------------- scales ----------------
+    // Two groups of warps take units of 1024 codes in turn: the one loads while the other waits for
+    // stages and fills them.
+    const int q = (warp - kEpiWarps) & (kScaleWarps - 1), r = 32 * q + lane;   // this lane's channel, and row of each half
+    const bool second = warp >= kEpiWarps + kScaleWarps;
+    const int len = (int)(((int64_t)A.K + 31) / 32);
+    const uint32_t cells = smem_u32(base) + 2u * kBlockBytes + 16u * (uint32_t)lane + 4u * (uint32_t)q;
+    Place at = {0, 1u};
+    bool ok = true, mine = !second;
+#pragma unroll 1
+    for (int64_t t = pair; t < tiles && ok; t += pairs) {
+      const uint8_t* row[3] = {};
+      bool live[3] = {}, known = false;
+#pragma unroll 1
+      for (int k = 0; k < steps && ok; k += kUnit, mine = !mine) {
+        if (!mine) {
+          at.forward(min(kUnit, steps - k), kStages);
+          continue;
+        }
+        if (!known) {
+          const Item it = tile_at(items, t);
+          const int j = it.j0 + 128 * (int)rank + r;
+          live[0] = j < A.N;
+          row[0] = A.ws + it.e * A.gws + (int64_t)j * A.ldws;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            live[1 + h] = 128 * h + r < it.rows;
+            row[1 + h] = A.as + (it.r0 + 128 * h + r) * A.ldas;
+          }
+          known = true;
+        }
+        uint32_t v[3][2][4];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) load_scales(v[p], row[p], live[p], whole != 0, 8 * k, len);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (k + 2 * h >= steps) break;
+          // (two stages together: the fence takes 200 clocks, and the MMAs free the stages in their order)
+          const bool two = k + 2 * h + 1 < steps;
+          const Place p0 = at;
+          at.forward(1, kStages);
+          Place p1 = p0;
+          if (two) {
+            p1 = at;
+            at.forward(1, kStages);
+          }
+          ok = __all_sync(kFull, mbar_wait_cluster(&sh->empty[p1.s], p1.ph, failed));
+          if (!ok) break;
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            if (z == 1 && !two) break;
+            const uint32_t to = cells + (uint32_t)((z ? p1.s : p0.s) * kStageBytes);
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int p = 0; p < 3; ++p)   // channels' two cells; of either 128 codes the rows' two halves
+                sts32(to + (uint32_t)(kCell * (p == 0 ? y : 2 + 2 * y + (p - 1))), v[p][h][2 * z + y]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive_rank0(&sh->full[p0.s]);
+            if (two) mbar_arrive_rank0(&sh->full[p1.s]);
+          }
+        }
+      }
+    }
+  } else if (warp == kCopyWarp) {
+    // ---------------- copies ----------------
+    if (lane == 0) {
+      uint32_t s = 0, ph = 1;
+      int64_t copied = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int64_t t = pair; t < tiles && ok; t += pairs) {
+        const Item it = tile_at(items, t);
+        const int half = (it.rows + 31) / 32 * 16;   // rows of a CTA
+        const int wy = it.j0 + 128 * (int)rank, ay = (int)it.r0 + half * (int)rank;
+#pragma unroll 1
+        for (int k = 0; k < steps; ++k) {
+          ok = mbar_wait_cluster(&sh->empty[s], ph, failed);
+          if (!ok) break;
+          const uint32_t to = smem_u32(base) + s * (uint32_t)kStageBytes, bar = rank0_address(&sh->full[s]);
+          if (rank == 0) mbar_arrive_tx(&sh->full[s], 4 * kBlockBytes);
+          copy_w(to, &maps.w, k * kStepBytes, wy, it.e, bar);
+          copy_a(to + kBlockBytes, &maps.a, k * kStepBytes, ay, bar);
+          ++copied;
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+      if (!ok && rank == 0) {
+        // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd one or
+        // a scale warp stopped earlier, the wait's limit is time enough for what is in flight)
+        for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
+          mbar_wait(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
+      }
+    }
+  } else if (rank == 0) {
+    // ---------------- MMAs of the pair ----------------
+    const bool lead = elect_one();
+    const uint32_t d = uniform(tmem);
+    const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
+    const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + 2u * kBlockBytes));
+    uint32_t s = 0, ph = 0, slot = 0, made = 0;
+    int64_t g = 0;                       // stages used
+    uint32_t old = 0, oph = 0;           // the stage kSlots before
+    bool ok = true;
+#pragma unroll 1
+    for (int64_t t = pair; t < tiles && ok; t += pairs, ++made) {
+      const Item it = tile_at(items, t);
+      const uint32_t acc = d + (made & 1u) * (uint32_t)(TP - kShared);
+      const uint32_t idesc = uniform(idesc_f4(TP, (it.rows + 31) & ~31));
+      // the columns that this accumulator shares with the one before are read, and all of its own
+      // were before those
+      if (made > 0) ok = __all_sync(kFull, mbar_wait_cluster(&sh->drained, (made - 1) & 1u, failed));
+      if (!ok) break;
+      // The scales of a step go to tensor memory before the MMAs of the step before it are issued:
+      // they then arrive while those run.
+      uint32_t last = s, last_slot = slot;
+      auto multiply = [&](int k) {
+        const uint64_t ad = desc0 + (uint64_t)(last * (uint32_t)(kStageBytes >> 4)), bd = ad + (uint64_t)(kBlockBytes >> 4);
+        const uint32_t sf = d + (uint32_t)kSfCol + (uint32_t)kSlotCols * last_slot;
+        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e == 0 || left > 32 * e)
+            mma_mx4_pair(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
+                         sf + 4 * (e >> 1), sf + 8 + 8 * (e >> 1), (k > 0 || e > 0) ? 1u : 0u);
+        mma_commit_pair(&sh->empty[last]);
+      };
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k, ++g) {
+        ok = __all_sync(kFull, mbar_wait_cluster(&sh->full[s], ph, failed));
+        // the MMAs that read the scales in this slot
+        if (ok && g >= kSlots) {
+          ok = __all_sync(kFull, mbar_wait_cluster(&sh->empty[old], oph, failed));
+          if (++old == kStages) {
+            old = 0;
+            oph ^= 1u;
+          }
+        }
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (lead) {
+          const uint64_t cd = cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4));
+          const uint32_t sf = d + (uint32_t)kSfCol + (uint32_t)kSlotCols * slot;
+#pragma unroll
+          for (int e = 0; e < 6; ++e) copy_cell_pair(sf + 4 * e, cd + (uint64_t)(e * (kCell >> 4)));
+          if (k > 0) multiply(k - 1);
+        }
+        __syncwarp();
+        last = s;
+        last_slot = slot;
+        if (++slot == kSlots) slot = 0;
+        if (++s == kStages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+      if (ok && lead) multiply(steps - 1);
+      __syncwarp();
+      if (ok && lead) mma_commit_pair(&sh->done[made & 1u]);
+      __syncwarp();
+    }
+    if (lead) {
+      // no MMA outlives its operands and its tensor memory
+      mma_commit_pair(&sh->left);
+      mbar_wait(&sh->left, 0, &sh->left_failed);
+    }
+    __syncwarp();
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  pair_sync();   // no CTA releases TMEM or leaves while its peer may still use the pair
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  // did a wait of either CTA expire?
+  uint32_t peer;
+  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.u32 %0, [a];\n}"
+               : "=r"(peer) : "r"(smem_u32(&sh->failed)), "r"(rank ^ 1u) : "memory");
+  const bool redo = peer != 0u || *failed != 0;
+  // the last arrival that the even CTA's commits send here
+  if (rank != 0 && threadIdx.x == 0) mbar_wait(&sh->left, 0, &sh->left_failed);
+  __syncwarp();
+  pair_sync();
+  if (redo) {
+    for (int64_t t = pair; t < tiles; t += pairs) {
+      Item it = tile_at(items, t);
+      it.j0 += 128 * (int)rank;
+      plain_rows(A, it, 0, 1);
+    }
+  }
+}
+
+template <typename TOut>
+cudaError_t launch_pair(const Mx4Args& A, const Maps& maps, cudaStream_t st, int expire) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(done, k_mx4_pair<TOut>, 227 * 1024);
+  if (e != cudaSuccess) return e;
+  const int ctiles = (int)(((int64_t)A.N + TP - 1) / TP);
+  const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1;
+  const int64_t rtiles = A.offsets ? some + (A.n - some) / TP : (A.n + TP - 1) / TP;   // at most
+  const int64_t pairs = std::min<int64_t>(sm_count() / 2, ctiles * rtiles);
+  return launch_kernel(k_mx4_pair<TOut>, dim3((unsigned)(2 * pairs)), dim3(kThreads), (size_t)pair_smem(A.offsets ? A.E : 0), st,
+                       true, A, maps, ctiles, (int)scales_whole(A), expire);
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_pair(const Mx4Args& A, cudaStream_t st, int expire) {
+  static_assert(pair_smem(kPairGroups) <= 227 * 1024, "shared memory");
+  Maps maps;
+  if (!code_maps(A, 128, &maps)) return cudaErrorNotSupported;
+  if (A.type == BMLP_F32) return launch_pair<float>(A, maps, st, expire);
+  if (A.type == BMLP_F16) return launch_pair<__half>(A, maps, st, expire);
+  return launch_pair<__nv_bfloat16>(A, maps, st, expire);
+}
+
+}  // namespace bk

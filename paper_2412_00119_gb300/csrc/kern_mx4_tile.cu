@@ -8,13 +8,13 @@
 // Warps:
 //   - one thread copies stages of 256 codes of every row into a ring (rows at places that
 //     tensor copies cannot take: eight warps do, shifting whole 16-byte pieces);
-//   - four warps take the scales of 512 codes (16 bytes) of every row, a row each lane's own,
-//     through a ring into the stages, as cells of 128 rows x 128 codes: the four bytes
+//   - eight warps, four at a time, load the scales of 1024 codes (32 bytes) of every row, a row each lane's
+//     own, and store them to the stages as cells of 128 rows x 128 codes: the four bytes
 //     of row r at 16 (r % 32) + 4 (r / 32), which is how the MMA wants them in the lanes and
 //     columns of tensor memory;
 //   - one warp copies a stage's cells there (to all four quarters of the lanes) and issues the
 //     MMAs, 64 codes (two blocks) each;
-//   - eight warps write finished tiles while the next one's MMAs run (two accumulators).
+//   - four warps write finished tiles while the next one's MMAs run (two accumulators).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share K and add their sums up
 // in the order of their ranks, through distributed shared memory.
 // By group: the row tiles of a group start at its first row; what a tile has of the next
@@ -28,7 +28,6 @@
 
 #include <cuda.h>
 
-#include "int8_common.cuh"
 #include "mx4_common.cuh"
 #include "tc_common.cuh"
 
@@ -41,14 +40,14 @@ using namespace mx4;
 constexpr int CM = 128;                  // channels of a tile
 constexpr int kMaxRows = 128;
 constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
-constexpr int kEpiWarps = 8, kScaleWarps = 4, kMmaWarp = kEpiWarps + kScaleWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kEpiWarps = 4, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCopyWarp = kMmaWarp + 1;
 constexpr int kLoadWarps = 8;
 constexpr int kRawRow = kStepBytes + 16; // of a row at any place: the chunks around 128 bytes
 constexpr int kDeep = 3;                 // steps of them in flight, and the one that is read
 constexpr int kMaxStages = 8;
-constexpr int kCell = 512;               // bytes of the scales of 128 rows x 128 codes
 constexpr int kCells = 4 * kCell;        // of a stage: two of the channels, two of the rows
 constexpr int kSlotCols = 16;            // of tensor memory for them
+constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
 
 struct __align__(8) TileShared {
   unsigned long long full[kMaxStages], empty[kMaxStages];
@@ -68,10 +67,9 @@ struct TilePlan {
   int whole;       // every row's scales start at a multiple of 16 bytes
 };
 
-constexpr int kScaleRing = 6;            // 512 codes' scales of every row in flight (three where rows start anywhere)
 __host__ __device__ constexpr int stage_size(int nt) { return (CM + nt) * kStepBytes + kCells; }
 int64_t tile_smem(const Mx4Args& A, int nt, int stages, bool tma) {
-  return 1024 + (tma ? 0 : (int64_t)kDeep * kRawRow * (CM + nt)) + (int64_t)stages * stage_size(nt) + kScaleRing * 16 * (CM + nt) + (int64_t)sizeof(TileShared) +
+  return 1024 + (tma ? 0 : (int64_t)kDeep * kRawRow * (CM + nt)) + (int64_t)stages * stage_size(nt) + (int64_t)sizeof(TileShared) +
          (A.offsets ? 8 * ((int64_t)A.E + 1) : 0);
 }
 
@@ -107,22 +105,10 @@ __device__ __forceinline__ void mma_mx4(uint32_t tmem_d, uint64_t adesc, uint64_
       ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate));
 }
 
-// Descriptor of a cell: 32 rows of 16 bytes one after another, no swizzle.
-__device__ __forceinline__ uint64_t cell_desc(uint32_t saddr) {
-  uint64_t d = (saddr & 0x3FFFFu) >> 4;
-  d |= (uint64_t)(128 >> 4) << 16;   // from 8 rows to the next, in either sense
-  d |= (uint64_t)(128 >> 4) << 32;
-  d |= (uint64_t)1 << 46;            // descriptor version (sm_100 family)
-  return d;
-}
 // A cell to four columns of tensor memory, 32 lanes in each quarter.
 __device__ __forceinline__ void copy_cell(uint32_t tmem_to, uint64_t cell) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem_to), "l"(cell) : "memory");
 }
-__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
-  asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
-}
-
 __device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -135,18 +121,6 @@ __device__ __forceinline__ void copy_a(uint32_t dst, const CUtensorMap* map, int
 }
 
 // The tiles of a CTA (or of a cluster of them), one after another: row tile u, channel tile ct.
-struct Item {
-  int e;          // group
-  int rows;
-  int64_t r0;     // first row
-  int j0;         // first channel
-};
-struct Items {
-  const int32_t* tile0;   // by group: its first row tile (E + 1); null: one group
-  const int32_t* row0;    // and its first row
-  int E, nt, ctiles, step_u, step_c;
-  int64_t rtiles, n;
-};
 struct Cursor {
   int64_t u;
   int ct;
@@ -160,42 +134,8 @@ struct Cursor {
       ++u;
     }
   }
-  __device__ __forceinline__ Item at(const Items& I) const {
-    Item it;
-    it.j0 = CM * ct;
-    int64_t end = I.n;
-    if (I.tile0) {
-      int lo = 0, hi = I.E;      // the last group with tile0 <= u
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (I.tile0[mid] <= u) lo = mid; else hi = mid;
-      }
-      it.e = lo;
-      it.r0 = I.row0[lo] + (u - I.tile0[lo]) * I.nt;
-      end = I.row0[lo + 1];
-    } else {
-      it.e = 0;
-      it.r0 = u * I.nt;
-    }
-    it.rows = (int)min((int64_t)I.nt, end - it.r0);
-    return it;
-  }
+  __device__ __forceinline__ Item at(const Items& I) const { return I.at(u, CM * ct); }
 };
-
-template <typename T>
-__device__ __forceinline__ T output(float sum, bool has_rs, float rs, bool has_bias, float bias) {
-  const float y = has_rs ? __fmul_rn(sum, rs) : sum;
-  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
-}
-
-// A tile's outputs on CUDA cores (columns first, first + step, ..), by all threads: only after a
-// wait has expired.
-static __device__ __noinline__ void plain_rows(const Mx4Args& A, const Item& it, int first, int step) {
-  for (int64_t k = threadIdx.x; k < (int64_t)CM * it.rows; k += blockDim.x) {
-    const int j = it.j0 + (int)(k % CM), x = (int)(k / CM);
-    if (x % step == first && j < A.N) put_out(A, it.r0 + x, j, it.e, plain_sum(A, it.r0 + x, j, it.e));
-  }
-}
 
 // Outputs of rows rank, rank + S, .. of a tile from the S CTAs' sums ([row][channel] at `sums` of each
 // one's shared memory), added in the order of their ranks: a warp takes a row, a lane four channels.
@@ -249,16 +189,15 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
   }
 }
 
+// kTma: the codes come by tensor copies (else their rows start anywhere).
 template <typename TOut, bool kTma>
 __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps), kTma ? 2 : 1)
-    k_mx4_tile(const Mx4Args A, const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap amap,
-               const TilePlan P, int expire) {
+    k_mx4_tile(const Mx4Args A, const __grid_constant__ Maps maps, const TilePlan P, int expire) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int stage_bytes = stage_size(P.nt);
-  uint8_t* scales = base + P.stages * stage_bytes;
-  const int ring_bytes = kScaleRing * 16 * (CM + P.nt);
-  TileShared* sh = reinterpret_cast<TileShared*>(scales + ring_bytes + (kTma ? 0 : kDeep * kRawRow * (CM + P.nt)));
+  uint8_t* ring = base + P.stages * stage_bytes;
+  TileShared* sh = reinterpret_cast<TileShared*>(ring + (kTma ? 0 : kDeep * kRawRow * (CM + P.nt)));
   int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t S = (uint32_t)P.split, rank = S > 1 ? cluster_rank() : 0u;
@@ -283,40 +222,12 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (kTma && warp == kCopyWarp && lane == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&amap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.w) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
   }
   pdl_wait();
   pdl_trigger();
-  if (A.offsets && warp == 0) {
-    // the groups' first rows and first row tiles
-    int row = 0, tile = 0;
-    for (int e0 = 0; e0 <= A.E; e0 += 32) {
-      const int e = e0 + lane;
-      int r = e <= A.E ? clamp_offset(A.offsets[e], 0, A.n) : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o *= 2) {
-        const int v = __shfl_up_sync(kFull, r, o);
-        if (lane >= o) r = max(r, v);
-      }
-      r = max(r, row);
-      if (e <= A.E) groups[A.E + 1 + e] = r;
-      row = __shfl_sync(kFull, r, 31);
-    }
-    __syncwarp();
-    for (int e0 = 0; e0 <= A.E; e0 += 32) {
-      const int e = e0 + lane;
-      const int mine = e < A.E ? (groups[A.E + 2 + e] - groups[A.E + 1 + e] + P.nt - 1) / P.nt : 0;
-      int t = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o *= 2) {
-        const int v = __shfl_up_sync(kFull, t, o);
-        if (lane >= o) t += v;
-      }
-      if (e <= A.E) groups[e] = tile + t - mine;
-      tile += __shfl_sync(kFull, t, 31);
-    }
-  }
+  if (A.offsets && warp == 0) group_tiles(A, P.nt, groups);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -333,7 +244,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 
   if (warp < kEpiWarps) {
     // ---------------- outputs ----------------
-    const int quarter = warp & 3, half = warp >> 2;
+    const int quarter = warp;
     const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
     bool ok = true;
     uint32_t seen = 0;
@@ -344,10 +255,10 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       const bool live = j < A.N;
       // what the outputs need from memory, asked for before the sums are there
       const float bias = has_bias && live ? A.bias[it.e * A.ldb + j] : 0.0f;
-      float rs[kMaxRows / 32];   // of 16 rows each, every other 16 of the tile
+      float rs[kMaxRows / 32];   // of 32 rows each
 #pragma unroll
       for (int c = 0; c < kMaxRows / 32; ++c) {
-        const int x = 16 * (2 * c + half) + (lane & 15);
+        const int x = 32 * c + lane;
         rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
       }
       const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)P.nt;
@@ -355,8 +266,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-      for (int c = 0; c < kMaxRows / 32; ++c) {
-        const int x0 = 16 * (2 * c + half);
+      for (int c = 0; c < kMaxRows / 16; ++c) {
+        const int x0 = 16 * c;
         if (x0 >= it.rows) break;
         uint32_t v[16];
         tmem_load16(v, tacc + (uint32_t)x0);
@@ -370,7 +281,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
           TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j;
 #pragma unroll
           for (int x = 0; x < 16; ++x, to += A.ldo) {
-            const TOut y = output<TOut>(__uint_as_float(v[x]), has_rs, __shfl_sync(kFull, rs[c], x), has_bias, bias);
+            const TOut y = output<TOut>(__uint_as_float(v[x]), has_rs, __shfl_sync(kFull, rs[c >> 1], 16 * (c & 1) + x), has_bias, bias);
             if (x < left && live) *to = y;
           }
         }
@@ -382,120 +293,91 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     if (expire && threadIdx.x == 0) *failed = 1;
   } else if (warp < kMmaWarp) {
     // ---------------- scales ----------------
-    const int q = warp - kEpiWarps;
+    // Two groups of warps take units of 1024 codes in turn: the one loads while the other waits for
+    // stages and fills them.
+    const int q = (warp - kEpiWarps) & (kScaleWarps - 1), r = 32 * q + lane;   // this lane's channel and row
+    const bool second = warp >= kEpiWarps + kScaleWarps, has_row = r < P.nt, whole = P.whole != 0;
     const int len = (int)(((int64_t)A.K + 31) / 32);
-    const int r = 32 * q + lane;         // this lane's channel and row
-    const bool whole = P.whole != 0, has_row = r < P.nt;
-    const int depth = whole ? kScaleRing : kScaleRing / 2, pitch = whole ? 16 : 32;
-    const uint32_t slot_bytes = (uint32_t)(pitch * (CM + P.nt));
-    const uint32_t ring = smem_u32(scales) + (uint32_t)(pitch * r);
     const uint32_t cells = smem_u32(base) + (uint32_t)(stage_bytes - kCells) + 16u * (uint32_t)lane + 4u * (uint32_t)q;
-    const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.as));
-    // the chunks that are copied next, and what is left of their rows from there on
-    const int8_t *wfrom = any, *afrom = any;
-    int wleft = 0, aleft = 0, nc = c0;
-    Cursor ahead(items, first);
-    auto rows_of = [&]() {
-      const Item it = ahead.at(items);
-      const bool wlive = it.j0 + r < A.N, alive = r < it.rows;
-      const int8_t* w = reinterpret_cast<const int8_t*>(A.ws) + it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws;
-      const int8_t* a = reinterpret_cast<const int8_t*>(A.as) + (it.r0 + r) * A.ldas;
-      const int ws = i8::row_shift<1>(w), as = i8::row_shift<1>(a);
-      wfrom = wlive ? w - ws + 16 * c0 : any;
-      afrom = alive ? a - as + 16 * c0 : any;
-      wleft = wlive ? len + ws - 16 * c0 : 0;
-      aleft = alive ? len + as - 16 * c0 : 0;
-    };
-    auto chunk = [&](uint32_t to, const int8_t* from, int left) {
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                   ::"r"(to), "l"(left > 0 ? from : any), "r"(min(16, max(0, left))) : "memory");
-    };
-    auto copy = [&](uint32_t slot) {
-      if (ahead.live(items)) {
-        const uint32_t to = ring + slot * slot_bytes;
-        chunk(to, wfrom, wleft);
-        if (!whole) chunk(to + 16u, wfrom + 16, wleft - 16);
-        if (has_row) {
-          chunk(to + (uint32_t)(pitch * CM), afrom, aleft);
-          if (!whole) chunk(to + (uint32_t)(pitch * CM) + 16u, afrom + 16, aleft - 16);
-        }
-        wfrom += 16;
-        afrom += 16;
-        wleft -= 16;
-        aleft -= 16;
-        if (++nc == c1) {
-          nc = c0;
-          ahead.next(items);
-          if (ahead.live(items)) rows_of();
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    if (ahead.live(items)) rows_of();
+    Place at = {0, 1u}, passed = at;
+    int others = 0;                      // steps of the other group's unit before this one, from `passed` on
+    bool ok = true, mine = !second;
 #pragma unroll 1
-    for (int d = 0; d < depth - 1; ++d) copy((uint32_t)d);
-    uint32_t s = 0, ph = 1, from = 0;
-    bool ok = true;
+    for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
+      const uint8_t *wrow = nullptr, *arow = nullptr;
+      bool wlive = false, alive = false, known = false;
 #pragma unroll 1
-    for (Cursor at(items, first); at.live(items) && ok; at.next(items)) {
-      int wshift = 0, ashift = 0;
-      if (!whole) {
-        const Item it = at.at(items);
-        wshift = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.ws + it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws));
-        ashift = i8::row_shift<1>(reinterpret_cast<const int8_t*>(A.as + (it.r0 + r) * A.ldas));
-      }
-#pragma unroll 1
-      for (int c = c0; c < c1 && ok; ++c) {
-        if (whole) asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing - 2) : "memory");
-        else asm volatile("cp.async.wait_group %0;" ::"n"(kScaleRing / 2 - 2) : "memory");
-        // (a lane reads what it copied itself)
-        uint32_t w[4], a[4] = {0u, 0u, 0u, 0u};
-        const uint32_t src = ring + from * slot_bytes;
-        i8::lds_chunk(w, src);
-        if (has_row) i8::lds_chunk(a, src + (uint32_t)(pitch * CM));
-        if (!whole) {
-          uint32_t hi[4], m[4];
-          i8::lds_chunk(hi, src + 16u);
-          i8::merge16(m, w, hi, wshift);
-#pragma unroll
-          for (int y = 0; y < 4; ++y) w[y] = m[y];
-          if (has_row) {
-            i8::lds_chunk(hi, src + (uint32_t)(pitch * CM) + 16u);
-            i8::merge16(m, a, hi, ashift);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) a[y] = m[y];
-          }
+      for (int k = k0; k < k1 && ok; k += kUnit, mine = !mine) {
+        if (!mine) {
+          passed = at;
+          others = min(kUnit, k1 - k);
+          at.forward(others, P.stages);
+          continue;
         }
-        copy(from == 0 ? (uint32_t)depth - 1 : from - 1);
-        if (++from == (uint32_t)depth) from = 0;
+        if (!known) {
+          const Item it = cur.at(items);
+          wlive = it.j0 + r < A.N;
+          alive = r < it.rows;
+          wrow = A.ws + it.e * A.gws + (int64_t)(it.j0 + r) * A.ldws;
+          arow = A.as + (it.r0 + r) * A.ldas;
+          known = true;
+        }
+        uint32_t w[2][4], a[2][4];
+        load_scales(w, wrow, wlive, whole, 8 * k, len);
+        load_scales(a, arow, alive, whole, 8 * k, len);
+        // A wait tells a phase from the next by its parity, so the phase two before the one that is waited
+        // for must be known to be over.  The last wait of this group's unit before tells that of the MMAs
+        // up to kUnit + 1 + stages steps back, and the next asks for 2 stages - 1 (the second of two stages).
+        if (P.stages < kUnit + 2)
+          for (; others > 0 && ok; --others, passed.forward(1, P.stages))
+            ok = __all_sync(kFull, mbar_wait(&sh->empty[passed.s], passed.ph, failed));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (2 * c + h >= k1) break;
-          ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
-          if (!ok) break;
-          const uint32_t to = cells + s * (uint32_t)stage_bytes;
+          if (!ok || k + 2 * h >= k1) break;
+          // Two stages at a time where the ring is long: the fence takes 200 clocks.  (The MMAs free
+          // the stages in their order.)
+          const bool two = k + 2 * h + 1 < k1, both = two && P.stages >= 4;
+          const Place p0 = at;
+          at.forward(1, P.stages);
+          const Place p1 = at;
+          if (two) at.forward(1, P.stages);
+          auto put = [&](int s, int y0) {
+            const uint32_t to = cells + (uint32_t)(s * stage_bytes);
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            sts32(to + (uint32_t)(kCell * y), w[2 * h + y]);
-            if (has_row) sts32(to + (uint32_t)(kCell * (2 + y)), a[2 * h + y]);
-          }
+            for (int y = 0; y < 2; ++y) {
+              sts32(to + (uint32_t)(kCell * y), w[h][y0 + y]);
+              if (has_row) sts32(to + (uint32_t)(kCell * (2 + y)), a[h][y0 + y]);
+            }
+          };
+          const Place& wait = both ? p1 : p0;
+          ok = __all_sync(kFull, mbar_wait(&sh->empty[wait.s], wait.ph, failed));
+          if (!ok) break;
+          put(p0.s, 0);
+          if (both) put(p1.s, 2);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sh->full[s]);
-          if (++s == (uint32_t)P.stages) {
-            s = 0;
-            ph ^= 1u;
+          if (lane == 0) {
+            mbar_arrive(&sh->full[p0.s]);
+            if (both) mbar_arrive(&sh->full[p1.s]);
+          }
+          if (two && !both) {
+            ok = __all_sync(kFull, mbar_wait(&sh->empty[p1.s], p1.ph, failed));
+            if (!ok) break;
+            put(p1.s, 2);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->full[p1.s]);
           }
         }
       }
     }
-    cp_async_wait_all();
   } else if (warp == kMmaWarp) {
     // ---------------- MMAs ----------------
     const bool lead = elect_one();
     const uint32_t d = uniform(tmem);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
     const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + (uint32_t)(stage_bytes - kCells)));
+    const uint32_t sf0 = d + 2u * (uint32_t)P.nt;
     uint32_t s = 0, ph = 0, made = 0;
     bool ok = true;
 #pragma unroll 1
@@ -505,32 +387,41 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       const uint32_t idesc = uniform(idesc_f4(CM, (it.rows + 15) & ~15));
       ok = __all_sync(kFull, mbar_wait(&sh->drained[b], ((made >> 1) & 1u) ^ 1u, failed));
       if (!ok) break;
+      // The scales of a step go to tensor memory before the MMAs of the step before it are issued:
+      // they then arrive while those run.
+      uint32_t last = s;
+      auto multiply = [&](int k, uint32_t at) {
+        const uint64_t ad = desc0 + (uint64_t)(at * (uint32_t)(stage_bytes >> 4)), bd = ad + (uint64_t)(CM * kStepBytes >> 4);
+        const uint32_t sf = sf0 + (uint32_t)kSlotCols * at;
+        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e == 0 || left > 32 * e)
+            mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
+                    sf + 4 * (e >> 1), sf + 8 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
+        mma_commit(&sh->empty[at]);
+      };
 #pragma unroll 1
       for (int k = k0; k < k1; ++k) {
         ok = __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t off = (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
-        const uint64_t ad = desc0 + off, bd = ad + (uint64_t)(CM * kStepBytes >> 4), cd = cells0 + off;
-        const uint32_t sf = d + 2u * (uint32_t)P.nt + (uint32_t)kSlotCols * s;
-        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
         if (lead) {
-          // (copies and MMAs of a thread run in their order)
+          const uint64_t cd = cells0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
+          const uint32_t sf = sf0 + (uint32_t)kSlotCols * s;
 #pragma unroll
           for (int e = 0; e < 4; ++e) copy_cell(sf + 4 * e, cd + (uint64_t)(e * (kCell >> 4)));
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e == 0 || left > 32 * e)
-              mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
-                      sf + 4 * (e >> 1), sf + 8 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
-          mma_commit(&sh->empty[s]);
+          if (k > k0) multiply(k - 1, last);
         }
         __syncwarp();
+        last = s;
         if (++s == (uint32_t)P.stages) {
           s = 0;
           ph ^= 1u;
         }
       }
+      if (ok && lead) multiply(k1 - 1, last);
+      __syncwarp();
       if (ok && lead) mma_commit(&sh->done[b]);
       __syncwarp();
     }
@@ -555,8 +446,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
           if (!ok) break;
           const uint32_t to = smem_u32(base + s * stage_bytes), bar = smem_u32(&sh->full[s]);
           mbar_arrive_tx(&sh->full[s], (uint32_t)(stage_bytes - kCells));
-          copy_w(to, &wmap, k * kStepBytes, it.j0, it.e, bar);
-          copy_a(to + CM * kStepBytes, &amap, k * kStepBytes, (int)it.r0, bar);
+          copy_w(to, &maps.w, k * kStepBytes, it.j0, it.e, bar);
+          copy_a(to + CM * kStepBytes, &maps.a, k * kStepBytes, (int)it.r0, bar);
           ++copied;
           if (++s == (uint32_t)P.stages) {
             s = 0;
@@ -564,10 +455,12 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
           }
         }
       }
-      if (!ok)
-        // no copy outlives its CTA
+      if (!ok) {
+        // no copy outlives its CTA (a phase of codes may lack the scale warps' arrivals, and then
+        // the wait's limit is time enough)
         for (int64_t k = copied > P.stages ? copied - P.stages : 0; k < copied; ++k)
-          mbar_wait(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed);
+          mbar_wait(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed, 2000000ull);
+      }
     }
   } else {
     // ---------------- loads ----------------
@@ -576,7 +469,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     const int w = warp - kCopyWarp, c = lane & 7, sub = lane >> 3, mine = P.nt / kLoadWarps;
     const int len = (int)bytes;
     const uint32_t raw_bytes = (uint32_t)(kRawRow * (CM + P.nt));
-    const uint32_t raw = smem_u32(base + P.stages * stage_bytes + ring_bytes) + (uint32_t)(kRawRow * 16 * w);
+    const uint32_t raw = smem_u32(ring) + (uint32_t)(kRawRow * 16 * w);
     const uint32_t raw_a = raw + (uint32_t)(kRawRow * (CM - 16 * w + mine * w));
     const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.a));
     const int8_t *wrow = any, *arow = any;   // the warp's first
@@ -690,8 +583,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 }
 
 template <typename TOut, bool kTma>
-cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const CUtensorMap& wmap, const CUtensorMap& amap, cudaStream_t st,
-                        int expire) {
+cudaError_t launch_mode(const Mx4Args& A, const TilePlan& P, const Maps& maps, cudaStream_t st, int expire) {
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_smem(done, k_mx4_tile<TOut, kTma>, 227 * 1024);
   if (e != cudaSuccess) return e;
@@ -708,12 +600,18 @@ cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const CUtensorMap& 
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = P.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_mx4_tile<TOut, kTma>, A, wmap, amap, P, expire);
+  return cudaLaunchKernelEx(&cfg, k_mx4_tile<TOut, kTma>, A, maps, P, expire);
 }
 
-// Whether rows start at multiples of 16 bytes.
-bool rows_whole(const uint8_t* p, int64_t ld, int64_t rows) {
-  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(rows > 1 ? ld : 0)) & 15) == 0;
+template <typename TOut>
+cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const Maps& maps, bool tma, cudaStream_t st, int expire) {
+  return tma ? launch_mode<TOut, true>(A, P, maps, st, expire) : launch_mode<TOut, false>(A, P, maps, st, expire);
+}
+
+// Whether the pairs run faster.
+bool pair_wins(const Mx4Args& A) {
+  const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = A.n / some;
+  return A.E <= kPairGroups && mean > 128 && ((mean + 255) / 256) * some * ((A.N + 255) / 256) >= sm_count() / 2;
 }
 
 }  // namespace
@@ -726,12 +624,18 @@ cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
   const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = (A.n + some - 1) / some;
   const int64_t parts = (mean + kMaxRows - 1) / kMaxRows;
   P.nt = (int)std::min<int64_t>(kMaxRows, ((mean + parts - 1) / parts + 15) / 16 * 16);
+  // (two stages at least: the MMAs of one are issued when the next one is there)
+  while (P.nt > 16 && tile_smem(A, P.nt, 2, false) > 227 * 1024) P.nt -= 16;
   const int64_t rtiles = A.offsets ? some + (A.n - some) / P.nt : (A.n + P.nt - 1) / P.nt;   // at most
   const int64_t tiles = rtiles * P.ctiles;
   const int64_t chunks = ((int64_t)A.K + 511) / 512;
-  const int64_t bytes = ((int64_t)A.K + 1) / 2;
-  CUtensorMap wmap, amap;
-  const bool tma = code_map(&wmap, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) && code_map(&amap, A.a, bytes, A.n, A.lda, 0, 0, P.nt);
+  P.whole = scales_whole(A);
+  Maps maps;
+  if (pair_wins(A)) {
+    const cudaError_t e = launch_mx4_pair(A, st, expire);
+    if (e != cudaErrorNotSupported) return e;
+  }
+  const bool tma = code_maps(A, P.nt, &maps);
   // two CTAs of an SM where their tensor memory and registers have room
   const bool two = tma && P.nt <= 64;
   P.cols = two ? 256 : 512;
@@ -741,15 +645,9 @@ cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
   P.split = 1;
   while (P.split < 8 && 2 * P.split <= chunks && tiles * P.split * 2 <= slots) P.split *= 2;
   P.ctas = (int)(P.split > 1 ? tiles * P.split : std::min(tiles, slots));
-  P.whole = rows_whole(A.as, A.ldas, A.n) && rows_whole(A.ws, A.ldws, A.N) && (A.E == 1 || (A.gws & 15) == 0);
-  if (tma) {
-    if (A.type == BMLP_F32) return launch_tile<float, true>(A, P, wmap, amap, st, expire);
-    if (A.type == BMLP_F16) return launch_tile<__half, true>(A, P, wmap, amap, st, expire);
-    return launch_tile<__nv_bfloat16, true>(A, P, wmap, amap, st, expire);
-  }
-  if (A.type == BMLP_F32) return launch_tile<float, false>(A, P, wmap, amap, st, expire);
-  if (A.type == BMLP_F16) return launch_tile<__half, false>(A, P, wmap, amap, st, expire);
-  return launch_tile<__nv_bfloat16, false>(A, P, wmap, amap, st, expire);
+  if (A.type == BMLP_F32) return launch_tile<float>(A, P, maps, tma, st, expire);
+  if (A.type == BMLP_F16) return launch_tile<__half>(A, P, maps, tma, st, expire);
+  return launch_tile<__nv_bfloat16>(A, P, maps, tma, st, expire);
 }
 
 }  // namespace bk

@@ -6,16 +6,15 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "bmlp_internal.cuh"
+#include "int8_common.cuh"
 
 namespace bk {
 namespace mx4 {
 
-// Map of rows of codes, box_rows of 128 bytes (256 codes) at a time in the 128B-swizzled order that
-// the MMAs read; groups > 0: of groups of rows.  False where tensor copies cannot take them:
-// rows or groups that do not start at multiples of 16 bytes.
+// Map of rows of codes, 128 bytes of box_rows rows at a time, in the 128B-swizzled order that the MMAs read; groups > 0: of groups of rows.  False where tensor copies cannot
+// take them: rows or groups that do not start at multiples of 16 bytes.
 inline bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t bytes, int64_t rows, int64_t ld, int64_t groups,
-                     int64_t group_ld, int box_rows) {
+                    int64_t group_ld, int box_rows) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -37,8 +36,22 @@ inline bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t bytes, int6
   const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)group_ld};
   const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, groups > 0 ? 3 : 2, const_cast<uint8_t*>(codes), dims, strides, box, steps,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Maps of a call's codes: of the channels (128 at a time) and of the rows.
+struct Maps {
+  CUtensorMap w, a;
+};
+inline bool code_maps(const Mx4Args& A, int rows, Maps* m) {
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+  return code_map(&m->w, A.w, bytes, A.N, A.ldw, A.E, A.gw, 128) && code_map(&m->a, A.a, bytes, A.n, A.lda, 0, 0, rows);
+}
+
+// Whether every row's scales start at a multiple of 16 bytes.
+inline bool scales_whole(const Mx4Args& A) {
+  return ((reinterpret_cast<uintptr_t>(A.as) | reinterpret_cast<uintptr_t>(A.ws) | (uintptr_t)(A.n > 1 ? A.ldas : 0) |
+           (uintptr_t)(A.N > 1 ? A.ldws : 0) | (uintptr_t)(A.E > 1 ? A.gws : 0)) & 15) == 0;
 }
 
 // Rows [first, last) of a group.  Offsets that decrease or leave 0..n are taken as the
@@ -47,10 +60,7 @@ __device__ __forceinline__ int clamp_offset(int32_t offset, int low, int64_t n) 
   return max(low, min((int)n, (int)offset));
 }
 
-template <typename T> __device__ __forceinline__ T out_cast(float y);
-template <> __device__ __forceinline__ float out_cast(float y) { return y; }
-template <> __device__ __forceinline__ __half out_cast(float y) { return __float2half_rn(y); }
-template <> __device__ __forceinline__ __nv_bfloat16 out_cast(float y) { return __float2bfloat16_rn(y); }
+using i8::out_cast;
 
 // Product of two bytes of codes: the sum of two exact products (multiples of 1/4).
 __device__ __forceinline__ float pair_product(uint32_t a, uint32_t b) {
@@ -84,6 +94,129 @@ __device__ __forceinline__ void put_out(const Mx4Args& A, int64_t i, int j, int 
   else if (A.type == BMLP_F16) static_cast<__half*>(A.out)[at] = out_cast<__half>(y);
   else static_cast<__nv_bfloat16*>(A.out)[at] = out_cast<__nv_bfloat16>(y);
 }
+
+// An output from its sum.
+template <typename T>
+__device__ __forceinline__ T output(float sum, bool has_rs, float rs, bool has_bias, float bias) {
+  const float y = has_rs ? __fmul_rn(sum, rs) : sum;
+  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
+}
+
+// Where a tile is.
+struct Item {
+  int e;          // group
+  int rows;
+  int64_t r0;     // first row
+  int j0;         // first channel
+};
+// The row tiles of a call.
+struct Items {
+  const int32_t* tile0;   // by group: its first row tile (E + 1); null: one group
+  const int32_t* row0;    // and its first row
+  int E, nt, ctiles, step_u, step_c;
+  int64_t rtiles, n;
+  __device__ __forceinline__ Item at(int64_t u, int j0) const {
+    Item it;
+    it.j0 = j0;
+    int64_t end = n;
+    if (tile0) {
+      int lo = 0, hi = E;      // the last group with tile0 <= u
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (tile0[mid] <= u) lo = mid; else hi = mid;
+      }
+      it.e = lo;
+      it.r0 = row0[lo] + (u - tile0[lo]) * nt;
+      end = row0[lo + 1];
+    } else {
+      it.e = 0;
+      it.r0 = u * nt;
+    }
+    it.rows = (int)min((int64_t)nt, end - it.r0);
+    return it;
+  }
+};
+// The groups' first row tiles (groups[0..E]) and first rows (groups[E + 1..2 E + 1]), by one warp.
+__device__ __forceinline__ void group_tiles(const Mx4Args& A, int nt, int32_t* groups) {
+  const int lane = threadIdx.x & 31;
+  int row = 0, tile = 0;
+  for (int e0 = 0; e0 <= A.E; e0 += 32) {
+    const int e = e0 + lane;
+    int r = e <= A.E ? clamp_offset(A.offsets[e], 0, A.n) : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, r, o);
+      if (lane >= o) r = max(r, v);
+    }
+    r = max(r, row);
+    if (e <= A.E) groups[A.E + 1 + e] = r;
+    row = __shfl_sync(0xffffffffu, r, 31);
+  }
+  __syncwarp();
+  for (int e0 = 0; e0 <= A.E; e0 += 32) {
+    const int e = e0 + lane;
+    const int mine = e < A.E ? (groups[A.E + 2 + e] - groups[A.E + 1 + e] + nt - 1) / nt : 0;
+    int t = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += v;
+    }
+    if (e <= A.E) groups[e] = tile + t - mine;
+    tile += __shfl_sync(0xffffffffu, t, 31);
+  }
+}
+
+// 128 channels' outputs of a tile on CUDA cores (rows first, first + step, ..), by all threads: only after a
+// wait has expired.
+static __device__ __noinline__ void plain_rows(const Mx4Args& A, const Item& it, int first, int step) {
+  for (int64_t k = threadIdx.x; k < (int64_t)128 * it.rows; k += blockDim.x) {
+    const int j = it.j0 + (int)(k % 128), x = (int)(k / 128);
+    if (x % step == first && j < A.N) put_out(A, it.r0 + x, j, it.e, plain_sum(A, it.r0 + x, j, it.e));
+  }
+}
+
+constexpr int kCell = 512;               // bytes of the scales of 128 rows x 128 codes: those of row r at 16 (r % 32) + 4 (r / 32)
+// Descriptor of a cell: 32 rows of 16 bytes one after another, no swizzle.
+__device__ __forceinline__ uint64_t cell_desc(uint32_t saddr) {
+  uint64_t d = (saddr & 0x3FFFFu) >> 4;
+  d |= (uint64_t)(128 >> 4) << 16;   // from 8 rows to the next, in either sense
+  d |= (uint64_t)(128 >> 4) << 32;
+  d |= (uint64_t)1 << 46;            // descriptor version (sm_100 family)
+  return d;
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+
+// The scale bytes of 1024 codes (32) of a row from byte k (a multiple of 16) on, zeros from len on.  whole: the row
+// starts at a multiple of 16 bytes.
+__device__ __forceinline__ void load_scales(uint32_t (&v)[2][4], const uint8_t* row, bool live, bool whole, int k, int len) {
+  const int8_t* p = reinterpret_cast<const int8_t*>(row);
+  if (!live) {
+#pragma unroll
+    for (int y = 0; y < 8; ++y) v[y >> 2][y & 3] = 0u;
+  } else if (whole) {
+    i8::load16<16>(v[0], p, 0, k, len);
+    i8::load16<16>(v[1], p, 0, k + 16, len);
+  } else {
+    const int shift = i8::row_shift<1>(p);
+    i8::load16<1>(v[0], p, shift, k, len);
+    i8::load16<1>(v[1], p, shift, k + 16, len);
+  }
+}
+// Place in a ring of stages, and the parity of its "empty" barrier's phase that a writer waits for.
+struct Place {
+  int s;
+  uint32_t ph;
+  __device__ __forceinline__ void forward(int steps, int stages) {
+    s += steps;
+    while (s >= stages) {
+      s -= stages;
+      ph ^= 1u;
+    }
+  }
+};
 
 }  // namespace mx4
 }  // namespace bk
