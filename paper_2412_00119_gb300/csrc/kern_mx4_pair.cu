@@ -7,15 +7,14 @@
 // of the rows: 32 KB per 256 codes, in 512 clocks of MMA; its tensor memory receives the sums of
 // its channels and all rows, and it needs the scales of its channels and of all rows there.
 // The grid is persistent, a pair per two SMs.  Two accumulators of 256 columns and the scales
-// do not fit tensor memory side by side: the accumulators share 80 columns, which the epilogue
-// reads first.  Warps of a CTA: eight write outputs, eight bring scales, one thread copies codes
-// (both CTAs' copies complete on the even one's barriers), and on the even CTA one warp issues
-// the copies of scales to tensor memory and the MMAs.
+// do not fit tensor memory side by side: the accumulators share 128 columns, which the epilogue
+// reads first.  Warps of a CTA: 16 write outputs, eight bring scales, one thread copies codes
+// (both CTAs' copies complete on the even one's barriers), and on the even CTA one warp
+// copies the scales to tensor memory and one issues the MMAs.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 
 #include "mx4_common.cuh"
-#include "tc_common.cuh"
 
 namespace bk {
 namespace {
@@ -30,11 +29,12 @@ constexpr int kCells = 6 * kCell;        // of a stage: two of the channels, fou
 constexpr int kStageBytes = 2 * kBlockBytes + kCells;
 constexpr int kStages = 6;
 constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
-constexpr int kEpiWarps = 8, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kEpiWarps = 16, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCellWarp = kMmaWarp + 1,
+              kCopyWarp = kCellWarp + 1;
 constexpr int kThreads = 32 * (kCopyWarp + 1);
-constexpr int kShared = 80;              // columns of both accumulators
+constexpr int kShared = 128;             // columns of both accumulators
 constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
-constexpr int kSlots = 3, kSlotCols = 24;
+constexpr int kSlots = 5, kSlotCols = 24;
 static_assert(kSfCol + kSlots * kSlotCols <= 512 && kStageBytes % 1024 == 0, "tensor memory, swizzle atoms");
 // A wait tells a phase from the next by its parity, so the phase two before the one that is waited for must be
 // known to be over.  The last wait of a scale warp's unit before tells that of the MMAs up to kUnit + 1 +
@@ -43,9 +43,9 @@ static_assert(kStages >= kUnit + 2, "phases");
 constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
 
 struct __align__(8) PairShared {
-  unsigned long long full[kStages], empty[kStages];
+  unsigned long long scaled[kStages], full[kStages], empty[kStages];   // cells; codes, and scales in tensor memory; read
   unsigned long long done[2], drained;
-  unsigned long long left;
+  unsigned long long left, cells_left;
   uint32_t tmem_base;
   int failed, left_failed;
 };
@@ -60,29 +60,6 @@ __device__ __forceinline__ uint32_t pair_rank() {
 }
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Bounded wait with cluster-scope acquire (the barrier collects arrivals of the peer).
-__device__ __forceinline__ bool mbar_wait_cluster(unsigned long long* bar, uint32_t parity, volatile int* failed) {
-  const uint32_t a = smem_u32(bar);
-  uint32_t ok;
-  auto try_wait = [&]() {
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-        " selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok) : "r"(a), "r"(parity) : "memory");
-  };
-  try_wait();
-  if (ok) return true;
-  const unsigned long long t0 = clock64();
-  while (true) {
-    try_wait();
-    if (ok) return true;
-    if (*failed) return false;
-    if (clock64() - t0 > kWaitCycles) {
-      *failed = 1;
-      return false;
-    }
-  }
 }
 // The barrier at this offset in CTA 0 of the cluster, and an arrival on it.  Its release is the CTA's own: what
 // the arrivals here tell of lies in this CTA's shared memory (cells, through the fence of the proxies) or tensor
@@ -114,6 +91,10 @@ __device__ __forceinline__ void mma_commit_pair(unsigned long long* bar) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
       ::"r"(smem_u32(bar)), "h"(mask) : "memory");
+}
+// The same on a barrier of this CTA alone.
+__device__ __forceinline__ void commit_here(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // Tensor copies to this CTA's shared memory, completing on a barrier of either CTA of the pair.
 __device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -151,12 +132,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&sh->full[s], 1 + 2 * kScaleWarps);
+      mbar_init(&sh->full[s], 2);
+      mbar_init(&sh->scaled[s], 2 * kScaleWarps);
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) mbar_init(&sh->done[b], 1);
     mbar_init(&sh->drained, 2 * kEpiWarps);
     mbar_init(&sh->left, 1);
+    mbar_init(&sh->cells_left, 1);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -184,7 +167,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (warp < kEpiWarps) {
     // ---------------- outputs ----------------
-    const int quarter = warp & 3, half = warp >> 2;
+    const int quarter = warp & 3, part = warp >> 2;   // blocks of 16 rows: part, part + 4, ..
     const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
     uint32_t seen = 0;
     bool ok = true;
@@ -195,54 +178,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const bool live = j < A.N;
       // what the outputs need from memory, asked for before the sums are there
       const float bias = has_bias && live ? A.bias[it.e * A.ldb + j] : 0.0f;
-      float rs[TP / 32];   // of 16 rows each, every other 16 of the tile
+      float rs[4];
 #pragma unroll
-      for (int c = 0; c < TP / 32; ++c) {
-        const int x = 16 * (2 * c + half) + (lane & 15);
+      for (int c = 0; c < 4; ++c) {
+        const int x = 16 * (4 * c + part) + (lane & 15);
         rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
       }
       const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)(TP - kShared);
-      ok = __all_sync(kFull, mbar_wait_cluster(&sh->done[b], (seen >> 1) & 1u, failed));
+      ok = __all_sync(kFull, wait_phase<true>(&sh->done[b], (seen >> 1) & 1u, failed));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      // the columns that the accumulators share: the second one's first five blocks of 16, the first one's last
-      constexpr int kFirst = kShared / 16;
-      static_assert(kShared == 80 && TP == 256, "blocks 0 to 4 and 11 to 15");
-      const int lo = b ? 0 : TP / 16 - kFirst, hi = lo + kFirst;
-      const int c0 = (lo - half + 1) / 2, some = (hi - half + 1) / 2 - c0;   // this warp's: 2 c + half in lo .. hi - 1
-      uint32_t v[3][16];
+      // the columns that the accumulators share: the second one's first eight blocks of 16, the first one's last
+      static_assert(kShared == 128 && TP == 256, "blocks 0 to 7 and 8 to 15: two of each warp's");
+      const int c0 = b ? 0 : 2;   // this warp's first of two
+      uint32_t v[2][16];
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
-        if (i < some) tmem_load16(v[i], tacc + 16u * (uint32_t)(2 * (c0 + i) + half));
+      for (int i = 0; i < 2; ++i) tmem_load16(v[i], tacc + 16u * (uint32_t)(4 * (c0 + i) + part));
 #pragma unroll
-      for (int i = 0; i < 3; ++i) tmem_wait_ld(v[i]);
+      for (int i = 0; i < 2; ++i) tmem_wait_ld(v[i]);
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive_rank0(&sh->drained);
       auto put = [&](const uint32_t (&f)[16], int c) {
-        const int x0 = 16 * (2 * c + half), left = it.rows - x0;
+        const int x0 = 16 * (4 * c + part), left = it.rows - x0;
         if (left <= 0 || expire) return;
         float by = rs[0];
 #pragma unroll
-        for (int i = 1; i < TP / 32; ++i)
+        for (int i = 1; i < 4; ++i)
           if (c == i) by = rs[i];
-        TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j;
-#pragma unroll
-        for (int x = 0; x < 16; ++x, to += A.ldo) {
-          const TOut y = output<TOut>(__uint_as_float(f[x]), has_rs, __shfl_sync(kFull, by, x), has_bias, bias);
-          if (x < left && live) *to = y;
-        }
+        put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, f, by, 0, bias, left, live);
       };
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
-        if (i < some) put(v[i], c0 + i);
+      for (int i = 0; i < 2; ++i) put(v[i], c0 + i);
       // (read before the next tile's arrival: after that this accumulator may be written again)
 #pragma unroll 1
-      for (int i = some; i < TP / 32; ++i) {
-        const int c = (c0 + i) & (TP / 32 - 1);
-        if (16 * (2 * c + half) >= it.rows) continue;
+      for (int i = 2; i < 4; ++i) {
+        const int c = c0 ^ i;
+        if (16 * (4 * c + part) >= it.rows) continue;
         uint32_t f[16];
-        tmem_load16(f, tacc + 16u * (uint32_t)(2 * c + half));
+        tmem_load16(f, tacc + 16u * (uint32_t)(4 * c + part));
         tmem_wait_ld(f);
         put(f, c);
       }
@@ -295,7 +269,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             p1 = at;
             at.forward(1, kStages);
           }
-          ok = __all_sync(kFull, mbar_wait_cluster(&sh->empty[p1.s], p1.ph, failed));
+          ok = __all_sync(kFull, wait_phase<true>(&sh->empty[p1.s], p1.ph, failed));
           if (!ok) break;
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
@@ -310,8 +284,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive_rank0(&sh->full[p0.s]);
-            if (two) mbar_arrive_rank0(&sh->full[p1.s]);
+            mbar_arrive_rank0(&sh->scaled[p0.s]);
+            if (two) mbar_arrive_rank0(&sh->scaled[p1.s]);
           }
         }
       }
@@ -329,7 +303,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int wy = it.j0 + 128 * (int)rank, ay = (int)it.r0 + half * (int)rank;
 #pragma unroll 1
         for (int k = 0; k < steps; ++k) {
-          ok = mbar_wait_cluster(&sh->empty[s], ph, failed);
+          ok = wait_phase<true>(&sh->empty[s], ph, failed);
           if (!ok) break;
           const uint32_t to = smem_u32(base) + s * (uint32_t)kStageBytes, bar = rank0_address(&sh->full[s]);
           if (rank == 0) mbar_arrive_tx(&sh->full[s], 4 * kBlockBytes);
@@ -343,51 +317,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
       if (!ok && rank == 0) {
-        // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd one or
-        // a scale warp stopped earlier, the wait's limit is time enough for what is in flight)
+        // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd
+        // one stopped earlier, the wait's limit is time enough for what is in flight)
         for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
-          mbar_wait(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
+          wait_phase(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
-  } else if (rank == 0) {
-    // ---------------- MMAs of the pair ----------------
+  } else if (rank == 0 && warp == kCellWarp) {
+    // ---------------- scales to the pair's tensor memory ----------------
     const bool lead = elect_one();
-    const uint32_t d = uniform(tmem);
-    const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
     const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + 2u * kBlockBytes));
-    uint32_t s = 0, ph = 0, slot = 0, made = 0;
-    int64_t g = 0;                       // stages used
-    uint32_t old = 0, oph = 0;           // the stage kSlots before
+    const uint32_t sf0 = uniform(tmem) + (uint32_t)kSfCol;
+    uint32_t s = 0, ph = 0, slot = 0, old = 0, oph = 0;   // (old: the stage kSlots before)
+    int fresh = kSlots;                                   // slots that nothing has read yet
     bool ok = true;
 #pragma unroll 1
-    for (int64_t t = pair; t < tiles && ok; t += pairs, ++made) {
-      const Item it = tile_at(items, t);
-      const uint32_t acc = d + (made & 1u) * (uint32_t)(TP - kShared);
-      const uint32_t idesc = uniform(idesc_f4(TP, (it.rows + 31) & ~31));
-      // the columns that this accumulator shares with the one before are read, and all of its own
-      // were before those
-      if (made > 0) ok = __all_sync(kFull, mbar_wait_cluster(&sh->drained, (made - 1) & 1u, failed));
-      if (!ok) break;
-      // The scales of a step go to tensor memory before the MMAs of the step before it are issued:
-      // they then arrive while those run.
-      uint32_t last = s, last_slot = slot;
-      auto multiply = [&](int k) {
-        const uint64_t ad = desc0 + (uint64_t)(last * (uint32_t)(kStageBytes >> 4)), bd = ad + (uint64_t)(kBlockBytes >> 4);
-        const uint32_t sf = d + (uint32_t)kSfCol + (uint32_t)kSlotCols * last_slot;
-        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e == 0 || left > 32 * e)
-            mma_mx4_pair(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
-                         sf + 4 * (e >> 1), sf + 8 + 8 * (e >> 1), (k > 0 || e > 0) ? 1u : 0u);
-        mma_commit_pair(&sh->empty[last]);
-      };
+    for (int64_t t = pair; t < tiles && ok; t += pairs) {
 #pragma unroll 1
-      for (int k = 0; k < steps; ++k, ++g) {
-        ok = __all_sync(kFull, mbar_wait_cluster(&sh->full[s], ph, failed));
-        // the MMAs that read the scales in this slot
-        if (ok && g >= kSlots) {
-          ok = __all_sync(kFull, mbar_wait_cluster(&sh->empty[old], oph, failed));
+      for (int k = 0; k < steps; ++k) {
+        ok = __all_sync(kFull, wait_phase<true>(&sh->scaled[s], ph, failed));
+        if (fresh > 0) {
+          --fresh;
+        } else {
+          // the MMAs that read the scales in this slot
+          ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[old], oph, failed));
           if (++old == kStages) {
             old = 0;
             oph ^= 1u;
@@ -396,30 +349,70 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (lead) {
-          const uint64_t cd = cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4));
-          const uint32_t sf = d + (uint32_t)kSfCol + (uint32_t)kSlotCols * slot;
 #pragma unroll
-          for (int e = 0; e < 6; ++e) copy_cell_pair(sf + 4 * e, cd + (uint64_t)(e * (kCell >> 4)));
-          if (k > 0) multiply(k - 1);
+          for (int e = 0; e < 6; ++e)
+            copy_cell_pair(sf0 + (uint32_t)kSlotCols * slot + 4 * e, cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4) + e * (kCell >> 4)));
+          commit_here(&sh->full[s]);
         }
         __syncwarp();
-        last = s;
-        last_slot = slot;
         if (++slot == kSlots) slot = 0;
         if (++s == kStages) {
           s = 0;
           ph ^= 1u;
         }
       }
-      if (ok && lead) multiply(steps - 1);
-      __syncwarp();
+    }
+    if (lead) {
+      commit_here(&sh->cells_left);
+      wait_phase(&sh->cells_left, 0, &sh->left_failed);
+    }
+    __syncwarp();
+  } else if (rank == 0 && warp == kMmaWarp) {
+    // ---------------- MMAs of the pair ----------------
+    const bool lead = elect_one();
+    const uint32_t d = uniform(tmem);
+    const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
+    uint32_t s = 0, ph = 0, slot = 0, made = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int64_t t = pair; t < tiles && ok; t += pairs, ++made) {
+      const Item it = tile_at(items, t);
+      const uint32_t acc = d + (made & 1u) * (uint32_t)(TP - kShared);
+      const uint32_t idesc = uniform(idesc_f4(TP, (it.rows + 31) & ~31));
+      // the columns that this accumulator shares with the one before are read, and all of its own
+      // were before those
+      if (made > 0) ok = __all_sync(kFull, wait_phase<true>(&sh->drained, (made - 1) & 1u, failed));
+      if (!ok) break;
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k) {
+        ok = __all_sync(kFull, wait_phase<true>(&sh->full[s], ph, failed));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4)), bd = ad + (uint64_t)(kBlockBytes >> 4);
+        const uint32_t sf = d + (uint32_t)kSfCol + (uint32_t)kSlotCols * slot;
+        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
+        if (lead) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e == 0 || left > 32 * e)
+              mma_mx4_pair(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
+                           sf + 4 * (e >> 1), sf + 8 + 8 * (e >> 1), (k > 0 || e > 0) ? 1u : 0u);
+          mma_commit_pair(&sh->empty[s]);
+        }
+        __syncwarp();
+        if (++slot == kSlots) slot = 0;
+        if (++s == kStages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
       if (ok && lead) mma_commit_pair(&sh->done[made & 1u]);
       __syncwarp();
     }
     if (lead) {
       // no MMA outlives its operands and its tensor memory
       mma_commit_pair(&sh->left);
-      mbar_wait(&sh->left, 0, &sh->left_failed);
+      wait_phase(&sh->left, 0, &sh->left_failed);
     }
     __syncwarp();
   }
@@ -435,7 +428,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                : "=r"(peer) : "r"(smem_u32(&sh->failed)), "r"(rank ^ 1u) : "memory");
   const bool redo = peer != 0u || *failed != 0;
   // the last arrival that the even CTA's commits send here
-  if (rank != 0 && threadIdx.x == 0) mbar_wait(&sh->left, 0, &sh->left_failed);
+  if (rank != 0 && threadIdx.x == 0) wait_phase(&sh->left, 0, &sh->left_failed);
   __syncwarp();
   pair_sync();
   if (redo) {

@@ -12,8 +12,8 @@
 //     own, and store them to the stages as cells of 128 rows x 128 codes: the four bytes
 //     of row r at 16 (r % 32) + 4 (r / 32), which is how the MMA wants them in the lanes and
 //     columns of tensor memory;
-//   - one warp copies a stage's cells there (to all four quarters of the lanes) and issues the
-//     MMAs, 64 codes (two blocks) each;
+//   - one warp copies a stage's cells there, to all four quarters of the lanes;
+//   - one warp issues the MMAs, 64 codes (two blocks) each;
 //   - four warps write finished tiles while the next one's MMAs run (two accumulators).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share K and add their sums up
 // in the order of their ranks, through distributed shared memory.
@@ -29,7 +29,6 @@
 #include <cuda.h>
 
 #include "mx4_common.cuh"
-#include "tc_common.cuh"
 
 namespace bk {
 namespace {
@@ -39,8 +38,9 @@ using namespace mx4;
 
 constexpr int CM = 128;                  // channels of a tile
 constexpr int kMaxRows = 128;
+constexpr int kTwoRows = 32;             // rows of a tile up to which an SM has two CTAs
 constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
-constexpr int kEpiWarps = 4, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCopyWarp = kMmaWarp + 1;
+constexpr int kScaleWarps = 4;           // of a group; two groups
 constexpr int kLoadWarps = 8;
 constexpr int kRawRow = kStepBytes + 16; // of a row at any place: the chunks around 128 bytes
 constexpr int kDeep = 3;                 // steps of them in flight, and the one that is read
@@ -50,9 +50,9 @@ constexpr int kSlotCols = 16;            // of tensor memory for them
 constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
 
 struct __align__(8) TileShared {
-  unsigned long long full[kMaxStages], empty[kMaxStages];
+  unsigned long long scaled[kMaxStages], full[kMaxStages], empty[kMaxStages];   // cells; codes, and scales in tensor memory; read
   unsigned long long done[2], drained[2];
-  unsigned long long left;
+  unsigned long long left, cells_left;
   uint32_t tmem_base;
   int failed, left_failed;
 };
@@ -175,7 +175,7 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
       union { TOut e[4]; uint2 two; uint4 four; } out;
       const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) out.e[e] = output<TOut>(v[e], A.row_scale != nullptr, by, A.bias != nullptr, bias[e]);
+      for (int e = 0; e < 4; ++e) out.e[e] = output<TOut>(v[e], by, bias[e]);
       TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x) * A.ldo + j;
       if (vec) {
         if constexpr (sizeof(TOut) == 4) *reinterpret_cast<uint4*>(to) = out.four;
@@ -189,10 +189,14 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
   }
 }
 
-// kTma: the codes come by tensor copies (else their rows start anywhere).
-template <typename TOut, bool kTma>
-__global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps), kTma ? 2 : 1)
+// kTma: the codes come by tensor copies (else their rows start anywhere).  kEpiWarps: that write outputs.
+template <int kEpiWarps, bool kTma> struct Warps {
+  static constexpr int kMma = kEpiWarps + 2 * kScaleWarps, kCopy = kMma + 2, kAll = kCopy + (kTma ? 1 : kLoadWarps);
+};
+template <typename TOut, int kEpiWarps, bool kTma>
+__global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps == 4 ? 2 : 1)
     k_mx4_tile(const Mx4Args A, const __grid_constant__ Maps maps, const TilePlan P, int expire) {
+  constexpr int kMmaWarp = Warps<kEpiWarps, kTma>::kMma, kCellWarp = kMmaWarp + 1, kCopyWarp = kCellWarp + 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int stage_bytes = stage_size(P.nt);
@@ -205,7 +209,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P.stages; ++s) {
-      mbar_init(&sh->full[s], kScaleWarps + (kTma ? 1 : kLoadWarps));
+      mbar_init(&sh->full[s], 1 + (kTma ? 1 : kLoadWarps));
+      mbar_init(&sh->scaled[s], kScaleWarps);
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -213,6 +218,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       mbar_init(&sh->drained[b], kEpiWarps);
     }
     mbar_init(&sh->left, 1);
+    mbar_init(&sh->cells_left, 1);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -244,7 +250,8 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 
   if (warp < kEpiWarps) {
     // ---------------- outputs ----------------
-    const int quarter = warp;
+    constexpr int kParts = kEpiWarps / 4, kEach = (kEpiWarps == 4 ? kTwoRows : kMaxRows) / 16 / kParts;   // blocks of 16 rows: part, part + kParts, ..
+    const int quarter = warp & 3, part = warp >> 2;
     const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
     bool ok = true;
     uint32_t seen = 0;
@@ -255,19 +262,19 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       const bool live = j < A.N;
       // what the outputs need from memory, asked for before the sums are there
       const float bias = has_bias && live ? A.bias[it.e * A.ldb + j] : 0.0f;
-      float rs[kMaxRows / 32];   // of 32 rows each
+      float rs[kEach];
 #pragma unroll
-      for (int c = 0; c < kMaxRows / 32; ++c) {
-        const int x = 32 * c + lane;
+      for (int c = 0; c < kEach; ++c) {
+        const int x = 16 * (kParts * c + part) + (lane & 15);
         rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
       }
       const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)P.nt;
-      ok = __all_sync(kFull, mbar_wait(&sh->done[b], (seen >> 1) & 1u, failed));
+      ok = __all_sync(kFull, wait_phase(&sh->done[b], (seen >> 1) & 1u, failed));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-      for (int c = 0; c < kMaxRows / 16; ++c) {
-        const int x0 = 16 * c;
+      for (int c = 0; c < kEach; ++c) {
+        const int x0 = 16 * (kParts * c + part);
         if (x0 >= it.rows) break;
         uint32_t v[16];
         tmem_load16(v, tacc + (uint32_t)x0);
@@ -277,13 +284,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
 #pragma unroll
           for (int x = 0; x < 16; ++x) to[x * CM] = __uint_as_float(v[x]);
         } else if (!expire) {
-          const int left = it.rows - x0;
-          TOut* to = static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j;
-#pragma unroll
-          for (int x = 0; x < 16; ++x, to += A.ldo) {
-            const TOut y = output<TOut>(__uint_as_float(v[x]), has_rs, __shfl_sync(kFull, rs[c >> 1], 16 * (c & 1) + x), has_bias, bias);
-            if (x < left && live) *to = y;
-          }
+          put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, v, rs[c], 0, bias, it.rows - x0, live);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
         // up to kUnit + 1 + stages steps back, and the next asks for 2 stages - 1 (the second of two stages).
         if (P.stages < kUnit + 2)
           for (; others > 0 && ok; --others, passed.forward(1, P.stages))
-            ok = __all_sync(kFull, mbar_wait(&sh->empty[passed.s], passed.ph, failed));
+            ok = __all_sync(kFull, wait_phase(&sh->empty[passed.s], passed.ph, failed));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (!ok || k + 2 * h >= k1) break;
@@ -350,23 +351,23 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
             }
           };
           const Place& wait = both ? p1 : p0;
-          ok = __all_sync(kFull, mbar_wait(&sh->empty[wait.s], wait.ph, failed));
+          ok = __all_sync(kFull, wait_phase(&sh->empty[wait.s], wait.ph, failed));
           if (!ok) break;
           put(p0.s, 0);
           if (both) put(p1.s, 2);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive(&sh->full[p0.s]);
-            if (both) mbar_arrive(&sh->full[p1.s]);
+            mbar_arrive(&sh->scaled[p0.s]);
+            if (both) mbar_arrive(&sh->scaled[p1.s]);
           }
           if (two && !both) {
-            ok = __all_sync(kFull, mbar_wait(&sh->empty[p1.s], p1.ph, failed));
+            ok = __all_sync(kFull, wait_phase(&sh->empty[p1.s], p1.ph, failed));
             if (!ok) break;
             put(p1.s, 2);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh->full[p1.s]);
+            if (lane == 0) mbar_arrive(&sh->scaled[p1.s]);
           }
         }
       }
@@ -376,7 +377,6 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
     const bool lead = elect_one();
     const uint32_t d = uniform(tmem);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
-    const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + (uint32_t)(stage_bytes - kCells)));
     const uint32_t sf0 = d + 2u * (uint32_t)P.nt;
     uint32_t s = 0, ph = 0, made = 0;
     bool ok = true;
@@ -385,50 +385,70 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
       const Item it = at.at(items);
       const uint32_t b = made & 1u, acc = d + b * (uint32_t)P.nt;
       const uint32_t idesc = uniform(idesc_f4(CM, (it.rows + 15) & ~15));
-      ok = __all_sync(kFull, mbar_wait(&sh->drained[b], ((made >> 1) & 1u) ^ 1u, failed));
+      ok = __all_sync(kFull, wait_phase(&sh->drained[b], ((made >> 1) & 1u) ^ 1u, failed));
       if (!ok) break;
-      // The scales of a step go to tensor memory before the MMAs of the step before it are issued:
-      // they then arrive while those run.
-      uint32_t last = s;
-      auto multiply = [&](int k, uint32_t at) {
-        const uint64_t ad = desc0 + (uint64_t)(at * (uint32_t)(stage_bytes >> 4)), bd = ad + (uint64_t)(CM * kStepBytes >> 4);
-        const uint32_t sf = sf0 + (uint32_t)kSlotCols * at;
-        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e == 0 || left > 32 * e)
-            mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
-                    sf + 4 * (e >> 1), sf + 8 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
-        mma_commit(&sh->empty[at]);
-      };
 #pragma unroll 1
       for (int k = k0; k < k1; ++k) {
-        ok = __all_sync(kFull, mbar_wait(&sh->full[s], ph, failed));
+        ok = __all_sync(kFull, wait_phase(&sh->full[s], ph, failed));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4)), bd = ad + (uint64_t)(CM * kStepBytes >> 4);
+        const uint32_t sf = sf0 + (uint32_t)kSlotCols * s;
+        const int left = (int)min((int64_t)kStepBytes, bytes - (int64_t)k * kStepBytes);
         if (lead) {
-          const uint64_t cd = cells0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4));
-          const uint32_t sf = sf0 + (uint32_t)kSlotCols * s;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) copy_cell(sf + 4 * e, cd + (uint64_t)(e * (kCell >> 4)));
-          if (k > k0) multiply(k - 1, last);
+          for (int e = 0; e < 4; ++e)
+            if (e == 0 || left > 32 * e)
+              mma_mx4(acc, ad + 2 * e, bd + 2 * e, idesc | (uint32_t)((e & 1) * 2) << 4 | (uint32_t)((e & 1) * 2) << 29,
+                      sf + 4 * (e >> 1), sf + 8 + 4 * (e >> 1), (k > k0 || e > 0) ? 1u : 0u);
+          mma_commit(&sh->empty[s]);
         }
         __syncwarp();
-        last = s;
         if (++s == (uint32_t)P.stages) {
           s = 0;
           ph ^= 1u;
         }
       }
-      if (ok && lead) multiply(k1 - 1, last);
-      __syncwarp();
       if (ok && lead) mma_commit(&sh->done[b]);
       __syncwarp();
     }
     if (lead) {
       // no MMA outlives its operands and its tensor memory
       mma_commit(&sh->left);
-      mbar_wait(&sh->left, 0, &sh->left_failed);
+      wait_phase(&sh->left, 0, &sh->left_failed);
+    }
+    __syncwarp();
+  } else if (warp == kCellWarp) {
+    // ---------------- scales to tensor memory ----------------
+    // (by the MMA warp a step took 700 clocks of its issue, 53 a copy or MMA)
+    const bool lead = elect_one();
+    const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + (uint32_t)(stage_bytes - kCells)));
+    const uint32_t sf0 = uniform(tmem) + 2u * (uint32_t)P.nt;
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (Cursor at(items, first); at.live(items) && ok; at.next(items)) {
+#pragma unroll 1
+      for (int k = k0; k < k1; ++k) {
+        ok = __all_sync(kFull, wait_phase(&sh->scaled[s], ph, failed));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (lead) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            copy_cell(sf0 + (uint32_t)kSlotCols * s + 4 * e, cells0 + (uint64_t)(s * (uint32_t)(stage_bytes >> 4) + e * (kCell >> 4)));
+          mma_commit(&sh->full[s]);
+        }
+        __syncwarp();
+        if (++s == (uint32_t)P.stages) {
+          s = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+    if (lead) {
+      mma_commit(&sh->cells_left);
+      wait_phase(&sh->cells_left, 0, &sh->left_failed);
     }
     __syncwarp();
   } else if constexpr (kTma) {
@@ -442,7 +462,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
         const Item it = at.at(items);
 #pragma unroll 1
         for (int k = k0; k < k1; ++k) {
-          ok = mbar_wait(&sh->empty[s], ph, failed);
+          ok = wait_phase(&sh->empty[s], ph, failed);
           if (!ok) break;
           const uint32_t to = smem_u32(base + s * stage_bytes), bar = smem_u32(&sh->full[s]);
           mbar_arrive_tx(&sh->full[s], (uint32_t)(stage_bytes - kCells));
@@ -456,10 +476,10 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
         }
       }
       if (!ok) {
-        // no copy outlives its CTA (a phase of codes may lack the scale warps' arrivals, and then
-        // the wait's limit is time enough)
+        // no copy outlives its CTA (a phase may lack the scales' arrival, and then the wait's limit is
+        // time enough)
         for (int64_t k = copied > P.stages ? copied - P.stages : 0; k < copied; ++k)
-          mbar_wait(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed, 2000000ull);
+          wait_phase(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
   } else {
@@ -519,7 +539,7 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
         asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 2) : "memory");
         __syncwarp();   // every lane's copies of this step, and its reads of the step before
         copy(from == 0 ? kDeep - 1 : from - 1);
-        ok = __all_sync(kFull, mbar_wait(&sh->empty[s], ph, failed));
+        ok = __all_sync(kFull, wait_phase(&sh->empty[s], ph, failed));
         if (!ok) break;
         const uint32_t to = smem_u32(base + s * stage_bytes);
         auto part = [&](const int8_t* row, int64_t ld, int all, uint32_t src, int r0) {
@@ -582,14 +602,14 @@ __global__ void __launch_bounds__(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoad
   }
 }
 
-template <typename TOut, bool kTma>
+template <typename TOut, int kEpiWarps, bool kTma>
 cudaError_t launch_mode(const Mx4Args& A, const TilePlan& P, const Maps& maps, cudaStream_t st, int expire) {
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = allow_smem(done, k_mx4_tile<TOut, kTma>, 227 * 1024);
+  const cudaError_t e = allow_smem(done, k_mx4_tile<TOut, kEpiWarps, kTma>, 227 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.ctas);
-  cfg.blockDim = dim3(32 * (kTma ? kCopyWarp + 1 : kCopyWarp + kLoadWarps));
+  cfg.blockDim = dim3(32 * Warps<kEpiWarps, kTma>::kAll);
   cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages, kTma);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -600,12 +620,13 @@ cudaError_t launch_mode(const Mx4Args& A, const TilePlan& P, const Maps& maps, c
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = P.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_mx4_tile<TOut, kTma>, A, maps, P, expire);
+  return cudaLaunchKernelEx(&cfg, k_mx4_tile<TOut, kEpiWarps, kTma>, A, maps, P, expire);
 }
 
 template <typename TOut>
 cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const Maps& maps, bool tma, cudaStream_t st, int expire) {
-  return tma ? launch_mode<TOut, true>(A, P, maps, st, expire) : launch_mode<TOut, false>(A, P, maps, st, expire);
+  if (!tma) return launch_mode<TOut, 8, false>(A, P, maps, st, expire);
+  return P.nt > kTwoRows ? launch_mode<TOut, 16, true>(A, P, maps, st, expire) : launch_mode<TOut, 4, true>(A, P, maps, st, expire);
 }
 
 // Whether the pairs run faster.
@@ -624,8 +645,6 @@ cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
   const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = (A.n + some - 1) / some;
   const int64_t parts = (mean + kMaxRows - 1) / kMaxRows;
   P.nt = (int)std::min<int64_t>(kMaxRows, ((mean + parts - 1) / parts + 15) / 16 * 16);
-  // (two stages at least: the MMAs of one are issued when the next one is there)
-  while (P.nt > 16 && tile_smem(A, P.nt, 2, false) > 227 * 1024) P.nt -= 16;
   const int64_t rtiles = A.offsets ? some + (A.n - some) / P.nt : (A.n + P.nt - 1) / P.nt;   // at most
   const int64_t tiles = rtiles * P.ctiles;
   const int64_t chunks = ((int64_t)A.K + 511) / 512;
@@ -637,7 +656,7 @@ cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
   }
   const bool tma = code_maps(A, P.nt, &maps);
   // two CTAs of an SM where their tensor memory and registers have room
-  const bool two = tma && P.nt <= 64;
+  const bool two = tma && P.nt <= kTwoRows;
   P.cols = two ? 256 : 512;
   const int64_t room = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0, tma);
   P.stages = (int)std::min<int64_t>(two ? (256 - 2 * P.nt) / kSlotCols : kMaxStages, room / stage_size(P.nt));

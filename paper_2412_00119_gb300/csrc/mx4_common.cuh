@@ -7,6 +7,7 @@
 #include <cuda_fp16.h>
 
 #include "int8_common.cuh"
+#include "tc_common.cuh"
 
 namespace bk {
 namespace mx4 {
@@ -95,11 +96,60 @@ __device__ __forceinline__ void put_out(const Mx4Args& A, int64_t i, int j, int 
   else static_cast<__nv_bfloat16*>(A.out)[at] = out_cast<__nv_bfloat16>(y);
 }
 
-// An output from its sum.
+// An output from its sum; rs 1, bias 0 where there is none.
 template <typename T>
-__device__ __forceinline__ T output(float sum, bool has_rs, float rs, bool has_bias, float bias) {
-  const float y = has_rs ? __fmul_rn(sum, rs) : sum;
-  return out_cast<T>(has_bias ? __fadd_rn(y, bias) : y);
+__device__ __forceinline__ T output(float sum, float rs, float bias) { return out_cast<T>(__fadd_rn(__fmul_rn(sum, rs), bias)); }
+
+// A lane's channel of 16 rows, of which `rows` are some: to[0], to[ldo], ..  rs: of row x in lane lane0 + x.
+template <typename T>
+__device__ __forceinline__ void put_rows(T* to, int64_t ldo, const uint32_t (&sums)[16], float rs, int lane0, float bias, int rows,
+                                         bool live) {
+  T y[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) y[x] = output<T>(__uint_as_float(sums[x]), __shfl_sync(0xffffffffu, rs, lane0 + x), bias);
+  if (!live) return;
+  if (rows >= 16) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x, to += ldo) *to = y[x];
+  } else {
+#pragma unroll
+    for (int x = 0; x < 15; ++x, to += ldo)
+      if (x < rows) *to = y[x];
+  }
+}
+
+// Bounded waits as in tc_common.cuh, kCluster: with cluster-scope acquire (the barrier collects arrivals of the
+// peer).  A try may sleep for some 50 us: waiting warps that try again and again take the shared
+// memory's queue from the others.
+template <bool kCluster = false>
+__device__ __forceinline__ bool wait_phase(unsigned long long* bar, uint32_t parity, volatile int* failed,
+                                           unsigned long long limit = tc::kWaitCycles) {
+  const uint32_t a = tc::smem_u32(bar);
+  uint32_t ok;
+  auto try_wait = [&]() {
+    if constexpr (kCluster)
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 50000;\n"
+          " selp.u32 %0, 1, 0, p;\n}"
+          : "=r"(ok) : "r"(a), "r"(parity) : "memory");
+    else
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 50000;\n"
+          " selp.u32 %0, 1, 0, p;\n}"
+          : "=r"(ok) : "r"(a), "r"(parity) : "memory");
+  };
+  try_wait();
+  if (ok) return true;
+  const unsigned long long t0 = clock64();
+  while (true) {
+    try_wait();
+    if (ok) return true;
+    if (*failed) return false;
+    if (clock64() - t0 > limit) {
+      *failed = 1;
+      return false;
+    }
+  }
 }
 
 // Where a tile is.
