@@ -385,10 +385,6 @@ struct Mx4Args {
 cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire);
 // The tensor-core tiles of one CTA (kern_mx4_tile.cu).
 cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire);
-// Pairs of CTAs (kern_mx4_pair.cu), up to kPairGroups groups; cudaErrorNotSupported (and no launch)
-// where tensor copies cannot take the operands.
-constexpr int kPairGroups = 256;
-cudaError_t launch_mx4_pair(const Mx4Args& A, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

@@ -36,10 +36,10 @@ constexpr int kShared = 128;             // columns of both accumulators
 constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
 constexpr int kSlots = 5, kSlotCols = 24;
 static_assert(kSfCol + kSlots * kSlotCols <= 512 && kStageBytes % 1024 == 0, "tensor memory, swizzle atoms");
-// A wait tells a phase from the next by its parity, so the phase two before the one that is waited for must be
-// known to be over.  The last wait of a scale warp's unit before tells that of the MMAs up to kUnit + 1 +
-// kStages steps back, and the next asks for 2 kStages - 1 (the second of two stages).
-static_assert(kStages >= kUnit + 2, "phases");
+// A wait tells a phase from the next but one by nothing (a barrier's phases have a parity), so that one must be
+// over: a unit's first step waits for the MMAs of kStages steps before, and what its group of scale
+// warps waited for last tells of those up to kUnit + 1 + kStages.
+static_assert(kStages > kUnit, "phases");
 constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
 
 struct __align__(8) PairShared {
@@ -260,7 +260,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (k + 2 * h >= steps) break;
-          // (two stages together: the fence takes 200 clocks, and the MMAs free the stages in their order)
+          // (two stages together: the fence takes 200 clocks)
           const bool two = k + 2 * h + 1 < steps;
           const Place p0 = at;
           at.forward(1, kStages);
@@ -269,7 +269,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             p1 = at;
             at.forward(1, kStages);
           }
-          ok = __all_sync(kFull, wait_phase<true>(&sh->empty[p1.s], p1.ph, failed));
+          ok = __all_sync(kFull, wait_phase<true>(&sh->empty[p0.s], p0.ph, failed));
+          if (two) ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[p1.s], p1.ph, failed));
           if (!ok) break;
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
@@ -455,10 +456,8 @@ cudaError_t launch_pair(const Mx4Args& A, const Maps& maps, cudaStream_t st, int
 
 }  // namespace
 
-cudaError_t launch_mx4_pair(const Mx4Args& A, cudaStream_t st, int expire) {
+cudaError_t launch_mx4_pair(const Mx4Args& A, const mx4::Maps& maps, cudaStream_t st, int expire) {
   static_assert(pair_smem(kPairGroups) <= 227 * 1024, "shared memory");
-  Maps maps;
-  if (!code_maps(A, 128, &maps)) return cudaErrorNotSupported;
   if (A.type == BMLP_F32) return launch_pair<float>(A, maps, st, expire);
   if (A.type == BMLP_F16) return launch_pair<__half>(A, maps, st, expire);
   return launch_pair<__nv_bfloat16>(A, maps, st, expire);

@@ -7,7 +7,7 @@
 // and a warp's lanes hold 32 neighbouring channels of a row, as the output wants them.
 // Warps:
 //   - one thread copies stages of 256 codes of every row into a ring (rows at places that
-//     tensor copies cannot take: eight warps do, shifting whole 16-byte pieces);
+//     tensor copies cannot take: four warps copy the 16-byte chunks around them, and eight shift those to their places);
 //   - eight warps, four at a time, load the scales of 1024 codes (32 bytes) of every row, a row each lane's
 //     own, and store them to the stages as cells of 128 rows x 128 codes: the four bytes
 //     of row r at 16 (r % 32) + 4 (r / 32), which is how the MMA wants them in the lanes and
@@ -20,11 +20,11 @@
 // By group: the row tiles of a group start at its first row; what a tile has of the next
 // group's rows is multiplied and dropped.
 // Every wait is bounded; if one expires the CTA's tiles are made again on CUDA cores.
-// Measured (us): 1 x 8192 -> 8192 11.0, 100 x 4096 -> 8192 10.3, 96 x 4096 -> 2048 by 32 24.9, 16384 x 8192 ->
-// 8192 619.  (Scales one piece ahead in registers: 16.3, 19.3, 41, 1182, a turn then takes a
-// memory latency.  Stored to tensor memory by four warps, each with all rows': 11.6, 17.4, 26.4,
-// 748, 1,550 clocks of theirs per 512 codes.)
+// Measured (us): 1 x 8192 -> 8192 12.0, 100 x 4096 -> 8192 9.3, 96 x 4096 -> 2048 by 32 26, rows of 500 bytes at
+// odd places 1000 x 1000 -> 525 9.7.  A step of 256 codes takes 600 clocks where its MMAs (128 rows)
+// take 256: a tensor copy brings a row's 128 bytes in 2.4 clocks.
 #include <algorithm>
+#include <cmath>
 
 #include <cuda.h>
 
@@ -41,9 +41,9 @@ constexpr int kMaxRows = 128;
 constexpr int kTwoRows = 32;             // rows of a tile up to which an SM has two CTAs
 constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
 constexpr int kScaleWarps = 4;           // of a group; two groups
-constexpr int kLoadWarps = 8;
+constexpr int kRawWarps = 4, kShiftWarps = 8;
 constexpr int kRawRow = kStepBytes + 16; // of a row at any place: the chunks around 128 bytes
-constexpr int kDeep = 3;                 // steps of them in flight, and the one that is read
+constexpr int kMaxDeep = 6;              // steps of them in the ring
 constexpr int kMaxStages = 8;
 constexpr int kCells = 4 * kCell;        // of a stage: two of the channels, two of the rows
 constexpr int kSlotCols = 16;            // of tensor memory for them
@@ -51,6 +51,7 @@ constexpr int kUnit = 4;                 // steps whose scales a lane loads at o
 
 struct __align__(8) TileShared {
   unsigned long long scaled[kMaxStages], full[kMaxStages], empty[kMaxStages];   // cells; codes, and scales in tensor memory; read
+  unsigned long long raw_full[kMaxDeep], raw_empty[kMaxDeep];
   unsigned long long done[2], drained[2];
   unsigned long long left, cells_left;
   uint32_t tmem_base;
@@ -60,6 +61,7 @@ struct __align__(8) TileShared {
 struct TilePlan {
   int nt;          // rows of a tile, a multiple of 16
   int stages;
+  int deep;        // steps in the ring of rows that start anywhere; 0: tensor copies
   int cols;        // of tensor memory
   int split;       // CTAs that share K
   int ctiles;      // channel tiles
@@ -68,8 +70,8 @@ struct TilePlan {
 };
 
 __host__ __device__ constexpr int stage_size(int nt) { return (CM + nt) * kStepBytes + kCells; }
-int64_t tile_smem(const Mx4Args& A, int nt, int stages, bool tma) {
-  return 1024 + (tma ? 0 : (int64_t)kDeep * kRawRow * (CM + nt)) + (int64_t)stages * stage_size(nt) + (int64_t)sizeof(TileShared) +
+int64_t tile_smem(const Mx4Args& A, int nt, int stages, int deep) {
+  return 1024 + (int64_t)deep * kRawRow * (CM + nt) + (int64_t)stages * stage_size(nt) + (int64_t)sizeof(TileShared) +
          (A.offsets ? 8 * ((int64_t)A.E + 1) : 0);
 }
 
@@ -191,17 +193,17 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
 
 // kTma: the codes come by tensor copies (else their rows start anywhere).  kEpiWarps: that write outputs.
 template <int kEpiWarps, bool kTma> struct Warps {
-  static constexpr int kMma = kEpiWarps + 2 * kScaleWarps, kCopy = kMma + 2, kAll = kCopy + (kTma ? 1 : kLoadWarps);
+  static constexpr int kMma = kEpiWarps + 2 * kScaleWarps, kCopy = kMma + 2, kAll = kCopy + (kTma ? 1 : kRawWarps + kShiftWarps);
 };
 template <typename TOut, int kEpiWarps, bool kTma>
-__global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps == 4 ? 2 : 1)
+__global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEpiWarps == 4 ? 2 : 1)
     k_mx4_tile(const Mx4Args A, const __grid_constant__ Maps maps, const TilePlan P, int expire) {
   constexpr int kMmaWarp = Warps<kEpiWarps, kTma>::kMma, kCellWarp = kMmaWarp + 1, kCopyWarp = kCellWarp + 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int stage_bytes = stage_size(P.nt);
   uint8_t* ring = base + P.stages * stage_bytes;
-  TileShared* sh = reinterpret_cast<TileShared*>(ring + (kTma ? 0 : kDeep * kRawRow * (CM + P.nt)));
+  TileShared* sh = reinterpret_cast<TileShared*>(ring + P.deep * kRawRow * (CM + P.nt));
   int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t S = (uint32_t)P.split, rank = S > 1 ? cluster_rank() : 0u;
@@ -209,9 +211,13 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P.stages; ++s) {
-      mbar_init(&sh->full[s], 1 + (kTma ? 1 : kLoadWarps));
+      mbar_init(&sh->full[s], 1 + (kTma ? 1 : kShiftWarps));
       mbar_init(&sh->scaled[s], kScaleWarps);
       mbar_init(&sh->empty[s], 1);
+    }
+    for (int s = 0; s < P.deep; ++s) {
+      mbar_init(&sh->raw_full[s], 32 * kRawWarps);
+      mbar_init(&sh->raw_empty[s], kShiftWarps);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&sh->done[b], 1);
@@ -250,7 +256,7 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
 
   if (warp < kEpiWarps) {
     // ---------------- outputs ----------------
-    constexpr int kParts = kEpiWarps / 4, kEach = (kEpiWarps == 4 ? kTwoRows : kMaxRows) / 16 / kParts;   // blocks of 16 rows: part, part + kParts, ..
+    constexpr int kParts = kEpiWarps / 4, kEach = (kTma && kEpiWarps == 4 ? kTwoRows : kMaxRows) / 16 / kParts;   // blocks of 16 rows: part, part + kParts, ..
     const int quarter = warp & 3, part = warp >> 2;
     const bool has_rs = A.row_scale != nullptr, has_bias = A.bias != nullptr;
     bool ok = true;
@@ -300,19 +306,20 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
     const bool second = warp >= kEpiWarps + kScaleWarps, has_row = r < P.nt, whole = P.whole != 0;
     const int len = (int)(((int64_t)A.K + 31) / 32);
     const uint32_t cells = smem_u32(base) + (uint32_t)(stage_bytes - kCells) + 16u * (uint32_t)lane + 4u * (uint32_t)q;
-    Place at = {0, 1u}, passed = at;
-    int others = 0;                      // steps of the other group's unit before this one, from `passed` on
+    // A wait tells a phase from the next but one by nothing (a barrier's phases have a parity), so that one must
+    // be over: a unit's first step waits for the MMAs of P.stages steps before, and what this group waited
+    // for last tells of those up to kUnit + 1 + P.stages.  Shorter rings have one group.
+    const bool alone = P.stages <= kUnit;
+    Place at = {0, 1u};
     bool ok = true, mine = !second;
 #pragma unroll 1
     for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
       const uint8_t *wrow = nullptr, *arow = nullptr;
       bool wlive = false, alive = false, known = false;
 #pragma unroll 1
-      for (int k = k0; k < k1 && ok; k += kUnit, mine = !mine) {
+      for (int k = k0; k < k1 && ok; k += kUnit, mine = mine == alone) {
         if (!mine) {
-          passed = at;
-          others = min(kUnit, k1 - k);
-          at.forward(others, P.stages);
+          at.forward(min(kUnit, k1 - k), P.stages);
           continue;
         }
         if (!known) {
@@ -326,18 +333,11 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
         uint32_t w[2][4], a[2][4];
         load_scales(w, wrow, wlive, whole, 8 * k, len);
         load_scales(a, arow, alive, whole, 8 * k, len);
-        // A wait tells a phase from the next by its parity, so the phase two before the one that is waited
-        // for must be known to be over.  The last wait of this group's unit before tells that of the MMAs
-        // up to kUnit + 1 + stages steps back, and the next asks for 2 stages - 1 (the second of two stages).
-        if (P.stages < kUnit + 2)
-          for (; others > 0 && ok; --others, passed.forward(1, P.stages))
-            ok = __all_sync(kFull, wait_phase(&sh->empty[passed.s], passed.ph, failed));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (!ok || k + 2 * h >= k1) break;
-          // Two stages at a time where the ring is long: the fence takes 200 clocks.  (The MMAs free
-          // the stages in their order.)
-          const bool two = k + 2 * h + 1 < k1, both = two && P.stages >= 4;
+          // two stages at a time where the ring is long: the fence takes 200 clocks
+          const bool two = k + 2 * h + 1 < k1, both = two && !alone;
           const Place p0 = at;
           at.forward(1, P.stages);
           const Place p1 = at;
@@ -350,8 +350,8 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
               if (has_row) sts32(to + (uint32_t)(kCell * (2 + y)), a[h][y0 + y]);
             }
           };
-          const Place& wait = both ? p1 : p0;
-          ok = __all_sync(kFull, wait_phase(&sh->empty[wait.s], wait.ph, failed));
+          ok = __all_sync(kFull, wait_phase(&sh->empty[p0.s], p0.ph, failed));
+          if (both) ok = ok && __all_sync(kFull, wait_phase(&sh->empty[p1.s], p1.ph, failed));
           if (!ok) break;
           put(p0.s, 0);
           if (both) put(p1.s, 2);
@@ -483,88 +483,92 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kEpiWarps =
       }
     }
   } else {
-    // ---------------- loads ----------------
-    // Each warp for itself: the aligned 16-byte chunks around 16 channels' and nt / 8 rows' codes
-    // to a ring, kDeep steps ahead, and from there, shifted to their places, to the stage.
-    const int w = warp - kCopyWarp, c = lane & 7, sub = lane >> 3, mine = P.nt / kLoadWarps;
+    // ---------------- rows that start anywhere ----------------
     const int len = (int)bytes;
-    const uint32_t raw_bytes = (uint32_t)(kRawRow * (CM + P.nt));
-    const uint32_t raw = smem_u32(ring) + (uint32_t)(kRawRow * 16 * w);
-    const uint32_t raw_a = raw + (uint32_t)(kRawRow * (CM - 16 * w + mine * w));
-    const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.a));
-    const int8_t *wrow = any, *arow = any;   // the warp's first
-    int wlive = 0, alive = 0, nk = k0;       // how many of its rows there are
-    Cursor ahead(items, first);
-    auto rows_of = [&](const Item& it) {
-      const int j = it.j0 + 16 * w, i = mine * w;
-      wlive = min(16, A.N - j);
-      alive = min(mine, it.rows - i);
-      wrow = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)j * A.ldw;
-      arow = reinterpret_cast<const int8_t*>(A.a) + (it.r0 + i) * A.lda;
-    };
-    auto copy = [&](uint32_t slot) {
-      if (ahead.live(items)) {
-        const int k = nk * kStepBytes;
-        auto part = [&](const int8_t* rows, int64_t ld, int all, int live, uint32_t to) {
-          const int8_t* row = rows + sub * ld;
-          for (int r = sub; r < all; r += 4, row += 4 * ld)
-            i8::copy_chunk(to + (uint32_t)(kRawRow * r + 16 * c), row, i8::row_shift<1>(row), k + 16 * c, r < live ? len : -16, any);
-          if (lane < all) {
-            row = rows + lane * ld;
-            i8::copy_chunk(to + (uint32_t)(kRawRow * lane + 128), row, i8::row_shift<1>(row), k + 128, lane < live ? len : -16, any);
+    const uint32_t raw0 = smem_u32(ring), raw_bytes = (uint32_t)(kRawRow * (CM + P.nt));
+    uint32_t slot = 0, rph = 0;
+    bool ok = true;
+    if (warp < kCopyWarp + kRawWarps) {
+      // Four warps copy the aligned 16-byte chunks around 128 bytes of every row to a ring.  (Not the warps that
+      // fill the stages: their fence would wait for the copies ahead, a memory latency each step.)
+      const int l = (int)threadIdx.x - 32 * kCopyWarp, c = l & 7, sub = l >> 3;
+      const int8_t* any = i8::aligned16(reinterpret_cast<const int8_t*>(A.a));
+#pragma unroll 1
+      for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
+        const Item it = cur.at(items);
+        const int8_t* w0 = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)it.j0 * A.ldw;
+        const int8_t* a0 = reinterpret_cast<const int8_t*>(A.a) + it.r0 * A.lda;
+        const int wlive = A.N - it.j0;
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k) {
+          ok = __all_sync(kFull, wait_phase(&sh->raw_empty[slot], rph ^ 1u, failed));
+          if (!ok) break;
+          const uint32_t to = raw0 + slot * raw_bytes;
+          const int byte = k * kStepBytes;
+          auto part = [&](const int8_t* rows, int64_t ld, int all, int live, uint32_t dst) {
+            const int8_t* row = rows + sub * ld;
+#pragma unroll 4
+            for (int r = sub; r < all; r += 4 * kRawWarps, row += 4 * kRawWarps * ld)
+              i8::copy_chunk(dst + (uint32_t)(kRawRow * r + 16 * c), row, i8::row_shift<1>(row), byte + 16 * c, r < live ? len : -16, any);
+            if (l < all) {
+              row = rows + l * ld;
+              i8::copy_chunk(dst + (uint32_t)(kRawRow * l + 128), row, i8::row_shift<1>(row), byte + 128, l < live ? len : -16, any);
+            }
+          };
+          part(w0, A.ldw, CM, wlive, to);
+          part(a0, A.lda, P.nt, it.rows, to + (uint32_t)(kRawRow * CM));
+          cp_async_arrive(&sh->raw_full[slot]);
+          if (++slot == (uint32_t)P.deep) {
+            slot = 0;
+            rph ^= 1u;
           }
-        };
-        part(wrow, A.ldw, 16, wlive, raw + slot * raw_bytes);
-        part(arow, A.lda, mine, alive, raw_a + slot * raw_bytes);
-        if (++nk == k1) {
-          nk = k0;
-          ahead.next(items);
-          if (ahead.live(items)) rows_of(ahead.at(items));
         }
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    if (ahead.live(items)) rows_of(ahead.at(items));
+      cp_async_wait_all();
+    } else {
+      // Eight warps shift them to their places in the stages: 16 channels and nt / 8 rows each.
+      const int w = warp - kCopyWarp - kRawWarps, c = lane & 7, sub = lane >> 3, mine = P.nt / kShiftWarps;
+      uint32_t s = 0, ph = 1;
 #pragma unroll 1
-    for (int d = 0; d < kDeep - 1; ++d) copy((uint32_t)d);
-    uint32_t s = 0, ph = 1, from = 0;
-    bool ok = true;
+      for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
+        const Item it = cur.at(items);
+        const int8_t* w0 = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)(it.j0 + 16 * w + sub) * A.ldw;
+        const int8_t* a0 = reinterpret_cast<const int8_t*>(A.a) + (it.r0 + mine * w + sub) * A.lda;
 #pragma unroll 1
-    for (Cursor cur(items, first); cur.live(items) && ok; cur.next(items)) {
-      const Item it = cur.at(items);
-      const int8_t* w0 = reinterpret_cast<const int8_t*>(A.w) + it.e * A.gw + (int64_t)(it.j0 + 16 * w + sub) * A.ldw;
-      const int8_t* a0 = reinterpret_cast<const int8_t*>(A.a) + (it.r0 + mine * w + sub) * A.lda;
-#pragma unroll 1
-      for (int k = k0; k < k1; ++k) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 2) : "memory");
-        __syncwarp();   // every lane's copies of this step, and its reads of the step before
-        copy(from == 0 ? kDeep - 1 : from - 1);
-        ok = __all_sync(kFull, wait_phase(&sh->empty[s], ph, failed));
-        if (!ok) break;
-        const uint32_t to = smem_u32(base + s * stage_bytes);
-        auto part = [&](const int8_t* row, int64_t ld, int all, uint32_t src, int r0) {
-#pragma unroll 2
-          for (int r = sub; r < all; r += 4, row += 4 * ld) {
-            uint32_t lo[4], hi[4], v[4];
-            i8::lds_chunk(lo, src + (uint32_t)(kRawRow * r + 16 * c));
-            i8::lds_chunk(hi, src + (uint32_t)(kRawRow * r + 16 * c + 16));
-            i8::merge16(v, lo, hi, i8::row_shift<1>(row));
-            sts128(to + 128u * (uint32_t)(r0 + r) + 16u * (uint32_t)(c ^ ((r0 + r) & 7)), v);
+        for (int k = k0; k < k1; ++k) {
+          ok = __all_sync(kFull, wait_phase(&sh->raw_full[slot], rph, failed));
+          ok = ok && __all_sync(kFull, wait_phase(&sh->empty[s], ph, failed));
+          if (!ok) break;
+          const uint32_t to = smem_u32(base + s * stage_bytes), src = raw0 + slot * raw_bytes;
+          auto part = [&](const int8_t* row, int64_t ld, int all, int r0) {
+#pragma unroll 4
+            for (int r = sub; r < all; r += 4, row += 4 * ld) {
+              uint32_t lo[4], hi[4], v[4];
+              i8::lds_chunk(lo, src + (uint32_t)(kRawRow * (r0 + r) + 16 * c));
+              i8::lds_chunk(hi, src + (uint32_t)(kRawRow * (r0 + r) + 16 * c + 16));
+              i8::merge16(v, lo, hi, i8::row_shift<1>(row));
+              sts128(to + 128u * (uint32_t)(r0 + r) + 16u * (uint32_t)(c ^ ((r0 + r) & 7)), v);
+            }
+          };
+          part(w0, A.ldw, 16, 16 * w);
+          part(a0, A.lda, mine, CM + mine * w);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&sh->raw_empty[slot]);
+            mbar_arrive(&sh->full[s]);
           }
-        };
-        part(w0, A.ldw, 16, raw + from * raw_bytes, 16 * w);
-        part(a0, A.lda, mine, raw_a + from * raw_bytes, CM + mine * w);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh->full[s]);
-        if (++from == kDeep) from = 0;
-        if (++s == (uint32_t)P.stages) {
-          s = 0;
-          ph ^= 1u;
+          if (++slot == (uint32_t)P.deep) {
+            slot = 0;
+            rph ^= 1u;
+          }
+          if (++s == (uint32_t)P.stages) {
+            s = 0;
+            ph ^= 1u;
+          }
         }
       }
     }
-    cp_async_wait_all();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -610,7 +614,7 @@ cudaError_t launch_mode(const Mx4Args& A, const TilePlan& P, const Maps& maps, c
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)P.ctas);
   cfg.blockDim = dim3(32 * Warps<kEpiWarps, kTma>::kAll);
-  cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages, kTma);
+  cfg.dynamicSmemBytes = (size_t)tile_smem(A, P.nt, P.stages, P.deep);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -629,40 +633,70 @@ cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const Maps& maps, b
   return P.nt > kTwoRows ? launch_mode<TOut, 16, true>(A, P, maps, st, expire) : launch_mode<TOut, 4, true>(A, P, maps, st, expire);
 }
 
-// Whether the pairs run faster.
-bool pair_wins(const Mx4Args& A) {
-  const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = A.n / some;
-  return A.E <= kPairGroups && mean > 128 && ((mean + 255) / 256) * some * ((A.N + 255) / 256) >= sm_count() / 2;
+// What a call costs, in us, by lines fitted to measurements of every plan at some 40 sizes: a launch and
+// what follows the last sum; per round of tiles its steps of 256 codes and its outputs; CTAs that share K.
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t some_groups(const Mx4Args& A) { return A.offsets ? std::min<int64_t>(A.E, A.n) : 1; }
+// Row tiles at most, and on average (of a group's rows the last one is half full).
+int64_t most_row_tiles(const Mx4Args& A, int nt) {
+  const int64_t some = some_groups(A);
+  return A.offsets ? some + (A.n - some) / nt : up(A.n, nt);
+}
+double row_tiles(const Mx4Args& A, int nt) {
+  const double some = (double)some_groups(A);
+  return A.offsets ? std::max(some, (double)A.n / nt + 0.5 * some) : (double)up(A.n, nt);
+}
+double tile_cost(const Mx4Args& A, int nt, int split, bool tma) {
+  const double ctiles = (double)up(A.N, CM), steps = (double)up(up(A.K, 256), split), sms = (double)sm_count();
+  const bool two = tma && nt <= kTwoRows;
+  // (clusters of eight: more than a dozen find no room at once)
+  const double room = split == 8 ? 100.0 : (two ? 2 : 1) * sms;
+  if (split > 1 && ((double)most_row_tiles(A, nt) * ctiles * split > room || 512ll * split > A.K)) return 1e30;
+  const double ctas = row_tiles(A, nt) * ctiles * split, rounds = std::ceil(ctas / ((two ? 2 : 1) * sms));
+  const double step = tma ? (two && ctas > sms ? 0.36 : 0.20 + 0.0006 * nt) : 0.88 + 0.003 * nt;
+  return 4.2 + rounds * (steps * step + 0.3 + 0.008 * nt) + (split > 1 ? 2.1 + 0.05 * split : 0.0);
+}
+double pair_cost(const Mx4Args& A) {
+  const double tiles = row_tiles(A, 256) * (double)up(A.N, 256), steps = (double)up(A.K, 256);
+  return 7.9 + std::ceil(tiles / (sm_count() / 2)) * std::max(3.0, 0.4 * steps);
 }
 
 }  // namespace
 
 cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
-  const int sms = sm_count();
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
   TilePlan P = {};
-  P.ctiles = (int)(((int64_t)A.N + CM - 1) / CM);
-  // rows of a tile: the rows, or a group's on average, in equal parts
-  const int64_t some = A.offsets ? std::min<int64_t>(A.E, A.n) : 1, mean = (A.n + some - 1) / some;
-  const int64_t parts = (mean + kMaxRows - 1) / kMaxRows;
-  P.nt = (int)std::min<int64_t>(kMaxRows, ((mean + parts - 1) / parts + 15) / 16 * 16);
-  const int64_t rtiles = A.offsets ? some + (A.n - some) / P.nt : (A.n + P.nt - 1) / P.nt;   // at most
-  const int64_t tiles = rtiles * P.ctiles;
-  const int64_t chunks = ((int64_t)A.K + 511) / 512;
-  P.whole = scales_whole(A);
   Maps maps;
-  if (pair_wins(A)) {
-    const cudaError_t e = launch_mx4_pair(A, st, expire);
-    if (e != cudaErrorNotSupported) return e;
+  const bool tma = codes_whole(A);
+  double best = 1e30;
+  const int64_t mean = up(A.n, some_groups(A));
+  for (int nt = 16; nt <= kMaxRows; nt += nt < 64 ? 16 : 32) {
+    for (int split = 1; split <= 8; split *= 2) {
+      const double us = tile_cost(A, nt, split, tma);
+      if (us < best) {
+        best = us;
+        P.nt = nt;
+        P.split = split;
+      }
+    }
+    if (nt >= mean && !A.offsets) break;
   }
-  const bool tma = code_maps(A, P.nt, &maps);
+  const bool pairs = tma && A.E <= kPairGroups && pair_cost(A) < best;
+  if (tma && (!code_map(&maps.w, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) ||
+              !code_map(&maps.a, A.a, bytes, A.n, A.lda, 0, 0, pairs ? 128 : P.nt)))
+    return cudaErrorInvalidValue;
+  if (pairs) return launch_mx4_pair(A, maps, st, expire);
+  P.ctiles = (int)up(A.N, CM);
+  const int64_t tiles = most_row_tiles(A, P.nt) * P.ctiles;
+  P.whole = scales_whole(A);
   // two CTAs of an SM where their tensor memory and registers have room
   const bool two = tma && P.nt <= kTwoRows;
   P.cols = two ? 256 : 512;
-  const int64_t room = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0, tma);
-  P.stages = (int)std::min<int64_t>(two ? (256 - 2 * P.nt) / kSlotCols : kMaxStages, room / stage_size(P.nt));
-  const int64_t slots = (two ? 2 : 1) * (int64_t)sms;
-  P.split = 1;
-  while (P.split < 8 && 2 * P.split <= chunks && tiles * P.split * 2 <= slots) P.split *= 2;
+  // (the ring takes up to half)
+  const int64_t all = (two ? 113 : 227) * 1024 - tile_smem(A, P.nt, 0, 0), row = kRawRow * (int64_t)(CM + P.nt);
+  P.deep = tma ? 0 : (int)std::min<int64_t>(kMaxDeep, all / 2 / row);
+  P.stages = (int)std::min<int64_t>(kMaxStages, (all - P.deep * row) / stage_size(P.nt));
+  const int64_t slots = (two ? 2 : 1) * (int64_t)sm_count();
   P.ctas = (int)(P.split > 1 ? tiles * P.split : std::min(tiles, slots));
   if (A.type == BMLP_F32) return launch_tile<float>(A, P, maps, tma, st, expire);
   if (A.type == BMLP_F16) return launch_tile<__half>(A, P, maps, tma, st, expire);

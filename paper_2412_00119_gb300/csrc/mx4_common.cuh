@@ -12,8 +12,8 @@
 namespace bk {
 namespace mx4 {
 
-// Map of rows of codes, 128 bytes of box_rows rows at a time, in the 128B-swizzled order that the MMAs read; groups > 0: of groups of rows.  False where tensor copies cannot
-// take them: rows or groups that do not start at multiples of 16 bytes.
+// Map of rows of codes, 128 bytes of box_rows rows at a time, in the 128B-swizzled order that the MMAs read;
+// groups > 0: of groups of rows.  (Rows and groups start at multiples of 16 bytes.)
 inline bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t bytes, int64_t rows, int64_t ld, int64_t groups,
                     int64_t group_ld, int box_rows) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -30,9 +30,7 @@ inline bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t bytes, int6
   const int64_t least = (bytes + 15) / 16 * 16;
   if (rows == 1) ld = least;                  // (a stride that nothing uses)
   if (groups <= 1) group_ld = least;
-  if (!encode || ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)ld | (uintptr_t)group_ld) & 15) != 0 || group_ld == 0 ||
-      ld >= (1ll << 40) || group_ld >= (1ll << 40))
-    return false;
+  if (!encode) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)bytes, (cuuint64_t)rows, (cuuint64_t)groups};
   const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)group_ld};
   const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
@@ -44,11 +42,13 @@ inline bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t bytes, int6
 struct Maps {
   CUtensorMap w, a;
 };
-inline bool code_maps(const Mx4Args& A, int rows, Maps* m) {
-  const int64_t bytes = ((int64_t)A.K + 1) / 2;
-  return code_map(&m->w, A.w, bytes, A.N, A.ldw, A.E, A.gw, 128) && code_map(&m->a, A.a, bytes, A.n, A.lda, 0, 0, rows);
-}
 
+// Whether tensor copies can take the codes of both.
+inline bool codes_whole(const Mx4Args& A) {
+  const uint64_t a = A.n > 1 ? (uint64_t)A.lda : 0, w = A.N > 1 ? (uint64_t)A.ldw : 0, g = A.E > 1 ? (uint64_t)A.gw : 16;
+  return ((reinterpret_cast<uintptr_t>(A.a) | reinterpret_cast<uintptr_t>(A.w) | a | w | g) & 15) == 0 && g != 0 &&
+         a < (1ull << 40) && w < (1ull << 40) && g < (1ull << 40);
+}
 // Whether every row's scales start at a multiple of 16 bytes.
 inline bool scales_whole(const Mx4Args& A) {
   return ((reinterpret_cast<uintptr_t>(A.as) | reinterpret_cast<uintptr_t>(A.ws) | (uintptr_t)(A.n > 1 ? A.ldas : 0) |
@@ -239,20 +239,48 @@ __device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
   asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 
-// The scale bytes of 1024 codes (32) of a row from byte k (a multiple of 16) on, zeros from len on.  whole: the row
-// starts at a multiple of 16 bytes.
+// kChunks aligned 16-byte chunks from p on, of which the first `size` bytes are read (none where size <= 0) and the
+// rest are zeros; tail: where there may be a chunk of which a part is.  No branches: all loads are
+// under way together.
+template <int kChunks>
+__device__ __forceinline__ void load_chunks(uint32_t (&v)[kChunks][4], const int8_t* p, int size, bool tail) {
+#pragma unroll
+  for (int h = 0; h < kChunks; ++h) {
+    v[h][0] = v[h][1] = v[h][2] = v[h][3] = 0u;
+    asm volatile("{\n .reg .pred q;\n setp.ge.s32 q, %5, 16;\n @q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                 : "+r"(v[h][0]), "+r"(v[h][1]), "+r"(v[h][2]), "+r"(v[h][3]) : "l"(p + 16 * h), "r"(size - 16 * h));
+  }
+  if (tail) {
+    const int h = size >> 4, left = size > 0 && h < kChunks ? size & 15 : 0;   // the chunk, and its bytes
+    uint32_t b[15];
+#pragma unroll
+    for (int x = 0; x < 15; ++x) {
+      b[x] = 0u;
+      asm volatile("{\n .reg .pred q;\n setp.gt.s32 q, %2, %3;\n @q ld.global.nc.u8 %0, [%1];\n}"
+                   : "+r"(b[x]) : "l"(p + 16 * h + x), "r"(left), "r"(x));
+    }
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const uint32_t w = b[4 * y] | b[4 * y + 1] << 8 | b[4 * y + 2] << 16 | (y < 3 ? b[y < 3 ? 4 * y + 3 : 0] << 24 : 0u);
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i)
+        if (i == h) v[i][y] |= w;
+    }
+  }
+}
+
+// The scale bytes of 1024 codes (32) of a row from byte k (a multiple of 16) on, zeros from len on.  whole: every
+// row starts at a multiple of 16 bytes.
 __device__ __forceinline__ void load_scales(uint32_t (&v)[2][4], const uint8_t* row, bool live, bool whole, int k, int len) {
   const int8_t* p = reinterpret_cast<const int8_t*>(row);
-  if (!live) {
-#pragma unroll
-    for (int y = 0; y < 8; ++y) v[y >> 2][y & 3] = 0u;
-  } else if (whole) {
-    i8::load16<16>(v[0], p, 0, k, len);
-    i8::load16<16>(v[1], p, 0, k + 16, len);
+  if (whole) {
+    load_chunks<2>(v, p + k, live ? len - k : 0, len - k < 32);
   } else {
     const int shift = i8::row_shift<1>(p);
-    i8::load16<1>(v[0], p, shift, k, len);
-    i8::load16<1>(v[1], p, shift, k + 16, len);
+    uint32_t c[3][4];
+    load_chunks<3>(c, p + (k - shift), live ? len - k + shift : 0, len - k < 48);
+    i8::merge16(v[0], c[0], c[1], shift);
+    i8::merge16(v[1], c[1], c[2], shift);
   }
 }
 // Place in a ring of stages, and the parity of its "empty" barrier's phase that a writer waits for.
@@ -269,4 +297,8 @@ struct Place {
 };
 
 }  // namespace mx4
+
+// Pairs of CTAs (kern_mx4_pair.cu), up to kPairGroups groups; maps: of 128 rows at a time.
+constexpr int kPairGroups = 256;
+cudaError_t launch_mx4_pair(const Mx4Args& A, const mx4::Maps& maps, cudaStream_t st, int expire);
 }  // namespace bk

@@ -511,6 +511,35 @@ def test_groups_that_share_weights():
         assert torch.equal(out[i:j].double(), decoded(a[i:j], sa[i:j], K) @ decoded(w[2 * e], sw[2 * e], K).t())
 
 
+@gpu
+@pytest.mark.parametrize("n,K,N,E", [(16, 4096, 60000, 1), (32, 2048, 60000, 1), (5000, 2048, 300, 1), (1000, 4096, 4096, 1),
+                                     (3000, 2304, 3000, 1), (96, 4096, 2048, 32), (200, 1280, 4096, 30), (4000, 1536, 2048, 5)])
+@pytest.mark.parametrize("pad", [-1, 0, 1])
+def test_no_wait_expires(n, K, N, E, pad):
+    """Several tiles, rings and units a CTA: the calls end long before a bounded wait (2 s) would, so none was
+    taken as expired (an expired one costs time only)."""
+    a, sa = coded(n, K, 1, pad=pad)
+    w, sw = coded((E, N), K, 2, pad=pad)
+    at = torch.linspace(0, n, E + 1).to(torch.int32).to(DEV)
+    out = torch.empty((n, N), dtype=torch.bfloat16, device=DEV)
+
+    def call():
+        if E == 1:
+            B.bmlp_mx4_matmul(a, sa, w[0], sw[0], out)
+        else:
+            B.bmlp_mx4_matmul_grouped(a, sa, w, sw, at, out)
+
+    call()
+    torch.cuda.synchronize()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    for _ in range(3):
+        call()
+    end.record()
+    torch.cuda.synchronize()
+    assert begin.elapsed_time(end) < 1000
+
+
 # -- as they are used ------------------------------------------------------------------
 
 @gpu
