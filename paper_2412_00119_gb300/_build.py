@@ -7,14 +7,18 @@ library needs only the driver at run time.
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
+import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libbmlp.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")    # bmlp.py uses it where it is there
 SOURCES = ["bmlp_api.cu", "bmlp_noalloc.cu", "kern_forward.cu", "kern_forward_tc.cu", "kern_eval_tc.cu",
            "kern_update.cu", "kern_binarize.cu", "kern_expand.cu", "kern_peaks.cu", "kern_forward_b1.cu",
            "kern_update_rows.cu", "kern_update_ws.cu", "kern_quantize.cu", "kern_int8.cu",
@@ -40,12 +44,50 @@ def _stale(out: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _marshal_job(force: bool):
+    """The compiler's command for the marshalling of torch tensors (csrc/marshal.cpp), None
+    where it is up to date or there is no torch to build it with."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    try:
+        found = importlib.util.find_spec("torch")
+    except (ImportError, ValueError):
+        found = None
+    if found is None or not found.origin:
+        return None
+    at = os.path.dirname(found.origin)
+    header = os.path.join(at, "include", "torch", "csrc", "autograd", "python_variable.h")
+    if not os.path.exists(header):
+        return None
+    deps = [src, os.path.join(ROOT, "include", "bmlp.h"), os.path.join(at, "version.py")]
+    if not (force or _stale(MARSHAL, [d for d in deps if os.path.exists(d)])):
+        return None
+    cuda = os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"),
+            "-I", os.path.join(at, "include"), "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-I", sysconfig.get_paths()["include"], "-I", cuda, src, "-L", os.path.join(at, "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", MARSHAL]
+
+
+def _make_marshal(cmd) -> None:
+    """An accelerator of the binding alone: without it the calls go the interpreter's way."""
+    out = MARSHAL + ".tmp%d" % os.getpid()
+    res = subprocess.run(cmd[:-1] + [out], capture_output=True, text=True)
+    if res.returncode == 0:
+        os.replace(out, MARSHAL)
+    else:
+        print("csrc/marshal.cpp is not built; calls with torch tensors take some 4 us longer:\n" + res.stderr[-2000:])
+
+
 def build(force: bool = False, verbose: bool = False, extra=()) -> str:
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
     headers.append(os.path.join(ROOT, "include", "bmlp.h"))
     objs, jobs = [], []
+    marshal = _marshal_job(force)
+    beside = threading.Thread(target=_make_marshal, args=(marshal,)) if marshal else None
+    if beside:
+        beside.start()
     for src in SOURCES:
         sp = os.path.join(CSRC, src)
         op = os.path.join(objdir, src.replace(".cu", ".o"))
@@ -69,6 +111,8 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
             print(res.stdout + res.stderr)
             raise RuntimeError("link failed")
         os.replace(tmp, LIB)
+    if beside:
+        beside.join()
     return LIB
 
 

@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import importlib.util
 import os
 import sys
 import threading
@@ -511,6 +512,44 @@ def bmlp_int8_sign(a, w, out, threshold=None, stream=None, workspace=None, expir
 
 
 # -- microscaled 4-bit front end ---------------------------------------------------
+#
+# Calls on the current stream go through csrc/marshal.cpp, which takes the tensors' pointers and
+# strides natively where everything about them is as it should be; whatever it does not
+# take comes back as SLOW and goes the way below it, with the checks and errors there.
+
+class _NoMarshal:
+    SLOW = 1000
+
+    @staticmethod
+    def quantize(*_):
+        return _NoMarshal.SLOW
+
+    norm_quantize = dequantize = matmul = matmul_grouped = quantize
+
+
+_native = None        # the module, or _NoMarshal where it is not built
+
+
+def _marshal():
+    global _native
+    with _lock:
+        if _native is None:
+            found = _NoMarshal
+            if os.path.exists(_build.MARSHAL):
+                try:
+                    import torch   # noqa: F401  (the module's symbols are torch's)
+                    spec = importlib.util.spec_from_file_location("_marshal", _build.MARSHAL)
+                    found = importlib.util.module_from_spec(spec)
+                    spec.loader.exec_module(found)
+                except ImportError:     # (of another torch's making)
+                    found = _NoMarshal
+            _native = found
+    if _native is not _NoMarshal:
+        L = lib()
+        _native.init(*(C.cast(getattr(L, name), _vp).value for name in (
+            "bmlp_mx4_quantize", "bmlp_mx4_norm_quantize", "bmlp_mx4_dequantize", "bmlp_mx4_matmul",
+            "bmlp_mx4_matmul_grouped")))
+    return _native
 
 def bmlp_mx4_empty(n, K, device="cuda"):
     """(codes, scales) for n rows of K values: n x ceil(K/2) and n x ceil(K/32) bytes
@@ -531,6 +570,13 @@ def _codes(q, scale, n, K, what):
 def bmlp_mx4_quantize(x, q, scale, stream=None):
     """4-bit codes q (n x ceil(K/2) uint8) and scales (n x ceil(K/32) uint8) of the rows
     of x (n x K fp32 / fp16 / bf16, on the device; row strides are kept)."""
+    if stream is None:
+        M = _native or _marshal()
+        rc = M.quantize(x, q, scale)
+        if rc == 0:
+            return
+        if rc != M.SLOW:
+            _check(rc)
     torch = _torch or _use_torch()
     shape = n, K = x.shape
     if K >> 31:
@@ -550,6 +596,13 @@ def bmlp_mx4_norm_quantize(x, gain, q, scale, row_scale, res=None, sum_out=None,
     uint8), scales (n x ceil(K/32) uint8) and a factor per row (row_scale, n fp32);
     sum_out (may be x or res): x + res in their type.  gain, res, sum_out: x's type,
     each may be None."""
+    if stream is None:
+        M = _native or _marshal()
+        rc = M.norm_quantize(x, gain, q, scale, row_scale, res, sum_out, eps)
+        if rc == 0:
+            return
+        if rc != M.SLOW:
+            _check(rc)
     torch = _torch or _use_torch()
     shape = n, K = x.shape
     if K >> 31:
@@ -572,6 +625,13 @@ def bmlp_mx4_norm_quantize(x, gain, q, scale, row_scale, res=None, sum_out=None,
 def bmlp_mx4_dequantize(q, scale, out, row_scale=None, stream=None):
     """out (n x K fp32 / fp16 / bf16) = the values of codes q and scales, times row_scale
     (n fp32) where it is given."""
+    if stream is None:
+        M = _native or _marshal()
+        rc = M.dequantize(q, scale, out, row_scale)
+        if rc == 0:
+            return
+        if rc != M.SLOW:
+            _check(rc)
     torch = _torch or _use_torch()
     shape = n, K = out.shape
     if K >> 31:
@@ -592,6 +652,13 @@ def bmlp_mx4_matmul(a, a_scale, w, w_scale, out, row_scale=None, bias=None, stre
     n x ceil(K/32) uint8 scales) times those of w (N of them) transposed, times row_scale
     (n fp32) plus bias (N fp32).  For odd K the last byte's high bits are 0.  expired:
     bmlp_debug_mx4_matmul."""
+    if stream is None and not expired:
+        M = _native or _marshal()
+        rc = M.matmul(a, a_scale, w, w_scale, out, row_scale, bias)
+        if rc == 0:
+            return
+        if rc != M.SLOW:
+            _check(rc)
     torch = _torch or _use_torch()
     n, K = a.shape[0], 2 * a.shape[1]
     N = w.shape[0]
@@ -631,6 +698,13 @@ def bmlp_mx4_matmul_grouped(a, a_scale, w, w_scale, offsets, out, row_scale=None
     """bmlp_mx4_matmul with E matrices of weights: w (E x N x ceil(K/2) uint8), w_scale
     (E x N x ceil(K/32) uint8), bias (E x N fp32); rows offsets[e] <= i < offsets[e + 1] of a
     by the e-th (offsets: E + 1 int32 on the device).  Rows of no group stay as they are."""
+    if stream is None and not expired:
+        M = _native or _marshal()
+        rc = M.matmul_grouped(a, a_scale, w, w_scale, offsets, out, row_scale, bias)
+        if rc == 0:
+            return
+        if rc != M.SLOW:
+            _check(rc)
     torch = _torch or _use_torch()
     n, K = a.shape[0], 2 * a.shape[1]
     E, N = w.shape[0], w.shape[1]
