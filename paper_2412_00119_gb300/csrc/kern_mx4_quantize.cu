@@ -70,6 +70,22 @@ template <typename T, int V> struct Values {
         }
     }
   }
+  // The bits, as fp32, of the largest |value|.  (The order of |values| is that of their bits, in each type.)
+  __device__ __forceinline__ uint32_t most() const {
+    if constexpr (std::is_same<T, float>::value) {
+      uint32_t m = 0u;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+      return m;
+    } else {
+      uint32_t m = 0u;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+      m = max(m & 0xFFFFu, m >> 16);
+      if constexpr (std::is_same<T, __half>::value) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+      else return m << 16;
+    }
+  }
   __device__ __forceinline__ float get(int i) const {
     if constexpr (std::is_same<T, float>::value) return __uint_as_float(w[i]);
     else if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (16 * (i % 2)))));
@@ -107,10 +123,15 @@ __device__ __forceinline__ uint32_t code_pair(float lo, float hi) {
 // Codes of a lane's V values u and their block's scale byte.  Blocks of 32 are 32 / V
 // neighbouring lanes'; every lane of the warp calls.
 template <int V>
-__device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t& s) {
+__device__ __forceinline__ uint32_t largest(const float (&u)[V]) {
   uint32_t m = 0u;
 #pragma unroll
   for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(u[i]) & 0x7FFFFFFFu);
+  return m;
+}
+// m: bits of the lane's largest |u|.
+template <int V>
+__device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t m, uint32_t& s) {
   if constexpr (V == 1) {
     m = __reduce_max_sync(kFullMask, m);
   } else {
@@ -154,6 +175,17 @@ __device__ __forceinline__ void store_codes(uint8_t* q, uint8_t* scale, int64_t 
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 
+// Unit t of n rows of `parts` units.
+__device__ __forceinline__ void unit_at(int64_t t, int64_t parts, bool narrow, int64_t& row, int64_t& part) {
+  if (narrow) {   // (a 64-bit division takes as long as the rest of a unit)
+    row = (uint32_t)t / (uint32_t)parts;
+    part = (uint32_t)t - (uint32_t)row * (uint32_t)parts;
+  } else {
+    row = t / parts;
+    part = t - row * parts;
+  }
+}
+
 template <typename T, int V, int kAhead>
 __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A) {
   pdl_wait();
@@ -161,9 +193,12 @@ __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A)
   constexpr int kPart = 32 * V * kAhead;
   const int lane = threadIdx.x & 31;
   const int64_t parts = ((int64_t)A.K + kPart - 1) / kPart, total = A.n * parts;
+  const bool narrow = total < (1ll << 31);
   for (int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < total;
        t += (int64_t)gridDim.x * (kThreads / 32)) {
-    const int64_t row = t / parts, e0 = (t % parts) * kPart + V * lane;
+    int64_t row, part;
+    unit_at(t, parts, narrow, row, part);
+    const int64_t e0 = part * kPart + V * lane;
     const T* x = static_cast<const T*>(A.x) + row * A.ldx;
     Values<T, V> v[kAhead];
 #pragma unroll
@@ -175,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A)
 #pragma unroll
       for (int i = 0; i < V; ++i) u[i] = v[a].get(i);
       uint32_t s;
-      const uint32_t c = make_codes<V>(u, s);
+      const uint32_t c = make_codes<V>(u, v[a].most(), s);
       store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, A.K - e, c, s);
     }
   }
@@ -229,7 +264,7 @@ __global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const M
         for (int i = 0; i < V; ++i) u[i] = __fmul_rn(u[i], g[a].get(i));
       }
       uint32_t s;
-      const uint32_t c = make_codes<V>(u, s);
+      const uint32_t c = make_codes<V>(u, largest<V>(u), s);
       store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, left, c, s);
     }
   }
@@ -259,7 +294,7 @@ __global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const M
 }
 
 // ---------------------------------------------------------------------------
-// Codes to values: a lane takes V codes at a time.
+// Codes to values.
 // ---------------------------------------------------------------------------
 // The two values of a byte of codes.
 __device__ __forceinline__ float2 pair_values(uint32_t byte) {
@@ -268,47 +303,59 @@ __device__ __forceinline__ float2 pair_values(uint32_t byte) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-template <typename T, int V>
+// A warp takes kAhead times 32 V neighbouring codes of a row at a time: all its loads, then its stores.
+template <typename T, int V, int kAhead>
 __global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArgs A) {
   pdl_wait();
   pdl_trigger();
-  const int64_t parts = ((int64_t)A.K + V - 1) / V, total = A.n * parts;
-  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < total; t += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = t / parts, e = (t % parts) * V, left = A.K - e;
-    const uint8_t* q = A.q + row * A.ldq + (e >> 1);
-    uint32_t c = 0u;
-    if constexpr (V == 8) {
-      if (left >= V - 1) {
-        c = *reinterpret_cast<const uint32_t*>(q);
+  constexpr int kPart = 32 * V * kAhead;
+  const int lane = threadIdx.x & 31;
+  const int64_t parts = ((int64_t)A.K + kPart - 1) / kPart, total = A.n * parts;
+  const bool narrow = total < (1ll << 31);
+  for (int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < total;
+       t += (int64_t)gridDim.x * (kThreads / 32)) {
+    int64_t row, part;
+    unit_at(t, parts, narrow, row, part);
+    const int64_t e0 = part * kPart + V * lane;
+    const uint8_t *q = A.q + row * A.ldq, *scale = A.scale + row * A.ldc;
+    uint32_t c[kAhead], s[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t e = e0 + 32 * V * a, left = A.K - e;
+      c[a] = 0u;
+      s[a] = left > 0 ? scale[e >> 5] : 0u;
+      if constexpr (V == 8) {
+        if (left >= V - 1) {
+          c[a] = *reinterpret_cast<const uint32_t*>(q + (e >> 1));
+        } else {
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i)
+            if (2 * i < left) c[a] |= (uint32_t)q[(e >> 1) + i] << (8 * i);
+        }
       } else {
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i)
-          if (2 * i < left) c |= (uint32_t)q[i] << (8 * i);
+        if (left > 0) c[a] = q[e >> 1];
       }
-    } else {
-      c = *q;
     }
-    const uint32_t s = A.scale[row * A.ldc + (e >> 5)];
-    // 2^(s-127): below 2^-126 a subnormal number; 255 is NaN
-    const float unit = __uint_as_float(s == 0u ? 0x00400000u : (s == 255u ? 0x7FFFFFFFu : s << 23));
-    float f[V];
+    const float by = A.row_scale ? A.row_scale[row] : 1.0f;
 #pragma unroll
-    for (int i = 0; i < V; i += 2) {
-      const float2 two = pair_values((c >> (4 * i)) & 255u);
-      f[i] = two.x * unit;
-      f[i + 1] = two.y * unit;
-    }
-    if (A.row_scale) {
-      const float by = A.row_scale[row];
+    for (int a = 0; a < kAhead; ++a) {
+      const int64_t e = e0 + 32 * V * a, left = A.K - e;
+      // 2^(s-127): below 2^-126 a subnormal number; 255 is NaN
+      const float unit = __uint_as_float(s[a] == 0u ? 0x00400000u : (s[a] == 255u ? 0x7FFFFFFFu : s[a] << 23));
+      float f[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) f[i] *= by;
-    }
-    T* out = static_cast<T*>(A.out) + row * A.ldo + e;
-    if constexpr (V == 8) {
-      store_values<T, V>(out, f, left);
-    } else {
-      out[0] = from_f32<T>(f[0]);
-      if (left > 1) out[1] = from_f32<T>(f[1]);
+      for (int i = 0; i < V; i += 2) {
+        const float2 two = pair_values((c[a] >> (4 * i)) & 255u);
+        f[i] = two.x * unit * by;
+        f[i + 1] = two.y * unit * by;
+      }
+      T* out = static_cast<T*>(A.out) + row * A.ldo + e;
+      if constexpr (V == 8) {
+        store_values<T, V>(out, f, left);
+      } else {
+        if (left > 0) out[0] = from_f32<T>(f[0]);
+        if (left > 1) out[1] = from_f32<T>(f[1]);
+      }
     }
   }
 }
@@ -322,11 +369,18 @@ unsigned grid_of(int64_t units, int per_cta) {
   return (unsigned)std::min<int64_t>((units + per_cta - 1) / per_cta, 64ll * sm_count());
 }
 
-template <typename T, int V>
-cudaError_t launch_plain(const Mx4QuantArgs& A, cudaStream_t st) {
-  constexpr int kAhead = 4;
+template <typename T, int V, int kAhead>
+cudaError_t launch_units(const Mx4QuantArgs& A, cudaStream_t st) {
   const int64_t parts = ((int64_t)A.K + 32 * V * kAhead - 1) / (32 * V * kAhead);
   return launch_kernel(k_mx4_quantize<T, V, kAhead>, dim3(grid_of(A.n * parts, kThreads / 32)), dim3(kThreads), 0, st, true, A);
+}
+// Four loads ahead where a row has as many and every SM a few dozen warps' units of them (8192 x 8192 bf16
+// 34 us); by single values also in short rows, whose loads are few (30,000 x 100 bf16 9.6 us, one
+// ahead 17.0).
+bool ahead_pays(int64_t n, int K, int V) { return K >= 128 * V && n * (K / (128 * V)) >= 32ll * sm_count(); }
+template <typename T, int V>
+cudaError_t launch_plain(const Mx4QuantArgs& A, cudaStream_t st) {
+  return ahead_pays(A.n, A.K, V) || (V == 1 && A.n >= 8ll * sm_count()) ? launch_units<T, V, 4>(A, st) : launch_units<T, V, 1>(A, st);
 }
 
 template <typename T, bool kRes, bool kSmall, int V>
@@ -359,12 +413,19 @@ cudaError_t launch_type(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
   return wide ? launch_v<T, V>(A, norm, st) : launch_v<T, 1>(A, norm, st);
 }
 
+template <typename T, int V, int kAhead>
+cudaError_t launch_back(const Mx4DequantArgs& A, cudaStream_t st) {
+  const int64_t parts = ((int64_t)A.K + 32 * V * kAhead - 1) / (32 * V * kAhead);
+  return launch_kernel(k_mx4_dequantize<T, V, kAhead>, dim3(grid_of(A.n * parts, kThreads / 32)), dim3(kThreads), 0, st, true, A);
+}
+template <typename T, int V>
+cudaError_t launch_back(const Mx4DequantArgs& A, cudaStream_t st) {
+  return ahead_pays(A.n, A.K, V) ? launch_back<T, V, 4>(A, st) : launch_back<T, V, V == 2 ? 2 : 1>(A, st);
+}
 template <typename T>
 cudaError_t launch_dequant(const Mx4DequantArgs& A, cudaStream_t st) {
   const bool wide = rows_at(A.out, A.ldo * (int64_t)sizeof(T), A.n, 16) && rows_at(A.q, A.ldq, A.n, 4);
-  const int64_t units = A.n * (((int64_t)A.K + (wide ? 7 : 1)) / (wide ? 8 : 2));
-  return wide ? launch_kernel(k_mx4_dequantize<T, 8>, dim3(grid_of(units, kThreads)), dim3(kThreads), 0, st, true, A)
-              : launch_kernel(k_mx4_dequantize<T, 2>, dim3(grid_of(units, kThreads)), dim3(kThreads), 0, st, true, A);
+  return wide ? launch_back<T, 8>(A, st) : launch_back<T, 2>(A, st);
 }
 
 }  // namespace
