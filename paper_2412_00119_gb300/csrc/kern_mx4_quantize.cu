@@ -44,15 +44,23 @@ __device__ __forceinline__ float row_factor(float sumsq, float sumsq_up, int K, 
   return root > 0.0f ? (up ? (1.0f / root) * kUp : 1.0f / root) : 0.0f;
 }
 
-// V values as they lie in memory (V > 1: 16 bytes, aligned).
-template <typename T, int V> struct Values {
+// V values as they lie in memory (V > 1: 16 bytes; wide: aligned).
+template <typename T, int V, bool kWide = true> struct Values {
   static constexpr int kWords = V > 1 ? 4 : 1;
   uint32_t w[kWords];
   // the first `left` of those at p; zeros in the others' place
   __device__ __forceinline__ void load(const T* p, int64_t left) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0u;
-    if (left >= V) {
+    if constexpr (V > 1 && !kWide) {
+      // one by one: the lines stay in L1 meanwhile
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < left) {
+          if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+          else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
+        }
+    } else if (left >= V) {
       if constexpr (V > 1) {
         const uint4 v = *reinterpret_cast<const uint4*>(p);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
@@ -93,9 +101,9 @@ template <typename T, int V> struct Values {
   }
 };
 
-template <typename T, int V>
+template <typename T, int V, bool kWide = true>
 __device__ __forceinline__ void store_values(T* p, const float (&f)[V], int64_t left) {
-  if constexpr (V > 1) {
+  if constexpr (V > 1 && kWide) {
     if (left >= V) {
       constexpr int kEach = 16 / (int)sizeof(T);
 #pragma unroll
@@ -154,12 +162,12 @@ __device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t m, 
 }
 
 // Codes and scale of a lane's V values from element e of a row on, `left` of which are the row's.
-template <int V>
+template <int V, bool kWide = true>
 __device__ __forceinline__ void store_codes(uint8_t* q, uint8_t* scale, int64_t e, int64_t left, uint32_t c, uint32_t s) {
   const int lane = threadIdx.x & 31;
   if constexpr (V == 1) {
     if ((lane & 1) == 0 && left > 0) q[e >> 1] = (uint8_t)c;   // (past the row: zeros)
-  } else if (left >= V) {
+  } else if (kWide && left >= V) {
     if constexpr (V == 8) *reinterpret_cast<uint32_t*>(q + (e >> 1)) = c;
     else *reinterpret_cast<uint16_t*>(q + (e >> 1)) = (uint16_t)c;
   } else {
@@ -186,7 +194,7 @@ __device__ __forceinline__ void unit_at(int64_t t, int64_t parts, bool narrow, i
   }
 }
 
-template <typename T, int V, int kAhead>
+template <typename T, int V, bool kWideX, bool kWideQ, int kAhead>
 __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A) {
   pdl_wait();
   pdl_trigger();
@@ -200,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A)
     unit_at(t, parts, narrow, row, part);
     const int64_t e0 = part * kPart + V * lane;
     const T* x = static_cast<const T*>(A.x) + row * A.ldx;
-    Values<T, V> v[kAhead];
+    Values<T, V, kWideX> v[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) v[a].load(x + e0 + 32 * V * a, A.K - (e0 + 32 * V * a));
 #pragma unroll
@@ -211,7 +219,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A)
       for (int i = 0; i < V; ++i) u[i] = v[a].get(i);
       uint32_t s;
       const uint32_t c = make_codes<V>(u, v[a].most(), s);
-      store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, A.K - e, c, s);
+      store_codes<V, kWideQ>(A.q + row * A.ldq, A.scale + row * A.ldc, e, A.K - e, c, s);
     }
   }
 }
@@ -219,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A)
 // ---------------------------------------------------------------------------
 // With it: a row's threads are a warp (kWarpRow) or a CTA.
 // ---------------------------------------------------------------------------
-template <typename T, bool kRes, bool kSmall, int V, int kAhead, bool kWarpRow>
+template <typename T, bool kRes, bool kSmall, int V, bool kWide, int kAhead, bool kWarpRow>
 __global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const Mx4QuantArgs A) {
   pdl_wait();
   pdl_trigger();
@@ -235,7 +243,7 @@ __global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const M
   const int64_t step = (int64_t)threads * V;
   // (whole warps: the lanes of one meet in make_codes)
   for (int64_t e0 = V * tid; e0 - V * lane < A.K; e0 += kAhead * step) {
-    Values<T, V> v[kAhead], r[kRes ? kAhead : 1], g[kAhead];
+    Values<T, V, kWide> v[kAhead], r[kRes ? kAhead : 1], g[kAhead];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) v[a].load(x + e0 + a * step, A.K - (e0 + a * step));
     if constexpr (kRes) {
@@ -258,14 +266,14 @@ __global__ void __launch_bounds__(kWarpRow ? kThreads : 1024) k_mx4_norm(const M
         if constexpr (kSmall) sq_up += (u[i] * kUp) * (u[i] * kUp);
       }
       // (these values of x and res are read: sum_out may be one of them)
-      if (sum) store_values<T, V>(sum + e, u, left);
+      if (sum) store_values<T, V, kWide>(sum + e, u, left);
       if (gain) {
 #pragma unroll
         for (int i = 0; i < V; ++i) u[i] = __fmul_rn(u[i], g[a].get(i));
       }
       uint32_t s;
       const uint32_t c = make_codes<V>(u, largest<V>(u), s);
-      store_codes<V>(A.q + row * A.ldq, A.scale + row * A.ldc, e, left, c, s);
+      store_codes<V, kWide>(A.q + row * A.ldq, A.scale + row * A.ldc, e, left, c, s);
     }
   }
 #pragma unroll
@@ -369,48 +377,59 @@ unsigned grid_of(int64_t units, int per_cta) {
   return (unsigned)std::min<int64_t>((units + per_cta - 1) / per_cta, 64ll * sm_count());
 }
 
-template <typename T, int V, int kAhead>
+// Four loads ahead where a row has as many and every SM a few dozen warps' units of them (8192 x 8192 bf16
+// 34 us).
+bool ahead_pays(int64_t n, int K, int V) { return K >= 128 * V && n * (K / (128 * V)) >= 32ll * sm_count(); }
+template <typename T, int V, bool kWideX, bool kWideQ, int kAhead>
 cudaError_t launch_units(const Mx4QuantArgs& A, cudaStream_t st) {
   const int64_t parts = ((int64_t)A.K + 32 * V * kAhead - 1) / (32 * V * kAhead);
-  return launch_kernel(k_mx4_quantize<T, V, kAhead>, dim3(grid_of(A.n * parts, kThreads / 32)), dim3(kThreads), 0, st, true, A);
+  return launch_kernel(k_mx4_quantize<T, V, kWideX, kWideQ, kAhead>, dim3(grid_of(A.n * parts, kThreads / 32)), dim3(kThreads), 0, st,
+                       true, A);
 }
-// Four loads ahead where a row has as many and every SM a few dozen warps' units of them (8192 x 8192 bf16
-// 34 us); by single values also in short rows, whose loads are few (30,000 x 100 bf16 9.6 us, one
-// ahead 17.0).
-bool ahead_pays(int64_t n, int K, int V) { return K >= 128 * V && n * (K / (128 * V)) >= 32ll * sm_count(); }
-template <typename T, int V>
+template <typename T, int V, bool kWideX, bool kWideQ>
 cudaError_t launch_plain(const Mx4QuantArgs& A, cudaStream_t st) {
-  return ahead_pays(A.n, A.K, V) || (V == 1 && A.n >= 8ll * sm_count()) ? launch_units<T, V, 4>(A, st) : launch_units<T, V, 1>(A, st);
+  return ahead_pays(A.n, A.K, V) ? launch_units<T, V, kWideX, kWideQ, 4>(A, st) : launch_units<T, V, kWideX, kWideQ, 1>(A, st);
 }
 
-template <typename T, bool kRes, bool kSmall, int V>
+template <typename T, bool kRes, bool kSmall, int V, bool kWide>
 cudaError_t launch_norm(const Mx4QuantArgs& A, cudaStream_t st) {
   constexpr int kAhead = V > 1 ? 2 : 4;
   const int64_t vecs = ((int64_t)A.K + V - 1) / V;
   if (vecs <= 128)
-    return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kAhead, true>, dim3((unsigned)((A.n + kThreads / 32 - 1) / (kThreads / 32))),
+    return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kWide, kAhead, true>, dim3((unsigned)((A.n + kThreads / 32 - 1) / (kThreads / 32))),
                          dim3(kThreads), 0, st, true, A);
+  // (few rows: a thread of its own for each vector, and none ahead; 1 x 8192 bf16 with residual)
+  if (A.n <= 2 * sm_count() && vecs <= 1024)
+    return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kWide, 1, false>, dim3((unsigned)A.n), dim3((unsigned)((vecs + 31) / 32 * 32)), 0, st,
+                         true, A);
   const int64_t want = A.n <= 2 * sm_count() ? vecs : (vecs + kAhead - 1) / kAhead;
   const int threads = (int)std::min<int64_t>(1024, (want + 31) / 32 * 32);
-  return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kAhead, false>, dim3((unsigned)A.n), dim3((unsigned)threads), 0, st, true, A);
+  return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kWide, kAhead, false>, dim3((unsigned)A.n), dim3((unsigned)threads), 0, st, true, A);
 }
 
-template <typename T, int V>
-cudaError_t launch_v(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
-  if (!norm) return launch_plain<T, V>(A, st);
+template <typename T, int V, bool kWide>
+cudaError_t launch_rows(const Mx4QuantArgs& A, cudaStream_t st) {
   // (the squares of fp16 values do not leave fp32)
   if constexpr (!std::is_same<T, __half>::value)
-    if (A.eps < kSmallEps) return A.res ? launch_norm<T, true, true, V>(A, st) : launch_norm<T, false, true, V>(A, st);
-  return A.res ? launch_norm<T, true, false, V>(A, st) : launch_norm<T, false, false, V>(A, st);
+    if (A.eps < kSmallEps) return A.res ? launch_norm<T, true, true, V, kWide>(A, st) : launch_norm<T, false, true, V, kWide>(A, st);
+  return A.res ? launch_norm<T, true, false, V, kWide>(A, st) : launch_norm<T, false, false, V, kWide>(A, st);
 }
 
 template <typename T>
 cudaError_t launch_type(const Mx4QuantArgs& A, bool norm, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
   constexpr int64_t kSize = (int64_t)sizeof(T);
-  const bool wide = rows_at(A.x, A.ldx * kSize, A.n, 16) && (!A.res || rows_at(A.res, A.ldr * kSize, A.n, 16)) &&
-                    (!A.sum || rows_at(A.sum, A.lds * kSize, A.n, 16)) && rows_at(A.gain, 0, 1, 16) && rows_at(A.q, A.ldq, A.n, V / 2);
-  return wide ? launch_v<T, V>(A, norm, st) : launch_v<T, 1>(A, norm, st);
+  const bool x = rows_at(A.x, A.ldx * kSize, A.n, 16), q = rows_at(A.q, A.ldq, A.n, V / 2);
+  if (!norm) {
+    if (x) return q ? launch_plain<T, V, true, true>(A, st) : launch_plain<T, V, true, false>(A, st);
+    // (one by one: 20,000 x 2002 bf16 40 us by eight, 44 by four; 30,000 x 100 6.9, 5.8)
+    if (A.K >= 1024 || V == 4) return q ? launch_plain<T, V, false, true>(A, st) : launch_plain<T, V, false, false>(A, st);
+    return rows_at(A.q, A.ldq, A.n, 2) ? launch_plain<T, 4, false, true>(A, st) : launch_plain<T, 4, false, false>(A, st);
+  }
+  const bool wide = x && q && (!A.res || rows_at(A.res, A.ldr * kSize, A.n, 16)) &&
+                    (!A.sum || rows_at(A.sum, A.lds * kSize, A.n, 16)) && rows_at(A.gain, 0, 1, 16);
+  // (of 16 bits too four values, whose loads and stores one by one are fewer at a time)
+  return wide ? launch_rows<T, V, true>(A, st) : launch_rows<T, 4, false>(A, st);
 }
 
 template <typename T, int V, int kAhead>

@@ -192,6 +192,7 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
 }
 
 // kTma: the codes come by tensor copies (else their rows start anywhere).  kEpiWarps: that write outputs.
+__device__ __forceinline__ int64_t up_steps(int K) { return (((int64_t)K + 1) / 2 + kStepBytes - 1) / kStepBytes; }
 template <int kEpiWarps, bool kTma> struct Warps {
   static constexpr int kMma = kEpiWarps + 2 * kScaleWarps, kCopy = kMma + 2, kAll = kCopy + (kTma ? 1 : kRawWarps + kShiftWarps);
 };
@@ -236,6 +237,15 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEp
   if (kTma && warp == kCopyWarp && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.w) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+    // the first stages' weights on their way to L2 while the launch before this one ends
+    if (!A.offsets) {
+      const int ks = (int)up_steps(A.K), chunks0 = (ks + 1) / 2, from = 2 * (int)((int64_t)chunks0 * rank / S);
+      const int to = min(min(2 * (int)((int64_t)chunks0 * (rank + 1) / S), ks), from + P.stages);
+      const int j0 = CM * (int)((blockIdx.x / S) % (uint32_t)P.ctiles);
+      for (int k = from; k < to; ++k)
+        asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
+                     ::"l"(&maps.w), "r"(k * kStepBytes), "r"(j0), "r"(0) : "memory");
+    }
   }
   pdl_wait();
   pdl_trigger();
