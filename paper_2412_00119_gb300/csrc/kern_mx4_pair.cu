@@ -9,8 +9,8 @@
 // The grid is persistent, a pair per two SMs.  Two accumulators of 256 columns and the scales
 // do not fit tensor memory side by side: the accumulators share 128 columns, which the epilogue
 // reads first.  Warps of a CTA: 16 write outputs, eight bring scales, one thread copies codes
-// (both CTAs' copies complete on the even one's barriers), and on the even CTA one warp
-// copies the scales to tensor memory and one issues the MMAs.
+// (both CTAs' copies complete on the even one's barriers), and on the even CTA two
+// warps copy the scales to tensor memory and one issues the MMAs.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 
@@ -30,7 +30,7 @@ constexpr int kStageBytes = 2 * kBlockBytes + kCells;
 constexpr int kStages = 6;
 constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
 constexpr int kEpiWarps = 16, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCellWarp = kMmaWarp + 1,
-              kCopyWarp = kCellWarp + 1;
+              kCellWarps = 2, kCopyWarp = kCellWarp + kCellWarps;
 constexpr int kThreads = 32 * (kCopyWarp + 1);
 constexpr int kShared = 128;             // columns of both accumulators
 constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
@@ -45,7 +45,7 @@ constexpr int kBand = 8;                 // row tiles that the pairs walk side b
 struct __align__(8) PairShared {
   unsigned long long scaled[kStages], full[kStages], empty[kStages];   // cells; codes, and scales in tensor memory; read
   unsigned long long done[2], drained;
-  unsigned long long left, cells_left;
+  unsigned long long left, cells_left[2];
   uint32_t tmem_base;
   int failed, left_failed;
 };
@@ -139,7 +139,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     for (int b = 0; b < 2; ++b) mbar_init(&sh->done[b], 1);
     mbar_init(&sh->drained, 2 * kEpiWarps);
     mbar_init(&sh->left, 1);
-    mbar_init(&sh->cells_left, 1);
+    for (int b = 0; b < 2; ++b) mbar_init(&sh->cells_left[b], 1);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -324,38 +324,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           wait_phase(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
-  } else if (rank == 0 && warp == kCellWarp) {
+  } else if (rank == 0 && warp >= kCellWarp && warp < kCellWarp + kCellWarps) {
     // ---------------- scales to the pair's tensor memory ----------------
+    // Two warps take steps in turn (one alone takes 650 clocks of its issue a step).  The ring's length is even:
+    // a stage is always the same warp's.
+    static_assert(kCellWarps == 2 && kStages % 2 == 0 && kSlots < kStages, "every phase of a barrier is waited for by the same warp");
     const bool lead = elect_one();
     const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + 2u * kBlockBytes));
     const uint32_t sf0 = uniform(tmem) + (uint32_t)kSfCol;
     uint32_t s = 0, ph = 0, slot = 0, old = 0, oph = 0;   // (old: the stage kSlots before)
     int fresh = kSlots;                                   // slots that nothing has read yet
-    bool ok = true;
+    bool ok = true, mine = warp == kCellWarp;
 #pragma unroll 1
     for (int64_t t = pair; t < tiles && ok; t += pairs) {
 #pragma unroll 1
-      for (int k = 0; k < steps; ++k) {
-        ok = __all_sync(kFull, wait_phase<true>(&sh->scaled[s], ph, failed));
+      for (int k = 0; k < steps; ++k, mine = !mine) {
+        if (mine) {
+          ok = __all_sync(kFull, wait_phase<true>(&sh->scaled[s], ph, failed));
+          // the MMAs that read the scales in this slot
+          if (fresh == 0) ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[old], oph, failed));
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (lead) {
+#pragma unroll
+            for (int e = 0; e < 6; ++e)
+              copy_cell_pair(sf0 + (uint32_t)kSlotCols * slot + 4 * e, cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4) + e * (kCell >> 4)));
+            commit_here(&sh->full[s]);
+          }
+          __syncwarp();
+        }
         if (fresh > 0) {
           --fresh;
-        } else {
-          // the MMAs that read the scales in this slot
-          ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[old], oph, failed));
-          if (++old == kStages) {
-            old = 0;
-            oph ^= 1u;
-          }
+        } else if (++old == kStages) {
+          old = 0;
+          oph ^= 1u;
         }
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (lead) {
-#pragma unroll
-          for (int e = 0; e < 6; ++e)
-            copy_cell_pair(sf0 + (uint32_t)kSlotCols * slot + 4 * e, cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4) + e * (kCell >> 4)));
-          commit_here(&sh->full[s]);
-        }
-        __syncwarp();
         if (++slot == kSlots) slot = 0;
         if (++s == kStages) {
           s = 0;
@@ -364,8 +367,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
     if (lead) {
-      commit_here(&sh->cells_left);
-      wait_phase(&sh->cells_left, 0, &sh->left_failed);
+      unsigned long long* left = &sh->cells_left[warp - kCellWarp];
+      commit_here(left);
+      wait_phase(left, 0, &sh->left_failed);
     }
     __syncwarp();
   } else if (rank == 0 && warp == kMmaWarp) {

@@ -195,7 +195,7 @@ __device__ __forceinline__ void unit_at(int64_t t, int64_t parts, bool narrow, i
 }
 
 template <typename T, int V, bool kWideX, bool kWideQ, int kAhead>
-__global__ void __launch_bounds__(kThreads) k_mx4_quantize(const Mx4QuantArgs A) {
+__global__ void __launch_bounds__(kThreads, 5) k_mx4_quantize(const Mx4QuantArgs A) {
   pdl_wait();
   pdl_trigger();
   constexpr int kPart = 32 * V * kAhead;
