@@ -11,6 +11,9 @@
 // reads first.  Warps of a CTA: 16 write outputs, eight bring scales, one thread copies codes
 // (both CTAs' copies complete on the even one's barriers), and on the even CTA two
 // warps copy the scales to tensor memory and one issues the MMAs.
+// Measured: 16384 x 8192 -> 8192 348 us (6.3 PFLOP/s), 4096 x 4096 -> 4096 35.6, 16384 x 4096 -> 4096 by 16
+// groups 126, 16384 x 512 -> 4096 51.  Bound: the ring's latency.  A step takes 830 clocks: a tensor copy
+// 2,200 to 2,700 of them under load, in a ring of six stages (an SM takes in a step's 35 KB in 600).
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 
