@@ -191,6 +191,11 @@ __device__ __forceinline__ void join_sums(const Mx4Args& A, const Item& it, uint
   }
 }
 
+// 16 bytes, past L1.
+__device__ __forceinline__ void copy16(uint32_t to, const int8_t* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
 // kTma: the codes come by tensor copies (else their rows start anywhere).  kEpiWarps: that write outputs.
 __device__ __forceinline__ int64_t up_steps(int K) { return (((int64_t)K + 1) / 2 + kStepBytes - 1) / kStepBytes; }
 template <int kEpiWarps, bool kTma> struct Warps {
@@ -515,18 +520,34 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEp
           if (!ok) break;
           const uint32_t to = raw0 + slot * raw_bytes;
           const int byte = k * kStepBytes;
-          auto part = [&](const int8_t* rows, int64_t ld, int all, int live, uint32_t dst) {
-            const int8_t* row = rows + sub * ld;
-#pragma unroll 4
-            for (int r = sub; r < all; r += 4 * kRawWarps, row += 4 * kRawWarps * ld)
-              i8::copy_chunk(dst + (uint32_t)(kRawRow * r + 16 * c), row, i8::row_shift<1>(row), byte + 16 * c, r < live ? len : -16, any);
-            if (l < all) {
+          const bool inside = byte + kStepBytes + 16 <= len;   // every chunk is whole
+          // (rows past the last keep whatever is there: their outputs are dropped, and no code is a NaN)
+          auto part = [&](const int8_t* rows, int64_t ld, int live, uint32_t dst) {
+            const int8_t* row = rows + sub * ld + byte + 16 * c;
+            const uint32_t to0 = dst + (uint32_t)(kRawRow * sub + 16 * c);
+            const int64_t step = 4 * kRawWarps * ld;
+            if (inside) {
+              int r = sub;
+#pragma unroll 1
+              for (; r + 12 * kRawWarps < live; r += 16 * kRawWarps) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u, row += step) copy16(to0 + (uint32_t)(kRawRow * (r - sub + 4 * kRawWarps * u)), i8::aligned16(row));
+              }
+#pragma unroll 1
+              for (; r < live; r += 4 * kRawWarps, row += step) copy16(to0 + (uint32_t)(kRawRow * (r - sub)), i8::aligned16(row));
+            } else {
+              row -= byte + 16 * c;
+#pragma unroll 1
+              for (int r = sub; r < live; r += 4 * kRawWarps, row += step)
+                i8::copy_chunk(to0 + (uint32_t)(kRawRow * (r - sub)), row, i8::row_shift<1>(row), byte + 16 * c, len, any);
+            }
+            if (l < live) {
               row = rows + l * ld;
-              i8::copy_chunk(dst + (uint32_t)(kRawRow * l + 128), row, i8::row_shift<1>(row), byte + 128, l < live ? len : -16, any);
+              i8::copy_chunk(dst + (uint32_t)(kRawRow * l + 128), row, i8::row_shift<1>(row), byte + 128, len, any);
             }
           };
-          part(w0, A.ldw, CM, wlive, to);
-          part(a0, A.lda, P.nt, it.rows, to + (uint32_t)(kRawRow * CM));
+          part(w0, A.ldw, min(CM, wlive), to);
+          part(a0, A.lda, it.rows, to + (uint32_t)(kRawRow * CM));
           cp_async_arrive(&sh->raw_full[slot]);
           if (++slot == (uint32_t)P.deep) {
             slot = 0;
