@@ -11,7 +11,7 @@
 // length, with the sum of squares running beside.  The maximum is taken on the bits of |u| as
 // unsigned integers, whose order is the values' order with infinities and NaNs on top.
 // Bound: memory, and the instructions beside it.  8192 x 8192 bf16 34 us (5.0 TB/s), back to values 27 (6.4), the
-// norm of 8191 x 4096 bf16 with residual 40 (5.4); 24,095 x 787 fp32, rows at odd places, 22, 26 and 51.
+// norm of 8191 x 4096 bf16 with residual 37 (6.0); 24,095 x 787 fp32, rows at odd places, 22, 26 and 51.
 #include <algorithm>
 #include <type_traits>
 
