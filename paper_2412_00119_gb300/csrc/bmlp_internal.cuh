@@ -367,7 +367,7 @@ struct Mx4DequantArgs {
   int32_t K, type;
 };
 cudaError_t launch_mx4_dequantize(const Mx4DequantArgs& A, cudaStream_t st);
-// Product of such rows (kern_mx4_product.cu), by one matrix of weights (E = 1, offsets null)
+// Product of such rows (kern_mx4_tile.cu, kern_mx4_pair.cu), by one matrix of weights (E = 1, offsets null)
 // or by that of each row's group.  Strides of codes and scales (ld..: rows, g..: groups) in bytes.
 struct Mx4Args {
   const uint8_t* a;
@@ -383,8 +383,6 @@ struct Mx4Args {
 };
 // expire != 0: the CTAs take a wait as expired (tests).
 cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire);
-// The tensor-core tiles of one CTA (kern_mx4_tile.cu).
-cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

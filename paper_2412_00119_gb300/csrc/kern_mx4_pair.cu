@@ -39,9 +39,9 @@ constexpr int kShared = 128;             // columns of both accumulators
 constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
 constexpr int kSlots = 5, kSlotCols = 24;
 static_assert(kSfCol + kSlots * kSlotCols <= 512 && kStageBytes % 1024 == 0, "tensor memory, swizzle atoms");
-// A wait tells a phase from the next but one by nothing (a barrier's phases have a parity), so that one must be
-// over: a unit's first step waits for the MMAs of kStages steps before, and what its group of scale
-// warps waited for last tells of those up to kUnit + 1 + kStages.
+// A wait knows a phase by its parity alone, so the phase two before it must be known to be over.  A unit's first
+// step waits for the MMAs of kStages steps before, hence those of 2 kStages before must be done; the last wait
+// of its group of scale warps tells that of those of kUnit + 1 + kStages before.
 static_assert(kStages > kUnit, "phases");
 constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
 
@@ -209,7 +209,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 1; i < 4; ++i)
           if (c == i) by = rs[i];
-        put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, f, by, 0, bias, left, live);
+        put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, f, by, bias, left, live);
       };
 #pragma unroll
       for (int i = 0; i < 2; ++i) put(v[i], c0 + i);

@@ -1,4 +1,6 @@
-// kern_mx4_tile.cu -- the microscaled 4-bit product on the tensor cores, tiles of one CTA.
+// kern_mx4_tile.cu -- the product of microscaled 4-bit rows on the tensor cores,
+//   y_ij = row_scale_i sum_b 2^(sa_ib + sw_jb - 254) sum_{k in block b} a_ik w_jk + bias_j,
+// with one matrix of weights or that of each row's group: tiles of one CTA, and the choice of kernel.
 //
 // The codes lie in memory as tcgen05.mma kind::mxf4 wants them in shared memory (K-major, two
 // to a byte), so tensor copies take them there, zeros past the operands' ends, and nobody
@@ -14,7 +16,7 @@
 //     columns of tensor memory;
 //   - one warp copies a stage's cells there, to all four quarters of the lanes;
 //   - one warp issues the MMAs, 64 codes (two blocks) each;
-//   - four warps write finished tiles while the next one's MMAs run (two accumulators).
+//   - 4, 8 or 16 warps write finished tiles while the next one's MMAs run (two accumulators).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share K and add their sums up
 // in the order of their ranks, through distributed shared memory.
 // By group: the row tiles of a group start at its first row; what a tile has of the next
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEp
 #pragma unroll
           for (int x = 0; x < 16; ++x) to[x * CM] = __uint_as_float(v[x]);
         } else if (!expire) {
-          put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, v, rs[c], 0, bias, it.rows - x0, live);
+          put_rows(static_cast<TOut*>(A.out) + (it.r0 + x0) * A.ldo + j, A.ldo, v, rs[c], bias, it.rows - x0, live);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -321,9 +323,9 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEp
     const bool second = warp >= kEpiWarps + kScaleWarps, has_row = r < P.nt, whole = P.whole != 0;
     const int len = (int)(((int64_t)A.K + 31) / 32);
     const uint32_t cells = smem_u32(base) + (uint32_t)(stage_bytes - kCells) + 16u * (uint32_t)lane + 4u * (uint32_t)q;
-    // A wait tells a phase from the next but one by nothing (a barrier's phases have a parity), so that one must
-    // be over: a unit's first step waits for the MMAs of P.stages steps before, and what this group waited
-    // for last tells of those up to kUnit + 1 + P.stages.  Shorter rings have one group.
+    // A wait knows a phase by its parity alone, so the phase two before it must be known to be over.  A unit's
+    // first step waits for the MMAs of P.stages steps before, hence those of 2 P.stages before must be done;
+    // this group's last wait tells that of those of kUnit + 1 + P.stages before.  Shorter rings have one group.
     const bool alone = P.stages <= kUnit;
     Place at = {0, 1u};
     bool ok = true, mine = !second;
@@ -696,7 +698,7 @@ double pair_cost(const Mx4Args& A) {
 
 }  // namespace
 
-cudaError_t launch_mx4_tile(const Mx4Args& A, cudaStream_t st, int expire) {
+cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
   const int64_t bytes = ((int64_t)A.K + 1) / 2;
   TilePlan P = {};
   Maps maps;

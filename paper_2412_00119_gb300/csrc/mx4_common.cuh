@@ -1,5 +1,5 @@
-// mx4_common.cuh -- what the kernels of the microscaled 4-bit product share: the groups'
-// rows, one output after its sum, and sums on CUDA cores.
+// mx4_common.cuh -- what the kernels of the microscaled 4-bit product share: maps of the operands, the groups'
+// row tiles, outputs, waits, the scales' way to shared memory, and sums on CUDA cores.
 #pragma once
 
 #include <cuda.h>
@@ -100,13 +100,13 @@ __device__ __forceinline__ void put_out(const Mx4Args& A, int64_t i, int j, int 
 template <typename T>
 __device__ __forceinline__ T output(float sum, float rs, float bias) { return out_cast<T>(__fadd_rn(__fmul_rn(sum, rs), bias)); }
 
-// A lane's channel of 16 rows, of which `rows` are some: to[0], to[ldo], ..  rs: of row x in lane lane0 + x.
+// A lane's channel of 16 rows, of which `rows` are some: to[0], to[ldo], ..  rs: of row x in lane x.
 template <typename T>
-__device__ __forceinline__ void put_rows(T* to, int64_t ldo, const uint32_t (&sums)[16], float rs, int lane0, float bias, int rows,
+__device__ __forceinline__ void put_rows(T* to, int64_t ldo, const uint32_t (&sums)[16], float rs, float bias, int rows,
                                          bool live) {
   T y[16];
 #pragma unroll
-  for (int x = 0; x < 16; ++x) y[x] = output<T>(__uint_as_float(sums[x]), __shfl_sync(0xffffffffu, rs, lane0 + x), bias);
+  for (int x = 0; x < 16; ++x) y[x] = output<T>(__uint_as_float(sums[x]), __shfl_sync(0xffffffffu, rs, x), bias);
   if (!live) return;
   if (rows >= 16) {
 #pragma unroll
@@ -119,8 +119,7 @@ __device__ __forceinline__ void put_rows(T* to, int64_t ldo, const uint32_t (&su
 }
 
 // Bounded waits as in tc_common.cuh, kCluster: with cluster-scope acquire (the barrier collects arrivals of the
-// peer).  A try may sleep for some 50 us: waiting warps that try again and again take the shared
-// memory's queue from the others.
+// peer).  A try may sleep for some 50 us, in place of many tries (16384 x 8192 -> 8192 by tiles 502 -> 498 us).
 template <bool kCluster = false>
 __device__ __forceinline__ bool wait_phase(unsigned long long* bar, uint32_t parity, volatile int* failed,
                                            unsigned long long limit = tc::kWaitCycles) {

@@ -827,6 +827,68 @@ def test_binding_refusals():
         grouped(u8(2, 32), u8(2, 2), u8(3, 4, 32), u8(3, 4, 2), i32(4), t((2, 4)))   # host memory
 
 
+@gpu
+def test_refusals_of_device_tensors():
+    """What the native marshalling does not take comes to the same checks and errors, and the library's own
+    refusals come through it."""
+    t = lambda *s, d=torch.float32: torch.zeros(s, dtype=d, device=DEV)   # noqa: E731
+    u8 = lambda *s: t(*s, d=U8)   # noqa: E731
+    with pytest.raises(TypeError):
+        B.bmlp_mx4_quantize(t(2, 64, d=torch.float64), u8(2, 32), u8(2, 2))
+    with pytest.raises(TypeError):
+        B.bmlp_mx4_quantize(t(2, 64), t(2, 32, d=torch.int8), u8(2, 2))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_quantize(t(2, 64), u8(2, 31), u8(2, 2))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_quantize(t(64, 2).t(), u8(2, 32), u8(2, 2))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_norm_quantize(t(2, 64), t(63), u8(2, 32), u8(2, 2), t(2))
+    with pytest.raises(B.BmlpError):
+        B.bmlp_mx4_norm_quantize(t(2, 64), None, u8(2, 32), u8(2, 2), None)
+    with pytest.raises(B.BmlpError, match="eps"):
+        B.bmlp_mx4_norm_quantize(t(2, 64), None, u8(2, 32), u8(2, 2), t(2), eps=-1.0)
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_dequantize(u8(2, 32), u8(2, 2), t(2, 62))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_matmul(u8(2, 32), u8(2, 2), u8(4, 32), u8(4, 2), t(2, 5))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_matmul(u8(2, 32), u8(2, 2), u8(4, 32), u8(4, 2), t(2, 4), row_scale=t(3))
+    with pytest.raises(B.BmlpError, match="device pointers"):
+        B.bmlp_mx4_matmul(u8(2, 32), u8(2, 2), u8(4, 32).cpu(), u8(4, 2), t(2, 4))
+    with pytest.raises(ValueError):
+        B.bmlp_mx4_matmul_grouped(u8(2, 32), u8(2, 2), u8(3, 4, 32), u8(3, 4, 2), t(3, d=torch.int32), t(2, 4))
+    E = B.BMLP_MX4_MAX_GROUPS + 1
+    with pytest.raises(B.BmlpError, match="E outside"):
+        B.bmlp_mx4_matmul_grouped(u8(2, 32), u8(2, 2), u8(E, 1, 32), u8(E, 1, 2), t(E + 1, d=torch.int32), t(2, 1))
+    with pytest.raises(B.BmlpError, match="row stride"):
+        B.bmlp_mx4_quantize(t(1, 64).expand(2, 64), u8(2, 32), u8(2, 2))
+
+
+@gpu
+def test_both_ways_of_marshalling_agree():
+    """On the current stream (native) and on one given by hand (the interpreter's way)."""
+    n, K, N, E = 70, 1001, 130, 3
+    x, res = hidden(n, K, 1, torch.bfloat16).to(DEV), hidden(n, K, 2, torch.bfloat16).to(DEV)
+    w, sw = coded((E, N), 2 * ((K + 1) // 2), 3, pad=3)
+    w = w.clone()
+    at = torch.tensor([0, 20, 20, 60], dtype=torch.int32, device=DEV)
+    bias = torch.randn((E, N), generator=torch.Generator().manual_seed(1)).to(DEV)
+    st = torch.cuda.current_stream()
+    got = []
+    for stream in (None, st):
+        q, s = B.bmlp_mx4_empty(n, K)
+        q2, s2 = B.bmlp_mx4_empty(n, K)
+        by, total, back = torch.empty(n, device=DEV), torch.empty_like(x), torch.empty((n, K), device=DEV)
+        out, grouped = torch.zeros((n, N), device=DEV), torch.zeros((n, N), dtype=torch.float16, device=DEV)
+        B.bmlp_mx4_quantize(x, q2, s2, stream=stream)
+        B.bmlp_mx4_norm_quantize(x, None, q, s, by, res=res, sum_out=total, eps=EPS, stream=stream)
+        B.bmlp_mx4_dequantize(q, s, back, row_scale=by, stream=stream)
+        B.bmlp_mx4_matmul(q, s, w[0], sw[0], out, row_scale=by, bias=bias[0], stream=stream)
+        B.bmlp_mx4_matmul_grouped(q, s, w, sw, at, grouped, row_scale=by, bias=bias, stream=stream)
+        got.append([v.clone() for v in (q2, s2, q, s, by, total, back, out, grouped)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_sizes_past_31_bits_are_refused():
     x = torch.empty((1,), dtype=U8).expand(1 << 31).unsqueeze(0)
     with pytest.raises((B.BmlpError, ValueError)):
