@@ -638,6 +638,36 @@ def test_two_streams_at_once():
 
 
 @gpu
+def test_beside_other_kernels():
+    """Every plan of the products on three streams, mixed with the 8-bit product: CTAs of several of them share
+    the SMs and their tensor memory."""
+    jobs = []
+    for n, K, N, pad in [(1, 4096, 4096, -1), (20, 2048, 3000, -1), (100, 4096, 2048, -1), (1500, 1024, 2048, -1),
+                         (3000, 2048, 1024, -1), (70, 1000, 500, 1), (400, 700, 300, 0), (9, 8192, 256, -1)]:
+        (a, sa), (w, sw) = coded(n, K, 1, span=0, pad=pad), coded(N, K, 2, span=0, pad=pad)
+        want = (decoded(a, sa, K) @ decoded(w, sw, K).t()).float()
+        jobs.append((want, [torch.empty((n, N), device=DEV) for _ in range(3)],
+                     lambda st, out, a=a, sa=sa, w=w, sw=sw: B.bmlp_mx4_matmul(a, sa, w, sw, out, stream=st)))
+    for n, K, N in [(40, 1024, 2048), (2000, 1024, 1024)]:
+        a, w = (torch.randint(-128, 128, (m, K), dtype=torch.int8).to(DEV) for m in (n, N))
+        jobs.append(((a.double() @ w.double().t()).int(), [torch.empty((n, N), dtype=torch.int32, device=DEV) for _ in range(3)],
+                     lambda st, out, a=a, w=w: B.bmlp_int8_matmul(a, w, out, stream=st)))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for rep in range(6):
+        for k in range(3 * len(jobs)):
+            want, outs, call = jobs[(7 * k + rep) % len(jobs)]
+            i = k % 3
+            call(streams[i], outs[i])
+        torch.cuda.synchronize()
+        for want, outs, _ in jobs:
+            for out in outs:
+                assert torch.equal(out, want)
+                out.fill_(-1)
+        torch.cuda.synchronize()
+
+
+@gpu
 def test_back_to_back_calls_do_not_mix():
     """Calls that depend on one another, with nothing between them: each kernel may start while
     the one before it ends."""
