@@ -9,6 +9,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import importlib.util
 import os
+import runpy
 import shutil
 import subprocess
 import sysconfig
@@ -18,7 +19,6 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libbmlp.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")    # bmlp.py uses it where it is there
 SOURCES = ["bmlp_api.cu", "bmlp_noalloc.cu", "kern_forward.cu", "kern_forward_tc.cu", "kern_eval_tc.cu",
            "kern_update.cu", "kern_binarize.cu", "kern_expand.cu", "kern_peaks.cu", "kern_forward_b1.cu",
            "kern_update_rows.cu", "kern_update_ws.cu", "kern_quantize.cu", "kern_int8.cu",
@@ -43,9 +43,16 @@ def _stale(out: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def marshal_path(version: str, git_version: str) -> str:
+    """The marshalling of torch tensors (csrc/marshal.cpp) for this interpreter and that torch, whose tensors it
+    reads as they lie in memory: under a name of its own for each, so that no other one's is ever loaded."""
+    tag = "".join(c if c.isalnum() or c in ".+" else "_" for c in "%s-%s" % (version, (git_version or "")[:12]))
+    return os.path.join(HERE, "_marshal-%s.%s.so" % (tag, sysconfig.get_config_var("SOABI")))
+
+
 def _marshal_job(force: bool):
-    """The compiler's command for the marshalling of torch tensors (csrc/marshal.cpp), None
-    where it is up to date or there is no torch to build it with."""
+    """The compiler's command for the marshalling of torch tensors, None where it is up to date or
+    there is no torch to build it with."""
     src = os.path.join(CSRC, "marshal.cpp")
     try:
         found = importlib.util.find_spec("torch")
@@ -57,22 +64,23 @@ def _marshal_job(force: bool):
     header = os.path.join(at, "include", "torch", "csrc", "autograd", "python_variable.h")
     if not os.path.exists(header):
         return None
-    deps = [src, os.path.join(ROOT, "include", "bmlp.h"), os.path.join(at, "version.py")]
-    if not (force or _stale(MARSHAL, [d for d in deps if os.path.exists(d)])):
+    torch = runpy.run_path(os.path.join(at, "version.py"))    # (assignments alone)
+    out = marshal_path(torch["__version__"], torch.get("git_version"))
+    if not (force or _stale(out, [src, os.path.join(ROOT, "include", "bmlp.h"), os.path.join(at, "version.py")])):
         return None
     cuda = os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", os.path.join(ROOT, "include"),
             "-I", os.path.join(at, "include"), "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
             "-I", sysconfig.get_paths()["include"], "-I", cuda, src, "-L", os.path.join(at, "lib"),
-            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", MARSHAL]
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", out]
 
 
 def _make_marshal(cmd) -> None:
     """An accelerator of the binding alone: without it the calls go the interpreter's way."""
-    out = MARSHAL + ".tmp%d" % os.getpid()
+    out = cmd[-1] + ".tmp%d" % os.getpid()
     res = subprocess.run(cmd[:-1] + [out], capture_output=True, text=True)
     if res.returncode == 0:
-        os.replace(out, MARSHAL)
+        os.replace(out, cmd[-1])
     else:
         print("csrc/marshal.cpp is not built; calls with torch tensors take some 4 us longer:\n" + res.stderr[-2000:])
 

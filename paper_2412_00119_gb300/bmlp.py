@@ -527,29 +527,30 @@ class _NoMarshal:
     norm_quantize = dequantize = matmul = matmul_grouped = quantize
 
 
-_native = None        # the module, or _NoMarshal where it is not built
+_native = None        # the module, or _NoMarshal where there is none for this torch and interpreter
 
 
 def _marshal():
     global _native
+    L = lib()     # (first: it may build both)
+    import torch  # (the module's symbols are torch's)
     with _lock:
         if _native is None:
             found = _NoMarshal
-            if os.path.exists(_build.MARSHAL):
+            path = _build.marshal_path(torch.__version__, torch.version.git_version)
+            if os.path.exists(path):
                 try:
-                    import torch   # noqa: F401  (the module's symbols are torch's)
-                    spec = importlib.util.spec_from_file_location("_marshal", _build.MARSHAL)
+                    spec = importlib.util.spec_from_file_location("_marshal", path)
                     found = importlib.util.module_from_spec(spec)
                     spec.loader.exec_module(found)
-                except ImportError:     # (of another torch's making)
+                    found.init(*(C.cast(getattr(L, name), _vp).value for name in (
+                        "bmlp_mx4_quantize", "bmlp_mx4_norm_quantize", "bmlp_mx4_dequantize", "bmlp_mx4_matmul",
+                        "bmlp_mx4_matmul_grouped")))
+                except ImportError:     # (a library that it needs is not there)
                     found = _NoMarshal
-            _native = found
-    if _native is not _NoMarshal:
-        L = lib()
-        _native.init(*(C.cast(getattr(L, name), _vp).value for name in (
-            "bmlp_mx4_quantize", "bmlp_mx4_norm_quantize", "bmlp_mx4_dequantize", "bmlp_mx4_matmul",
-            "bmlp_mx4_matmul_grouped")))
+            _native = found   # last: callers read it without the lock
     return _native
+
 
 def bmlp_mx4_empty(n, K, device="cuda"):
     """(codes, scales) for n rows of K values: n x ceil(K/2) and n x ceil(K/32) bytes

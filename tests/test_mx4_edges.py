@@ -1,0 +1,91 @@
+"""The 4-bit front end past its other tests: the binding's native module and the torch it belongs to, the kernel of
+each instance and plan, rows at odd places, operands that tensor copies refuse, and values at
+the ends of fp32."""
+import os
+import shutil
+
+import pytest
+import torch
+
+from paper_2412_00119_gb300 import _build, bmlp as B
+from test_mx4 import DEV
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _device(request):
+    if request.node.get_closest_marker("gpu"):
+        if not torch.cuda.is_available():
+            pytest.skip("needs a GPU")
+        torch.cuda.set_device(DEV)
+
+
+# -- the binding's native module ---------------------------------------------------------
+
+def own_module():
+    return _build.marshal_path(torch.__version__, torch.version.git_version)
+
+
+@pytest.fixture
+def unloaded(monkeypatch):
+    """As before the first call."""
+    B._marshal()
+    monkeypatch.setattr(B, "_native", None)
+
+
+def test_module_of_another_torch_is_not_loaded(unloaded, monkeypatch):
+    """It reads tensors as they lie in its own torch's memory."""
+    names = {own_module(), _build.marshal_path("1.0", torch.version.git_version),
+             _build.marshal_path(torch.__version__, "0" * 40), _build.marshal_path(torch.__version__, None)}
+    assert len(names) == 4 and all(os.path.dirname(n) == _build.HERE for n in names)
+    monkeypatch.setattr(torch, "__version__", "1.0")
+    assert B._marshal() is B._NoMarshal
+    monkeypatch.undo()
+
+
+def test_module_that_the_first_call_builds_is_found(unloaded, monkeypatch, tmp_path):
+    if not os.path.exists(own_module()):
+        pytest.skip("built where there are torch's headers")
+    real, path = own_module(), str(tmp_path / os.path.basename(own_module()))
+    L = B.lib()
+
+    def building():
+        shutil.copy(real, path)
+        return L
+
+    monkeypatch.setattr(B, "lib", building)
+    monkeypatch.setattr(_build, "marshal_path", lambda *_: path)
+    assert B._marshal() is not B._NoMarshal
+
+
+@gpu
+def test_native_module_takes_calls():
+    """It is there, takes what is as it should be (0), and leaves the rest to the interpreter's way (SLOW)."""
+    M = B._marshal()
+    if _build._marshal_job(force=True) is None:
+        pytest.skip("no torch headers to build it with")
+    assert M is not B._NoMarshal
+    n, K, N, E = 5, 64, 8, 2
+    x = torch.randn((n, K), device=DEV)
+    q, s = B.bmlp_mx4_empty(n, K)
+    w, ws = B.bmlp_mx4_empty((E, N), K)
+    B.bmlp_mx4_quantize(torch.randn((E * N, K), device=DEV), w.flatten(0, 1), ws.flatten(0, 1))
+    by, out = torch.empty(n, device=DEV), torch.empty((n, N), device=DEV)
+    at = torch.tensor([0, 2, 5], dtype=torch.int32, device=DEV)
+    good = [(M.quantize, [x, q, s]), (M.norm_quantize, [x, None, q, s, by, None, None, 1e-6]),
+            (M.dequantize, [q, s, torch.empty_like(x), by]), (M.matmul, [q, s, w[0], ws[0], out, by, None]),
+            (M.matmul_grouped, [q, s, w, ws, at, out, None, None])]
+    for call, args in good:
+        assert call(*args) == 0
+        for i, a in enumerate(args):
+            if not isinstance(a, torch.Tensor):
+                continue
+            for wrong in (None, 3, a.cpu(), a.double(), a[:-1], a.unsqueeze(0)):
+                if wrong is None and call in (M.dequantize, M.matmul) and a is by:
+                    continue
+                assert call(*args[:i], wrong, *args[i + 1:]) == M.SLOW, (call, i)
+    assert M.quantize(x, q.t(), s) == M.SLOW
+    with pytest.raises(TypeError):
+        M.quantize(x, q)
+    torch.cuda.synchronize()
