@@ -26,10 +26,14 @@ namespace {
 constexpr unsigned kFullMask = 0xffffffffu;
 constexpr uint32_t kInfBits = 0x7F800000u;
 
-template <typename T> __device__ __forceinline__ T from_f32(float v);
-template <> __device__ __forceinline__ float from_f32(float v) { return v; }
-template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
+// A value's bits in type T.  Rows are read and written as bits, with the same types for both: a sum may be
+// stored where its row was read, and accesses of different types may change places in a compiler's hands.
+template <typename T> struct Bits { typedef uint16_t Type; };
+template <> struct Bits<float> { typedef uint32_t Type; };
+template <typename T> __device__ __forceinline__ typename Bits<T>::Type bits_of(float v);
+template <> __device__ __forceinline__ uint32_t bits_of<float>(float v) { return __float_as_uint(v); }
+template <> __device__ __forceinline__ uint16_t bits_of<__half>(float v) { return __half_as_ushort(__float2half_rn(v)); }
+template <> __device__ __forceinline__ uint16_t bits_of<__nv_bfloat16>(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // Below this eps (2^-80) a row's factor may hang on squares that are lost in fp32, those of
 // |h| < 2^-63.  Such rows have a sum below kSmallSum (2^-90: what a greater one has lost is
@@ -43,6 +47,20 @@ __device__ __forceinline__ float row_factor(float sumsq, float sumsq_up, int K, 
   const bool up = small && sumsq < kSmallSum;
   const float root = up ? sqrtf(sumsq_up / (float)K + eps * kUp * kUp) : sqrtf(sumsq / (float)K + eps);
   return root > 0.0f ? (up ? (1.0f / root) * kUp : 1.0f / root) : 0.0f;
+}
+
+// The 32 bits at word i of a vector of them.
+template <typename T, int V>
+__device__ __forceinline__ uint32_t word_of(const float (&f)[V], int i) {
+  if constexpr (std::is_same<T, float>::value) {
+    return __float_as_uint(f[i]);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
 }
 
 // V values as they lie in memory (V > 1: 16 bytes; wide: aligned).
@@ -106,20 +124,18 @@ template <typename T, int V, bool kWide = true>
 __device__ __forceinline__ void store_values(T* p, const float (&f)[V], int64_t left) {
   if constexpr (V > 1 && kWide) {
     if (left >= V) {
-      constexpr int kEach = 16 / (int)sizeof(T);
+      constexpr int kWords = V * (int)sizeof(T) / 4;
+      static_assert(kWords % 4 == 0, "whole vectors");
 #pragma unroll
-      for (int h = 0; h < V; h += kEach) {
-        union { uint4 w; T e[kEach]; } u;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) u.e[i] = from_f32<T>(f[h + i]);
-        *reinterpret_cast<uint4*>(p + h) = u.w;
-      }
+      for (int i = 0; i < kWords; i += 4)
+        *reinterpret_cast<uint4*>(p + 4 * i / (int)sizeof(T)) =
+            make_uint4(word_of<T>(f, i), word_of<T>(f, i + 1), word_of<T>(f, i + 2), word_of<T>(f, i + 3));
       return;
     }
   }
 #pragma unroll
   for (int i = 0; i < V; ++i)
-    if (i < left) p[i] = from_f32<T>(f[i]);
+    if (i < left) reinterpret_cast<typename Bits<T>::Type*>(p)[i] = bits_of<T>(f[i]);
 }
 
 // Two codes in a byte, ties to the even code.
@@ -359,12 +375,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArg
         f[i + 1] = two.y * unit * by;
       }
       T* out = static_cast<T*>(A.out) + row * A.ldo + e;
-      if constexpr (V == 8) {
-        store_values<T, V>(out, f, left);
-      } else {
-        if (left > 0) out[0] = from_f32<T>(f[0]);
-        if (left > 1) out[1] = from_f32<T>(f[1]);
-      }
+      store_values<T, V, V == 8>(out, f, left);
     }
   }
 }

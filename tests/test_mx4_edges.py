@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2412_00119_gb300 import _build, bmlp as B
-from test_mx4 import DEV
+from test_mx4 import DEV, EPS, TYPES, hidden, plain_codes, rows, same_codes, unpack, untouched
 
 gpu = pytest.mark.gpu
 
@@ -89,3 +89,27 @@ def test_native_module_takes_calls():
     with pytest.raises(TypeError):
         M.quantize(x, q)
     torch.cuda.synchronize()
+
+
+# -- rows to codes and back ----------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,K", [(5, 1), (300, 7), (40, 129), (9, 1001), (3, 4099), (400, 4099), (5, 9001), (2, 33001)])
+def test_norm_in_place_at_odd_places(n, K, dtype):
+    """The sum over the rows that it is made of, where they start anywhere."""
+    x, res = hidden(n, K, 1, dtype), hidden(n, K, 2, dtype)
+    h = x.float() + res.float()
+    want, (c, s) = h.to(dtype), plain_codes(h)
+    for eps in (EPS, 0.0):
+        for pad, off in ((0, 0), (3, 1)):
+            for into in (0, 1):
+                (xb, xd), (rb, rd) = rows(n, K, dtype, pad, off, fill=3), rows(n, K, dtype, pad, off, fill=3)
+                xd.copy_(x)
+                rd.copy_(res)
+                q, sd = B.bmlp_mx4_empty(n, K)
+                by = torch.empty((n,), device=DEV)
+                B.bmlp_mx4_norm_quantize(xd, None, q, sd, by, res=rd, sum_out=(xd, rd)[into], eps=eps)
+                assert torch.equal((xd, rd)[into].cpu(), want) and torch.equal((rd, xd)[into].cpu(), (res, x)[into])
+                assert untouched(xb, n, K, pad, off, 3) and untouched(rb, n, K, pad, off, 3)
+                assert torch.equal(sd.cpu(), s) and same_codes(unpack(q.cpu(), K), c)
