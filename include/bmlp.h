@@ -382,8 +382,8 @@ int bmlp_mx4_norm_quantize(const void* x, int64_t ldx, const void* res, int64_t 
                            void* cuda_stream);
 
 /* Values of codes: out = code 2^(s - 127), times row_scale where it is not NULL (fp32, one
- * rounding), rounded to out_type (without row_scale exact in fp32 and bf16, but for values of 2^128
- * on, which become infinite).
+ * rounding of the product), rounded to out_type (without row_scale exact in fp32 and bf16, but for
+ * values of 2^128 on, which become infinite).
  *   q, scale: n rows of K codes and their scales.  row_scale: n, or NULL.
  *   out: n x K of out_type (BMLP_F32, BMLP_F16 or BMLP_BF16), row stride ldo. */
 int bmlp_mx4_dequantize(const uint8_t* q, int64_t ldq, const uint8_t* scale, int64_t lds, const float* row_scale,

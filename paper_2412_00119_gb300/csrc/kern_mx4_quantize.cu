@@ -374,6 +374,16 @@ __global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArg
         f[i] = two.x * unit * by;
         f[i + 1] = two.y * unit * by;
       }
+      if (s[a] - 253u < 2u) {
+        // 2^126 and 2^127: a value may be past fp32 where its product with the row's factor is not
+        // (a sixteenth of it has the same one rounding: the least is 2^-28)
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+          const float2 two = pair_values((c[a] >> (4 * i)) & 255u);
+          f[i] = two.x * (unit * 0.0625f) * by * 16.0f;
+          f[i + 1] = two.y * (unit * 0.0625f) * by * 16.0f;
+        }
+      }
       T* out = static_cast<T*>(A.out) + row * A.ldo + e;
       store_values<T, V, V == 8>(out, f, left);
     }

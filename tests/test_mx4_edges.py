@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2412_00119_gb300 import _build, bmlp as B
-from test_mx4 import DEV, EPS, TYPES, hidden, plain_codes, rows, same_codes, unpack, untouched
+from test_mx4 import DEV, EPS, TYPES, coded, decoded, hidden, plain_codes, rows, same_codes, unpack, untouched
 
 gpu = pytest.mark.gpu
 
@@ -113,3 +113,24 @@ def test_norm_in_place_at_odd_places(n, K, dtype):
                 assert torch.equal((xd, rd)[into].cpu(), want) and torch.equal((rd, xd)[into].cpu(), (res, x)[into])
                 assert untouched(xb, n, K, pad, off, 3) and untouched(rb, n, K, pad, off, 3)
                 assert torch.equal(sd.cpu(), s) and same_codes(unpack(q.cpu(), K), c)
+
+
+@gpu
+@pytest.mark.parametrize("K", [64, 1001])
+def test_values_past_fp32_times_a_small_factor(K):
+    """Of scales 2^126 and 2^127: the value leaves fp32, its product with the row's factor has one rounding."""
+    by = torch.tensor([1.0, 0.3, 2.0 ** -10, -2.0 ** -126 * 1.7, 2.0 ** -149, 0.0, 3.0, float("inf"), float("nan")], device=DEV)
+    n = len(by)
+    for pad in (-1, 3):
+        q, s = coded(n, K, 5, span=4, base=251, pad=pad)
+        # (code and factor have 27 bits together: exact in 64)
+        want = (decoded(q, torch.where(s == 255, 254, s), K) * by.double()[:, None]).float()
+        want = torch.where((s == 255).repeat_interleave(32, -1)[:, :K], float("nan"), want)
+        for t in TYPES:
+            _, out = rows(n, K, t, max(pad, 0))
+            B.bmlp_mx4_dequantize(q, s, out, row_scale=by)
+            assert torch.equal(out.isnan(), want.isnan())
+            assert torch.equal(out.nan_to_num(nan=-7.0, posinf=1e9, neginf=-1e9),
+                               want.to(t).nan_to_num(nan=-7.0, posinf=1e9, neginf=-1e9))
+            B.bmlp_mx4_dequantize(q, s, out)
+            assert torch.equal(out.nan_to_num(nan=-7.0), decoded(q, s, K).float().to(t).nan_to_num(nan=-7.0))
