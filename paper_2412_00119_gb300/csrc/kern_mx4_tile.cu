@@ -696,13 +696,9 @@ double pair_cost(const Mx4Args& A) {
   return 9.0 + std::ceil(tiles / (sm_count() / 2)) * std::max(3.5, 0.4 * steps);
 }
 
-}  // namespace
-
-cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
-  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+// The plan of the tiles, and whether pairs are taken in their place.
+TilePlan plan_of(const Mx4Args& A, bool tma, bool& pairs) {
   TilePlan P = {};
-  Maps maps;
-  const bool tma = codes_whole(A);
   double best = 1e30;
   const int64_t mean = up(A.n, some_groups(A));
   for (int nt = 16; nt <= kMaxRows; nt += nt < 64 ? 16 : 32) {
@@ -716,11 +712,7 @@ cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
     }
     if (nt >= mean && !A.offsets) break;
   }
-  const bool pairs = tma && A.E <= kPairGroups && pair_cost(A) < best;
-  if (tma && (!code_map(&maps.w, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) ||
-              !code_map(&maps.a, A.a, bytes, A.n, A.lda, 0, 0, pairs ? 128 : P.nt)))
-    return cudaErrorInvalidValue;
-  if (pairs) return launch_mx4_pair(A, maps, st, expire);
+  pairs = tma && A.E <= kPairGroups && pair_cost(A) < best;
   P.ctiles = (int)up(A.N, CM);
   const int64_t tiles = most_row_tiles(A, P.nt) * P.ctiles;
   P.whole = scales_whole(A);
@@ -733,6 +725,23 @@ cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
   P.stages = (int)std::min<int64_t>(kMaxStages, (all - P.deep * row) / stage_size(P.nt));
   const int64_t slots = (two ? 2 : 1) * (int64_t)sm_count();
   P.ctas = (int)(P.split > 1 ? tiles * P.split : std::min(tiles, slots));
+  return P;
+}
+
+}  // namespace
+
+cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
+  const int64_t bytes = ((int64_t)A.K + 1) / 2;
+  Maps maps;
+  bool tma = codes_whole(A), pairs = false;
+  TilePlan P = plan_of(A, tma, pairs);
+  if (tma && (!code_map(&maps.w, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) ||
+              !code_map(&maps.a, A.a, bytes, A.n, A.lda, 0, 0, pairs ? 128 : P.nt))) {
+    // strides that the driver gives no map for: as rows at any place
+    tma = false;
+    P = plan_of(A, tma, pairs);
+  }
+  if (pairs) return launch_mx4_pair(A, maps, st, expire);
   if (A.type == BMLP_F32) return launch_tile<float>(A, P, maps, tma, st, expire);
   if (A.type == BMLP_F16) return launch_tile<__half>(A, P, maps, tma, st, expire);
   return launch_tile<__nv_bfloat16>(A, P, maps, tma, st, expire);

@@ -119,18 +119,52 @@ def test_norm_in_place_at_odd_places(n, K, dtype):
 @pytest.mark.parametrize("K", [64, 1001])
 def test_values_past_fp32_times_a_small_factor(K):
     """Of scales 2^126 and 2^127: the value leaves fp32, its product with the row's factor has one rounding."""
-    by = torch.tensor([1.0, 0.3, 2.0 ** -10, -2.0 ** -126 * 1.7, 2.0 ** -149, 0.0, 3.0, float("inf"), float("nan")], device=DEV)
+    by = torch.tensor([1.0, 0.3, 2.0 ** -10, -2.0 ** -126 * 1.7, 2.0 ** -149, 0.0, 3.0, float("inf"), float("nan")])
     n = len(by)
     for pad in (-1, 3):
         q, s = coded(n, K, 5, span=4, base=251, pad=pad)
-        # (code and factor have 27 bits together: exact in 64)
-        want = (decoded(q, torch.where(s == 255, 254, s), K) * by.double()[:, None]).float()
-        want = torch.where((s == 255).repeat_interleave(32, -1)[:, :K], float("nan"), want)
-        for t in TYPES:
-            _, out = rows(n, K, t, max(pad, 0))
-            B.bmlp_mx4_dequantize(q, s, out, row_scale=by)
-            assert torch.equal(out.isnan(), want.isnan())
-            assert torch.equal(out.nan_to_num(nan=-7.0, posinf=1e9, neginf=-1e9),
-                               want.to(t).nan_to_num(nan=-7.0, posinf=1e9, neginf=-1e9))
-            B.bmlp_mx4_dequantize(q, s, out)
-            assert torch.equal(out.nan_to_num(nan=-7.0), decoded(q, s, K).float().to(t).nan_to_num(nan=-7.0))
+        # (on the CPU: a device's pow in 64 bits is off by a bit at 2^122; code and factor have 27 bits together)
+        value = decoded(q.cpu(), s.cpu(), K)
+        for factor in (by, None):
+            want = (value if factor is None else value * factor.double()[:, None]).float()
+            for t in TYPES:
+                _, out = rows(n, K, t, max(pad, 0))
+                B.bmlp_mx4_dequantize(q, s, out, row_scale=None if factor is None else factor.to(DEV))
+                got, ref = out.cpu().double(), want.to(t).double()
+                bad = (got != ref) & ~(got.isnan() & ref.isnan())
+                assert not bad.any(), (t, pad, torch.nonzero(bad)[:5].tolist(), got[bad][:5], ref[bad][:5])
+
+
+# -- operands of products ------------------------------------------------------------------
+
+@gpu
+@pytest.mark.parametrize("n,K,N", [(90, 256, 70), (9, 1000, 130), (300, 100, 200)])
+def test_groups_in_other_orders(n, K, N):
+    """Groups whose rows lie between one another's (a group stride below the row stride), and a group stride that is no multiple of the rows'."""
+    E, kb, ks = 3, (K + 1) // 2, (K + 31) // 32
+    a, sa = coded(n, K, 1, span=1)
+    at = torch.tensor([0, n // 4, n // 4, n - 3], dtype=torch.int32, device=DEV)
+
+    def laid(t, order):
+        size = t.shape[-1]
+        wide = (size + 15) // 16 * 16
+        if order == "between":
+            buf = torch.full((N, E, wide), 255, dtype=t.dtype, device=DEV)
+            v = buf[..., :size].transpose(0, 1)
+        else:
+            buf = torch.full((E * (N * wide + 16),), 255, dtype=t.dtype, device=DEV)
+            v = buf.as_strided((E, N, size), (N * wide + 16, wide, 1))
+        v.copy_(t)
+        return v
+
+    w, sw = coded((E, N), K, 3, span=1)
+    want = torch.full((n, N), -5.0, dtype=torch.float64, device=DEV)
+    for e in range(E):
+        r = slice(int(at[e]), int(at[e + 1]))
+        want[r] = decoded(a[r], sa[r], K) @ decoded(w[e], sw[e], K).t()
+    for order in ("between", "apart"):
+        wl, sl = laid(w, order), laid(sw, order)
+        assert (wl.shape[-1], sl.shape[-1]) == (kb, ks) and (order == "apart" or wl.stride(0) < wl.stride(1))
+        out = torch.full((n, N), -5.0, device=DEV)
+        B.bmlp_mx4_matmul_grouped(a, sa, wl, sl, at, out)
+        assert torch.equal(out.double(), want), order
