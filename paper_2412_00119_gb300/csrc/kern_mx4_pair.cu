@@ -64,17 +64,21 @@ __device__ __forceinline__ uint32_t pair_rank() {
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// The barrier at this offset in CTA 0 of the cluster, and an arrival on it.  Its release is the CTA's own: what
-// the arrivals here tell of lies in this CTA's shared memory (cells, through the fence of the proxies) or tensor
-// memory (columns that were read), where the pair's copies and MMAs meet it.  (A release for the
-// cluster waits for every load and store under way, 1,500 clocks each.)
+// The barrier at this offset in CTA 0 of the cluster, and arrivals on it.
 __device__ __forceinline__ uint32_t rank0_address(unsigned long long* bar) {
   uint32_t remote;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(smem_u32(bar)));
   return remote;
 }
+// That what this thread knows of shared memory (cells) is there for who waits: it takes some 700 clocks, and
+// longer in a warp that has loads and stores under way, since it waits for those.
+__device__ __forceinline__ void mbar_release_rank0(unsigned long long* bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
+}
+// That columns of tensor memory are read: between tcgen05.fence::before_thread_sync here and ::after_thread_sync
+// there the arrival has to order execution alone, and releases no memory.
 __device__ __forceinline__ void mbar_arrive_rank0(unsigned long long* bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
 }
 
 __device__ __forceinline__ void mma_mx4_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa,
@@ -136,7 +140,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sh->full[s], 2);
-      mbar_init(&sh->scaled[s], 2 * kScaleWarps);
+      mbar_init(&sh->scaled[s], kScaleWarps + (rank == 0 ? 1 : 0));   // (and a relay of the odd CTA)
       mbar_init(&sh->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) mbar_init(&sh->done[b], 1);
@@ -288,8 +292,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive_rank0(&sh->scaled[p0.s]);
-            if (two) mbar_arrive_rank0(&sh->scaled[p1.s]);
+            mbar_arrive(&sh->scaled[p0.s]);
+            if (two) mbar_arrive(&sh->scaled[p1.s]);
           }
         }
       }
@@ -327,7 +331,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           wait_phase(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
-  } else if (rank == 0 && warp >= kCellWarp && warp < kCellWarp + kCellWarps) {
+  } else if (rank == 0 && warp >= kCellWarp) {
     // ---------------- scales to the pair's tensor memory ----------------
     // Two warps take steps in turn (one alone takes 650 clocks of its issue a step).  The ring's length is even:
     // a stage is always the same warp's.
@@ -375,7 +379,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       wait_phase(left, 0, &sh->left_failed);
     }
     __syncwarp();
-  } else if (rank == 0 && warp == kMmaWarp) {
+  } else if (rank != 0) {
+    // ---------------- relays ----------------
+    // The even CTA's copies read the odd one's cells: a warp waits for a stage's scale warps here and releases to the
+    // cluster what it has acquired.  Three warps without loads of their own take stages in turn, the
+    // ring's length is a multiple of three: a stage is always the same warp's.
+    constexpr int kRelays = kCopyWarp - kMmaWarp;
+    static_assert(kRelays == 3 && kStages % kRelays == 0, "every phase of a barrier is waited for by the same warp");
+    if (lane == 0) {
+      const uint32_t mine = (uint32_t)(warp - kMmaWarp);
+      uint32_t s = 0, ph = 0, turn = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int64_t t = pair; t < tiles && ok; t += pairs) {
+#pragma unroll 1
+        for (int k = 0; k < steps; ++k) {
+          if (turn == mine) {
+            ok = wait_phase(&sh->scaled[s], ph, failed);
+            if (!ok) break;
+            mbar_release_rank0(&sh->scaled[s]);
+          }
+          if (++turn == kRelays) turn = 0;
+          if (++s == kStages) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
     // ---------------- MMAs of the pair ----------------
     const bool lead = elect_one();
     const uint32_t d = uniform(tmem);
