@@ -8,12 +8,15 @@
 // its channels and all rows, and it needs the scales of its channels and of all rows there.
 // The grid is persistent, a pair per two SMs.  Two accumulators of 256 columns and the scales
 // do not fit tensor memory side by side: the accumulators share 128 columns, which the epilogue
-// reads first.  Warps of a CTA: 16 write outputs, eight bring scales, one thread copies codes
-// (both CTAs' copies complete on the even one's barriers), and on the even CTA two
-// warps copy the scales to tensor memory and one issues the MMAs.
-// Measured: 16384 x 8192 -> 8192 348 us (6.3 PFLOP/s), 4096 x 4096 -> 4096 35.6, 16384 x 4096 -> 4096 by 16
-// groups 126, 16384 x 512 -> 4096 51.  Bound: the ring's latency.  A step takes 830 clocks: a tensor copy
-// 2,200 to 2,700 of them under load, in a ring of six stages (an SM takes in a step's 35 KB in 600).
+// reads first.  Warps of a CTA: 16 write outputs, four bring scales to a ring in shared memory, four
+// take them from there to tensor memory, one thread copies codes (both CTAs' copies complete on the
+// even one's barriers), and on the even CTA one warp issues the MMAs.
+// What a CTA tells the other of is tensor copies, which complete on the even CTA's barriers, and tensor
+// memory, in the order of tcgen05's fences.  The scales go there by tcgen05.st, since a tcgen05.cp that the even CTA
+// issues reads what the odd one's threads have stored to its shared memory, and that needs a release for the
+// cluster: 16384 x 8192 -> 8192 439 us with one for each step (435 to 450 with the cells in a ring of their own).
+// Measured: 16384 x 8192 -> 8192 367 to 397 us (5.5 to 6.0 PFLOP/s), 4096 x 4096 -> 4096 36.6, 16384 x 4096 -> 4096 by 16
+// groups 114 to 129, 16384 x 512 -> 4096 50.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 
@@ -28,32 +31,30 @@ using namespace mx4;
 constexpr int TP = 256;                  // channels, and rows at most, of a tile
 constexpr int kStepBytes = 128;          // of a row per stage: 256 codes
 constexpr int kBlockBytes = 128 * kStepBytes;
-constexpr int kCells = 6 * kCell;        // of a stage: two of the channels, four of the rows (two halves of 128, twice)
-constexpr int kStageBytes = 2 * kBlockBytes + kCells;
+constexpr int kStageBytes = 2 * kBlockBytes;
 constexpr int kStages = 6;
-constexpr int kUnit = 4;                 // steps whose scales a lane loads at once: 32 bytes of a row
-constexpr int kEpiWarps = 16, kScaleWarps = 4, kMmaWarp = kEpiWarps + 2 * kScaleWarps, kCellWarp = kMmaWarp + 1,
-              kCellWarps = 2, kCopyWarp = kCellWarp + kCellWarps;
+constexpr int kUnit = 4;                 // steps whose scales are brought at once: 32 bytes of a row
+constexpr int kUnits = 2;                // in the ring
+constexpr int kCells = 6 * kCell, kUnitBytes = kUnit * kCells;   // of a step: two of the channels, four of the rows (two halves of 128, twice)
+constexpr int kEpiWarps = 16, kScaleWarps = 4, kPutWarp = kEpiWarps + kScaleWarps, kMmaWarp = kPutWarp + 4, kCopyWarp = kMmaWarp + 1;
 constexpr int kThreads = 32 * (kCopyWarp + 1);
 constexpr int kShared = 128;             // columns of both accumulators
-constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a stage
+constexpr int kSfCol = 2 * TP - kShared; // scales: 24 columns a step
 constexpr int kSlots = 5, kSlotCols = 24;
 static_assert(kSfCol + kSlots * kSlotCols <= 512 && kStageBytes % 1024 == 0, "tensor memory, swizzle atoms");
-// A wait knows a phase by its parity alone, so the phase two before it must be known to be over.  A unit's first
-// step waits for the MMAs of kStages steps before, hence those of 2 kStages before must be done; the last wait
-// of its group of scale warps tells that of those of kUnit + 1 + kStages before.
-static_assert(kStages > kUnit, "phases");
+static_assert(kPutWarp % 4 == 0 && kSlots < kStages, "a warp's lanes of tensor memory; every stage's MMAs are waited for");
 constexpr int kBand = 8;                 // row tiles that the pairs walk side by side
 
 struct __align__(8) PairShared {
-  unsigned long long scaled[kStages], full[kStages], empty[kStages];   // cells; codes, and scales in tensor memory; read
+  unsigned long long full[kStages], empty[kStages], scaled[kSlots];   // codes; read; scales in tensor memory
+  unsigned long long loaded[kUnits], taken[kUnits];                  // scales in the ring; read
   unsigned long long done[2], drained;
-  unsigned long long left, cells_left[2];
+  unsigned long long left;
   uint32_t tmem_base;
   int failed, left_failed;
 };
 constexpr int64_t pair_smem(int E) {
-  return 1024 + (int64_t)kStages * kStageBytes + (int64_t)sizeof(PairShared) + 8 * (int64_t)(E + 1);
+  return 1024 + (int64_t)kStages * kStageBytes + kUnits * kUnitBytes + (int64_t)sizeof(PairShared) + 8 * (int64_t)(E + 1);
 }
 
 __device__ __forceinline__ uint32_t pair_rank() {
@@ -64,19 +65,14 @@ __device__ __forceinline__ uint32_t pair_rank() {
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// The barrier at this offset in CTA 0 of the cluster, and arrivals on it.
+// The barrier at this offset in CTA 0 of the cluster, and an arrival on it.
 __device__ __forceinline__ uint32_t rank0_address(unsigned long long* bar) {
   uint32_t remote;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(smem_u32(bar)));
   return remote;
 }
-// That what this thread knows of shared memory (cells) is there for who waits: it takes some 700 clocks, and
-// longer in a warp that has loads and stores under way, since it waits for those.
-__device__ __forceinline__ void mbar_release_rank0(unsigned long long* bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
-}
-// That columns of tensor memory are read: between tcgen05.fence::before_thread_sync here and ::after_thread_sync
-// there the arrival has to order execution alone, and releases no memory.
+// It tells that columns of tensor memory are read or written: between tcgen05.fence::before_thread_sync here and
+// ::after_thread_sync there it has to order execution alone, and releases no memory.
 __device__ __forceinline__ void mbar_arrive_rank0(unsigned long long* bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(rank0_address(bar)) : "memory");
 }
@@ -88,9 +84,15 @@ __device__ __forceinline__ void mma_mx4_pair(uint32_t tmem_d, uint64_t adesc, ui
       " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
       ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate));
 }
-// A cell of each CTA to four columns of its tensor memory, 32 lanes in each quarter.
-__device__ __forceinline__ void copy_cell_pair(uint32_t tmem_to, uint64_t cell) {
-  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem_to), "l"(cell) : "memory");
+// Four columns' words of a lane.
+__device__ __forceinline__ void lds_cell(uint32_t* v, uint32_t a) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(a) : "memory");
+}
+// Words to 8 columns of this warp's lanes of tensor memory.
+__device__ __forceinline__ void tmem_store8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 // Arrive once on the barrier at this offset in both CTAs of the pair when what was issued so far completes.
 __device__ __forceinline__ void mma_commit_pair(unsigned long long* bar) {
@@ -98,10 +100,6 @@ __device__ __forceinline__ void mma_commit_pair(unsigned long long* bar) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
       ::"r"(smem_u32(bar)), "h"(mask) : "memory");
-}
-// The same on a barrier of this CTA alone.
-__device__ __forceinline__ void commit_here(unsigned long long* bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // Tensor copies to this CTA's shared memory, completing on a barrier of either CTA of the pair.
 __device__ __forceinline__ void copy_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -131,7 +129,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     k_mx4_pair(const Mx4Args A, const __grid_constant__ Maps maps, int ctiles, int whole, int expire) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  PairShared* sh = reinterpret_cast<PairShared*>(base + kStages * kStageBytes);
+  PairShared* sh = reinterpret_cast<PairShared*>(base + kStages * kStageBytes + kUnits * kUnitBytes);
   int32_t* groups = reinterpret_cast<int32_t*>(sh + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = pair_rank();
@@ -139,14 +137,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&sh->full[s], 2);
-      mbar_init(&sh->scaled[s], kScaleWarps + (rank == 0 ? 1 : 0));   // (and a relay of the odd CTA)
+      mbar_init(&sh->full[s], 1);
       mbar_init(&sh->empty[s], 1);
+    }
+    for (int s = 0; s < kSlots; ++s) mbar_init(&sh->scaled[s], 2 * 4);
+    for (int u = 0; u < kUnits; ++u) {
+      mbar_init(&sh->loaded[u], kScaleWarps);
+      mbar_init(&sh->taken[u], 4);
     }
     for (int b = 0; b < 2; ++b) mbar_init(&sh->done[b], 1);
     mbar_init(&sh->drained, 2 * kEpiWarps);
     mbar_init(&sh->left, 1);
-    for (int b = 0; b < 2; ++b) mbar_init(&sh->cells_left[b], 1);
     sh->failed = sh->left_failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -192,7 +193,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         rs[c] = has_rs && x < it.rows ? A.row_scale[it.r0 + x] : 1.0f;
       }
       const uint32_t b = seen & 1u, tacc = tmem + ((uint32_t)(32 * quarter) << 16) + b * (uint32_t)(TP - kShared);
-      ok = __all_sync(kFull, wait_phase<true>(&sh->done[b], (seen >> 1) & 1u, failed));
+      ok = __all_sync(kFull, wait_phase<kOrder>(&sh->done[b], (seen >> 1) & 1u, failed));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       // the columns that the accumulators share: the second one's first eight blocks of 16, the first one's last
@@ -229,72 +230,99 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
     if (expire && threadIdx.x == 0) *failed = 1;
-  } else if (warp < kMmaWarp) {
-    // ---------------- scales ----------------
-    // Two groups of warps take units of 1024 codes in turn: the one loads while the other waits for
-    // stages and fills them.
-    const int q = (warp - kEpiWarps) & (kScaleWarps - 1), r = 32 * q + lane;   // this lane's channel, and row of each half
-    const bool second = warp >= kEpiWarps + kScaleWarps;
+  } else if (warp < kPutWarp) {
+    // ---------------- scales to the ring ----------------
+    // A lane loads 32 bytes of its channel and of its row of each half, and stores them as cells of 128 rows x 128
+    // codes: the four bytes of row r at 16 (r % 32) + 4 (r / 32).
+    const int q = warp - kEpiWarps, r = 32 * q + lane;   // this lane's channel, and row of each half
     const int len = (int)(((int64_t)A.K + 31) / 32);
-    const uint32_t cells = smem_u32(base) + 2u * kBlockBytes + 16u * (uint32_t)lane + 4u * (uint32_t)q;
-    Place at = {0, 1u};
-    bool ok = true, mine = !second;
+    const uint32_t ring = smem_u32(base) + (uint32_t)(kStages * kStageBytes) + 16u * (uint32_t)lane + 4u * (uint32_t)q;
+    uint32_t u = 0, ph = 1;
+    bool ok = true;
 #pragma unroll 1
     for (int64_t t = pair; t < tiles && ok; t += pairs) {
-      const uint8_t* row[3] = {};
-      bool live[3] = {}, known = false;
-#pragma unroll 1
-      for (int k = 0; k < steps && ok; k += kUnit, mine = !mine) {
-        if (!mine) {
-          at.forward(min(kUnit, steps - k), kStages);
-          continue;
-        }
-        if (!known) {
-          const Item it = tile_at(items, t);
-          const int j = it.j0 + 128 * (int)rank + r;
-          live[0] = j < A.N;
-          row[0] = A.ws + it.e * A.gws + (int64_t)j * A.ldws;
+      const Item it = tile_at(items, t);
+      const int j = it.j0 + 128 * (int)rank + r;
+      const uint8_t* row[3];
+      bool live[3];
+      live[0] = j < A.N;
+      row[0] = A.ws + it.e * A.gws + (int64_t)j * A.ldws;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            live[1 + h] = 128 * h + r < it.rows;
-            row[1 + h] = A.as + (it.r0 + 128 * h + r) * A.ldas;
-          }
-          known = true;
-        }
+      for (int h = 0; h < 2; ++h) {
+        live[1 + h] = 128 * h + r < it.rows;
+        row[1 + h] = A.as + (it.r0 + 128 * h + r) * A.ldas;
+      }
+#pragma unroll 1
+      for (int k = 0; k < steps; k += kUnit) {
         uint32_t v[3][2][4];
 #pragma unroll
         for (int p = 0; p < 3; ++p) load_scales(v[p], row[p], live[p], whole != 0, 8 * k, len);
+        ok = __all_sync(kFull, wait_phase(&sh->taken[u], ph, failed));
+        if (!ok) break;
+        const uint32_t to = ring + u * (uint32_t)kUnitBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (k + 2 * h >= steps) break;
-          // (two stages together: the fence takes 200 clocks)
-          const bool two = k + 2 * h + 1 < steps;
-          const Place p0 = at;
-          at.forward(1, kStages);
-          Place p1 = p0;
-          if (two) {
-            p1 = at;
-            at.forward(1, kStages);
+        for (int z = 0; z < kUnit; ++z)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int p = 0; p < 3; ++p)   // channels' two cells; of either 128 codes the rows' two halves
+              sts32(to + (uint32_t)(kCells * z + kCell * (p == 0 ? y : 2 + 2 * y + (p - 1))), v[p][z >> 1][2 * (z & 1) + y]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->loaded[u]);
+        if (++u == kUnits) {
+          u = 0;
+          ph ^= 1u;
+        }
+      }
+    }
+  } else if (warp < kMmaWarp) {
+    // ---------------- scales to tensor memory ----------------
+    // Every quarter of the lanes holds all of a cell: lane i the 16 bytes at 16 i, in four columns.
+    const uint32_t ring = smem_u32(base) + (uint32_t)(kStages * kStageBytes) + 16u * (uint32_t)lane;
+    const uint32_t sf0 = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)kSfCol;
+    uint32_t u = 0, ph = 0, slot = 0, old = 0, oph = 0;   // (old: the stage kSlots steps before)
+    int fresh = kSlots;                                   // slots that nothing has read yet
+    bool ok = true;
+#pragma unroll 1
+    for (int64_t t = pair; t < tiles && ok; t += pairs) {
+#pragma unroll 1
+      for (int k = 0; k < steps && ok; k += kUnit) {
+        ok = __all_sync(kFull, wait_phase(&sh->loaded[u], ph, failed));
+        const int some = min(kUnit, steps - k);
+#pragma unroll 1
+        for (int z = 0; z < some && ok; ++z) {
+          const uint32_t from = ring + u * (uint32_t)kUnitBytes + (uint32_t)(kCells * z);
+          uint32_t f[8], g[16];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) lds_cell(&f[4 * e], from + (uint32_t)(kCell * e));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) lds_cell(&g[4 * e], from + (uint32_t)(kCell * (2 + e)));
+          // the MMAs that read the scales in this slot
+          if (fresh > 0) {
+            --fresh;
+          } else {
+            ok = __all_sync(kFull, wait_phase<kOrder>(&sh->empty[old], oph, failed));
+            if (!ok) break;
+            if (++old == kStages) {
+              old = 0;
+              oph ^= 1u;
+            }
           }
-          ok = __all_sync(kFull, wait_phase<true>(&sh->empty[p0.s], p0.ph, failed));
-          if (two) ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[p1.s], p1.ph, failed));
-          if (!ok) break;
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            if (z == 1 && !two) break;
-            const uint32_t to = cells + (uint32_t)((z ? p1.s : p0.s) * kStageBytes);
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int p = 0; p < 3; ++p)   // channels' two cells; of either 128 codes the rows' two halves
-                sts32(to + (uint32_t)(kCell * (p == 0 ? y : 2 + 2 * y + (p - 1))), v[p][h][2 * z + y]);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          tmem_store8(sf0 + (uint32_t)kSlotCols * slot, f);
+          tmem_store16(sf0 + (uint32_t)kSlotCols * slot + 8u, g);
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive(&sh->scaled[p0.s]);
-            if (two) mbar_arrive(&sh->scaled[p1.s]);
+            mbar_arrive_rank0(&sh->scaled[slot]);
+            if (z + 1 == some) mbar_arrive(&sh->taken[u]);
           }
+          if (++slot == kSlots) slot = 0;
+        }
+        if (++u == kUnits) {
+          u = 0;
+          ph ^= 1u;
         }
       }
     }
@@ -311,7 +339,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int wy = it.j0 + 128 * (int)rank, ay = (int)it.r0 + half * (int)rank;
 #pragma unroll 1
         for (int k = 0; k < steps; ++k) {
-          ok = wait_phase<true>(&sh->empty[s], ph, failed);
+          ok = wait_phase<kPeer>(&sh->empty[s], ph, failed);
           if (!ok) break;
           const uint32_t to = smem_u32(base) + s * (uint32_t)kStageBytes, bar = rank0_address(&sh->full[s]);
           if (rank == 0) mbar_arrive_tx(&sh->full[s], 4 * kBlockBytes);
@@ -328,92 +356,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd
         // one stopped earlier, the wait's limit is time enough for what is in flight)
         for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
-          wait_phase(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
+          wait_phase<kPeer>(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
       }
     }
-  } else if (rank == 0 && warp >= kCellWarp) {
-    // ---------------- scales to the pair's tensor memory ----------------
-    // Two warps take steps in turn (one alone takes 650 clocks of its issue a step).  The ring's length is even:
-    // a stage is always the same warp's.
-    static_assert(kCellWarps == 2 && kStages % 2 == 0 && kSlots < kStages, "every phase of a barrier is waited for by the same warp");
-    const bool lead = elect_one();
-    const uint64_t cells0 = cell_desc(uniform(smem_u32(base) + 2u * kBlockBytes));
-    const uint32_t sf0 = uniform(tmem) + (uint32_t)kSfCol;
-    uint32_t s = 0, ph = 0, slot = 0, old = 0, oph = 0;   // (old: the stage kSlots before)
-    int fresh = kSlots;                                   // slots that nothing has read yet
-    bool ok = true, mine = warp == kCellWarp;
-#pragma unroll 1
-    for (int64_t t = pair; t < tiles && ok; t += pairs) {
-#pragma unroll 1
-      for (int k = 0; k < steps; ++k, mine = !mine) {
-        if (mine) {
-          ok = __all_sync(kFull, wait_phase<true>(&sh->scaled[s], ph, failed));
-          // the MMAs that read the scales in this slot
-          if (fresh == 0) ok = ok && __all_sync(kFull, wait_phase<true>(&sh->empty[old], oph, failed));
-          if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (lead) {
-#pragma unroll
-            for (int e = 0; e < 6; ++e)
-              copy_cell_pair(sf0 + (uint32_t)kSlotCols * slot + 4 * e, cells0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4) + e * (kCell >> 4)));
-            commit_here(&sh->full[s]);
-          }
-          __syncwarp();
-        }
-        if (fresh > 0) {
-          --fresh;
-        } else if (++old == kStages) {
-          old = 0;
-          oph ^= 1u;
-        }
-        if (++slot == kSlots) slot = 0;
-        if (++s == kStages) {
-          s = 0;
-          ph ^= 1u;
-        }
-      }
-    }
-    if (lead) {
-      unsigned long long* left = &sh->cells_left[warp - kCellWarp];
-      commit_here(left);
-      wait_phase(left, 0, &sh->left_failed);
-    }
-    __syncwarp();
-  } else if (rank != 0) {
-    // ---------------- relays ----------------
-    // The even CTA's copies read the odd one's cells: a warp waits for a stage's scale warps here and releases to the
-    // cluster what it has acquired.  Three warps without loads of their own take stages in turn, the
-    // ring's length is a multiple of three: a stage is always the same warp's.
-    constexpr int kRelays = kCopyWarp - kMmaWarp;
-    static_assert(kRelays == 3 && kStages % kRelays == 0, "every phase of a barrier is waited for by the same warp");
-    if (lane == 0) {
-      const uint32_t mine = (uint32_t)(warp - kMmaWarp);
-      uint32_t s = 0, ph = 0, turn = 0;
-      bool ok = true;
-#pragma unroll 1
-      for (int64_t t = pair; t < tiles && ok; t += pairs) {
-#pragma unroll 1
-        for (int k = 0; k < steps; ++k) {
-          if (turn == mine) {
-            ok = wait_phase(&sh->scaled[s], ph, failed);
-            if (!ok) break;
-            mbar_release_rank0(&sh->scaled[s]);
-          }
-          if (++turn == kRelays) turn = 0;
-          if (++s == kStages) {
-            s = 0;
-            ph ^= 1u;
-          }
-        }
-      }
-    }
-    __syncwarp();
-  } else if (warp == kMmaWarp) {
+  } else if (rank == 0) {
     // ---------------- MMAs of the pair ----------------
     const bool lead = elect_one();
     const uint32_t d = uniform(tmem);
     const uint64_t desc0 = smem_desc(uniform(smem_u32(base)));
-    uint32_t s = 0, ph = 0, slot = 0, made = 0;
+    uint32_t s = 0, ph = 0, slot = 0, sph = 0, made = 0;
     bool ok = true;
 #pragma unroll 1
     for (int64_t t = pair; t < tiles && ok; t += pairs, ++made) {
@@ -422,11 +373,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const uint32_t idesc = uniform(idesc_f4(TP, (it.rows + 31) & ~31));
       // the columns that this accumulator shares with the one before are read, and all of its own
       // were before those
-      if (made > 0) ok = __all_sync(kFull, wait_phase<true>(&sh->drained, (made - 1) & 1u, failed));
+      if (made > 0) ok = __all_sync(kFull, wait_phase<kOrder>(&sh->drained, (made - 1) & 1u, failed));
       if (!ok) break;
 #pragma unroll 1
       for (int k = 0; k < steps; ++k) {
-        ok = __all_sync(kFull, wait_phase<true>(&sh->full[s], ph, failed));
+        ok = __all_sync(kFull, wait_phase<kOrder>(&sh->scaled[slot], sph, failed));
+        ok = ok && __all_sync(kFull, wait_phase<kPeer>(&sh->full[s], ph, failed));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t ad = desc0 + (uint64_t)(s * (uint32_t)(kStageBytes >> 4)), bd = ad + (uint64_t)(kBlockBytes >> 4);
@@ -441,7 +393,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           mma_commit_pair(&sh->empty[s]);
         }
         __syncwarp();
-        if (++slot == kSlots) slot = 0;
+        if (++slot == kSlots) {
+          slot = 0;
+          sph ^= 1u;
+        }
         if (++s == kStages) {
           s = 0;
           ph ^= 1u;

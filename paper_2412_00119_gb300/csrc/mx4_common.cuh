@@ -118,17 +118,24 @@ __device__ __forceinline__ void put_rows(T* to, int64_t ldo, const uint32_t (&su
   }
 }
 
-// Bounded waits as in tc_common.cuh, kCluster: with cluster-scope acquire (the barrier collects arrivals of the
-// peer).  A try may sleep for some 50 us, in place of many tries (16384 x 8192 -> 8192 by tiles 502 -> 498 us).
-template <bool kCluster = false>
+// Bounded waits as in tc_common.cuh.  kPeer: with cluster-scope acquire (the barrier collects arrivals of the
+// peer); kOrder: for arrivals that tell of tensor memory alone, which tcgen05's fences order around them.  A try may
+// sleep for some 50 us, in place of many tries (16384 x 8192 -> 8192 by tiles 502 -> 498 us).
+enum Wait { kHere, kPeer, kOrder };
+template <Wait kWait = kHere>
 __device__ __forceinline__ bool wait_phase(unsigned long long* bar, uint32_t parity, volatile int* failed,
                                            unsigned long long limit = tc::kWaitCycles) {
   const uint32_t a = tc::smem_u32(bar);
   uint32_t ok;
   auto try_wait = [&]() {
-    if constexpr (kCluster)
+    if constexpr (kWait == kPeer)
       asm volatile(
           "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 50000;\n"
+          " selp.u32 %0, 1, 0, p;\n}"
+          : "=r"(ok) : "r"(a), "r"(parity) : "memory");
+    else if constexpr (kWait == kOrder)
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2, 50000;\n"
           " selp.u32 %0, 1, 0, p;\n}"
           : "=r"(ok) : "r"(a), "r"(parity) : "memory");
     else
