@@ -427,6 +427,15 @@ int bmlp_debug_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale,
                           const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
                           int32_t out_type, int64_t ldo, void* cuda_stream);
 
+/* The same on the kernel of many rows (pairs of CTAs) whatever the sizes, for tests of it at its edges; expire:
+ * as above, or 0.  BMLP_EINVAL for operands that it does not take: codes in rows (groups) that start
+ * anywhere, or more than 256 groups. */
+int bmlp_debug_mx4_pairs(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                         const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                         const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                         const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                         int32_t out_type, int64_t ldo, int32_t expire, void* cuda_stream);
+
 /* One layer of forward-only evaluation (Sec. 3.1; Alg. 1 l.8-9):
  * a_out = sign(a_in W_l), sign(0) = +1, for n packed rows.  a_in: n rows of
  * ceil(K_{l-1}/64) words (pad bits 0); a_out: n rows of ceil(K_l/64) words,

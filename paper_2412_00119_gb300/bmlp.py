@@ -120,6 +120,9 @@ SIGNATURES = [
     ("bmlp_debug_mx4_matmul", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, _vp,
                                         C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
                                         C.c_int32, _vp, C.c_int32, C.c_int64, _vp]),
+    ("bmlp_debug_mx4_pairs", C.c_int, [_vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int64, _vp,
+                                       C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int32,
+                                       C.c_int32, _vp, C.c_int32, C.c_int64, C.c_int32, _vp]),
     ("bmlp_layer_forward_engine", C.c_int, [_vp, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp]),
 ]
 
@@ -723,6 +726,30 @@ def bmlp_mx4_matmul_grouped(a, a_scale, w, w_scale, offsets, out, row_scale=None
     rc = call(pa, lda, pas, ldas, _vector(row_scale, n, "row_scale", f32), pw, ldw, gw, pws, ldws, gws, pb, gb,
               _vector(offsets, E + 1, "offsets", torch.int32), E, n, K, N, po, _type(out, _real_types, "out"), ldo,
               _tensor_stream(stream, a))
+    if rc:
+        _check(rc)
+
+
+def bmlp_debug_mx4_pairs(a, a_scale, w, w_scale, offsets, out, row_scale=None, bias=None, stream=None, expired=False):
+    """bmlp_mx4_matmul_grouped (offsets None, w of two dimensions: bmlp_mx4_matmul) on the kernel of many rows,
+    whatever the sizes."""
+    torch = _torch or _use_torch()
+    if offsets is None:
+        w, w_scale, bias = w.unsqueeze(0), w_scale.unsqueeze(0), None if bias is None else bias.unsqueeze(0)
+    n, K = a.shape[0], 2 * a.shape[1]
+    E, N = w.shape[0], w.shape[1]
+    if (K | N) >> 31:
+        _int32(K, N)
+    u8, f32 = torch.uint8, torch.float32
+    pa, lda, pas, ldas = _codes(a, a_scale, n, K, "a")
+    pw, ldw, gw = _groups(w, (E, N, K // 2), "w", u8)
+    pws, ldws, gws = _groups(w_scale, (E, N, (K + 31) // 32), "w's scales", u8)
+    po, ldo = _rows(out, (n, N), "out", out.dtype)
+    pb, gb = (None, 0) if bias is None else _rows(bias, (E, N), "bias", f32)
+    rc = (_lib or lib()).bmlp_debug_mx4_pairs(
+        pa, lda, pas, ldas, _vector(row_scale, n, "row_scale", f32), pw, ldw, gw, pws, ldws, gws, pb, gb,
+        None if offsets is None else _vector(offsets, E + 1, "offsets", torch.int32), E, n, K, N, po,
+        _type(out, _real_types, "out"), ldo, expired, _tensor_stream(stream, a))
     if rc:
         _check(rc)
 

@@ -284,7 +284,7 @@ int mx4_quantize_call(const char* name, const Mx4QuantArgs& A, bool norm, void* 
 }
 
 // The same for the products.
-int mx4_call(const char* name, const Mx4Args& A, bool grouped, void* cuda_stream, int expire = 0) {
+int mx4_call(const char* name, const Mx4Args& A, bool grouped, void* cuda_stream, int expire = 0, bool pairs = false) {
   if (A.n < 0 || A.n > BMLP_MX4_MAX_ROWS || A.K < 1 || A.N < 1 || A.N > (1 << 30))
     return fail(nullptr, BMLP_EINVAL, "%s: n outside 0..%d, K < 1 or N outside 1..2^30", name, BMLP_MX4_MAX_ROWS);
   if (A.E < 1 || A.E > BMLP_MX4_MAX_GROUPS)
@@ -300,7 +300,9 @@ int mx4_call(const char* name, const Mx4Args& A, bool grouped, void* cuda_stream
       !usable(A.w, 0, here) || !usable(A.ws, 0, here) || !usable(A.row_scale, 2, here) || !usable(A.bias, 2, here) ||
       !usable(A.offsets, 2, here) || !usable(A.out, shift, here))
     return fail(nullptr, BMLP_EINVAL, "%s: buffers must be device pointers, aligned to their elements", name);
-  const cudaError_t e = launch_mx4(A, static_cast<cudaStream_t>(cuda_stream), expire);
+  const cudaError_t e = launch_mx4(A, static_cast<cudaStream_t>(cuda_stream), expire, pairs);
+  if (pairs && e == cudaErrorNotSupported)
+    return fail(nullptr, BMLP_EINVAL, "%s: pairs take codes in rows at multiples of 16 bytes and up to 256 groups", name);
   if (e != cudaSuccess) return cuda_fail(nullptr, e, name);
   return BMLP_OK;
 }
@@ -1170,6 +1172,16 @@ int bmlp_debug_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale,
   TraceRange trace("bmlp_debug_mx4_matmul");
   const Mx4Args A = {a, a_scale, row_scale, w, w_scale, bias, offsets, out, lda, ldas, ldw, gw, ldws, gws, gb, ldo, n, K, N, E, out_type};
   return mx4_call("bmlp_debug_mx4_matmul", A, E > 1, cuda_stream, 1);
+}
+
+int bmlp_debug_mx4_pairs(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas,
+                         const float* row_scale, const uint8_t* w, int64_t ldw, int64_t gw,
+                         const uint8_t* w_scale, int64_t ldws, int64_t gws, const float* bias, int64_t gb,
+                         const int32_t* offsets, int32_t E, int64_t n, int32_t K, int32_t N, void* out,
+                         int32_t out_type, int64_t ldo, int32_t expire, void* cuda_stream) {
+  TraceRange trace("bmlp_debug_mx4_pairs");
+  const Mx4Args A = {a, a_scale, row_scale, w, w_scale, bias, offsets, out, lda, ldas, ldw, gw, ldws, gws, gb, ldo, n, K, N, E, out_type};
+  return mx4_call("bmlp_debug_mx4_pairs", A, E > 1, cuda_stream, expire != 0, true);
 }
 
 int bmlp_get_state(const bmlp_t* hc, int32_t layer, int16_t* H_out, uint64_t* W_out, int8_t* P_out,

@@ -381,8 +381,8 @@ struct Mx4Args {
   int64_t lda, ldas, ldw, gw, ldws, gws, ldb, ldo, n;
   int32_t K, N, E, type;
 };
-// expire != 0: the CTAs take a wait as expired (tests).
-cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire);
+// For tests: expire != 0: the CTAs take a wait as expired; pairs: by pairs of CTAs or not at all (then cudaErrorNotSupported).
+cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire, bool pairs);
 // SMs of the current device (looked up once).
 int sm_count();
 // Tensor-core forward for evaluation on large batches: A (M x nw_in) against W

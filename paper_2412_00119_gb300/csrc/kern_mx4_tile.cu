@@ -730,17 +730,19 @@ TilePlan plan_of(const Mx4Args& A, bool tma, bool& pairs) {
 
 }  // namespace
 
-cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire) {
+cudaError_t launch_mx4(const Mx4Args& A, cudaStream_t st, int expire, bool only_pairs) {
   const int64_t bytes = ((int64_t)A.K + 1) / 2;
   Maps maps;
   bool tma = codes_whole(A), pairs = false;
   TilePlan P = plan_of(A, tma, pairs);
+  if (only_pairs) pairs = tma && A.E <= kPairGroups;
   if (tma && (!code_map(&maps.w, A.w, bytes, A.N, A.ldw, A.E, A.gw, CM) ||
               !code_map(&maps.a, A.a, bytes, A.n, A.lda, 0, 0, pairs ? 128 : P.nt))) {
     // strides that the driver gives no map for: as rows at any place
     tma = false;
     P = plan_of(A, tma, pairs);
   }
+  if (only_pairs && !pairs) return cudaErrorNotSupported;
   if (pairs) return launch_mx4_pair(A, maps, st, expire);
   if (A.type == BMLP_F32) return launch_tile<float>(A, P, maps, tma, st, expire);
   if (A.type == BMLP_F16) return launch_tile<__half>(A, P, maps, tma, st, expire);
