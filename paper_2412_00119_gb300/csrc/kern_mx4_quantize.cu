@@ -63,39 +63,29 @@ __device__ __forceinline__ uint32_t word_of(const float (&f)[V], int i) {
   }
 }
 
-// V values as they lie in memory (V > 1: 16 bytes; wide: aligned).
+// V values, of 16 bytes or of 8, as they lie in memory (wide: 16, aligned).
 template <typename T, int V, bool kWide = true> struct Values {
-  static constexpr int kWords = V > 1 ? 4 : 1;
+  static constexpr int kWords = V * (int)sizeof(T) / 4;
+  static_assert(kWide ? kWords == 4 : kWords == 4 || kWords == 2, "whole words");
   uint32_t w[kWords];
   // the first `left` of those at p; zeros in the others' place
   __device__ __forceinline__ void load(const T* p, int64_t left) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0u;
-    if constexpr (V > 1 && !kWide) {
-      // one by one: the lines stay in L1 meanwhile
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < left) {
-          if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
-          else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
-        }
-    } else if (left >= V) {
-      if constexpr (V > 1) {
+    if constexpr (kWide) {
+      if (left >= V) {
         const uint4 v = *reinterpret_cast<const uint4*>(p);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-      } else if constexpr (sizeof(T) == 4) {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
-      } else {
-        w[0] = *reinterpret_cast<const uint16_t*>(p);
+        return;
       }
-    } else if constexpr (V > 1) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < left) {
-          if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
-          else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
-        }
     }
+    // one by one: the lines stay in L1 meanwhile
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < left) {
+        if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+        else w[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + i) << (16 * (i % 2));
+      }
   }
   // The bits, as fp32, of the largest |value|.  (The order of |values| is that of their bits, in each type.)
   __device__ __forceinline__ uint32_t most() const {
@@ -122,7 +112,7 @@ template <typename T, int V, bool kWide = true> struct Values {
 
 template <typename T, int V, bool kWide = true>
 __device__ __forceinline__ void store_values(T* p, const float (&f)[V], int64_t left) {
-  if constexpr (V > 1 && kWide) {
+  if constexpr (kWide) {
     if (left >= V) {
       constexpr int kWords = V * (int)sizeof(T) / 4;
       static_assert(kWords % 4 == 0, "whole vectors");
@@ -145,8 +135,7 @@ __device__ __forceinline__ uint32_t code_pair(float lo, float hi) {
   return r;
 }
 
-// Codes of a lane's V values u and their block's scale byte.  Blocks of 32 are 32 / V
-// neighbouring lanes'; every lane of the warp calls.
+// Bits of the largest |u|.
 template <int V>
 __device__ __forceinline__ uint32_t largest(const float (&u)[V]) {
   uint32_t m = 0u;
@@ -154,27 +143,20 @@ __device__ __forceinline__ uint32_t largest(const float (&u)[V]) {
   for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(u[i]) & 0x7FFFFFFFu);
   return m;
 }
-// m: bits of the lane's largest |u|.
+// Codes of a lane's V values u and their block's scale byte s; m: bits of the lane's largest |u|.  Blocks of 32 are
+// 32 / V neighbouring lanes'; every lane of the warp calls.
 template <int V>
 __device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t m, uint32_t& s) {
-  if constexpr (V == 1) {
-    m = __reduce_max_sync(kFullMask, m);
-  } else {
+  static_assert(V == 4 || V == 8, "a lane's values");
 #pragma unroll
-    for (int o = 1; o < 32 / V; o *= 2) m = max(m, __shfl_xor_sync(kFullMask, m, o));
-  }
+  for (int o = 1; o < 32 / V; o *= 2) m = max(m, __shfl_xor_sync(kFullMask, m, o));
   const bool finite = m < kInfBits;
   const uint32_t e = m >> 23;
   s = finite ? (e > 2u ? e - 2u : 0u) : 255u;
   const float up = __uint_as_float(finite ? (254u - s) << 23 : 0u);
   uint32_t c = 0u;
-  if constexpr (V == 1) {
-    const float t = u[0] * up, next = __shfl_down_sync(kFullMask, t, 1);
-    c = code_pair(t, next);
-  } else {
 #pragma unroll
-    for (int i = 0; i < V; i += 2) c |= code_pair(u[i] * up, u[i + 1] * up) << (4 * i);
-  }
+  for (int i = 0; i < V; i += 2) c |= code_pair(u[i] * up, u[i + 1] * up) << (4 * i);
   return finite ? c : 0u;
 }
 
@@ -182,9 +164,7 @@ __device__ __forceinline__ uint32_t make_codes(const float (&u)[V], uint32_t m, 
 template <int V, bool kWide = true>
 __device__ __forceinline__ void store_codes(uint8_t* q, uint8_t* scale, int64_t e, int64_t left, uint32_t c, uint32_t s) {
   const int lane = threadIdx.x & 31;
-  if constexpr (V == 1) {
-    if ((lane & 1) == 0 && left > 0) q[e >> 1] = (uint8_t)c;   // (past the row: zeros)
-  } else if (kWide && left >= V) {
+  if (kWide && left >= V) {
     if constexpr (V == 8) *reinterpret_cast<uint32_t*>(q + (e >> 1)) = c;
     else *reinterpret_cast<uint16_t*>(q + (e >> 1)) = (uint16_t)c;
   } else {
@@ -415,7 +395,7 @@ cudaError_t launch_plain(const Mx4QuantArgs& A, cudaStream_t st) {
 
 template <typename T, bool kRes, bool kSmall, int V, bool kWide>
 cudaError_t launch_norm(const Mx4QuantArgs& A, cudaStream_t st) {
-  constexpr int kAhead = V > 1 ? 2 : 4;
+  constexpr int kAhead = 2;
   const int64_t vecs = ((int64_t)A.K + V - 1) / V;
   if (vecs <= 128)
     return launch_kernel(k_mx4_norm<T, kRes, kSmall, V, kWide, kAhead, true>, dim3((unsigned)((A.n + kThreads / 32 - 1) / (kThreads / 32))),
