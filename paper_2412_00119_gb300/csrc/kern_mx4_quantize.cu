@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArg
     for (int a = 0; a < kAhead; ++a) {
       const int64_t e = e0 + 32 * V * a, left = A.K - e;
       c[a] = 0u;
-      s[a] = left > 0 ? scale[e >> 5] : 0u;
+      s[a] = left > 0 ? scale[e >> 5] : 127u;
       if constexpr (V == 8) {
         if (left >= V - 1) {
           c[a] = *reinterpret_cast<const uint32_t*>(q + (e >> 1));
@@ -342,30 +342,48 @@ __global__ void __launch_bounds__(kThreads) k_mx4_dequantize(const Mx4DequantArg
       }
     }
     const float by = A.row_scale ? A.row_scale[row] : 1.0f;
+    auto put = [&](int a, const float (&f)[V]) {
+      const int64_t e = e0 + 32 * V * a;
+      store_values<T, V, V == 8>(static_cast<T*>(A.out) + row * A.ldo + e, f, A.K - e);
+    };
+    // 2^(s-127) times the row's factor is exact where it is a normal number, and its product with a code the one
+    // rounding.
+    float unit[kAhead];
+    bool plain = true;
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      const int64_t e = e0 + 32 * V * a, left = A.K - e;
-      // 2^(s-127): below 2^-126 a subnormal number; 255 is NaN
-      const float unit = __uint_as_float(s[a] == 0u ? 0x00400000u : (s[a] == 255u ? 0x7FFFFFFFu : s[a] << 23));
-      float f[V];
+      unit[a] = __uint_as_float(s[a] << 23) * by;
+      plain = plain && (__float_as_uint(unit[a]) & 0x7FFFFFFFu) - 0x00800000u < kInfBits - 0x00800000u;
+    }
+    if (__all_sync(kFullMask, plain)) {
 #pragma unroll
-      for (int i = 0; i < V; i += 2) {
-        const float2 two = pair_values((c[a] >> (4 * i)) & 255u);
-        f[i] = two.x * unit * by;
-        f[i + 1] = two.y * unit * by;
-      }
-      if (s[a] - 253u < 2u) {
-        // 2^126 and 2^127: a value may be past fp32 where its product with the row's factor is not
-        // (a sixteenth of it has the same one rounding: the least is 2^-28)
+      for (int a = 0; a < kAhead; ++a) {
+        float f[V];
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
           const float2 two = pair_values((c[a] >> (4 * i)) & 255u);
-          f[i] = two.x * (unit * 0.0625f) * by * 16.0f;
-          f[i + 1] = two.y * (unit * 0.0625f) * by * 16.0f;
+          f[i] = two.x * unit[a];
+          f[i + 1] = two.y * unit[a];
         }
+        put(a, f);
       }
-      T* out = static_cast<T*>(A.out) + row * A.ldo + e;
-      store_values<T, V, V == 8>(out, f, left);
+    } else {
+      // 0 is a subnormal number, 255 NaN.  Of 2^126 and 2^127 a value may be past fp32 where its product with the row's
+      // factor is not: a sixteenth of it has the same one rounding (the least such product is 2^-28).
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const bool far = s[a] - 253u < 2u;
+        const float value = __uint_as_float(s[a] == 0u ? 0x00400000u : (s[a] == 255u ? 0x7FFFFFFFu : (s[a] - (far ? 4u : 0u)) << 23));
+        const float back = far ? 16.0f : 1.0f;
+        float f[V];
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+          const float2 two = pair_values((c[a] >> (4 * i)) & 255u);
+          f[i] = two.x * value * by * back;
+          f[i + 1] = two.y * value * by * back;
+        }
+        put(a, f);
+      }
     }
   }
 }

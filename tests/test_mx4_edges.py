@@ -120,7 +120,8 @@ def test_norm_in_place_at_odd_places(n, K, dtype):
 @pytest.mark.parametrize("K", [64, 1001])
 def test_values_past_fp32_times_a_small_factor(K):
     """Of scales 2^126 and 2^127: the value leaves fp32, its product with the row's factor has one rounding."""
-    by = torch.tensor([1.0, 0.3, 2.0 ** -10, -2.0 ** -126 * 1.7, 2.0 ** -149, 0.0, 3.0, float("inf"), float("nan")])
+    by = torch.tensor([1.0, 0.3, 2.0 ** -10, -2.0 ** -126 * 1.7, 2.0 ** -149, 0.0, 3.0, float("inf"), float("nan"), 2.0 ** 124,
+                       -2.0 ** 126, 2.0 ** 123 * 1.9, -0.7])
     n = len(by)
     for pad in (-1, 3):
         q, s = coded(n, K, 5, span=4, base=251, pad=pad)
