@@ -96,12 +96,14 @@ PyObject* answer(F f) {
   return PyLong_FromLong(rc);
 }
 // The library's call, without the interpreter's lock, as ctypes makes it.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }   // (also where the call throws)
+};
 template <typename F>
 long unlocked(F f) {
-  PyThreadState* state = PyEval_SaveThread();
-  const long rc = f();
-  PyEval_RestoreThread(state);
-  return rc;
+  Unlocked here;
+  return f();
 }
 bool wrong(Py_ssize_t given, Py_ssize_t wanted) {
   if (given == wanted) return false;
