@@ -346,8 +346,7 @@ int64_t bmlp_int8_workspace(int64_t n, int32_t K, int32_t N);
  * cuda_stream, nothing is allocated and no workspace needed; may be captured.
  * Row strides are in elements for real values and in bytes for codes and scales,
  * and at least the row's length where there is more than one row; rows may start
- * anywhere (codes and scales in rows at multiples of 16 bytes run fastest, as
- * bmlp_mx4_matmul says).  n in 0..BMLP_MX4_MAX_ROWS, 0 is a no-op.  Outputs may not
+ * anywhere (which runs fastest: bmlp_mx4_matmul).  n in 0..BMLP_MX4_MAX_ROWS, 0 is a no-op.  Outputs may not
  * overlap inputs except where said.  BMLP_EINVAL for bad arguments, BMLP_ECUDA if a
  * launch fails.  None has a backward form, as the 8-bit front end.
  * ------------------------------------------------------------------------- */
@@ -398,7 +397,10 @@ int bmlp_mx4_dequantize(const uint8_t* q, int64_t ldq, const uint8_t* scale, int
  *   row_scale: n, bias: N (fp32); each may be NULL (1, 0).
  *   out: n x N of out_type (BMLP_F32, BMLP_F16 or BMLP_BF16), row stride ldo.
  * K in 1..2^31 - 1, N in 1..2^30; for odd K the unused four bits of a row of a or of w may
- * be anything if the other's are 0. */
+ * be anything if the other's are 0.
+ * Buffers and strides (rows', and groups') of codes that are multiples of 16 bytes run fastest:
+ * with codes at other places of either operand the product takes two to four times as long; with
+ * scales at other places up to 1.25 times. */
 int bmlp_mx4_matmul(const uint8_t* a, int64_t lda, const uint8_t* a_scale, int64_t ldas, const float* row_scale,
                     const uint8_t* w, int64_t ldw, const uint8_t* w_scale, int64_t ldws, const float* bias,
                     int64_t n, int32_t K, int32_t N, void* out, int32_t out_type, int64_t ldo, void* cuda_stream);

@@ -15,8 +15,10 @@
 // memory, in the order of tcgen05's fences.  The scales go there by tcgen05.st, since a tcgen05.cp that the even CTA
 // issues reads what the odd one's threads have stored to its shared memory, and that needs a release for the
 // cluster: 16384 x 8192 -> 8192 439 us with one for each step (435 to 450 with the cells in a ring of their own).
-// Measured: 16384 x 8192 -> 8192 367 to 397 us (5.5 to 6.0 PFLOP/s), 4096 x 4096 -> 4096 36.6, 16384 x 4096 -> 4096 by 16
-// groups 114 to 129, 16384 x 512 -> 4096 50.
+// Measured: 16384 x 8192 -> 8192 366 to 401 us (5.5 to 6.0 PFLOP/s), 4096 x 4096 -> 4096 35.5, 16384 x 4096 -> 4096 by 16
+// groups 114 to 129.  Bound: the scales' way.  A step takes 870 clocks, its MMAs 512: the MMA warp waits 350 for
+// scales and 170 for codes (an SM takes in a step's 32 KB in 600); the warps that take scales to tensor memory wait
+// 310 for the MMAs of five steps before, and are busy else.
 // Every wait is bounded; if one expires the pair's tiles are made again on CUDA cores.
 #include <algorithm>
 

@@ -10,8 +10,8 @@
 // codes: they need their own 32 values alone, and a row passes through once, whatever its
 // length, with the sum of squares running beside.  The maximum is taken on the bits of |u| as
 // unsigned integers, whose order is the values' order with infinities and NaNs on top.
-// Bound: memory, and the instructions beside it.  8192 x 8192 bf16 34 us (5.0 TB/s), back to values 27 (6.4), the
-// norm of 8191 x 4096 bf16 with residual 37 (6.0); 24,095 x 787 fp32, rows at odd places, 22, 26 and 51.
+// Bound: memory, and the instructions beside it.  8192 x 8192 bf16 34 us (5.0 TB/s), back to values 26 (6.5), the
+// norm of 8191 x 4096 bf16 with residual 37 (6.0); 24,095 x 787 fp32, rows at odd places, 22, 23 and 51.
 #include <algorithm>
 #include <type_traits>
 

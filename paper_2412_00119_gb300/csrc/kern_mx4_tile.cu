@@ -668,8 +668,9 @@ cudaError_t launch_tile(const Mx4Args& A, const TilePlan& P, const Maps& maps, b
 
 // What a call costs, in us, by lines fitted to measurements of every plan at some 40 sizes: a launch and
 // what follows the last sum; per round of tiles its steps of 256 codes and its outputs; CTAs that share K.
-// Of tiles and pairs the one that is taken is 0.3% above the better one in the mean at 60 other sizes, 12% at
-// worst (1450 x 8996 -> 9399 tiles 78, pairs 53; 466 x 886 -> 1149 6.6, 9.2).
+// At 80 other sizes what is taken is 1.1% above the best of all plans in the mean, 13% at worst (469 x 4877 -> 2746 by
+// 16 groups 29.9, by tiles of 48 rows 26.5; 1518 x 9285 -> 2772 by 4 tiles 49.7, pairs 44.1).  Far from the line:
+// 1450 x 8996 -> 9399 tiles 78, pairs 53; 466 x 886 -> 1149 6.6, 9.2.
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t some_groups(const Mx4Args& A) { return A.offsets ? std::min<int64_t>(A.E, A.n) : 1; }
 // Row tiles at most, and on average (of a group's rows the last one is half full).
