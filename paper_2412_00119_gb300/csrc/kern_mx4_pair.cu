@@ -354,12 +354,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (!ok && rank == 0) {
-        // no copy outlives its CTA: the last phases hold both CTAs' copies (where the odd
-        // one stopped earlier, the wait's limit is time enough for what is in flight)
-        for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
-          wait_phase<kPeer>(&sh->full[k % kStages], (uint32_t)(k / kStages) & 1u, &sh->left_failed, 2000000ull);
-      }
+      // The last stages' MMAs: the arrivals of their commits, to both CTAs, are not under way when one leaves.  After an
+      // expired wait the even CTA waits for the copies: none outlives its CTA, and the last phases hold both
+      // CTAs' (where the odd one stopped earlier, the wait's limit is time enough for what is in flight).
+      unsigned long long* last = ok || rank != 0 ? sh->empty : sh->full;
+      volatile int late = 0;   // (of its own: the MMAs' last wait goes on after one of these expires)
+      for (int64_t k = copied > kStages ? copied - kStages : 0; k < copied; ++k)
+        wait_phase<kPeer>(&last[k % kStages], (uint32_t)(k / kStages) & 1u, &late, ok ? kWaitCycles : 2000000ull);
     }
   } else if (rank == 0) {
     // ---------------- MMAs of the pair ----------------
@@ -426,7 +427,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                : "=r"(peer) : "r"(smem_u32(&sh->failed)), "r"(rank ^ 1u) : "memory");
   const bool redo = peer != 0u || *failed != 0;
   // the last arrival that the even CTA's commits send here
-  if (rank != 0 && threadIdx.x == 0) wait_phase(&sh->left, 0, &sh->left_failed);
+  if (rank != 0 && threadIdx.x == 0) wait_phase<kPeer>(&sh->left, 0, &sh->left_failed);
   __syncwarp();
   pair_sync();
   if (redo) {
