@@ -494,9 +494,10 @@ __global__ void __launch_bounds__(32 * Warps<kEpiWarps, kTma>::kAll, kTma && kEp
       }
       if (!ok) {
         // no copy outlives its CTA (a phase may lack the scales' arrival, and then the wait's limit is
-        // time enough)
+        // time enough; the flag is of its own: the MMAs' and cells' last waits go on after that)
+        volatile int late = 0;
         for (int64_t k = copied > P.stages ? copied - P.stages : 0; k < copied; ++k)
-          wait_phase(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &sh->left_failed, 2000000ull);
+          wait_phase(&sh->full[k % P.stages], (uint32_t)(k / P.stages) & 1u, &late, 2000000ull);
       }
     }
   } else {
